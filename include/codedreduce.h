@@ -362,6 +362,86 @@ cr_status_t cr_plan_tune_gradients(cr_plan_t *plan, int32_t block_kb, int32_t st
  * multi_stages: 2..4 (2 lets two CTAs share an SM). */
 cr_status_t cr_plan_tune_items(cr_plan_t *plan, int32_t item_order, int32_t multi_stages);
 
+/* ---- layers in front of the workers' model ---------------------------------------------------------
+ * The paper's image experiment trains a convolutional network (Section V); Eq. (g) and the decode ask two things of
+ * its layers.  The gradients of the partitions must ADD UP to the gradient of the whole data set, so no layer may
+ * couple the samples of different partitions: the normalisation is per sample (group norm).  And every worker that
+ * holds a partition must compute THE SAME partial gradient, or the decode of a redundant copy is not exact: dropout
+ * masks are functions of the element's index alone, sums have one fixed order (no atomics), integer products have no
+ * rounding at all.
+ *   - Tensors are channels last: rows of `channels` consecutive elements, one row per position, `ld` elements from
+ *     row to row (>= channels), the positions of a sample one after the other.  Element types are cr_elem_t; the
+ *     arithmetic is fp32 throughout, rounded once to the element type.  Buffers must be aligned to their element;
+ *     16-byte aligned bases and row strides enable 16-byte loads, anything else silently takes element loads.
+ *   - The plan gives the device, the launch count and the status word; its tree, code and dtype do not matter.
+ *   - Like the other device calls they only enqueue kernels (no copy, no allocation) and can be captured in a CUDA
+ *     graph.  Two calls that may overlap on the device need workspaces of their own. */
+typedef enum { CR_ELEM_F32 = 0, CR_ELEM_BF16 = 1, CR_ELEM_F16 = 2 } cr_elem_t;
+typedef enum { CR_ACT_NONE = 0, CR_ACT_RELU = 1, CR_ACT_SILU = 2 } cr_act_t; /* z, max(z, 0), z / (1 + e^-z) */
+
+/* Dropout of the elements of a tensor, from a counter-based generator; no mask is stored.  Element i of the tensor
+ * (row-major, the row stride not counted) has the index e = offset + i and the 16-bit number
+ * (W(e / 4) >> (16 * (e % 4))) & 0xffff, with W(j) output j (from 0) of SplitMix64 started at mix(seed), mix being
+ * that generator's own output function.  It is dropped if the number is below T = round(65536 p), else multiplied by
+ * 65536 / (65536 - T).  So the mask of a partition is the same wherever and beside whatever it is processed, given
+ * the index of its first element as `offset`; p is honoured to 2^-16 and the expectation is exact.
+ *   y = residual + dropout(x)   (residual NULL: y = dropout(x), which is also the backward pass, with dy for x)
+ * x, residual, y: [rows][cols] with row strides ld_x, ld_r, ld_y, one element type.  y may be x or residual itself
+ * (same stride).  0 <= p <= 1 (p = 1: everything dropped, whatever its value), rows and cols >= 0, offset >= 0. */
+cr_status_t cr_dropout(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r, void *y,
+                       int64_t ld_y, int64_t rows, int64_t cols, int32_t elem, double p, uint64_t seed, int64_t offset,
+                       void *stream);
+
+typedef struct {
+    int64_t samples;   /* >= 0 */
+    int64_t positions; /* rows per sample, >= 1 */
+    int32_t channels;  /* >= 1 */
+    int32_t groups;    /* divides channels; group g = channels g * channels / groups .. */
+    int32_t elem;      /* cr_elem_t of x, y, dy, dx */
+    int32_t act;       /* cr_act_t */
+    double eps;        /* >= 0, added to the variance (forward only) */
+    double p;          /* dropout behind the activation, 0 <= p <= 1; element index (n * positions + s) * channels + c */
+    uint64_t seed;
+    int64_t offset;    /* index of the first element, >= 0 */
+} cr_group_norm_t;
+
+/* y = dropout(act(gamma_c (x - mean) rstd + beta_c)), mean and rstd = 1 / sqrt(var + eps) over the positions and
+ * channels of each (sample, group), var the mean square distance from the mean.  gamma, beta: fp32 [channels] or NULL
+ * (ones, zeros).  mean, rstd: fp32 [samples][groups], written for the backward pass; both NULL if not wanted.  y may
+ * be x itself (same stride).  workspace: device scratch of cr_group_norm_workspace_bytes (CR_ERR_OOM if smaller). */
+size_t cr_group_norm_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc);
+cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const void *x, int64_t ld_x, const float *gamma,
+                          const float *beta, void *y, int64_t ld_y, float *mean, float *rstd, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* Gradients of cr_group_norm from dy, with the forward pass's x, mean, rstd, gamma, beta and dropout.  dx has the type
+ * of x (NULL: not wanted).  dgamma, dbeta: fp32 [partitions][ld_param], one row for every samples / partitions
+ * consecutive samples (partitions >= 1 divides samples) -- the partial gradients of the partitions, which can be
+ * written straight into longer rows of gradients; either may be NULL.  dx may be dy itself (same stride).
+ * workspace as above, of cr_group_norm_backward_workspace_bytes. */
+size_t cr_group_norm_backward_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc);
+cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc, const void *dy, int64_t ld_dy,
+                                   const void *x, int64_t ld_x, const float *gamma, const float *beta,
+                                   const float *mean, const float *rstd, void *dx, int64_t ld_dx, float *dgamma,
+                                   float *dbeta, int64_t ld_param, int64_t partitions, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
+/* 8-bit codes of the rows (tokens) of x [rows][cols]: scale[r] = max_c |x_rc| / 127, q_rc = rint(x_rc * m) with
+ * m = 127 / max_c |x_rc| rounded to fp32 (ties to even).  A row whose largest magnitude is below 2^-120 counts as zero
+ * (scale 0, codes 0); one that holds an infinity or a NaN gets scale NaN and codes 0.  q: [rows] at stride ld_q bytes;
+ * a stride that is a multiple of 16 lets cr_int8_product take its tensor-core form.  cols >= 1. */
+cr_status_t cr_quantize_rows(cr_plan_t *plan, const void *x, int64_t ld_x, int64_t rows, int64_t cols, int32_t elem,
+                             int8_t *q, int64_t ld_q, float *scale, void *stream);
+
+/* y[t][n] = (sum_k x[t][k] w[n][k]) * (x_scale[t] * w_scale[n]) + bias[n]: x [tokens][inner] and w [outer][inner]
+ * codes of 8 bits at row strides ld_x, ld_w (bytes), fp32 scales, bias fp32 [outer] or NULL, y [tokens][outer] of type
+ * `elem` at row stride ld_y.  The sum is exact (32-bit integers; 1 <= inner <= 131071 keeps it in range for every
+ * code), tokens and outer >= 0.  16-byte aligned x, w and strides that are multiples of 16 enable the tensor-core
+ * form.  The layer sits on the data: no gradient is taken through it. */
+cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w,
+                            int64_t ld_w, const float *w_scale, const float *bias, void *y, int64_t ld_y, int64_t tokens,
+                            int64_t outer, int64_t inner, int32_t elem, void *stream);
+
 /* Kernel launches enqueued by this plan's device calls so far. */
 int64_t cr_plan_launch_count(const cr_plan_t *plan);
 

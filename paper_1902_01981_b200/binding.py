@@ -26,6 +26,9 @@ CR_AGG_FUSED, CR_AGG_FUSED_LDG, CR_AGG_UNFUSED, CR_AGG_UNCODED_SUM = 0, 1, 2, 3
 CR_AGG_ALL_NODES = 0x100
 CR_AGG_FROM_CODED = 0x200
 CR_LOSS_SQUARED, CR_LOSS_LOGISTIC = 0, 1
+CR_ELEM_F32, CR_ELEM_BF16, CR_ELEM_F16 = 0, 1, 2
+CR_ACT_NONE, CR_ACT_RELU, CR_ACT_SILU = 0, 1, 2
+CR_ACT = {"none": CR_ACT_NONE, "relu": CR_ACT_RELU, "silu": CR_ACT_SILU}
 
 
 class cr_plan_desc_t(C.Structure):
@@ -33,6 +36,12 @@ class cr_plan_desc_t(C.Structure):
                 ("code", C.c_int32), ("dtype", C.c_int32), ("seed", C.c_uint64),
                 ("B_explicit", C.POINTER(C.c_double)), ("max_kappa", C.c_double),
                 ("device", C.c_int32), ("reserved", C.c_int32)]
+
+
+class cr_group_norm_t(C.Structure):
+    _fields_ = [("samples", C.c_int64), ("positions", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32),
+                ("elem", C.c_int32), ("act", C.c_int32), ("eps", C.c_double), ("p", C.c_double),
+                ("seed", C.c_uint64), ("offset", C.c_int64)]
 
 
 class CodedReduceError(RuntimeError):
@@ -96,6 +105,21 @@ _SIGNATURES = {
     "cr_plan_tune": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
     "cr_plan_tune_gradients": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32]),
     "cr_plan_tune_items": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32]),
+    "cr_dropout": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                             C.c_int64, C.c_int32, C.c_double, C.c_uint64, C.c_int64, C.c_void_p]),
+    "cr_group_norm_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(cr_group_norm_t)]),
+    "cr_group_norm": (C.c_int, [C.c_void_p, C.POINTER(cr_group_norm_t), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "cr_group_norm_backward_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(cr_group_norm_t)]),
+    "cr_group_norm_backward": (C.c_int, [C.c_void_p, C.POINTER(cr_group_norm_t), C.c_void_p, C.c_int64, C.c_void_p,
+                                         C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
+                                         C.c_size_t, C.c_void_p]),
+    "cr_quantize_rows": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_void_p,
+                                   C.c_int64, C.c_void_p, C.c_void_p]),
+    "cr_int8_product": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32,
+                                  C.c_void_p]),
     "cr_plan_launch_count": (C.c_int64, [C.c_void_p]),
     "cr_plan_last_kernel": (C.c_char_p, [C.c_void_p]),
 }
@@ -433,3 +457,160 @@ def slot_partitions(plan: int) -> np.ndarray:
     """[N, m] int32 table of the partition each slot holds (marshalling of cr_plan_get_slots)."""
     N = cr_plan_num_nodes(plan)
     return np.stack([cr_plan_get_slots(plan, v)[0] for v in range(N)])
+
+
+# ------------------------------------------------------------------ layers in front of the workers' model
+
+_elems = {}
+
+
+def _elem(t) -> int:
+    """cr_elem_t of a tensor's element type."""
+    if not _elems:
+        import torch
+        _elems.update({torch.float32: CR_ELEM_F32, torch.bfloat16: CR_ELEM_BF16, torch.float16: CR_ELEM_F16})
+    e = _elems.get(t.dtype)
+    if e is None:
+        raise ValueError(f"expected float32, bfloat16 or float16 elements, got {t.dtype}")
+    return e
+
+
+def _row_ptr(t, shape):
+    """(address, row stride) of a CUDA tensor whose leading dimensions form one sequence of equally spaced rows."""
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if t.shape != shape:
+        raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    width = shape[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), width
+    st = t.stride()
+    if width > 1 and st[-1] != 1:
+        raise ValueError("the elements of a row must be next to each other")
+    ld = 0
+    spaced = 1           # rows spanned by the dimensions seen so far, innermost first
+    for k in range(len(shape) - 2, -1, -1):
+        if shape[k] > 1:
+            if not ld:
+                ld = st[k]
+            elif st[k] != ld * spaced:
+                raise ValueError("the rows must be equally spaced")
+        spaced *= shape[k]
+    return t.data_ptr(), ld or width
+
+
+def _vector_ptr(t, count: int) -> int:
+    """Address of a contiguous fp32 CUDA tensor of `count` elements (None -> NULL)."""
+    if t is None:
+        return 0
+    if t.element_size() != 4 or not t.is_floating_point() or t.numel() != count:
+        raise ValueError(f"expected {count} float32 elements")
+    return _dev_ptr(t)
+
+
+def cr_dropout(plan: int, x, y, p: float, seed: int, offset: int = 0, residual=None, stream=None) -> None:
+    """y = residual + dropout(x) for row-major tensors of one shape; the mask depends on (seed, offset + index of the
+    element) only.  The backward pass is the same call on dy."""
+    shape, e = x.shape, _elem(x)
+    xp, ldx = _row_ptr(x, shape)
+    yp, ldy = _row_ptr(y, shape)
+    rp, ldr = (0, 0) if residual is None else _row_ptr(residual, shape)
+    if y.dtype != x.dtype or (residual is not None and residual.dtype != x.dtype):
+        raise ValueError("x, residual and y must have one element type")
+    cols = shape[-1] if len(shape) else 1
+    _check(lib().cr_dropout(plan, xp, ldx, rp, ldr, yp, ldy, x.numel() // cols if cols else 0, cols, e, p,
+                            seed, offset, _stream_ptr(stream)), "cr_dropout")
+
+
+def _group_norm_desc(x, groups, eps, act, p, seed, offset):
+    if x.dim() != 3:
+        raise ValueError("expected [samples, positions, channels]")
+    n, s, c = x.shape
+    return cr_group_norm_t(n, s, c, groups, _elem(x), act, eps, p, seed, offset)
+
+
+def cr_group_norm_workspace_bytes(plan: int, x, groups: int) -> int:
+    return lib().cr_group_norm_workspace_bytes(plan, _group_norm_desc(x, groups, 0.0, CR_ACT_NONE, 0.0, 0, 0))
+
+
+def cr_group_norm_backward_workspace_bytes(plan: int, x, groups: int) -> int:
+    return lib().cr_group_norm_backward_workspace_bytes(plan, _group_norm_desc(x, groups, 0.0, CR_ACT_NONE, 0.0, 0, 0))
+
+
+def cr_group_norm(plan: int, x, gamma, beta, groups: int, y, mean=None, rstd=None, eps: float = 1e-5,
+                  act: int = CR_ACT_NONE, p: float = 0.0, seed: int = 0, offset: int = 0, workspace=None,
+                  stream=None) -> None:
+    """y = dropout(act(group_norm(x))) for x [samples, positions, channels]; gamma, beta [channels] or None; mean, rstd
+    [samples, groups] (both or neither) are what the backward pass takes."""
+    desc = _group_norm_desc(x, groups, eps, act, p, seed, offset)
+    if y.dtype != x.dtype:
+        raise ValueError("x and y must have one element type")
+    xp, ldx = _row_ptr(x, x.shape)
+    yp, ldy = _row_ptr(y, x.shape)
+    stats = desc.samples * groups
+    wp, wb = _ptr_and_bytes(workspace)
+    _check(lib().cr_group_norm(plan, desc, xp, ldx, _vector_ptr(gamma, desc.channels), _vector_ptr(beta, desc.channels),
+                               yp, ldy, _vector_ptr(mean, stats), _vector_ptr(rstd, stats), wp, wb,
+                               _stream_ptr(stream)), "cr_group_norm")
+
+
+def cr_group_norm_backward(plan: int, dy, x, gamma, beta, mean, rstd, groups: int, dx=None, dgamma=None, dbeta=None,
+                           act: int = CR_ACT_NONE, p: float = 0.0, seed: int = 0, offset: int = 0, workspace=None,
+                           stream=None) -> None:
+    """dx (or None) and, for each of the partitions the samples are cut into, dgamma and dbeta [partitions, channels]
+    (None, or rows inside wider rows: both with one row stride)."""
+    desc = _group_norm_desc(x, groups, 0.0, act, p, seed, offset)
+    if dy.dtype != x.dtype or (dx is not None and dx.dtype != x.dtype):
+        raise ValueError("x, dy and dx must have one element type")
+    xp, ldx = _row_ptr(x, x.shape)
+    gp, ldg = _row_ptr(dy, x.shape)
+    dp, ldd = (0, 0) if dx is None else _row_ptr(dx, x.shape)
+    params, parts, ldp = [], 1, desc.channels
+    for t in (dgamma, dbeta):
+        if t is None:
+            params.append(0)
+            continue
+        if t.dim() != 2 or t.shape[1] != desc.channels or t.element_size() != 4 or not t.is_floating_point():
+            raise ValueError("parameter gradients are float32 [partitions, channels]")
+        ptr, ld = _row_ptr(t, t.shape)
+        if any(params) and (t.shape[0] != parts or ld != ldp):
+            raise ValueError("dgamma and dbeta must have one shape and row stride")
+        parts, ldp = t.shape[0], ld
+        params.append(ptr)
+    stats = desc.samples * groups
+    wp, wb = _ptr_and_bytes(workspace)
+    _check(lib().cr_group_norm_backward(plan, desc, gp, ldg, xp, ldx, _vector_ptr(gamma, desc.channels),
+                                        _vector_ptr(beta, desc.channels), _vector_ptr(mean, stats),
+                                        _vector_ptr(rstd, stats), dp, ldd, params[0], params[1], ldp, parts, wp, wb,
+                                        _stream_ptr(stream)), "cr_group_norm_backward")
+
+
+def _codes_ptr(t, shape):
+    import torch
+    if t.dtype != torch.int8:
+        raise ValueError(f"expected int8 codes, got {t.dtype}")
+    return _row_ptr(t, shape)
+
+
+def cr_quantize_rows(plan: int, x, q, scale, stream=None) -> None:
+    """q [rows, cols] int8 codes and scale [rows] of x [rows, cols]; a row stride of q that is a multiple of 16 lets
+    cr_int8_product take its tensor-core form."""
+    if x.dim() != 2:
+        raise ValueError("expected [rows, cols]")
+    xp, ldx = _row_ptr(x, x.shape)
+    qp, ldq = _codes_ptr(q, x.shape)
+    _check(lib().cr_quantize_rows(plan, xp, ldx, x.shape[0], x.shape[1], _elem(x), qp, ldq,
+                                  _vector_ptr(scale, x.shape[0]), _stream_ptr(stream)), "cr_quantize_rows")
+
+
+def cr_int8_product(plan: int, x, x_scale, w, w_scale, y, bias=None, stream=None) -> None:
+    """y [tokens, outer] = (x w^T) * x_scale * w_scale + bias for int8 codes x [tokens, inner], w [outer, inner]."""
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        raise ValueError("expected x [tokens, inner] and w [outer, inner]")
+    (m, k), n = x.shape, w.shape[0]
+    xp, ldx = _codes_ptr(x, x.shape)
+    wp, ldw = _codes_ptr(w, w.shape)
+    yp, ldy = _row_ptr(y, (m, n))
+    _check(lib().cr_int8_product(plan, xp, ldx, _vector_ptr(x_scale, m), wp, ldw, _vector_ptr(w_scale, n),
+                                 _vector_ptr(bias, n), yp, ldy, m, n, k, _elem(y), _stream_ptr(stream)),
+           "cr_int8_product")

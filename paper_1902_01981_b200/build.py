@@ -10,8 +10,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcodedreduce.so")
-SOURCES = ["cr_plan.cpp", "cr_kernels.cu", "cr_tc.cu", "cr_api.cu"]
-HEADERS = ["cr_plan.hpp", "cr_kernels.hpp"]
+SOURCES = ["cr_plan.cpp", "cr_kernels.cu", "cr_tc.cu", "cr_layers.cu", "cr_int8.cu", "cr_api.cu"]
+HEADERS = ["cr_plan.hpp", "cr_kernels.hpp", "cr_layers.hpp", "cr_elem.cuh"]
 
 
 def _nvcc() -> str:
@@ -33,7 +33,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compile the library if it is missing or older than its sources; return its path."""
     if not force and not _stale():
         return LIB
-    cmd = [_nvcc(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
+    cmd = [_nvcc(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "--threads", "0",
            "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if verbose:
         cmd += ["-Xptxas", "-v"]

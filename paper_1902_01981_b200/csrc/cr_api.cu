@@ -13,6 +13,7 @@
 
 #include "codedreduce.h"
 #include "cr_kernels.hpp"
+#include "cr_layers.hpp"
 #include "cr_plan.hpp"
 
 namespace {
@@ -1203,6 +1204,153 @@ cr_status_t cr_partial_gradients_static(cr_plan_t *plan, const float *X, const f
                                                  plan->hp.N * plan->hp.m, rows, plan->hp.d, scratch, G_slots, CR_LOSS_SQUARED,
                                                  plan->dev.sm_count, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
     if (e != cudaSuccess) { note_cuda(e, "cr_partial_gradients_static"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+}  // extern "C"
+
+// ---- layers ----------------------------------------------------------------------------------------
+
+namespace {
+
+bool known_elem(int32_t elem) { return elem == CR_ELEM_F32 || elem == CR_ELEM_BF16 || elem == CR_ELEM_F16; }
+bool on_element(const void *p, int32_t elem) {
+    return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(cr::elem_bytes(elem) - 1)) == 0;
+}
+// Row strides up to 2^40 elements and extents up to 2^46 elements keep every offset in 64 bits.
+bool good_rows(int64_t rows, int64_t cols, int64_t ld) {
+    return ld >= cols && ld <= (1ll << 40) && (rows == 0 || ld == 0 || rows <= (1ll << 46) / ld);
+}
+bool good_dropout(double p, int64_t offset) { return p >= 0.0 && p <= 1.0 && offset >= 0; }   // a NaN fails both
+
+bool good_desc(const cr_group_norm_t *d) {
+    return d && d->samples >= 0 && d->positions >= 1 && d->positions <= (1ll << 40) && d->channels >= 1 && d->groups >= 1 &&
+           d->channels % d->groups == 0 && known_elem(d->elem) && d->act >= CR_ACT_NONE && d->act <= CR_ACT_SILU &&
+           d->eps >= 0.0 && good_dropout(d->p, d->offset) &&
+           // blocks and (sample, group) pairs are counted in 31 bits
+           d->samples <= 0x7fffffffll / std::max<int64_t>(d->groups, (d->channels + 255) / 256);
+}
+
+cr::GroupNormArgs group_norm_args(const cr_group_norm_t &d) {
+    cr::GroupNormArgs a;
+    a.samples = d.samples; a.positions = d.positions; a.channels = d.channels; a.groups = d.groups;
+    a.elem = d.elem; a.act = d.act; a.eps = (float)d.eps;
+    a.drop = cr::make_drop(d.p, d.seed, d.offset);
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+cr_status_t cr_dropout(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r, void *y,
+                       int64_t ld_y, int64_t rows, int64_t cols, int32_t elem, double p, uint64_t seed, int64_t offset,
+                       void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (rows < 0 || cols < 0 || !known_elem(elem) || !good_dropout(p, offset)) return CR_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return CR_OK;
+    if (!x || !y || !good_rows(rows, cols, ld_x) || !good_rows(rows, cols, ld_y)) return CR_ERR_INVALID_ARG;
+    if (residual && !good_rows(rows, cols, ld_r)) return CR_ERR_INVALID_ARG;
+    if (!on_element(x, elem) || !on_element(y, elem) || !on_element(residual, elem)) return CR_ERR_INVALID_ARG;
+    cudaError_t e = cr::launch_dropout(x, residual, y, rows, cols, ld_x, ld_r, ld_y, elem, cr::make_drop(p, seed, offset),
+                                       plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_dropout"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+size_t cr_group_norm_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc) {
+    if (!plan || !good_desc(desc)) return 0;
+    return cr::group_norm_workspace_bytes(desc->samples, desc->positions, desc->channels, desc->groups, desc->elem);
+}
+
+cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const void *x, int64_t ld_x, const float *gamma,
+                          const float *beta, void *y, int64_t ld_y, float *mean, float *rstd, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_desc(desc) || (mean == nullptr) != (rstd == nullptr)) return CR_ERR_INVALID_ARG;
+    if (desc->samples == 0) return CR_OK;
+    if (!x || !y || desc->positions > (1ll << 46) / desc->samples) return CR_ERR_INVALID_ARG;
+    const int64_t rows = desc->samples * desc->positions;
+    if (!good_rows(rows, desc->channels, ld_x) || !good_rows(rows, desc->channels, ld_y)) return CR_ERR_INVALID_ARG;
+    if (!on_element(x, desc->elem) || !on_element(y, desc->elem)) return CR_ERR_INVALID_ARG;
+    const size_t need = cr_group_norm_workspace_bytes(plan, desc);
+    if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+    cr::GroupNormArgs a = group_norm_args(*desc);
+    a.x = x; a.ld_x = ld_x; a.y = y; a.ld_y = ld_y; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
+    a.workspace = static_cast<float *>(workspace);
+    cudaError_t e = cr::launch_group_norm(a, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_group_norm"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+size_t cr_group_norm_backward_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc) {
+    if (!plan || !good_desc(desc)) return 0;
+    return cr::group_norm_backward_workspace_bytes(desc->samples, desc->positions, desc->channels, desc->groups, desc->elem);
+}
+
+cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc, const void *dy, int64_t ld_dy,
+                                   const void *x, int64_t ld_x, const float *gamma, const float *beta,
+                                   const float *mean, const float *rstd, void *dx, int64_t ld_dx, float *dgamma,
+                                   float *dbeta, int64_t ld_param, int64_t partitions, void *workspace,
+                                   size_t workspace_bytes, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_desc(desc) || partitions < 1 || desc->samples % partitions != 0) return CR_ERR_INVALID_ARG;
+    if ((dgamma || dbeta) && (!good_rows(partitions, desc->channels, ld_param) ||
+                              partitions > 0x7fffffffll / ((desc->channels + 31) / 32)))
+        return CR_ERR_INVALID_ARG;
+    if (desc->samples > 0) {
+        if (!dy || !x || !mean || !rstd || desc->positions > (1ll << 46) / desc->samples) return CR_ERR_INVALID_ARG;
+        const int64_t rows = desc->samples * desc->positions;
+        if (!good_rows(rows, desc->channels, ld_x) || !good_rows(rows, desc->channels, ld_dy)) return CR_ERR_INVALID_ARG;
+        if (dx && !good_rows(rows, desc->channels, ld_dx)) return CR_ERR_INVALID_ARG;
+        if (!on_element(x, desc->elem) || !on_element(dy, desc->elem) || !on_element(dx, desc->elem)) return CR_ERR_INVALID_ARG;
+    }
+    if (!dx && !dgamma && !dbeta) return CR_OK;
+    const size_t need = cr_group_norm_backward_workspace_bytes(plan, desc);
+    if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+    cr::GroupNormArgs a = group_norm_args(*desc);
+    a.x = x; a.ld_x = ld_x; a.dy = dy; a.ld_dy = ld_dy; a.y = dx; a.ld_y = ld_dx; a.gamma = gamma; a.beta = beta;
+    a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
+    a.dgamma = dgamma; a.dbeta = dbeta; a.ld_param = ld_param; a.partitions = partitions;
+    a.workspace = static_cast<float *>(workspace);
+    cudaError_t e = cr::launch_group_norm_backward(a, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_group_norm_backward"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+cr_status_t cr_quantize_rows(cr_plan_t *plan, const void *x, int64_t ld_x, int64_t rows, int64_t cols, int32_t elem,
+                             int8_t *q, int64_t ld_q, float *scale, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (rows < 0 || rows > 0x7fffffffll || cols < 1 || !known_elem(elem)) return CR_ERR_INVALID_ARG;
+    if (rows == 0) return CR_OK;
+    if (!x || !q || !scale || !good_rows(rows, cols, ld_x) || !good_rows(rows, cols, ld_q) || !on_element(x, elem)) return CR_ERR_INVALID_ARG;
+    cudaError_t e = cr::launch_quantize_rows(x, rows, cols, ld_x, elem, q, ld_q, scale, plan->dev,
+                                             reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_quantize_rows"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w,
+                            int64_t ld_w, const float *w_scale, const float *bias, void *y, int64_t ld_y, int64_t tokens,
+                            int64_t outer, int64_t inner, int32_t elem, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    // 2^14 * 131071 < 2^31: the largest inner length whose sum stays in 32 bits for every code
+    if (tokens < 0 || outer < 0 || inner < 1 || inner > 131071 || !known_elem(elem)) return CR_ERR_INVALID_ARG;
+    if (tokens > 0x7fffffffll || outer > 0x7fffffffll) return CR_ERR_INVALID_ARG;
+    if (tokens == 0 || outer == 0) return CR_OK;
+    if (!x || !w || !x_scale || !w_scale || !y || !on_element(y, elem)) return CR_ERR_INVALID_ARG;
+    if (!good_rows(tokens, inner, ld_x) || !good_rows(outer, inner, ld_w) || !good_rows(tokens, outer, ld_y)) return CR_ERR_INVALID_ARG;
+    cr::Int8ProductArgs a;
+    a.x = x; a.ld_x = ld_x; a.x_scale = x_scale; a.w = w; a.ld_w = ld_w; a.w_scale = w_scale; a.bias = bias;
+    a.y = y; a.ld_y = ld_y; a.tokens = tokens; a.outer = outer; a.inner = inner; a.elem = elem;
+    cudaError_t e = cr::launch_int8_product(a, plan->d_status, plan->dev, plan->tune, plan->encode,
+                                            reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_int8_product"); return CR_ERR_CUDA; }
     return CR_OK;
 }
 

@@ -1,0 +1,182 @@
+// Vectors of 32-, bf16- and f16-elements, and the counter-based generator of the dropout masks.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "cr_layers.hpp"
+
+namespace cr {
+
+// `VEC` consecutive elements as they lie in memory: 16 bytes, or one element.
+template <typename T, int VEC>
+struct Packed {
+    static constexpr int kWords = VEC * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+};
+template <typename T>
+struct Packed<T, 1> {
+    T e;
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// Data that is read once goes past L1; not the read-only path, since an output may be the input's own buffer.
+template <typename T, int VEC>
+__device__ __forceinline__ Packed<T, VEC> load_packed(const T *p) {
+    Packed<T, VEC> r;
+    if constexpr (VEC == 1) {
+        r.e = *p;
+    } else {
+        static_assert(sizeof(r) == 16, "a vector is 16 bytes");
+        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p) : "memory");
+    }
+    return r;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_packed(T *p, const Packed<T, VEC> &r) {
+    if constexpr (VEC == 1) {
+        *p = r.e;
+    } else {
+        asm volatile("st.global.L1::no_allocate.v4.b32 [%0], {%1, %2, %3, %4};"
+                     ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]) : "memory");
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void unpack(const Packed<T, VEC> &r, float (&v)[VEC]) {
+    if constexpr (VEC == 1) {
+        v[0] = to_float(r.e);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = __uint_as_float(r.w[i]);
+    } else if constexpr (__is_same(T, __nv_bfloat16)) {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+            v[2 * i] = __uint_as_float(r.w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&r.w[i]));
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Packed<T, VEC> pack(const float (&v)[VEC]) {
+    Packed<T, VEC> r;
+    if constexpr (VEC == 1) {
+        r.e = from_float<T>(v[0]);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) r.w[i] = __float_as_uint(v[i]);
+    } else if constexpr (__is_same(T, __nv_bfloat16)) {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            r.w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+            r.w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+    }
+    return r;
+}
+
+// ---- the generator -------------------------------------------------------------------------------
+//
+// SplitMix64 (Steele, Lea, Flood, "Fast splittable pseudorandom number generators", 2014) read by index: the i-th
+// output of the stream that starts at `key` is a function of key and i alone, so every element's number can be had
+// anywhere, in any order, and no mask is stored.  One 64-bit output serves four consecutive elements with 16 bits each
+// (the lowest bits the first).  About 20 integer instructions per output, 5 per element: under the time the element's
+// bytes take from HBM, which a cipher-like generator with its ten rounds would not be.
+
+constexpr unsigned long long kMixGamma = 0x9E3779B97F4A7C15ull;
+__host__ __device__ __forceinline__ unsigned long long mix64(unsigned long long z) {
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
+__device__ __forceinline__ unsigned long long drop_word(unsigned long long key, unsigned long long i) {
+    return mix64(key + (i + 1) * kMixGamma);
+}
+
+// v[i] = kept ? v[i] * scale : 0 for the VEC elements from index e on.  A dropped element is selected away, not
+// multiplied by zero: an infinity or a NaN in its place leaves a zero.
+template <int VEC>
+__device__ __forceinline__ void drop(float (&v)[VEC], const DropSpec &d, unsigned long long e) {
+    const unsigned long long first = e >> 2;
+    const uint32_t shift = (uint32_t)e & 3u;
+    if (d.scale == 0.f) {   // threshold 65536: everything goes
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = 0.f;
+        return;
+    }
+    const uint32_t limit = d.threshold << 16;
+    if constexpr (VEC == 1) {
+        const uint32_t lane = (uint32_t)(drop_word(d.key, first) >> (16 * shift)) & 0xffffu;
+        v[0] = lane >= d.threshold ? v[0] * d.scale : 0.f;
+    } else {
+        // z of output `first`; the following ones are one addition away
+        unsigned long long z = d.key + (first + 1) * kMixGamma;
+        uint32_t w[VEC / 2 + 2];
+#pragma unroll
+        for (int j = 0; j < VEC / 4; ++j, z += kMixGamma) {
+            const unsigned long long o = mix64(z);
+            w[2 * j] = (uint32_t)o;
+            w[2 * j + 1] = (uint32_t)(o >> 32);
+        }
+        if (shift) {   // the vector straddles one output more: move its 16-bit numbers into place
+            const unsigned long long o = mix64(z);
+            w[VEC / 2] = (uint32_t)o;
+            w[VEC / 2 + 1] = (uint32_t)(o >> 32);
+            const bool whole = shift & 2u;
+#pragma unroll
+            for (int j = 0; j <= VEC / 2; ++j) w[j] = whole ? w[j + 1] : w[j];
+            const uint32_t bits = (shift & 1u) * 16u;
+#pragma unroll
+            for (int j = 0; j < VEC / 2; ++j) w[j] = __funnelshift_r(w[j], w[j + 1], bits);
+        }
+#pragma unroll
+        for (int j = 0; j < VEC / 2; ++j) {
+            v[2 * j] = (w[j] << 16) >= limit ? v[2 * j] * d.scale : 0.f;
+            v[2 * j + 1] = w[j] >= limit ? v[2 * j + 1] * d.scale : 0.f;   // the low half cannot lift it over the limit
+        }
+    }
+}
+
+// ---- activations -----------------------------------------------------------------------------------
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == kActRelu) return z < 0.f ? 0.f : z;   // a NaN stays one
+    if constexpr (ACT == kActSilu) return __fdividef(z, 1.f + __expf(-z));
+    return z;
+}
+// Derivative of the activation at z.
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == kActSilu) {
+        const float s = __fdividef(1.f, 1.f + __expf(-z));
+        return s * fmaf(z, 1.f - s, 1.f);
+    }
+    return 1.f;
+}
+
+}  // namespace cr

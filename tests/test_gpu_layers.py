@@ -1,0 +1,520 @@
+"""Group norm with activation and dropout, dropout, 8-bit codes and products against 64-bit arithmetic."""
+import numpy as np
+import pytest
+
+from oracle import cr_layers as O
+from paper_1902_01981_b200 import binding as B
+from paper_1902_01981_b200 import build as cr_build
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+# Rounding of a stored value: half a unit of the last place of bf16 (8 bits) and f16 (11 bits; also its smallest step),
+# a whole one of f32 (24 bits).
+ROUND = {"f32": 2.0 ** -23, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 0.0, "bf16": 0.0, "f16": 2.0 ** -24}
+# fp32 arithmetic before that: a value is a dozen operations of 2^-24 each on numbers of the size of the largest
+# output, and the statistics are sums of chains of at most a few hundred additions whose errors mostly cancel
+ARITH = 2e-5
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    cr_build.build()
+    assert torch.cuda.is_available()
+
+
+@pytest.fixture(scope="module")
+def plan():
+    p = B.cr_plan_create(4, 2, 1, 24, 1024, device=0)
+    yield p
+    torch.cuda.synchronize()
+    assert B.cr_plan_device_status(p) == B.CR_OK
+    B.cr_plan_destroy(p)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def place(values, dtype, pad=0, shift=0):
+    """`values` on the device as rows that are `pad` elements longer, `shift` elements behind an aligned address."""
+    shape = values.shape
+    store = torch.full((int(np.prod(shape[:-1])) * (shape[-1] + pad) + shift + 8,), float("nan"), dtype=TYPES[dtype], device="cuda")
+    strides, step = [1], shape[-1] + pad
+    for n in reversed(shape[1:-1]):
+        strides.insert(0, step)
+        step *= n
+    strides.insert(0, step)
+    view = torch.as_strided(store, shape, strides if len(shape) > 1 else [1], shift)
+    view.copy_(torch.from_numpy(np.asarray(values, dtype=np.float32)))
+    return view
+
+
+def check(got, want, dtype, extra=0.0):
+    got, want = f64(got), np.asarray(want)
+    size = np.max(np.abs(want)) if want.size else 0.0
+    tol = ROUND[dtype] * np.abs(want) + TINY[dtype] + ARITH * size + extra
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), f"{bad.sum()} of {bad.size}, worst {np.max(np.abs(got - want)):.3e} at size {size:.3e}"
+
+
+# ------------------------------------------------------------------------------------------------ group norm
+
+# samples, positions, channels, groups, pad, shift
+SHAPES = [
+    (1, 1, 1, 1, 0, 0),            # a group of one value
+    (2, 1, 16, 16, 0, 0),          # the same in vectors
+    (3, 1, 24, 3, 0, 0),           # one position
+    (3, 5, 7, 7, 0, 0),            # a group per channel, odd
+    (3, 5, 12, 3, 4, 1),           # rows inside wider rows, misaligned
+    (1, 64, 128, 32, 0, 0),        # four channels a group
+    (5, 221, 60, 5, 4, 0),         # twelve channels a group
+    (4, 33, 96, 8, 8, 0),
+    (2, 17, 4096, 4, 0, 0),        # more channels than a block has vectors
+    (1, 5000, 16, 2, 0, 0),        # many positions
+    (2, 1024, 64, 8, 0, 8),
+    (1, 20000, 40, 1, 0, 0),       # one group over everything
+    (70, 9, 32, 8, 0, 0),
+    (1, 70001, 32, 4, 0, 0),       # a sample of several megabytes
+]
+
+
+def norm_data(shape, seed, offset_mean=0.5):
+    n, s, c = shape
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((n, s, c)) * np.exp(0.3 * rng.standard_normal(c)) + offset_mean * rng.standard_normal(c)
+    return x, 1 + 0.2 * rng.standard_normal(c), 0.3 * rng.standard_normal(c), rng.standard_normal((n, s, c))
+
+
+def dev32(v):
+    return None if v is None else torch.from_numpy(np.asarray(v, dtype=np.float32)).cuda()
+
+
+def scratch(nbytes):
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+
+
+def forward(plan, x, gamma, beta, groups, dtype, pad=0, shift=0, **kw):
+    y = place(np.zeros(x.shape), dtype, pad, shift)
+    mean = torch.full((x.shape[0], groups), float("nan"), device="cuda")
+    rstd = torch.full((x.shape[0], groups), float("nan"), device="cuda")
+    ws = scratch(B.cr_group_norm_workspace_bytes(plan, x, groups))
+    B.cr_group_norm(plan, x, gamma, beta, groups, y, mean, rstd, workspace=ws, **kw)
+    return y, mean, rstd
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape", SHAPES)
+def test_group_norm_forward_and_backward(plan, shape, dtype):
+    n, s, c, groups, pad, shift = shape
+    act = ["none", "relu", "silu"][(n + s + groups) % 3]
+    p = [0.0, 0.3][(s + groups) % 2]
+    seed, offset = 1234567890123 + c, [0, 3, (1 << 33) + 2][(n + c) % 3]
+    xv, gv, bv, dyv = norm_data((n, s, c), seed % 1000)
+    x, dy = place(xv, dtype, pad, shift), place(dyv, dtype, pad, shift)
+    gamma, beta = dev32(gv), dev32(bv)
+    if n == 3:
+        gamma = beta = None
+    g64, b64 = (None, None) if gamma is None else (f64(gamma), f64(beta))
+    factors = O.dropout_factors((n, s, c), p, seed, offset) if p else None
+    kw = dict(act=B.CR_ACT[act], p=p, seed=seed, offset=offset)
+    y, mean, rstd = forward(plan, x, gamma, beta, groups, dtype, pad, shift, eps=1e-5, **kw)
+    want, mean64, rstd64, z = O.group_norm(f64(x), g64, b64, groups, 1e-5, act, factors)
+    check(mean, mean64, "f32", extra=1e-6 * np.max(np.abs(xv)))
+    # rstd: a group of one value has rstd = eps^-1/2 exactly; elsewhere the relative error of the variance halves
+    check(rstd, rstd64, "f32")
+    # z of a nearly constant group is rstd times a difference of nearly equal numbers, whose rounding rstd magnifies
+    spread = np.max(rstd64) * np.max(np.abs(xv)) * 2.0 ** -23
+    check(y, want, dtype, extra=4 * spread)
+    # backward, a partition per sample, rows of parameter gradients inside wider rows
+    parts = n
+    wide = torch.full((parts, 2 * c + 3), float("nan"), device="cuda")
+    dgamma, dbeta = wide[:, 1:c + 1], wide[:, c + 2:2 * c + 2]
+    dx = place(np.zeros(xv.shape), dtype, pad, shift)
+    ws = scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups))
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, dgamma, dbeta, workspace=ws, **kw)
+    dx64, dg64, db64, z, ag, ab = O.group_norm_backward(f64(dy), f64(x), g64, b64, groups, 1e-5, act, factors, parts)
+    # where z is within its own error of the kink of relu, either slope is right
+    edge = (np.abs(z) < 4 * spread + 1e-5) if act == "relu" else np.zeros(z.shape, bool)
+    top = np.max(np.abs(f64(dy))) * (1.0 if factors is None else np.max(factors))
+    near = edge.reshape(parts, -1, c).sum(1) * top
+    assert np.all(np.abs(f64(dbeta) - db64) <= 1e-5 * ab + near + 1e-30)
+    assert np.all(np.abs(f64(dgamma) - dg64) <= 1e-5 * ag + near * np.max(np.abs(z) + 1) + 4 * spread * ab + 1e-30)
+    assert torch.isnan(wide[:, 0]).all() and torch.isnan(wide[:, c + 1]).all() and torch.isnan(wide[:, 2 * c + 2]).all()
+    assert edge.mean() < 0.01 or z.size < 100
+    gsize = 1.0 if g64 is None else np.max(np.abs(g64))
+    extra = np.max(rstd64) * gsize * top * (np.max(near) / top / max(1, s) * 4 + 8 * spread + 1e-6)
+    check(torch.where(torch.from_numpy(edge).cuda(), torch.zeros_like(dx), dx), np.where(edge, 0, dx64), dtype, extra=extra)
+
+
+def test_a_group_of_one_value_has_no_gradient(plan):
+    xv, gv, bv, dyv = norm_data((4, 1, 8), 3)
+    x, dy = place(xv, "f32"), place(dyv, "f32")
+    gamma, beta = dev32(gv), dev32(bv)
+    y, mean, rstd = forward(plan, x, gamma, beta, 8, "f32")
+    assert torch.equal(y, beta.expand(4, 1, 8))
+    dx = torch.full_like(x, float("nan"))
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, 8, dx,
+                             workspace=scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, 8)))
+    assert torch.equal(dx, torch.zeros_like(dx))
+
+
+@pytest.mark.parametrize("shape", [(2, 50, 32, 4), (1, 3000, 64, 8), (2, 7, 30, 5)])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_group_norm_gradient_against_differences(plan, shape, act):
+    """<dL/dx, v> against (L(x + h v) - L(x - h v)) / 2h for L = <y, u>, and the same for gamma and beta, with the
+    kernel's own forward pass in fp32.  With h = 2^-6 the third-order term is about h^2 / 6 = 4e-5 of the value; the
+    rounding of y (2^-24 of values of a few units, over count^1/2 random terms, divided by h) adds 1e-5 count^1/2."""
+    n, s, c, groups = shape
+    xv, gv, bv, uv = norm_data((n, s, c), 77)
+    rng = np.random.default_rng(78)
+    p, seed, offset = 0.25, 99, 5
+    kw = dict(act=B.CR_ACT[act], p=p, seed=seed, offset=offset)
+    gamma, beta = dev32(gv), dev32(bv)
+    x, u = place(xv, "f32"), place(uv, "f32")
+    _, mean, rstd = forward(plan, x, gamma, beta, groups, "f32", **kw)
+    dx, dg, db = torch.empty_like(x), torch.empty((1, c), device="cuda"), torch.empty((1, c), device="cuda")
+    B.cr_group_norm_backward(plan, u, x, gamma, beta, mean, rstd, groups, dx, dg, db,
+                             workspace=scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups)), **kw)
+    h = 2.0 ** -6
+
+    def loss(x, gamma, beta):
+        return float(np.sum(f64(forward(plan, x, gamma, beta, groups, "f32", **kw)[0]) * f64(u)))
+
+    for which, grad in (("x", dx), ("gamma", dg[0]), ("beta", db[0])):
+        v = torch.from_numpy(rng.standard_normal(tuple(grad.shape)).astype(np.float32)).cuda()
+        args = {"x": x, "gamma": gamma, "beta": beta}
+        ends = [loss(**{**args, which: args[which] + sign * h * v}) for sign in (1, -1)]
+        slope = (ends[0] - ends[1]) / (2 * h)
+        want = float(np.sum(f64(grad) * f64(v)))
+        size = float(np.linalg.norm(f64(grad))) * float(np.linalg.norm(f64(v))) / np.sqrt(v.numel())
+        assert abs(slope - want) <= 1e-3 * (abs(want) + size) + 1e-5 * np.sqrt(x.numel())
+
+
+def test_partitions_add_up_and_do_not_see_each_other(plan):
+    """Per-partition gradients are what a worker that holds the partition alone computes, bit for bit: the same
+    samples, the index of its first element as offset."""
+    n, s, c, groups, parts = 12, 40, 64, 8, 4
+    xv, gv, bv, dyv = norm_data((n, s, c), 5)
+    x, dy = place(xv, "bf16"), place(dyv, "bf16")
+    gamma, beta = dev32(gv), dev32(bv)
+    kw = dict(act=B.CR_ACT_SILU, p=0.2, seed=11)
+    y, mean, rstd = forward(plan, x, gamma, beta, groups, "bf16", offset=7, **kw)
+    dx, dg, db = torch.empty_like(x), torch.empty((parts, c), device="cuda"), torch.empty((parts, c), device="cuda")
+    ws = scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups))
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, dg, db, workspace=ws, offset=7, **kw)
+    per = n // parts
+    for q in range(parts):
+        mine = slice(q * per, (q + 1) * per)
+        offset = 7 + q * per * s * c
+        y1, mean1, rstd1 = forward(plan, x[mine], gamma, beta, groups, "bf16", offset=offset, **kw)
+        assert torch.equal(y1, y[mine]) and torch.equal(mean1, mean[mine]) and torch.equal(rstd1, rstd[mine])
+        dx1, dg1, db1 = torch.empty_like(x[mine]), torch.empty((1, c), device="cuda"), torch.empty((1, c), device="cuda")
+        B.cr_group_norm_backward(plan, dy[mine], x[mine], gamma, beta, mean1, rstd1, groups, dx1, dg1, db1, workspace=ws,
+                                 offset=offset, **kw)
+        assert torch.equal(dx1, dx[mine]) and torch.equal(dg1[0], dg[q]) and torch.equal(db1[0], db[q])
+
+
+def test_a_nan_stays_in_its_group_and_statistics_survive_a_large_mean(plan):
+    n, s, c, groups = 3, 100, 32, 4
+    xv, gv, bv, _ = norm_data((n, s, c), 6)
+    x = place(xv, "f32")
+    x[1, 7, 9] = float("nan")
+    y, mean, rstd = forward(plan, x, dev32(gv), dev32(bv), groups, "f32")
+    dead = torch.zeros((n, s, c), dtype=torch.bool, device="cuda")
+    dead[1, :, 8:16] = True
+    assert torch.isnan(y[dead]).all() and torch.isfinite(y[~dead]).all()
+    # mean 4096, spread 1: x holds the spread to 2^-12 / 2, sums of squares of x itself would lose it
+    rng = np.random.default_rng(8)
+    x = place(4096 + rng.standard_normal((2, 3000, 32)), "f32")
+    y, mean, rstd = forward(plan, x, None, None, 4, "f32")
+    want, mean64, rstd64, _ = O.group_norm(f64(x), None, None, 4, 1e-5)
+    # the mean is known to half a unit of 4096 (2^-12); that is the error of x - mean, one part in 4096
+    assert np.max(np.abs(f64(mean) - mean64)) <= 2.0 ** -11
+    assert np.max(np.abs(f64(rstd) / rstd64 - 1)) <= 1e-5
+    assert np.max(np.abs(f64(y) - want)) <= 2.0 ** -10
+
+
+def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
+    xv, gv, bv, dyv = norm_data((6, 300, 64), 9)
+    gamma, beta = dev32(gv), dev32(bv)
+    x = place(xv, "f16")
+    y, mean, rstd = forward(plan, x, gamma, beta, 8, "f16", act=B.CR_ACT_RELU)
+    ws = scratch(B.cr_group_norm_workspace_bytes(plan, x, 8))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        x2 = x.clone()
+        B.cr_group_norm(plan, x2, gamma, beta, 8, x2, act=B.CR_ACT_RELU, workspace=ws)
+    side.synchronize()
+    assert torch.equal(x2, y)
+    dy = place(dyv, "f16")
+    ws = scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, 8))
+    dx, dg, db = torch.empty_like(x), torch.empty((2, 64), device="cuda"), torch.empty((2, 64), device="cuda")
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, 8, dx, dg, db, act=B.CR_ACT_RELU, workspace=ws)
+    only = torch.empty((2, 64), device="cuda")
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, 8, None, None, only, act=B.CR_ACT_RELU, workspace=ws)
+    assert torch.equal(only, db)
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, 8, dy, act=B.CR_ACT_RELU, workspace=ws)
+    assert torch.equal(dy, dx)
+
+
+def test_group_norm_of_no_samples(plan):
+    x = torch.empty((0, 5, 8), device="cuda")
+    B.cr_group_norm(plan, x, None, None, 2, torch.empty_like(x), torch.empty((0, 2), device="cuda"), torch.empty((0, 2), device="cuda"))
+    dg = torch.full((3, 8), float("nan"), device="cuda")
+    db = torch.full((3, 8), float("nan"), device="cuda")
+    B.cr_group_norm_backward(plan, x, x, None, None, torch.empty((0, 2), device="cuda"), torch.empty((0, 2), device="cuda"), 2,
+                             torch.empty_like(x), dg, db)
+    assert not dg.any() and not db.any()
+
+
+def test_group_norm_step_in_a_graph(plan):
+    xv, gv, bv, dyv = norm_data((8, 256, 64), 12)
+    x, dy, gamma, beta = place(xv, "bf16"), place(dyv, "bf16"), dev32(gv), dev32(bv)
+    y, mean, rstd = torch.empty_like(x), torch.empty((8, 8), device="cuda"), torch.empty((8, 8), device="cuda")
+    dx, dg, db = torch.empty_like(x), torch.empty((4, 64), device="cuda"), torch.empty((4, 64), device="cuda")
+    ws1 = scratch(B.cr_group_norm_workspace_bytes(plan, x, 8))
+    ws2 = scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, 8))
+    kw = dict(act=B.CR_ACT_SILU, p=0.1, seed=4)
+
+    def step():
+        B.cr_group_norm(plan, x, gamma, beta, 8, y, mean, rstd, workspace=ws1, **kw)
+        B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, 8, dx, dg, db, workspace=ws2, **kw)
+
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (y, mean, rstd, dx, dg, db)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for t in (y, mean, rstd, dx, dg, db):
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, (y, mean, rstd, dx, dg, db)))
+    del graph
+
+
+# ------------------------------------------------------------------------------------------------ dropout
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,cols,pad,shift", [(1, 1, 0, 0), (1, 7, 0, 0), (3, 8, 0, 0), (39, 5004, 0, 0), (5, 100, 12, 0),
+                                                 (17, 33, 3, 1), (4, 64, 0, 2), (300, 96, 32, 0), (1, 100003, 0, 0)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_dropout(plan, rows, cols, pad, shift, dtype, residual):
+    rng = np.random.default_rng(rows * cols)
+    p, seed = [0.5, 0.1, 0.9][(rows + cols) % 3], (1 << 63) + 12345
+    x = place(rng.standard_normal((rows, cols)), dtype, pad, shift)
+    r = place(rng.standard_normal((rows, cols)), dtype, 0, shift) if residual else None
+    for offset in (0, 1, 2, 3, (1 << 40) + 7):
+        y = place(np.zeros((rows, cols)), dtype, pad, 0)
+        B.cr_dropout(plan, x, y, p, seed, offset=offset, residual=r)
+        want = f64(x) * O.dropout_factors((rows, cols), p, seed, offset)
+        if residual:
+            want = want + f64(r)
+        else:
+            assert np.array_equal(f64(y) == 0, want == 0)     # the mask itself
+        assert np.all(np.abs(f64(y) - want) <= ROUND[dtype] * np.abs(want) + TINY[dtype] + 3e-7 * np.max(np.abs(f64(x))) * 10)
+
+
+def test_dropout_of_parts_is_the_part_of_the_dropout(plan):
+    x = torch.randn(1000, 37, device="cuda")
+    y = torch.empty_like(x)
+    B.cr_dropout(plan, x, y, 0.3, 42)
+    for a, b in ((0, 1), (1, 400), (400, 1000)):
+        part = torch.empty_like(x[a:b])
+        B.cr_dropout(plan, x[a:b], part, 0.3, 42, offset=a * 37)
+        assert torch.equal(part, y[a:b])
+    keep = float((y != 0).float().mean())
+    assert abs(keep - 0.7) <= 5 * (0.7 * 0.3 / 37000) ** 0.5      # five standard deviations
+    other = torch.empty_like(x)
+    B.cr_dropout(plan, x, other, 0.3, 43)
+    both = float(((y != 0) & (other != 0)).float().mean())         # independent masks keep 0.49 of the elements in common
+    assert abs(both - 0.49) <= 5 * (0.49 * 0.51 / 37000) ** 0.5
+
+
+def test_dropout_ends_of_p_and_dropped_infinities(plan):
+    for dtype in TYPES.values():
+        x = torch.randn(50, 64, device="cuda").to(dtype)
+        y = torch.empty_like(x)
+        B.cr_dropout(plan, x, y, 0.0, 1)
+        assert torch.equal(x, y)
+        bad = torch.full_like(x, float("nan"))
+        bad[::2] = float("inf")
+        B.cr_dropout(plan, bad, y, 1.0, 1)
+        assert not y.any()
+        B.cr_dropout(plan, bad, y, 1.0, 1, residual=x)
+        assert torch.equal(x, y)
+        B.cr_dropout(plan, bad, y, 0.5, 1)
+        gone = torch.from_numpy(O.dropout_factors((50, 64), 0.5, 1, 0) == 0).cuda()
+        assert not y[gone].any() and not torch.isfinite(y[~gone]).any()
+        z = x.clone()
+        B.cr_dropout(plan, x, y, 0.25, 9, residual=x)
+        B.cr_dropout(plan, z, z, 0.25, 9, residual=z)              # in place
+        assert torch.equal(y, z)
+    B.cr_dropout(plan, torch.empty((0, 5), device="cuda"), torch.empty((0, 5), device="cuda"), 0.5, 1)
+
+
+# ------------------------------------------------------------------------------------------------ 8-bit products
+
+def strided_codes(codes, ld, shift=0):
+    rows, cols = codes.shape
+    store = torch.full((rows * ld + shift + 16,), 77, dtype=torch.int8, device="cuda")
+    view = torch.as_strided(store, (rows, cols), (ld, 1), shift)
+    view.copy_(torch.from_numpy(codes.astype(np.int8)))
+    return view
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (3, 7, 0), (5, 64, 0), (2, 4096, 0), (39, 5004, 12), (4, 9000, 0), (1, 40000, 8), (6, 333, 3)])
+def test_quantize_rows(plan, rows, cols, pad, dtype):
+    rng = np.random.default_rng(cols)
+    values = rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))
+    if rows > 2:
+        values[1] = 0.0
+    x = place(values, dtype, pad)
+    for ld in ((cols + 15) // 16 * 16, cols):
+        q = strided_codes(np.full((rows, cols), 55), ld)
+        scale = torch.full((rows,), float("nan"), device="cuda")
+        B.cr_quantize_rows(plan, x, q, scale)
+        codes, want = O.quantize_rows(f64(x))
+        assert np.array_equal(q.cpu().numpy().astype(np.int64), codes)
+        assert np.array_equal(scale.cpu().numpy(), want)
+
+
+def test_quantize_rows_at_the_ends_of_the_range(plan):
+    x = torch.zeros(9, 256, device="cuda")
+    x[0] = torch.linspace(-1, 1, 256, device="cuda") * 3.4028234e38
+    x[1, 3] = float("inf")
+    x[2, 200] = float("nan")
+    x[3] = torch.linspace(-1, 1, 256, device="cuda") * 2.0 ** -120
+    x[4] = torch.linspace(-1, 1, 256, device="cuda") * 2.0 ** -121
+    x[5, 0] = 1e-45
+    x[6] = 5.0
+    x[7] = (torch.arange(256, device="cuda") - 127.5).clamp(-127, 127)     # ties: half a code everywhere
+    q = torch.full((9, 256), 55, dtype=torch.int8, device="cuda")
+    scale = torch.empty(9, device="cuda")
+    B.cr_quantize_rows(plan, x, q, scale)
+    codes, want = O.quantize_rows(x.cpu().numpy())
+    assert np.array_equal(q.cpu().numpy().astype(np.int64), codes)
+    assert np.array_equal(scale.cpu().numpy(), want, equal_nan=True)
+
+
+PRODUCTS = [(1, 1, 1), (1, 16, 16), (1, 4096, 512), (2, 64, 130), (3, 77, 7), (15, 128, 128), (16, 129, 129), (17, 640, 1),
+            (33, 160, 300), (39, 5004, 1001), (64, 256, 256), (65, 272, 257), (100, 1000, 96), (129, 512, 384), (200, 2048, 130),
+            (257, 96, 64), (300, 1040, 520), (1000, 48, 1000), (2048, 384, 256)]
+
+
+@pytest.mark.parametrize("elem", list(TYPES))
+@pytest.mark.parametrize("tokens,inner,outer", PRODUCTS)
+def test_int8_product(plan, tokens, inner, outer, elem):
+    rng = np.random.default_rng(tokens + inner + outer)
+    xc = rng.integers(-127, 128, (tokens, inner))
+    wc = rng.integers(-128, 128, (outer, inner))
+    xs, ws = np.exp(rng.standard_normal(tokens)).astype(np.float32) / 50, np.exp(rng.standard_normal(outer)).astype(np.float32) / 900
+    bias = rng.standard_normal(outer).astype(np.float32) if tokens % 2 else None
+    want, sums = O.int8_product(xc, wc, xs, ws, bias)
+    up = (inner + 15) // 16 * 16
+    # rows on 16-byte boundaries, wider rows, and rows that start anywhere; outputs inside wider rows
+    for ldx, ldw, shift, pad in ((up, up, 0, 0), (up + 16, up + 32, 16, 3), (inner, inner + 1, 1, 1)):
+        x, w = strided_codes(xc, ldx, shift), strided_codes(wc, ldw, shift)
+        y = place(np.zeros((tokens, outer)), elem, pad)
+        B.cr_int8_product(plan, x, dev32(xs), w, dev32(ws), y, bias=dev32(bias))
+        got = f64(y)
+        # the sum is exact; its conversion, the product of the scales, the product and the sum with the bias round once each
+        size = np.abs(sums * xs[:, None].astype(np.float64) * ws[None, :].astype(np.float64)) + (0 if bias is None else np.abs(bias))
+        assert np.all(np.abs(got - want) <= 4 * 2.0 ** -24 * size + ROUND[elem] * 1.01 * np.abs(want) + TINY[elem])
+
+
+def test_int8_product_longest_sum_and_nan_scales(plan):
+    inner = 131071
+    x = torch.full((2, 131072), -128, dtype=torch.int8, device="cuda")[:, :inner]
+    w = torch.full((130, 131072), -128, dtype=torch.int8, device="cuda")[:, :inner]
+    w[5] = 127
+    one = torch.ones(130, device="cuda")
+    y = torch.empty((2, 130), device="cuda")
+    B.cr_int8_product(plan, x, torch.tensor([1.0, float("nan")], device="cuda"), w, one, y)
+    want = torch.full((130,), float(128 * 128 * inner), device="cuda")
+    want[5] = float(-128 * 127 * inner)
+    assert torch.equal(y[0], want) and torch.isnan(y[1]).all()
+
+
+def test_int8_product_of_nothing_and_repeats_itself(plan):
+    w = torch.zeros((16, 64), dtype=torch.int8, device="cuda")
+    B.cr_int8_product(plan, torch.empty((0, 64), dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda"), w,
+                      torch.ones(16, device="cuda"), torch.empty((0, 16), device="cuda"))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randint(-127, 128, (300, 4096), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-127, 128, (1024, 4096), generator=g, device="cuda", dtype=torch.int8)
+    xs, ws = torch.rand(300, device="cuda"), torch.rand(1024, device="cuda")
+    full = torch.empty((300, 1024), device="cuda")
+    B.cr_int8_product(plan, x, xs, w, ws, full)
+    # a token's result does not depend on the tokens beside it (other tiles, other splits of k)
+    for a, b in ((0, 1), (1, 18), (18, 100), (100, 300)):
+        part = torch.empty((b - a, 1024), device="cuda")
+        B.cr_int8_product(plan, x[a:b], xs[a:b], w, ws, part)
+        assert torch.equal(part, full[a:b])
+
+
+# ------------------------------------------------------------------------------------------------ refusals
+
+def test_refusals_launch_nothing(plan):
+    x = torch.zeros(4, 10, 8, device="cuda")
+    y, stats = torch.empty_like(x), torch.empty((4, 2), device="cuda")
+    params = torch.empty((4, 8), device="cuda")
+    ws = scratch(1 << 20)
+    q, codes = torch.zeros((4, 64), dtype=torch.int8, device="cuda"), torch.zeros((4, 8), dtype=torch.int8, device="cuda")
+    one, out = torch.ones(4, device="cuda"), torch.empty((4, 4), device="cuda")
+    lib, before = B.lib(), B.cr_plan_launch_count(plan)
+    bad = B.CR_ERR_INVALID_ARG
+    p = lambda t: t.data_ptr()  # noqa: E731
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def desc(**kw):
+        v = dict(samples=4, positions=10, channels=8, groups=2, elem=0, act=0, eps=1e-5, p=0.0, seed=0, offset=0)
+        v.update(kw)
+        return B.cr_group_norm_t(**v)
+
+    for kw in (dict(samples=-1), dict(positions=0), dict(channels=0), dict(groups=0), dict(groups=3), dict(elem=3), dict(elem=-1), dict(act=3),
+               dict(eps=-1.0), dict(eps=float("nan")), dict(p=-0.1), dict(p=1.1), dict(p=float("nan")), dict(offset=-1)):
+        assert lib.cr_group_norm(plan, desc(**kw), p(x), 8, 0, 0, p(y), 8, 0, 0, p(ws), 1 << 20, stream) == bad, kw
+        assert lib.cr_group_norm_workspace_bytes(plan, desc(**kw)) == 0
+        assert lib.cr_group_norm_backward(plan, desc(**kw), p(x), 8, p(x), 8, 0, 0, p(stats), p(stats), p(y), 8, 0, 0, 8, 1, p(ws),
+                                          1 << 20, stream) == bad, kw
+    d = desc()
+    assert lib.cr_group_norm(plan, d, 0, 8, 0, 0, p(y), 8, 0, 0, p(ws), 1 << 20, stream) == bad           # no x
+    assert lib.cr_group_norm(plan, d, p(x), 7, 0, 0, p(y), 8, 0, 0, p(ws), 1 << 20, stream) == bad        # rows overlap
+    assert lib.cr_group_norm(plan, d, p(x) + 2, 8, 0, 0, p(y), 8, 0, 0, p(ws), 1 << 20, stream) == bad    # off its element
+    assert lib.cr_group_norm(plan, d, p(x), 8, 0, 0, p(y), 8, p(stats), 0, p(ws), 1 << 20, stream) == bad  # mean without rstd
+    assert lib.cr_group_norm(0, d, p(x), 8, 0, 0, p(y), 8, 0, 0, p(ws), 1 << 20, stream) == bad
+    back = lambda parts, ldp, nbytes, rstd=stats: lib.cr_group_norm_backward(  # noqa: E731
+        plan, d, p(x), 8, p(x), 8, 0, 0, p(stats), 0 if rstd is None else p(rstd), p(y), 8, p(params), 0, ldp, parts, p(ws), nbytes, stream)
+    assert back(3, 8, 1 << 20) == bad and back(0, 8, 1 << 20) == bad and back(4, 7, 1 << 20) == bad and back(4, 8, 1 << 20, None) == bad
+    need = lib.cr_group_norm_backward_workspace_bytes(plan, d)
+    assert need and back(4, 8, need - 1) == B.CR_ERR_OOM
+    drop = lambda ld=8, rows=40, elem=0, pr=0.5, off=0: lib.cr_dropout(plan, p(x), ld, 0, 0, p(y), 8, rows, 8, elem, pr, 1, off, stream)  # noqa: E731
+    assert [drop(ld=7), drop(rows=-1), drop(elem=9), drop(pr=2.0), drop(pr=float("nan")), drop(off=-4)] == [bad] * 6
+    quant = lambda rows=4, cols=8, ldq=8, elem=0: lib.cr_quantize_rows(plan, p(x), 8, rows, cols, elem, p(codes), ldq, p(one), stream)  # noqa: E731
+    assert [quant(rows=-1), quant(cols=0), quant(ldq=7), quant(elem=5)] == [bad] * 4
+    prod = lambda k=64, ld=64, elem=0, m=4, sc=one: lib.cr_int8_product(  # noqa: E731
+        plan, p(q), ld, p(sc) if sc is not None else 0, p(q), 64, p(one), 0, p(out), 4, m, 4, k, elem, stream)
+    assert [prod(k=0), prod(k=131072), prod(ld=63), prod(elem=3), prod(m=-1), prod(sc=None)] == [bad] * 6
+    host = B.cr_plan_create(4, 2, 1, 24, 1024, device=-1)
+    assert lib.cr_dropout(host, p(x), 8, 0, 0, p(y), 8, 40, 8, 0, 0.5, 1, 0, stream) == B.CR_ERR_CUDA
+    B.cr_plan_destroy(host)
+    assert B.cr_plan_launch_count(plan) == before
+    # the binding's own checks
+    for call in (lambda: B.cr_dropout(plan, x, y[:2], 0.5, 1), lambda: B.cr_dropout(plan, x, y.half(), 0.5, 1),
+                 lambda: B.cr_dropout(plan, x.double(), y, 0.5, 1), lambda: B.cr_dropout(plan, x.cpu(), y, 0.5, 1),
+                 lambda: B.cr_dropout(plan, x.transpose(0, 1), y.transpose(0, 1), 0.5, 1),
+                 lambda: B.cr_dropout(plan, x[..., ::2], y[..., ::2], 0.5, 1),
+                 lambda: B.cr_group_norm(plan, x, one, None, 2, y, workspace=ws),
+                 lambda: B.cr_group_norm(plan, x[0], None, None, 2, y[0], workspace=ws),
+                 lambda: B.cr_int8_product(plan, x[0], one, q, one, out), lambda: B.cr_int8_product(plan, q[:, :32], one, q, one, out),
+                 lambda: B.cr_quantize_rows(plan, x[0], q[:, :8], one)):
+        with pytest.raises(ValueError):
+            call()
+    assert B.cr_plan_launch_count(plan) == before
