@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcodedreduce.so")
 SOURCES = ["cr_plan.cpp", "cr_kernels.cu", "cr_tc.cu", "cr_layers.cu", "cr_int8.cu", "cr_api.cu"]
-HEADERS = ["cr_plan.hpp", "cr_kernels.hpp", "cr_layers.hpp", "cr_elem.cuh"]
+HEADERS = ["cr_plan.hpp", "cr_kernels.hpp", "cr_layers.hpp", "cr_elem.cuh", "cr_tcgen05.cuh"]
 
 
 def _nvcc() -> str:

@@ -10,6 +10,7 @@
 #include <cstdint>
 
 #include "cr_elem.cuh"
+#include "cr_tcgen05.cuh"
 
 namespace cr {
 namespace {
@@ -140,6 +141,248 @@ __global__ void __launch_bounds__(256) cr_int8_product_bytes_kernel(const Int8Pr
     }
 }
 
+// ---- product on the tensor cores ------------------------------------------------------------------------------------------
+//
+// The weights are the matrix operand of 128 rows, the tokens the columns: D[channel][token], 128 x TN 32-bit integers in
+// tensor memory, so one token needs a tile of 16 columns and not of 128 rows, and a warp that reads a column out holds
+// 32 neighbouring channels of one token, which it stores as they lie in y.
+// Warp 0 streams boxes of 128 bytes of k (128 weight rows, TN token rows, 128-byte swizzle) into a ring; one thread of
+// warp 1 issues four tcgen05.mma (kind::i8, 32 bytes of k each) per box into one of two accumulators; warps 2..5 read
+// the other one, scale it and store it.  CTAs are persistent over the tiles.
+// Where there are fewer tiles than SMs a cluster of `splits` CTAs shares a tile, each with its part of k: they leave
+// their integer sums in shared memory and every one of them adds up and stores its share of the tokens.
+
+struct TcArgs {
+    const float *x_scale, *w_scale, *bias;
+    void *y;
+    long long ld_y;
+    int tokens, outer;
+    int tiles_m, tiles_n;   // tiles of TN tokens, of 128 channels
+    int chunks;             // 128-byte chunks of k
+    int stages;
+    int *status;
+    unsigned long long wait_ns;
+};
+
+constexpr int kChunk = 128;           // bytes of k per box
+constexpr int kRows = 128;            // channels per tile
+constexpr int kBand = 12;             // tiles of tokens that share a sweep over the channels (L2 holds their rows)
+
+// Tiles are numbered so that CTAs which run together cover a near-square patch of the output.
+__device__ __forceinline__ void tile_at(const TcArgs &a, int t, int &tm, int &tn) {
+    const int per_band = kBand * a.tiles_n;
+    const int band = t / per_band, in = t - band * per_band;
+    const int height = min(kBand, a.tiles_m - band * kBand);
+    tn = in / height;
+    tm = band * kBand + in - tn * height;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_output(const TcArgs &a, int token, int channel, int sum, float xs, float ws, float b) {
+    static_cast<T *>(a.y)[(long long)token * a.ld_y + channel] = from_float<T>(fmaf((float)sum, xs * ws, b));
+}
+
+template <typename T, int TN>
+__global__ void __launch_bounds__(192, 1)
+cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const TcArgs a, const int splits) {
+    using namespace i8;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    constexpr uint32_t kWBytes = kRows * kChunk, kStage = kWBytes + TN * kChunk;
+    constexpr uint32_t kCols = 2 * TN < 32 ? 32 : 2 * TN;
+    const int S = a.stages;
+    unsigned char *ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint64_t *full = reinterpret_cast<uint64_t *>(ring + (size_t)S * kStage);
+    uint64_t *empty = full + S;
+    uint64_t *acc_full = empty + S, *acc_empty = acc_full + 2;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    volatile int *flags = reinterpret_cast<volatile int *>(tmem_slot + 1);   // [0] someone gave up, [1] never set
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = splits > 1 ? (int)cluster_rank() : 0;
+    const int first = (int)blockIdx.x / splits, step = (int)gridDim.x / splits;
+    const int tiles = a.tiles_m * a.tiles_n;
+    const int k0 = (int)((long long)a.chunks * rank / splits), k1 = (int)((long long)a.chunks * (rank + 1) / splits);
+
+    if (tid == 0) {
+        for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], 4); }
+        flags[0] = 0; flags[1] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(tmem_slot, kCols);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int issued = 0, s = 0;
+            uint32_t phase = 1;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step) {
+                int tm, tn;
+                tile_at(a, t, tm, tn);
+                for (int k = k0; k < k1; ++k) {
+                    if (!mbar_wait(&empty[s], phase, &flags[0], a.wait_ns)) { ok = false; break; }
+                    unsigned char *st = ring + (size_t)s * kStage;
+                    mbar_expect_tx(&full[s], kStage);
+                    tma_load_2d(st, &map_w, k * kChunk, tn * kRows, &full[s]);
+                    tma_load_2d(st + kWBytes, &map_x, k * kChunk, tm * TN, &full[s]);
+                    ++issued;
+                    if (++s == S) { s = 0; phase ^= 1; }
+                }
+            }
+            if (!ok) {
+                flags[0] = 1;
+                atomicExch(a.status, 1);
+                for (int i = issued > S ? issued - S : 0; i < issued; ++i)
+                    mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), &flags[1], a.wait_ns);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = instr_desc(kRows, TN);
+            int s = 0, use = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step, ++use) {
+                const int set = use & 1;
+                if (!mbar_wait(&acc_empty[set], (uint32_t)(((use >> 1) & 1) ^ 1), &flags[0], a.wait_ns)) { ok = false; break; }
+                tc_fence_after();
+                for (int k = k0; k < k1; ++k) {
+                    if (!mbar_wait(&full[s], phase, &flags[0], a.wait_ns)) { ok = false; break; }
+                    tc_fence_after();
+                    const unsigned char *st = ring + (size_t)s * kStage;
+#pragma unroll
+                    for (int q = 0; q < kChunk / 32; ++q)
+                        mma_i8(tmem + (uint32_t)(set * TN), smem_desc(st + q * 32), smem_desc(st + kWBytes + q * 32), idesc, (k > k0 || q > 0) ? 1u : 0u);
+                    mma_commit(&empty[s]);
+                    if (++s == S) { s = 0; phase ^= 1; }
+                }
+                if (ok) mma_commit(&acc_full[set]);
+            }
+            if (!ok) { flags[0] = 1; atomicExch(a.status, 1); }
+        }
+    } else {
+        const int q = warp & 3;
+        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
+        int use = 0;
+        for (int t = first; t < tiles; t += step, ++use) {
+            const int set = use & 1;
+            int tm, tn;
+            tile_at(a, t, tm, tn);
+            const int channel = tn * kRows + q * 32 + lane;
+            const bool mine = channel < a.outer;
+            const float ws = mine ? __ldg(a.w_scale + channel) : 0.f;
+            const float b = mine && a.bias ? __ldg(a.bias + channel) : 0.f;
+            const bool ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[set], (uint32_t)((use >> 1) & 1), &flags[0], a.wait_ns) ? 1 : 0) != 0;
+            if (!ok) {
+                if (lane == 0) { flags[0] = 1; atomicExch(a.status, 1); }
+                break;
+            }
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < TN; c += 16) {
+                const int token0 = tm * TN + c;
+                if (token0 >= a.tokens && splits == 1) break;
+                int r[16];
+                tmem_load_16(lanes + (uint32_t)(set * TN + c), r);
+                if (splits > 1) {
+                    // every MMA that read the ring has finished: its memory takes the sums
+                    int *sums = reinterpret_cast<int *>(ring);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sums[(c + j) * kRows + q * 32 + lane] = r[j];
+                } else {
+                    const float xs_mine = token0 + (lane & 15) < a.tokens ? __ldg(a.x_scale + token0 + (lane & 15)) : 0.f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float xs = __shfl_sync(0xffffffffu, xs_mine, j);
+                        if (mine && token0 + j < a.tokens) store_output<T>(a, token0 + j, channel, r[j], xs, ws, b);
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&acc_empty[set]);
+        }
+    }
+    // tensor memory goes back before the cluster meets: a CTA that holds some never waits for another CTA
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_free(tmem, kCols);
+    __syncthreads();
+    if (splits > 1) {
+        cluster_sync();      // all sums of the cluster are in place
+        int tm, tn;
+        tile_at(a, first, tm, tn);
+        const int c0 = TN * rank / splits, c1 = TN * (rank + 1) / splits;
+        for (int e = tid; e < (c1 - c0) * kRows; e += 192) {
+            const int c = c0 + e / kRows, l = e % kRows;
+            const int token = tm * TN + c, channel = tn * kRows + l;
+            if (token >= a.tokens || channel >= a.outer) continue;
+            const uint32_t at = smem_u32(ring) + (uint32_t)(c * kRows + l) * 4;
+            int sum = 0;
+            for (int r = 0; r < splits; ++r) sum += load_cluster(map_to_rank(at, (uint32_t)r));
+            store_output<T>(a, token, channel, sum, __ldg(a.x_scale + token), __ldg(a.w_scale + channel), a.bias ? __ldg(a.bias + channel) : 0.f);
+        }
+        cluster_sync();      // nobody leaves while its sums may be read
+    }
+}
+
+CUresult encode_codes(EncodeTiledFn encode, CUtensorMap *map, const void *base, int64_t cols, int64_t rows, int64_t ld, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {kChunk, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+template <typename T, int TN>
+cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &dev, const Tuning &tune, EncodeTiledFn encode,
+                      cudaStream_t stream, int64_t *launches) {
+    TcArgs a;
+    a.x_scale = p.x_scale; a.w_scale = p.w_scale; a.bias = p.bias; a.y = p.y; a.ld_y = p.ld_y;
+    a.tokens = (int)p.tokens; a.outer = (int)p.outer;
+    a.tiles_m = (int)((p.tokens + TN - 1) / TN); a.tiles_n = (int)((p.outer + kRows - 1) / kRows);
+    a.chunks = (int)((p.inner + kChunk - 1) / kChunk);
+    a.status = status; a.wait_ns = tune.wait_limit_ns;
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+    if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
+    int splits = 1;
+    while (splits < 8 && tiles * splits * 2 <= dev.sm_count && a.chunks >= 2 * splits * 2) splits *= 2;
+    constexpr size_t kStage = (kRows + TN) * kChunk;
+    const size_t tail = 1024 + 256;
+    const size_t room = (size_t)dev.smem_optin - tail;
+    int stages = (int)std::min<size_t>(8, room / kStage);
+    const int per_cta = (a.chunks + splits - 1) / splits;
+    // a ring no deeper than the CTA's work, but large enough for the sums of a split tile
+    if (tiles * splits <= dev.sm_count) stages = std::max(std::min(stages, per_cta), (int)((TN * kRows * 4 + kStage - 1) / kStage));
+    a.stages = stages;
+    const size_t smem = stages * kStage + (2 * stages + 4) * 8 + 16 + 1024;
+    CUtensorMap map_w, map_x;
+    if (encode_codes(encode, &map_w, p.w, p.inner, p.outer, p.ld_w, kRows) != CUDA_SUCCESS ||
+        encode_codes(encode, &map_x, p.x, p.inner, p.tokens, p.ld_x, TN) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+    cudaError_t e = cudaFuncSetAttribute(cr_int8_product_kernel<T, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : std::min<int64_t>(tiles, dev.sm_count)));
+    cfg.blockDim = dim3(192);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, cr_int8_product_kernel<T, TN>, map_w, map_x, a, splits);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
 template <typename F>
 cudaError_t by_type(int elem, F &&f) {
     switch (elem) {
@@ -169,9 +412,20 @@ cudaError_t launch_quantize_rows(const void *x, int64_t rows, int64_t cols, int6
     });
 }
 
-cudaError_t launch_int8_product(const Int8ProductArgs &a, int *, const DeviceInfo &, const Tuning &, EncodeTiledFn,
+cudaError_t launch_int8_product(const Int8ProductArgs &a, int *status, const DeviceInfo &dev, const Tuning &tune, EncodeTiledFn encode,
                                 cudaStream_t stream, int64_t *launches) {
     if (a.tokens == 0 || a.outer == 0) return cudaSuccess;
+    auto on16 = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 16 == 0; };
+    if (encode && on16(a.x, a.ld_x) && on16(a.w, a.ld_w)) {
+        return by_type(a.elem, [&](auto t) {
+            using T = decltype(t);
+            if (a.tokens <= 16) return launch_tc<T, 16>(a, status, dev, tune, encode, stream, launches);
+            if (a.tokens <= 32) return launch_tc<T, 32>(a, status, dev, tune, encode, stream, launches);
+            if (a.tokens <= 64) return launch_tc<T, 64>(a, status, dev, tune, encode, stream, launches);
+            if (a.tokens <= 128) return launch_tc<T, 128>(a, status, dev, tune, encode, stream, launches);
+            return launch_tc<T, 256>(a, status, dev, tune, encode, stream, launches);
+        });
+    }
     const int64_t blocks = ((a.tokens + 63) / 64) * ((a.outer + 63) / 64);
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
     return by_type(a.elem, [&](auto t) {
