@@ -156,9 +156,10 @@ def _dev_ptr(t) -> int:
 
 
 def _stream_ptr(stream) -> int:
-    import torch
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the raw handle of torch.cuda.current_stream(), without the object around it (3.4 -> 0.3 us a call)
+        import torch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
 
 

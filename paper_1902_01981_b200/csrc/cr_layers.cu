@@ -467,6 +467,7 @@ cudaError_t launch_group_norm(const GroupNormArgs &in, const DeviceInfo &, cudaS
     if (in.samples == 0) return cudaSuccess;
     GroupNormArgs a = in;
     const bool wide = vector_rows(a.elem, a.channels, {a.x, a.y}, {a.ld_x, a.ld_y});
+    if (wide && group_norm_on_chip(a)) return launch_group_norm_on_chip(a, stream, launches);
     const Split s = make_split(a.samples, a.positions, a.channels, a.groups, wide ? 16 / elem_bytes(a.elem) : 1);
     float *part_mean = a.workspace;
     float *part_m2 = part_mean + (size_t)a.samples * s.chunks * a.channels;
@@ -492,6 +493,15 @@ cudaError_t launch_group_norm(const GroupNormArgs &in, const DeviceInfo &, cudaS
     return by_type(a.elem, [&](auto t) { return wide ? run(t, Int<16 / (int)sizeof(t)>{}) : run(t, Int<1>{}); });
 }
 
+static cudaError_t launch_params(const GroupNormArgs &a, const float *sum1, const float *sum2, cudaStream_t stream, int64_t *launches) {
+    const unsigned tiles = (unsigned)((a.channels + 31) / 32);
+    cr_group_norm_params_kernel<<<tiles * (unsigned)a.partitions, kThreads, 0, stream>>>(sum1, sum2, a.samples / a.partitions, a.channels,
+                                                                                      a.ld_param, a.dbeta, a.dgamma);
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
 cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo &, cudaStream_t stream, int64_t *launches) {
     if (a.samples == 0) {
         const int64_t count = a.partitions * a.channels;
@@ -508,6 +518,15 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
     float *part1 = sum2 + plane, *part2 = part1 + plane * s.chunks;
     float *m1 = part2 + plane * s.chunks, *m2 = m1 + (size_t)a.samples * a.groups;
     const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
+    const bool params = a.dgamma || a.dbeta;
+    cudaError_t e;
+    if (wide && group_norm_backward_on_chip(a)) {
+        // a partition of one sample has its sums where they belong
+        if (a.partitions == a.samples) return launch_group_norm_grad_on_chip(a, a.dbeta, a.dgamma, a.ld_param, stream, launches);
+        e = launch_group_norm_grad_on_chip(a, params ? sum1 : nullptr, params ? sum2 : nullptr, a.channels, stream, launches);
+        if (e != cudaSuccess || !params) return e;
+        return launch_params(a, sum1, sum2, stream, launches);
+    }
     auto run = [&](auto t, auto v, auto act) {
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value, ACT = decltype(act)::value;
@@ -526,16 +545,11 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         }
         return cudaSuccess;
     };
-    cudaError_t e = by_type(a.elem, [&](auto t) {
+    e = by_type(a.elem, [&](auto t) {
         return by_act(a.act, [&](auto act) { return wide ? run(t, Int<16 / (int)sizeof(t)>{}, act) : run(t, Int<1>{}, act); });
     });
-    if (e != cudaSuccess || !(a.dgamma || a.dbeta)) return e;
-    const unsigned tiles = (unsigned)((a.channels + 31) / 32);
-    cr_group_norm_params_kernel<<<tiles * (unsigned)a.partitions, kThreads, 0, stream>>>(sum1, sum2, a.samples / a.partitions, a.channels,
-                                                                                      a.ld_param, a.dbeta, a.dgamma);
-    e = cudaGetLastError();
-    if (e == cudaSuccess) ++*launches;
-    return e;
+    if (e != cudaSuccess || !params) return e;
+    return launch_params(a, sum1, sum2, stream, launches);
 }
 
 cudaError_t launch_dropout(const void *x, const void *residual, void *y, int64_t rows, int64_t cols, int64_t ld_x,

@@ -51,6 +51,14 @@ size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, i
 cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 
+// The one-pass forms (cr_group_norm.cu): whether an item's slab fits the registers of a cluster, for vector rows; the
+// backward one leaves the channels' sums of each sample in sum1 (dz) and sum2 (dz xhat) at row stride ld_sum.
+bool group_norm_on_chip(const GroupNormArgs &a);
+bool group_norm_backward_on_chip(const GroupNormArgs &a);
+cudaError_t launch_group_norm_on_chip(const GroupNormArgs &a, cudaStream_t stream, int64_t *launches);
+cudaError_t launch_group_norm_grad_on_chip(const GroupNormArgs &a, float *sum1, float *sum2, int64_t ld_sum, cudaStream_t stream,
+                                           int64_t *launches);
+
 // y = residual + dropout(x) over [rows][cols] with row strides; residual may be null.
 cudaError_t launch_dropout(const void *x, const void *residual, void *y, int64_t rows, int64_t cols, int64_t ld_x,
                            int64_t ld_r, int64_t ld_y, int elem, const DropSpec &drop, const DeviceInfo &dev,
