@@ -116,10 +116,10 @@ __device__ __forceinline__ unsigned long long drop_word(unsigned long long key, 
     return mix64(key + (i + 1) * kMixGamma);
 }
 
-// v[i] = kept ? v[i] * scale : 0 for the VEC elements from index e on.  A dropped element is selected away, not
-// multiplied by zero: an infinity or a NaN in its place leaves a zero.
+// v[i] = kept ? v[i] : 0 for the VEC elements from index e on; the scale is left to the caller.  A dropped element is
+// selected away, not multiplied by zero: an infinity or a NaN in its place leaves a zero.
 template <int VEC>
-__device__ __forceinline__ void drop(float (&v)[VEC], const DropSpec &d, unsigned long long e) {
+__device__ __forceinline__ void drop_select(float (&v)[VEC], const DropSpec &d, unsigned long long e) {
     const unsigned long long first = e >> 2;
     const uint32_t shift = (uint32_t)e & 3u;
     if (d.scale == 0.f) {   // threshold 65536: everything goes
@@ -130,7 +130,7 @@ __device__ __forceinline__ void drop(float (&v)[VEC], const DropSpec &d, unsigne
     const uint32_t limit = d.threshold << 16;
     if constexpr (VEC == 1) {
         const uint32_t lane = (uint32_t)(drop_word(d.key, first) >> (16 * shift)) & 0xffffu;
-        v[0] = lane >= d.threshold ? v[0] * d.scale : 0.f;
+        v[0] = lane >= d.threshold ? v[0] : 0.f;
     } else {
         // z of output `first`; the following ones are one addition away
         unsigned long long z = d.key + (first + 1) * kMixGamma;
@@ -154,18 +154,92 @@ __device__ __forceinline__ void drop(float (&v)[VEC], const DropSpec &d, unsigne
         }
 #pragma unroll
         for (int j = 0; j < VEC / 2; ++j) {
-            v[2 * j] = (w[j] << 16) >= limit ? v[2 * j] * d.scale : 0.f;
-            v[2 * j + 1] = w[j] >= limit ? v[2 * j + 1] * d.scale : 0.f;   // the low half cannot lift it over the limit
+            v[2 * j] = (w[j] << 16) >= limit ? v[2 * j] : 0.f;
+            v[2 * j + 1] = w[j] >= limit ? v[2 * j + 1] : 0.f;   // the low half cannot lift it over the limit
         }
     }
 }
+template <int VEC>
+__device__ __forceinline__ void drop(float (&v)[VEC], const DropSpec &d, unsigned long long e) {
+    drop_select<VEC>(v, d, e);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] *= d.scale;
+}
+
+// ---- pairs -------------------------------------------------------------------------------------------
+//
+// Two fp32 operations in one instruction (add, mul, fma .f32x2): half the issue slots of the element-wise arithmetic.
+struct F2 {
+    float x, y;
+};
+__device__ __forceinline__ F2 f2(float x, float y) { return {x, y}; }
+__device__ __forceinline__ F2 f2(float x) { return {x, x}; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, c, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 r, a, b, c;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+
+// Elements as pairs.
+template <typename T, int VEC>
+__device__ __forceinline__ void unpack2(const Packed<T, VEC> &r, F2 (&v)[VEC / 2]) {
+    float f[VEC];
+    unpack<T, VEC>(r, f);
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) v[i] = {f[2 * i], f[2 * i + 1]};
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Packed<T, VEC> pack2(const F2 (&v)[VEC / 2]) {
+    float f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = v[i].x; f[2 * i + 1] = v[i].y; }
+    return pack<T, VEC>(f);
+}
+
+template <int VEC>
+__device__ __forceinline__ void drop_select2(F2 (&v)[VEC / 2], const DropSpec &d, unsigned long long e) {
+    float f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = v[i].x; f[2 * i + 1] = v[i].y; }
+    drop_select<VEC>(f, d, e);
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) v[i] = {f[2 * i], f[2 * i + 1]};
+}
 
 // ---- activations -----------------------------------------------------------------------------------
+//
+// 2^t and 1 / t to about one unit in the last place, subnormal numbers as zero: e^-z then leaves the range at
+// |z| = 87, where the sigmoid has long become 0 or 1.
+__device__ __forceinline__ float exp2_approx(float t) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
+}
+__device__ __forceinline__ float recip_approx(float t) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float sigmoid(float z) { return recip_approx(1.f + exp2_approx(-kLog2e * z)); }
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == kActRelu) return z < 0.f ? 0.f : z;   // a NaN stays one
-    if constexpr (ACT == kActSilu) return __fdividef(z, 1.f + __expf(-z));
+    if constexpr (ACT == kActSilu) return z * sigmoid(z);
     return z;
 }
 // Derivative of the activation at z.
@@ -173,7 +247,7 @@ template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
     if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : 0.f;
     if constexpr (ACT == kActSilu) {
-        const float s = __fdividef(1.f, 1.f + __expf(-z));
+        const float s = sigmoid(z);
         return s * fmaf(z, 1.f - s, 1.f);
     }
     return 1.f;

@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_grad_apply_kernel(cons
     }
 }
 
-// Parameter gradients of a partition: the sums of its samples, 32 channels a block, eight threads to a channel.
+// Parameter gradients of a partition: the sums over the rows (one or more a sample) of its samples, 32 channels a block, eight threads to a channel.
 __global__ void __launch_bounds__(kThreads) cr_group_norm_params_kernel(const float *sum1, const float *sum2, int64_t per, int channels,
                                                                         int64_t ld, float *dbeta, float *dgamma) {
     __shared__ float sm[2][8][32];
@@ -460,14 +460,15 @@ size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, i
         const Split s = make_split(samples, positions, channels, groups, vec);
         most = std::max(most, ((size_t)(s.chunks + 1) * channels + groups) * (size_t)samples * 8);
     }
-    return most;
+    // the one-pass form's rows of sums
+    return std::max(most, (size_t)group_norm_backward_on_chip(samples, positions, channels, groups, elem) * channels * (size_t)samples * 8);
 }
 
 cudaError_t launch_group_norm(const GroupNormArgs &in, const DeviceInfo &, cudaStream_t stream, int64_t *launches) {
     if (in.samples == 0) return cudaSuccess;
     GroupNormArgs a = in;
     const bool wide = vector_rows(a.elem, a.channels, {a.x, a.y}, {a.ld_x, a.ld_y});
-    if (wide && group_norm_on_chip(a)) return launch_group_norm_on_chip(a, stream, launches);
+    if (wide && group_norm_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem)) return launch_group_norm_on_chip(a, stream, launches);
     const Split s = make_split(a.samples, a.positions, a.channels, a.groups, wide ? 16 / elem_bytes(a.elem) : 1);
     float *part_mean = a.workspace;
     float *part_m2 = part_mean + (size_t)a.samples * s.chunks * a.channels;
@@ -493,9 +494,10 @@ cudaError_t launch_group_norm(const GroupNormArgs &in, const DeviceInfo &, cudaS
     return by_type(a.elem, [&](auto t) { return wide ? run(t, Int<16 / (int)sizeof(t)>{}) : run(t, Int<1>{}); });
 }
 
-static cudaError_t launch_params(const GroupNormArgs &a, const float *sum1, const float *sum2, cudaStream_t stream, int64_t *launches) {
+static cudaError_t launch_params(const GroupNormArgs &a, const float *sum1, const float *sum2, int rows_per_sample, cudaStream_t stream,
+                                 int64_t *launches) {
     const unsigned tiles = (unsigned)((a.channels + 31) / 32);
-    cr_group_norm_params_kernel<<<tiles * (unsigned)a.partitions, kThreads, 0, stream>>>(sum1, sum2, a.samples / a.partitions, a.channels,
+    cr_group_norm_params_kernel<<<tiles * (unsigned)a.partitions, kThreads, 0, stream>>>(sum1, sum2, a.samples / a.partitions * rows_per_sample, a.channels,
                                                                                       a.ld_param, a.dbeta, a.dgamma);
     const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) ++*launches;
@@ -520,12 +522,13 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
     const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
     const bool params = a.dgamma || a.dbeta;
     cudaError_t e;
-    if (wide && group_norm_backward_on_chip(a)) {
-        // a partition of one sample has its sums where they belong
-        if (a.partitions == a.samples) return launch_group_norm_grad_on_chip(a, a.dbeta, a.dgamma, a.ld_param, stream, launches);
+    if (const int cluster = wide ? group_norm_backward_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem) : 0) {
+        // a partition of one sample that one CTA holds has its sums where they belong
+        if (a.partitions == a.samples && cluster == 1) return launch_group_norm_grad_on_chip(a, a.dbeta, a.dgamma, a.ld_param, stream, launches);
+        sum2 = sum1 + plane * cluster;
         e = launch_group_norm_grad_on_chip(a, params ? sum1 : nullptr, params ? sum2 : nullptr, a.channels, stream, launches);
         if (e != cudaSuccess || !params) return e;
-        return launch_params(a, sum1, sum2, stream, launches);
+        return launch_params(a, sum1, sum2, cluster, stream, launches);
     }
     auto run = [&](auto t, auto v, auto act) {
         using T = decltype(t);
@@ -549,7 +552,7 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         return by_act(a.act, [&](auto act) { return wide ? run(t, Int<16 / (int)sizeof(t)>{}, act) : run(t, Int<1>{}, act); });
     });
     if (e != cudaSuccess || !params) return e;
-    return launch_params(a, sum1, sum2, stream, launches);
+    return launch_params(a, sum1, sum2, 1, stream, launches);
 }
 
 cudaError_t launch_dropout(const void *x, const void *residual, void *y, int64_t rows, int64_t cols, int64_t ld_x,

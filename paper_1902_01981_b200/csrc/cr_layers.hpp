@@ -51,10 +51,11 @@ size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, i
 cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 
-// The one-pass forms (cr_group_norm.cu): whether an item's slab fits the registers of a cluster, for vector rows; the
-// backward one leaves the channels' sums of each sample in sum1 (dz) and sum2 (dz xhat) at row stride ld_sum.
-bool group_norm_on_chip(const GroupNormArgs &a);
-bool group_norm_backward_on_chip(const GroupNormArgs &a);
+// The one-pass forms (cr_group_norm.cu), for vector rows: whether an item fits a cluster, for the backward pass with the
+// CTAs of that cluster (0: no).  The backward one leaves the sums of dz (sum1) and dz xhat (sum2) of each sample's
+// channels, a row of ld_sum for each CTA of the cluster.
+bool group_norm_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem);
+int group_norm_backward_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem);
 cudaError_t launch_group_norm_on_chip(const GroupNormArgs &a, cudaStream_t stream, int64_t *launches);
 cudaError_t launch_group_norm_grad_on_chip(const GroupNormArgs &a, float *sum1, float *sum2, int64_t ld_sum, cudaStream_t stream,
                                            int64_t *launches);
