@@ -7,6 +7,7 @@ The library is loaded on first use and a missing build raises: there is no fallb
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -157,10 +158,17 @@ def _dev_ptr(t) -> int:
 
 def _stream_ptr(stream) -> int:
     if stream is None:
-        # the raw handle of torch.cuda.current_stream(), without the object around it (3.4 -> 0.3 us a call)
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _current_stream()
     return stream.cuda_stream
+
+
+def _current_stream() -> int:
+    """Raw handle of torch.cuda.current_stream(), without the object around it (3.4 -> 0.2 us a call)."""
+    global _current_stream
+    import torch
+    device, raw = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+    _current_stream = lambda: raw(device())  # noqa: E731
+    return _current_stream()
 
 
 def _masks(masks, cols: int) -> np.ndarray:
@@ -205,6 +213,7 @@ def cr_plan_create(n: int, L: int, s: int, P: int, d: int, code: int = CR_CODE_C
 
 def cr_plan_destroy(plan: int) -> None:
     _groups_of_plan.pop(plan, None)      # the handle may be reused by a later plan
+    _group_norm_workspace.cache_clear()
     _check(lib().cr_plan_destroy(plan), "cr_plan_destroy")
 
 
@@ -482,10 +491,9 @@ def _row_ptr(t, shape):
         raise ValueError("expected a CUDA tensor")
     if t.shape != shape:
         raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    width = shape[-1]
     if t.is_contiguous():
-        return t.data_ptr(), width
-    st = t.stride()
+        return t.data_ptr(), shape[-1]
+    width, st = shape[-1], t.stride()
     if width > 1 and st[-1] != 1:
         raise ValueError("the elements of a row must be next to each other")
     ld = 0
@@ -493,8 +501,8 @@ def _row_ptr(t, shape):
     for k in range(len(shape) - 2, -1, -1):
         if shape[k] > 1:
             if not ld:
-                ld = st[k]
-            elif st[k] != ld * spaced:
+                ld = st[k] // spaced if st[k] % spaced == 0 else -1
+            if st[k] != ld * spaced:
                 raise ValueError("the rows must be equally spaced")
         spaced *= shape[k]
     return t.data_ptr(), ld or width
@@ -504,9 +512,9 @@ def _vector_ptr(t, count: int) -> int:
     """Address of a contiguous fp32 CUDA tensor of `count` elements (None -> NULL)."""
     if t is None:
         return 0
-    if t.element_size() != 4 or not t.is_floating_point() or t.numel() != count:
-        raise ValueError(f"expected {count} float32 elements")
-    return _dev_ptr(t)
+    if _elem(t) != CR_ELEM_F32 or t.numel() != count or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"expected {count} contiguous float32 elements on the device")
+    return t.data_ptr()
 
 
 def cr_dropout(plan: int, x, y, p: float, seed: int, offset: int = 0, residual=None, stream=None) -> None:
@@ -530,12 +538,19 @@ def _group_norm_desc(x, groups, eps, act, p, seed, offset):
     return cr_group_norm_t(n, s, c, groups, _elem(x), act, eps, p, seed, offset)
 
 
+@functools.lru_cache(maxsize=256)
+def _group_norm_workspace(backward: bool, plan: int, shape, groups: int, elem: int) -> int:
+    """The workspace is a function of these sizes (the plan's device included), so a loop asks once."""
+    fn = lib().cr_group_norm_backward_workspace_bytes if backward else lib().cr_group_norm_workspace_bytes
+    return fn(plan, cr_group_norm_t(*shape, groups, elem, CR_ACT_NONE, 0.0, 0.0, 0, 0))
+
+
 def cr_group_norm_workspace_bytes(plan: int, x, groups: int) -> int:
-    return lib().cr_group_norm_workspace_bytes(plan, _group_norm_desc(x, groups, 0.0, CR_ACT_NONE, 0.0, 0, 0))
+    return _group_norm_workspace(False, plan, x.shape, groups, _elem(x))
 
 
 def cr_group_norm_backward_workspace_bytes(plan: int, x, groups: int) -> int:
-    return lib().cr_group_norm_backward_workspace_bytes(plan, _group_norm_desc(x, groups, 0.0, CR_ACT_NONE, 0.0, 0, 0))
+    return _group_norm_workspace(True, plan, x.shape, groups, _elem(x))
 
 
 def cr_group_norm(plan: int, x, gamma, beta, groups: int, y, mean=None, rstd=None, eps: float = 1e-5,
@@ -571,7 +586,7 @@ def cr_group_norm_backward(plan: int, dy, x, gamma, beta, mean, rstd, groups: in
         if t is None:
             params.append(0)
             continue
-        if t.dim() != 2 or t.shape[1] != desc.channels or t.element_size() != 4 or not t.is_floating_point():
+        if t.dim() != 2 or t.shape[1] != desc.channels or _elem(t) != CR_ELEM_F32:
             raise ValueError("parameter gradients are float32 [partitions, channels]")
         ptr, ld = _row_ptr(t, t.shape)
         if any(params) and (t.shape[0] != parts or ld != ldp):

@@ -1231,8 +1231,9 @@ bool good_desc(const cr_group_norm_t *d) {
            d->samples <= 0x7fffffffll / std::max<int64_t>(d->groups, (d->channels + 255) / 256);
 }
 
-cr::GroupNormArgs group_norm_args(const cr_group_norm_t &d) {
+cr::GroupNormArgs group_norm_args(const cr_plan &plan, const cr_group_norm_t &d) {
     cr::GroupNormArgs a;
+    a.status = plan.d_status; a.wait_ns = plan.tune.wait_limit_ns; a.device = plan.device;
     a.samples = d.samples; a.positions = d.positions; a.channels = d.channels; a.groups = d.groups;
     a.elem = d.elem; a.act = d.act; a.eps = (float)d.eps;
     a.drop = cr::make_drop(d.p, d.seed, d.offset);
@@ -1277,7 +1278,7 @@ cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const vo
     if (!on_element(x, desc->elem) || !on_element(y, desc->elem)) return CR_ERR_INVALID_ARG;
     const size_t need = cr_group_norm_workspace_bytes(plan, desc);
     if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
-    cr::GroupNormArgs a = group_norm_args(*desc);
+    cr::GroupNormArgs a = group_norm_args(*plan, *desc);
     a.x = x; a.ld_x = ld_x; a.y = y; a.ld_y = ld_y; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
     a.workspace = static_cast<float *>(workspace);
     cudaError_t e = cr::launch_group_norm(a, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
@@ -1311,7 +1312,7 @@ cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc,
     if (!dx && !dgamma && !dbeta) return CR_OK;
     const size_t need = cr_group_norm_backward_workspace_bytes(plan, desc);
     if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
-    cr::GroupNormArgs a = group_norm_args(*desc);
+    cr::GroupNormArgs a = group_norm_args(*plan, *desc);
     a.x = x; a.ld_x = ld_x; a.dy = dy; a.ld_dy = ld_dy; a.y = dx; a.ld_y = ld_dx; a.gamma = gamma; a.beta = beta;
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
     a.dgamma = dgamma; a.dbeta = dbeta; a.ld_param = ld_param; a.partitions = partitions;
@@ -1347,7 +1348,7 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
     if (!good_rows(tokens, inner, ld_x) || !good_rows(outer, inner, ld_w) || !good_rows(tokens, outer, ld_y)) return CR_ERR_INVALID_ARG;
     cr::Int8ProductArgs a;
     a.x = x; a.ld_x = ld_x; a.x_scale = x_scale; a.w = w; a.ld_w = ld_w; a.w_scale = w_scale; a.bias = bias;
-    a.y = y; a.ld_y = ld_y; a.tokens = tokens; a.outer = outer; a.inner = inner; a.elem = elem;
+    a.y = y; a.ld_y = ld_y; a.tokens = tokens; a.outer = outer; a.inner = inner; a.elem = elem; a.device = plan->device;
     cudaError_t e = cr::launch_int8_product(a, plan->d_status, plan->dev, plan->tune, plan->encode,
                                             reinterpret_cast<cudaStream_t>(stream), &plan->launches);
     if (e != cudaSuccess) { note_cuda(e, "cr_int8_product"); return CR_ERR_CUDA; }

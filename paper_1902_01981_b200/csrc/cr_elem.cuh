@@ -30,7 +30,8 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
-// Data that is read once goes past L1; not the read-only path, since an output may be the input's own buffer.
+// Ordinary accesses, which the compiler may move past one another: an output may be the input's own buffer, so nothing
+// goes through the read-only path.
 template <typename T, int VEC>
 __device__ __forceinline__ Packed<T, VEC> load_packed(const T *p) {
     Packed<T, VEC> r;
@@ -38,19 +39,15 @@ __device__ __forceinline__ Packed<T, VEC> load_packed(const T *p) {
         r.e = *p;
     } else {
         static_assert(sizeof(r) == 16, "a vector is 16 bytes");
-        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p) : "memory");
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
     }
     return r;
 }
 template <typename T, int VEC>
 __device__ __forceinline__ void store_packed(T *p, const Packed<T, VEC> &r) {
-    if constexpr (VEC == 1) {
-        *p = r.e;
-    } else {
-        asm volatile("st.global.L1::no_allocate.v4.b32 [%0], {%1, %2, %3, %4};"
-                     ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]) : "memory");
-    }
+    if constexpr (VEC == 1) *p = r.e;
+    else *reinterpret_cast<uint4 *>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
 }
 template <typename T, int VEC>
 __device__ __forceinline__ void unpack(const Packed<T, VEC> &r, float (&v)[VEC]) {
@@ -168,28 +165,32 @@ __device__ __forceinline__ void drop(float (&v)[VEC], const DropSpec &d, unsigne
 
 // ---- pairs -------------------------------------------------------------------------------------------
 //
-// Two fp32 operations in one instruction (add, mul, fma .f32x2): half the issue slots of the element-wise arithmetic.
+// Two fp32 operations in one instruction (add, mul, fma .f32x2): half the issue slots of the element-wise arithmetic.  A
+// pair is kept as one 64-bit value, so that it stays in an aligned register pair between operations.
 struct F2 {
-    float x, y;
+    unsigned long long v;
 };
-__device__ __forceinline__ F2 f2(float x, float y) { return {x, y}; }
-__device__ __forceinline__ F2 f2(float x) { return {x, x}; }
+__device__ __forceinline__ F2 f2(float x, float y) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ F2 f2(float x) { return f2(x, x); }
+__device__ __forceinline__ float low(F2 a) { return __uint_as_float((uint32_t)a.v); }
+__device__ __forceinline__ float high(F2 a) { return __uint_as_float((uint32_t)(a.v >> 32)); }
 __device__ __forceinline__ F2 add2(F2 a, F2 b) {
     F2 r;
-    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
 }
 __device__ __forceinline__ F2 mul2(F2 a, F2 b) {
     F2 r;
-    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
 }
 __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
     F2 r;
-    asm("{\n.reg .b64 a, b, c, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 r, a, b, c;\nmov.b64 {%0, %1}, r;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
     return r;
 }
 
@@ -199,13 +200,13 @@ __device__ __forceinline__ void unpack2(const Packed<T, VEC> &r, F2 (&v)[VEC / 2
     float f[VEC];
     unpack<T, VEC>(r, f);
 #pragma unroll
-    for (int i = 0; i < VEC / 2; ++i) v[i] = {f[2 * i], f[2 * i + 1]};
+    for (int i = 0; i < VEC / 2; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
 }
 template <typename T, int VEC>
 __device__ __forceinline__ Packed<T, VEC> pack2(const F2 (&v)[VEC / 2]) {
     float f[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = v[i].x; f[2 * i + 1] = v[i].y; }
+    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = low(v[i]); f[2 * i + 1] = high(v[i]); }
     return pack<T, VEC>(f);
 }
 
@@ -213,10 +214,10 @@ template <int VEC>
 __device__ __forceinline__ void drop_select2(F2 (&v)[VEC / 2], const DropSpec &d, unsigned long long e) {
     float f[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = v[i].x; f[2 * i + 1] = v[i].y; }
+    for (int i = 0; i < VEC / 2; ++i) { f[2 * i] = low(v[i]); f[2 * i + 1] = high(v[i]); }
     drop_select<VEC>(f, d, e);
 #pragma unroll
-    for (int i = 0; i < VEC / 2; ++i) v[i] = {f[2 * i], f[2 * i + 1]};
+    for (int i = 0; i < VEC / 2; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
 }
 
 // ---- activations -----------------------------------------------------------------------------------

@@ -18,16 +18,22 @@
 #include "cr_tcgen05.cuh"
 
 #ifndef CR_GN_FMIN
-#define CR_GN_FMIN 3
-#define CR_GN_BMIN 2
+#define CR_GN_FMIN 6
+#define CR_GN_BMIN 4
 #define CR_GN_FNV 8
 #define CR_GN_BNV 4
+#endif
+#ifndef CR_GN_WIDE
+#define CR_GN_WIDE 64
+#endif
+#ifndef CR_GN_FTH
+#define CR_GN_FTH 128
+#define CR_GN_BTH 128
 #endif
 
 namespace cr {
 namespace {
 
-constexpr int kTH = 256, kWarps = kTH / 32;
 constexpr int kMaxCluster = 8;
 
 struct Slab {
@@ -39,7 +45,6 @@ struct Slab {
     int channels;
     int samples;
     int walkers;         // clusters that share the samples of a slab
-    int entries;         // backward: floats that one sample's sums of the CTA's lines need
     int64_t positions;
 };
 
@@ -47,8 +52,10 @@ struct Slab {
 struct Spot {
     int slab, rank, first_sample, rows, width, vpr, rt, col, j, c0, mine;   // j < 0: idle; mine: rows of this thread
     int groups, cv;                                                       // groups of the slab; vectors per group
+    int lanes;           // bit o: lanes that differ in bit o hold rows or columns of the same group; -1: not that simple
+    bool full;           // every thread has all its rows
 };
-template <int VEC>
+template <int VEC, int NV, int kTH>
 __device__ __forceinline__ Spot spot(const Slab &s) {
     Spot p;
     const uint32_t cluster = blockIdx.x / (uint32_t)s.cluster;
@@ -66,10 +73,14 @@ __device__ __forceinline__ Spot spot(const Slab &s) {
     p.mine = p.j < 0 || p.j >= p.rows ? 0 : (p.rows - p.j + p.rt - 1) / p.rt;
     p.groups = p.width / s.cg;
     p.cv = s.cg / VEC;
+    // whole rows in a warp and a power of two of vectors in a group: column bits below cv, row bits from vpr on
+    p.lanes = 32 % p.vpr == 0 && s.cg % VEC == 0 && (p.cv & (p.cv - 1)) == 0 ? (p.cv - 1) | (31 & ~(p.vpr - 1)) : -1;
+    p.full = kTH % p.vpr == 0 && p.rows == NV * p.rt;
     return p;
 }
 
 // Sums the entries [g * per, (g + 1) * per) of `in` into out[g] for g < count: a warp per group, in one order.
+template <int kWarps>
 __device__ __forceinline__ void fold(const float *in, float *out, int count, int per) {
     const int lane = (int)threadIdx.x & 31;
     for (int g = (int)threadIdx.x >> 5; g < count; g += kWarps) {
@@ -90,74 +101,120 @@ __device__ __forceinline__ void sum_rows_of_warp(float (&v)[N], int vpr) {
     }
 }
 
-// Sums over the CTA, by group; every thread gets the sums of its own groups (one where a vector lies inside a group,
-// else one per channel of the vector).  `area`: kTH * kG floats, another one in the next call; `sums`: [groups].
-// Where a warp holds whole rows and the groups a power of two of vectors, lanes add up the warp and one barrier does;
-// otherwise every entry goes through shared memory.
-template <int N, int VEC, bool UNI>
-__device__ __forceinline__ void sum_groups(float (&acc)[N][UNI ? 1 : VEC], const Spot &p, int cg, float *area, float *sums) {
+// Sums over the CTA, by group, of N numbers a thread has for each of its groups (one group where a vector lies inside
+// it, else one per channel of the vector).  After the barrier in it, group_sum gives any thread any group's sum.
+// Where a warp holds whole rows and the groups a power of two of vectors, lanes add up the warp and one number a warp and
+// group goes through shared memory; otherwise every entry does.  `area`: kTH * N * kG floats.
+template <int N, int VEC, bool UNI, int kWarps>
+__device__ __forceinline__ void put_groups(float (&acc)[N][UNI ? 1 : VEC], const Spot &p, int cg, float *area, float *sums) {
     constexpr int kG = UNI ? 1 : VEC;
-    const int lane = (int)threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
-    const bool folded = 32 % p.vpr == 0;
-    if (UNI && folded && (p.cv & (p.cv - 1)) == 0) {
+    if (UNI && p.lanes >= 0) {
         float t[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) t[n] = acc[n][0];
-        sum_rows_of_warp<N>(t, p.vpr);
-        for (int o = 1; o < p.cv; o <<= 1) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) t[n] += __shfl_xor_sync(0xffffffffu, t[n], o);
-        }
-        const int g = p.col / p.cv;
-        if (lane < p.vpr && p.col == g * p.cv) {
+        for (int b = 0; b < 5; ++b)
+            if (p.lanes >> b & 1) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) area[(n * p.groups + g) * kWarps + warp] = t[n];
+                for (int n = 0; n < N; ++n) t[n] += __shfl_xor_sync(0xffffffffu, t[n], 1 << b);
+            }
+        if (((int)threadIdx.x & 31 & p.lanes) == 0) {
+            float *mine = area + (p.col / p.cv) * (N * kWarps) + ((int)threadIdx.x >> 5);
+#pragma unroll
+            for (int n = 0; n < N; ++n) mine[n * kWarps] = t[n];
         }
         __syncthreads();
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const float4 *line = reinterpret_cast<const float4 *>(area + (n * p.groups + g) * kWarps);
-            const float4 a = line[0], b = line[1];
-            acc[n][0] = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
-        }
     } else {
+        if (p.j >= 0) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            if (p.j >= 0) {
+            for (int n = 0; n < N; ++n)
 #pragma unroll
-                for (int i = 0; i < kG; ++i) area[(p.col * kG + i) * p.rt + p.j] = acc[n][i];
-            }
-            __syncthreads();
-            fold(area, sums, p.groups, (UNI ? p.cv : cg) * p.rt);
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kG; ++i) acc[n][i] = sums[(p.col * VEC + i) / cg];
-            if (n + 1 < N) __syncthreads();
+                for (int i = 0; i < kG; ++i) area[((n * p.vpr + p.col) * kG + i) * p.rt + p.j] = acc[n][i];
         }
+        __syncthreads();
+        fold<kWarps>(area, sums, N * p.groups, (UNI ? p.cv : cg) * p.rt);
+        __syncthreads();
     }
 }
-
-// Writes `v` to the place of `mine` in the shared memory of every CTA of the cluster.  Each CTA hands out what it knows
-// and reads only its own memory after the one barrier that follows: a read from a peer is a round trip, these are not.
-__device__ __forceinline__ void hand_out(const float *mine, float v, int cluster) {
-    for (int r = 0; r < cluster; ++r)
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(i8::map_to_rank(i8::smem_u32(mine), (uint32_t)r)), "f"(v) : "memory");
+template <int N, bool UNI, int kWarps>
+__device__ __forceinline__ float group_sum(int n, int g, const Spot &p, const float *area, const float *sums) {
+    if (UNI && p.lanes >= 0) {
+        const float4 *line = reinterpret_cast<const float4 *>(area + (g * N + n) * kWarps);
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps / 4; ++w) {
+            const float4 v = line[w];
+            t += (v.x + v.y) + (v.z + v.w);
+        }
+        return t;
+    }
+    return sums[n * p.groups + g];
 }
+
 __device__ __forceinline__ void cluster_meet() {
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
+// The CTAs of a cluster tell each other two numbers per group.  Each writes its numbers into the memory of every CTA
+// (itself too) and the write itself counts on that CTA's barrier, so that only the threads that join the numbers wait,
+// and nothing is fenced; a barrier of the cluster would wait for the stores of the previous sample as well.  Two boxes
+// by turns: a CTA writes into a box again only after it has heard from everybody about the exchange in between, which
+// they take part in after they have read this one.
+struct Exchange {
+    float2 *box;          // [2][cluster][gmax]
+    uint64_t *bars;       // [2]
+    volatile int *given_up;
+    int turn = 0;
+
+    __device__ __forceinline__ float2 *at(int rank, int g, int cluster, int gmax) const {
+        return box + ((turn & 1) * cluster + rank) * gmax + g;
+    }
+    // by one thread, before the others' numbers are waited for
+    __device__ __forceinline__ void expect(int groups, int cluster) const {
+        i8::mbar_expect_tx(&bars[turn & 1], (uint32_t)(groups * cluster * 8));
+    }
+    __device__ __forceinline__ void tell(float2 v, int rank, int g, int cluster, int gmax) const {
+        const uint32_t to = i8::smem_u32(at(rank, g, cluster, gmax)), bar = i8::smem_u32(&bars[turn & 1]);
+        for (int r = 0; r < cluster; ++r)
+            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                         ::"r"(i8::map_to_rank(to, (uint32_t)r)), "f"(v.x), "f"(v.y), "r"(i8::map_to_rank(bar, (uint32_t)r)) : "memory");
+    }
+    __device__ __forceinline__ void hear(int *status, unsigned long long wait_ns) const {
+        if (!i8::mbar_wait(&bars[turn & 1], (uint32_t)((turn >> 1) & 1), given_up, wait_ns)) {
+            *given_up = 1;
+            atomicExch(status, 1);
+        }
+    }
+};
+// Sets the barriers up; the cluster meets once, since a CTA's memory may be written from outside only once it runs.
+__device__ __forceinline__ void open_exchange(Exchange &x, float *memory, int cluster, int gmax) {
+    x.box = reinterpret_cast<float2 *>(memory);
+    x.bars = reinterpret_cast<uint64_t *>(x.box + 2 * cluster * gmax);
+    x.given_up = reinterpret_cast<volatile int *>(x.bars + 2);
+    if (cluster > 1) {
+        if (threadIdx.x == 0) {
+            i8::mbar_init(&x.bars[0], 1);
+            i8::mbar_init(&x.bars[1], 1);
+            *x.given_up = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cluster_meet();
+    }
+}
+inline size_t exchange_bytes(int cluster, int gmax) { return (size_t)2 * cluster * gmax * 8 + 2 * 8 + 8; }
+
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // All but the newest group have landed (for the thread that issued them).
 __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 template <typename T>
-__device__ __forceinline__ Packed<T, 16 / (int)sizeof(T)> held(uint32_t at) {
+__device__ __forceinline__ Packed<T, 16 / (int)sizeof(T)> held(const uint4 *at) {
+    const uint4 v = *at;
     Packed<T, 16 / (int)sizeof(T)> r;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "r"(at) : "memory");
+    r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
     return r;
 }
 
@@ -171,373 +228,442 @@ __device__ __forceinline__ F2 z_of(F2 centred, F2 rstd, F2 gamma, F2 scaled, F2 
 }
 __device__ __forceinline__ F2 sigmoid2(F2 z) {
     const F2 t = mul2(z, f2(-kLog2e));
-    const F2 d = add2({exp2_approx(t.x), exp2_approx(t.y)}, f2(1.f));
-    return {recip_approx(d.x), recip_approx(d.y)};
+    const F2 d = add2(f2(exp2_approx(low(t)), exp2_approx(high(t))), f2(1.f));
+    return f2(recip_approx(low(d)), recip_approx(high(d)));
 }
 
 // The pair i of a vector, from one value per group (UNI) or per channel.
 template <bool UNI, int N>
 __device__ __forceinline__ F2 pair_of(const float (&v)[N], int i) {
     if constexpr (UNI) return f2(v[0]);
-    else return {v[2 * i], v[2 * i + 1]};
+    else return f2(v[2 * i], v[2 * i + 1]);
 }
 
+// The vectors of a thread: all NV of them where the CTA's share is full (no branches), else the first `mine`.
+template <int NV, typename F>
+__device__ __forceinline__ void for_rows(const Spot &p, F &&f) {
+    if (p.full) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) f(k);
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (k < p.mine) f(k);
+    }
+}
+
+// Forward.  Sums and squares are taken of x - pivot, the pivot being the group's very first value: one pass over the
+// vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
+// squares have lost digits to it, and the item is summed once more around the mean itself (all CTAs of the cluster see
+// the same numbers and decide alike).
 // UNI: every vector lies inside one group.
-template <typename T, int NV, bool UNI, int ACT>
+template <typename T, int NV, int kTH, bool UNI, int ACT>
 __global__ void __launch_bounds__(kTH, NV <= 8 ? CR_GN_FMIN : 1) cr_group_norm_kernel(const GroupNormArgs a, const Slab s) {
     constexpr int VEC = 16 / (int)sizeof(T), NP = VEC / 2, kG = UNI ? 1 : VEC;   // kG: groups a thread may touch
     extern __shared__ __align__(16) float sm[];
-    const Spot p = spot<VEC>(s);
-    if (s.cluster > 1) cluster_meet();         // a CTA's memory may be written from outside once the CTA runs
+    const Spot p = spot<VEC, NV, kTH>(s);
     const int gmax = s.sc / s.cg;
-    float *area = sm + 2 * NV * kTH * 4;       // [2][kTH * kG]
-    float *sums = area + 2 * kTH * kG;         // [gmax]
-    float *peers = sums + gmax;                // [2][cluster][2][gmax]: sums and centred squares of every CTA, two samples' worth
-    const uint32_t mine_at = i8::smem_u32(sm) + threadIdx.x * 16;
-    const T *src = static_cast<const T *>(a.x) + (((int64_t)p.first_sample * s.positions + (int64_t)p.rank * s.rows_per_cta + max(p.j, 0)) * a.ld_x + p.c0);
-    const int64_t step_x = (int64_t)p.rt * a.ld_x, step_y = (int64_t)p.rt * a.ld_y;
-    const int64_t next_x = (int64_t)s.walkers * s.positions * a.ld_x;
-    auto fetch = [&](int buf, const T *from) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k < p.mine) copy16(mine_at + (uint32_t)(buf * NV + k) * (kTH * 16), from + k * step_x);
-    };
-    fetch(0, src);
-    copies_issued();
-    F2 gamma[NP], beta[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        gamma[i] = a.gamma ? F2{__ldg(a.gamma + p.c0 + 2 * i), __ldg(a.gamma + p.c0 + 2 * i + 1)} : f2(1.f);
-        beta[i] = a.beta ? F2{__ldg(a.beta + p.c0 + 2 * i), __ldg(a.beta + p.c0 + 2 * i + 1)} : f2(0.f);
-    }
-    const float inv = 1.f / fmaxf((float)p.rows * (float)s.cg, 1.f);
-    const float all = (float)s.positions * (float)s.cg;
-    int buf = 0;
-    for (int n = p.first_sample; n < s.samples; n += s.walkers, buf ^= 1) {
-        src += next_x;
-        if (n + s.walkers < s.samples) fetch(buf ^ 1, src);
-        copies_issued();
-        copies_landed();
-        const uint32_t at = mine_at + (uint32_t)(buf * NV) * (kTH * 16);
-        // sums, then squares of the distances from the CTA's own mean
-        F2 t[NP];
-        float acc[1][kG], mean[kG], rstd[kG];
-        auto by_group = [&]() {
-            if constexpr (UNI) {
-                acc[0][0] = 0.f;
-#pragma unroll
-                for (int i = 0; i < NP; ++i) acc[0][0] += t[i].x + t[i].y;
-            } else {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) { acc[0][2 * i] = t[i].x; acc[0][2 * i + 1] = t[i].y; }
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < NP; ++i) t[i] = f2(0.f);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k < p.mine) {
-                F2 f[NP];
-                unpack2<T, VEC>(held<T>(at + k * (kTH * 16)), f);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) t[i] = add2(t[i], f[i]);
-            }
-        by_group();
-        sum_groups<1, VEC, UNI>(acc, p, s.cg, area, sums);
-#pragma unroll
-        for (int i = 0; i < kG; ++i) mean[i] = acc[0][i] * inv;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) t[i] = f2(0.f);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k < p.mine) {
-                F2 f[NP];
-                unpack2<T, VEC>(held<T>(at + k * (kTH * 16)), f);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const F2 m = pair_of<UNI>(mean, i), d = add2(f[i], {-m.x, -m.y});
-                    t[i] = fma2(d, d, t[i]);
-                }
-            }
-        by_group();
-        sum_groups<1, VEC, UNI>(acc, p, s.cg, area + kTH * kG, sums);
-        // the first thread of each group speaks for it
-        auto leads = [&](int i) { return p.j == 0 && (p.col * VEC + i) % s.cg == 0; };
-        if (s.cluster > 1) {
-            float *box = peers + (size_t)buf * s.cluster * 2 * gmax;
-#pragma unroll
-            for (int i = 0; i < kG; ++i)
-                if (leads(i)) {
-                    const int g = (p.col * VEC + i) / s.cg;
-                    hand_out(&box[p.rank * 2 * gmax + g], mean[i], s.cluster);
-                    hand_out(&box[(p.rank * 2 + 1) * gmax + g], acc[0][i], s.cluster);
-                }
-            cluster_meet();
-            // join the CTAs: means weighted by their rows, centred squares moved to the common mean
-#pragma unroll
-            for (int i = 0; i < kG; ++i) {
-                const float *in = box + (p.col * VEC + i) / s.cg;
-                float total = 0.f, m2 = 0.f;
-                for (int r = 0; r < s.cluster; ++r) {
-                    const int rows = (int)max((int64_t)0, min((int64_t)s.rows_per_cta, s.positions - (int64_t)r * s.rows_per_cta));
-                    total = fmaf((float)rows * (float)s.cg, in[r * 2 * gmax], total);
-                }
-                mean[i] = total / all;
-                for (int r = 0; r < s.cluster; ++r) {
-                    const int rows = (int)max((int64_t)0, min((int64_t)s.rows_per_cta, s.positions - (int64_t)r * s.rows_per_cta));
-                    const float d = in[r * 2 * gmax] - mean[i];
-                    m2 += rows ? fmaf((float)rows * (float)s.cg * d, d, in[(r * 2 + 1) * gmax]) : 0.f;
-                }
-                acc[0][i] = m2;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kG; ++i) {
-            rstd[i] = 1.f / sqrtf(acc[0][i] / all + a.eps);
-            if (a.mean && p.rank == 0 && leads(i)) {
-                const int64_t g = (int64_t)n * a.groups + p.slab * gmax + (p.col * VEC + i) / s.cg;
-                a.mean[g] = mean[i];
-                a.rstd[g] = rstd[i];
-            }
-        }
-        const int64_t row = (int64_t)n * s.positions + (int64_t)p.rank * s.rows_per_cta + max(p.j, 0);
-        T *dst = static_cast<T *>(a.y) + (row * a.ld_y + p.c0);
-        unsigned long long e = a.drop.offset + (unsigned long long)(row * s.channels + p.c0);
-        const unsigned long long step_e = (unsigned long long)p.rt * s.channels;
-        F2 scaled[NP];
-#pragma unroll
-        for (int i = 0; i < NP; ++i) scaled[i] = mul2(pair_of<UNI>(rstd, i), gamma[i]);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k < p.mine) {
-                F2 f[NP];
-                unpack2<T, VEC>(held<T>(at + k * (kTH * 16)), f);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const F2 m = pair_of<UNI>(mean, i);
-                    const F2 z = z_of<ACT>(add2(f[i], {-m.x, -m.y}), pair_of<UNI>(rstd, i), gamma[i], scaled[i], beta[i]);
-                    if constexpr (ACT == kActSilu) f[i] = mul2(z, sigmoid2(z));
-                    else f[i] = {act_value<ACT>(z.x), act_value<ACT>(z.y)};
-                }
-                if (a.drop.threshold) {
-                    drop_select2<VEC>(f, a.drop, e);
-#pragma unroll
-                    for (int i = 0; i < NP; ++i) f[i] = mul2(f[i], f2(a.drop.scale));
-                    e += step_e;
-                }
-                store_packed<T, VEC>(dst, pack2<T, VEC>(f));
-                dst += step_y;
-            }
-    }
-}
-
-// Backward: x and dy are read once; dz takes the place of dy, in registers.  sum1, sum2 (may be null): the sums of dz and
-// of dz xhat of each channel over this CTA's rows of a sample, [samples][cluster] rows of ld_sum.
-template <typename T, int NV, bool UNI, int ACT>
-__global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_grad_kernel(const GroupNormArgs a, const Slab s, float *sum1, float *sum2, int64_t ld_sum) {
-    constexpr int VEC = 16 / (int)sizeof(T), NP = VEC / 2, kG = UNI ? 1 : VEC;
-    extern __shared__ __align__(16) float sm[];
-    const Spot p = spot<VEC>(s);
-    if (s.cluster > 1) cluster_meet();
-    const int gmax = s.sc / s.cg;
-    float *area = sm + 4 * NV * kTH * 4;       // [2][kTH * max(kG, 2)]: by turns, sample after sample
-    float *entries = area + 2 * kTH * (UNI ? 2 : VEC);   // [2][lines][2 * width]
-    const bool folded = 32 % p.vpr == 0;
-    const int lines = folded ? kWarps : p.rt, line = folded ? (int)threadIdx.x >> 5 : p.j;
-    const bool puts = folded ? ((int)threadIdx.x & 31) < p.vpr : p.j >= 0;
-    const int both = 2 * p.width;
-    float *sums = entries + 2 * s.entries;
-    float *peers = sums + gmax;                // [2][cluster][2][gmax]
+    float *area = sm + 2 * NV * kTH * 4;       // [2][kTH * 2 * kG], by turns
+    float *ready = area + 4 * kTH * kG;        // [2][gmax]: mean, rstd
+    float *sums = ready + 2 * gmax;            // [2][gmax]
+    volatile int *again = reinterpret_cast<volatile int *>(sums + 2 * gmax);   // [2]: by turns
+    Exchange ex;
+    open_exchange(ex, sums + 2 * gmax + 2, s.cluster, gmax);
     const uint32_t mine_at = i8::smem_u32(sm) + threadIdx.x * 16;
     const int64_t row0 = (int64_t)p.first_sample * s.positions + (int64_t)p.rank * s.rows_per_cta + max(p.j, 0);
     const T *src = static_cast<const T *>(a.x) + (row0 * a.ld_x + p.c0);
-    const T *up = static_cast<const T *>(a.dy) + (row0 * a.ld_dy + p.c0);
-    const int64_t step_x = (int64_t)p.rt * a.ld_x, step_dy = (int64_t)p.rt * a.ld_dy, step_y = (int64_t)p.rt * a.ld_y;
-    const int64_t next = (int64_t)s.walkers * s.positions;
+    T *dst = static_cast<T *>(a.y) + (row0 * a.ld_y + p.c0);
+    const int64_t step_x = (int64_t)p.rt * a.ld_x, step_y = (int64_t)p.rt * a.ld_y;
+    const int64_t next_x = (int64_t)s.walkers * s.positions * a.ld_x, next_y = (int64_t)s.walkers * s.positions * a.ld_y;
     auto fetch = [&](int buf) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k < p.mine) {
-                copy16(mine_at + (uint32_t)(buf * 2 * NV + k) * (kTH * 16), src + k * step_x);
-                copy16(mine_at + (uint32_t)((buf * 2 + 1) * NV + k) * (kTH * 16), up + k * step_dy);
-            }
+        const T *from = src;
+        for_rows<NV>(p, [&](int k) {
+            copy16(mine_at + (uint32_t)(buf * NV + k) * (kTH * 16), from);
+            from += step_x;
+        });
     };
     fetch(0);
     copies_issued();
     F2 gamma[NP], beta[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        gamma[i] = a.gamma ? F2{__ldg(a.gamma + p.c0 + 2 * i), __ldg(a.gamma + p.c0 + 2 * i + 1)} : f2(1.f);
-        beta[i] = a.beta ? F2{__ldg(a.beta + p.c0 + 2 * i), __ldg(a.beta + p.c0 + 2 * i + 1)} : f2(0.f);
+        gamma[i] = a.gamma ? f2(__ldg(a.gamma + p.c0 + 2 * i), __ldg(a.gamma + p.c0 + 2 * i + 1)) : f2(1.f);
+        beta[i] = a.beta ? f2(__ldg(a.beta + p.c0 + 2 * i), __ldg(a.beta + p.c0 + 2 * i + 1)) : f2(0.f);
     }
-    const float all = (float)s.positions * (float)s.cg;
-    const bool one = s.positions * s.cg == 1;  // groups of one value have m1 = gamma dz and no gradient at all
-    const float kept = a.drop.threshold ? a.drop.scale : 1.f;
-    float mean[kG], rstd[kG];
-    auto statistics = [&](int n, float (&m)[kG], float (&r)[kG]) {
+    const float inv_all = 1.f / ((float)s.positions * (float)s.cg);
+    const int g = (int)threadIdx.x;            // the group this thread joins, if g < p.groups
+    int mine_g[kG];
 #pragma unroll
-        for (int i = 0; i < kG; ++i) {
-            const int64_t g = (int64_t)n * a.groups + (p.c0 + i) / s.cg;
-            m[i] = a.mean[g];
-            r[i] = a.rstd[g];
-        }
+    for (int i = 0; i < kG; ++i) mine_g[i] = (p.col * VEC + i) / s.cg;
+    // first values of the thread's groups, and of the group it joins
+    const T *firsts = static_cast<const T *>(a.x) + ((int64_t)p.first_sample * s.positions * a.ld_x + p.slab * s.sc);
+    T pivots[kG], pivot_g;
+    auto look_ahead = [&]() {
+#pragma unroll
+        for (int i = 0; i < kG; ++i) pivots[i] = firsts[mine_g[i] * s.cg];
+        pivot_g = firsts[(g < p.groups ? g : 0) * s.cg];
+        firsts += next_x;
     };
-    statistics(p.first_sample, mean, rstd);
+    look_ahead();
     int buf = 0;
     for (int n = p.first_sample; n < s.samples; n += s.walkers, buf ^= 1) {
-        float mean_next[kG], rstd_next[kG];
+        float m[kG];
+#pragma unroll
+        for (int i = 0; i < kG; ++i) m[i] = -to_float(pivots[i]);
+        float pivot = to_float(pivot_g);
+        src += next_x;
+        if (n + s.walkers < s.samples) {
+            fetch(buf ^ 1);
+            look_ahead();
+        }
+        copies_issued();
+        copies_landed();
+        const uint4 *at = reinterpret_cast<const uint4 *>(sm) + buf * NV * kTH + threadIdx.x;
+        F2 less[NP];                           // minus the pivot, then minus the mean
+#pragma unroll
+        for (int i = 0; i < NP; ++i) less[i] = pair_of<UNI>(m, i);
+        for (int pass = 0;; ++pass) {
+            F2 t1[NP], t2[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) t1[i] = t2[i] = f2(0.f);
+            for_rows<NV>(p, [&](int k) {
+                F2 f[NP];
+                unpack2<T, VEC>(held<T>(at + k * kTH), f);
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const F2 d = add2(f[i], less[i]);
+                    t1[i] = add2(t1[i], d);
+                    t2[i] = fma2(d, d, t2[i]);
+                }
+            });
+            float acc[2][kG];
+            if constexpr (UNI) {
+#pragma unroll
+                for (int i = 1; i < NP; ++i) {
+                    t1[0] = add2(t1[0], t1[i]);
+                    t2[0] = add2(t2[0], t2[i]);
+                }
+                acc[0][0] = low(t1[0]) + high(t1[0]);
+                acc[1][0] = low(t2[0]) + high(t2[0]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    acc[0][2 * i] = low(t1[i]);
+                    acc[0][2 * i + 1] = high(t1[i]);
+                    acc[1][2 * i] = low(t2[i]);
+                    acc[1][2 * i + 1] = high(t2[i]);
+                }
+            }
+            float *my_area = area + (ex.turn & 1) * 2 * kTH * kG;
+            if (threadIdx.x == 0) {
+                again[ex.turn & 1] = 0;
+                if (s.cluster > 1) ex.expect(p.groups, s.cluster);
+            }
+            put_groups<2, VEC, UNI, kTH / 32>(acc, p, s.cg, my_area, sums);
+            if (g < p.groups) {
+                float total = group_sum<2, UNI, kTH / 32>(0, g, p, my_area, sums), squares = group_sum<2, UNI, kTH / 32>(1, g, p, my_area, sums);
+                if (s.cluster > 1) {
+                    ex.tell(make_float2(total, squares), p.rank, g, s.cluster, gmax);
+                    ex.hear(a.status, a.wait_ns);
+                    total = squares = 0.f;
+                    for (int r = 0; r < s.cluster; ++r) {
+                        const float2 v = *ex.at(r, g, s.cluster, gmax);
+                        total += v.x;
+                        squares += v.y;
+                    }
+                }
+                const float off = total * inv_all, m2 = fmaxf(fmaf(-total, off, squares), 0.f);
+                if (pass == 0 && m2 * 16.f < squares) again[ex.turn & 1] = 1;
+                const float mean = pivot + off, rstd = 1.f / sqrtf(fmaf(m2, inv_all, a.eps));
+                pivot = mean;
+                ready[g] = mean;
+                ready[gmax + g] = rstd;
+                if (a.mean && p.rank == 0) {
+                    const int64_t to = (int64_t)n * a.groups + p.slab * gmax + g;
+                    a.mean[to] = mean;
+                    a.rstd[to] = rstd;
+                }
+            }
+            __syncthreads();
+            const int more = again[ex.turn & 1];
+            ++ex.turn;
+#pragma unroll
+            for (int i = 0; i < kG; ++i) m[i] = -ready[mine_g[i]];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) less[i] = pair_of<UNI>(m, i);
+            if (!more) break;
+        }
+        F2 scaled[NP], spread[NP];
+#pragma unroll
+        for (int i = 0; i < kG; ++i) m[i] = ready[gmax + mine_g[i]];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            spread[i] = pair_of<UNI>(m, i);
+            scaled[i] = mul2(spread[i], gamma[i]);
+        }
+        unsigned long long e = a.drop.offset + (unsigned long long)((row0 + (int64_t)(n - p.first_sample) * s.positions) * s.channels + p.c0);
+        T *to = dst;
+        for_rows<NV>(p, [&](int k) {
+            F2 f[NP];
+            unpack2<T, VEC>(held<T>(at + k * kTH), f);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const F2 z = z_of<ACT>(add2(f[i], less[i]), spread[i], gamma[i], scaled[i], beta[i]);
+                if constexpr (ACT == kActSilu) f[i] = mul2(z, sigmoid2(z));
+                else f[i] = f2(act_value<ACT>(low(z)), act_value<ACT>(high(z)));
+            }
+            if (a.drop.threshold) {
+                drop_select2<VEC>(f, a.drop, e);
+#pragma unroll
+                for (int i = 0; i < NP; ++i) f[i] = mul2(f[i], f2(a.drop.scale));
+                e += (unsigned long long)p.rt * s.channels;
+            }
+            store_packed<T, VEC>(to, pack2<T, VEC>(f));
+            to += step_y;
+        });
+        dst += next_y;
+    }
+    if (s.cluster > 1) cluster_meet();         // nobody leaves while a peer may still write to it
+}
+
+// Rows of channel sums that a CTA leaves for each sample: the lines of the CTA in this many shares.
+constexpr int kShares = 2;
+
+// Backward: x and dy are read once; dz takes the place of dy, in registers.  sum1, sum2 (may be null): the sums of dz and
+// of dz xhat of each channel over a share of this CTA's rows of a sample, [samples][cluster][shares] rows of ld_sum;
+// `whole`: one row per sample, cluster = 1.
+template <typename T, int NV, int kTH, bool UNI, int ACT>
+__global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_grad_kernel(const GroupNormArgs a, const Slab s, float *sum1, float *sum2, int64_t ld_sum, int whole) {
+    constexpr int VEC = 16 / (int)sizeof(T), NP = VEC / 2, kG = UNI ? 1 : VEC;
+    extern __shared__ __align__(16) float sm[];
+    const Spot p = spot<VEC, NV, kTH>(s);
+    const int gmax = s.sc / s.cg;
+    float *entries = sm + 4 * NV * kTH * 4;    // [2][rt][2 * width]: channel sums of the thread rows, by turns
+    float *area = entries + 4 * kTH * VEC;     // [2][kTH * 2 * kG]: by turns
+    float *ready = area + 4 * kTH * kG;        // [2][2][gmax]: by turns
+    float *sums = ready + 4 * gmax;            // [2][gmax]
+    Exchange ex;
+    open_exchange(ex, sums + 2 * gmax, s.cluster, gmax);
+    const int both = 2 * p.width;
+    const uint32_t mine_at = i8::smem_u32(sm) + threadIdx.x * 16;
+    const int64_t row0 = (int64_t)p.first_sample * s.positions + (int64_t)p.rank * s.rows_per_cta + max(p.j, 0);
+    const T *src = static_cast<const T *>(a.x) + (row0 * a.ld_x + p.c0);
+    const T *up = static_cast<const T *>(a.dy) + (row0 * a.ld_dy + p.c0);
+    T *dst = static_cast<T *>(a.y) + (row0 * a.ld_y + p.c0);
+    const int64_t step_x = (int64_t)p.rt * a.ld_x, step_dy = (int64_t)p.rt * a.ld_dy, step_y = (int64_t)p.rt * a.ld_y;
+    const int64_t next = (int64_t)s.walkers * s.positions;
+    auto fetch = [&](int buf) {
+        const T *from = src, *from_dy = up;
+        for_rows<NV>(p, [&](int k) {
+            copy16(mine_at + (uint32_t)(buf * 2 * NV + k) * (kTH * 16), from);
+            copy16(mine_at + (uint32_t)((buf * 2 + 1) * NV + k) * (kTH * 16), from_dy);
+            from += step_x;
+            from_dy += step_dy;
+        });
+    };
+    fetch(0);
+    copies_issued();
+    F2 gamma[NP], beta[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        gamma[i] = a.gamma ? f2(__ldg(a.gamma + p.c0 + 2 * i), __ldg(a.gamma + p.c0 + 2 * i + 1)) : f2(1.f);
+        beta[i] = a.beta ? f2(__ldg(a.beta + p.c0 + 2 * i), __ldg(a.beta + p.c0 + 2 * i + 1)) : f2(0.f);
+    }
+    const float inv_all = 1.f / ((float)s.positions * (float)s.cg);
+    const bool one = s.positions * s.cg == 1;  // groups of one value have m1 = gamma dz and no gradient at all
+    const float kept = a.drop.threshold ? a.drop.scale : 1.f;
+    const int g = (int)threadIdx.x;            // the group this thread joins, if g < p.groups
+    int mine_g[kG];
+#pragma unroll
+    for (int i = 0; i < kG; ++i) mine_g[i] = (p.col * VEC + i) / s.cg;
+    const float *mean_in = a.mean + (int64_t)p.first_sample * a.groups + p.slab * gmax;
+    const float *rstd_in = a.rstd + (int64_t)p.first_sample * a.groups + p.slab * gmax;
+    float mean[kG], rstd[kG];
+    auto look_ahead = [&]() {
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            mean[i] = mean_in[mine_g[i]];
+            rstd[i] = rstd_in[mine_g[i]];
+        }
+        mean_in += (int64_t)s.walkers * a.groups;
+        rstd_in += (int64_t)s.walkers * a.groups;
+    };
+    look_ahead();
+    int buf = 0;
+    for (int n = p.first_sample; n < s.samples; n += s.walkers, buf ^= 1) {
+        F2 dz[NV][NP], s1[NP], s2[NP], scaled[NP], less[NP], spread[NP];
+        {
+            float m[kG];
+#pragma unroll
+            for (int i = 0; i < kG; ++i) m[i] = -mean[i];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                s1[i] = s2[i] = f2(0.f);
+                less[i] = pair_of<UNI>(m, i);
+                spread[i] = pair_of<UNI>(rstd, i);
+                scaled[i] = mul2(gamma[i], spread[i]);
+            }
+        }
         if (n + s.walkers < s.samples) {
             src += next * a.ld_x;
             up += next * a.ld_dy;
             fetch(buf ^ 1);
-            statistics(n + s.walkers, mean_next, rstd_next);
+            look_ahead();
         }
         copies_issued();
         copies_landed();
-        const uint32_t at_x = mine_at + (uint32_t)(buf * 2 * NV) * (kTH * 16), at_dy = at_x + NV * kTH * 16;
-        const int64_t row = (int64_t)n * s.positions + (int64_t)p.rank * s.rows_per_cta + max(p.j, 0);
-        unsigned long long e = a.drop.offset + (unsigned long long)(row * s.channels + p.c0);
-        const unsigned long long step_e = (unsigned long long)p.rt * s.channels;
-        F2 dz[NV][NP], s1[NP], s2[NP], scaled[NP];
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            s1[i] = s2[i] = f2(0.f);
-            scaled[i] = mul2(gamma[i], pair_of<UNI>(rstd, i));
-        }
+        const uint4 *at_x = reinterpret_cast<const uint4 *>(sm) + buf * 2 * NV * kTH + threadIdx.x, *at_dy = at_x + NV * kTH;
+        unsigned long long e = a.drop.offset + (unsigned long long)((row0 + (int64_t)(n - p.first_sample) * s.positions) * s.channels + p.c0);
         // dz without the scale of the kept elements, which the sums and the coefficients of dx take in
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k < p.mine) {
-                F2 f[NP];
-                unpack2<T, VEC>(held<T>(at_x + k * (kTH * 16)), f);
-                unpack2<T, VEC>(held<T>(at_dy + k * (kTH * 16)), dz[k]);
-                if (a.drop.threshold) {
-                    drop_select2<VEC>(dz[k], a.drop, e);
-                    e += step_e;
-                }
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const F2 m = pair_of<UNI>(mean, i), centred = add2(f[i], {-m.x, -m.y});
-                    if constexpr (ACT != kActNone) {
-                        const F2 z = z_of<ACT>(centred, pair_of<UNI>(rstd, i), gamma[i], scaled[i], beta[i]);
-                        if constexpr (ACT == kActSilu) {
-                            const F2 sg = sigmoid2(z);
-                            dz[k][i] = mul2(dz[k][i], mul2(sg, fma2(z, fma2(sg, f2(-1.f), f2(1.f)), f2(1.f))));
-                        } else {
-                            dz[k][i] = {z.x > 0.f ? dz[k][i].x : 0.f, z.y > 0.f ? dz[k][i].y : 0.f};
-                        }
-                    }
-                    s1[i] = add2(s1[i], dz[k][i]);
-                    s2[i] = fma2(dz[k][i], centred, s2[i]);
-                }
+        for_rows<NV>(p, [&](int k) {
+            F2 f[NP];
+            unpack2<T, VEC>(held<T>(at_x + k * kTH), f);
+            unpack2<T, VEC>(held<T>(at_dy + k * kTH), dz[k]);
+            if (a.drop.threshold) {
+                drop_select2<VEC>(dz[k], a.drop, e);
+                e += (unsigned long long)p.rt * s.channels;
             }
-        if (sum1 || sum2) {     // the channels' sums, on their way while the groups are joined
-            float t[2 * VEC];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const F2 r = pair_of<UNI>(rstd, i);
-                t[2 * i] = s1[i].x * kept;
-                t[2 * i + 1] = s1[i].y * kept;
-                t[VEC + 2 * i] = s2[i].x * (r.x * kept);
-                t[VEC + 2 * i + 1] = s2[i].y * (r.y * kept);
+                const F2 centred = add2(f[i], less[i]);
+                if constexpr (ACT != kActNone) {
+                    const F2 z = z_of<ACT>(centred, spread[i], gamma[i], scaled[i], beta[i]);
+                    if constexpr (ACT == kActSilu) {
+                        const F2 sg = sigmoid2(z);
+                        dz[k][i] = mul2(dz[k][i], mul2(sg, fma2(z, fma2(sg, f2(-1.f), f2(1.f)), f2(1.f))));
+                    } else {
+                        dz[k][i] = f2(low(z) > 0.f ? low(dz[k][i]) : 0.f, high(z) > 0.f ? high(dz[k][i]) : 0.f);
+                    }
+                }
+                s1[i] = add2(s1[i], dz[k][i]);
+                s2[i] = fma2(dz[k][i], centred, s2[i]);
             }
-            if (folded) sum_rows_of_warp<2 * VEC>(t, p.vpr);
-            if (puts) {
-                float *mine = entries + (buf * lines + line) * both + p.col * VEC;
+        });
+        // the channels' sums, on their way while the groups are joined
+        float *my_entries = entries + buf * 2 * kTH * VEC;
+        if ((sum1 || sum2) && p.j >= 0) {
+            float *mine = my_entries + p.j * both + p.col * VEC;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    mine[i] = t[i];
-                    mine[p.width + i] = t[VEC + i];
+            for (int i = 0; i < NP; i += 2) {
+                const F2 u1 = mul2(s1[i], f2(kept)), v1 = mul2(s1[i + 1], f2(kept));
+                const F2 u2 = mul2(s2[i], mul2(spread[i], f2(kept))), v2 = mul2(s2[i + 1], mul2(spread[i + 1], f2(kept)));
+                *reinterpret_cast<float4 *>(mine + 2 * i) = make_float4(low(u1), high(u1), low(v1), high(v1));
+                *reinterpret_cast<float4 *>(mine + p.width + 2 * i) = make_float4(low(u2), high(u2), low(v2), high(v2));
+            }
+        }
+        // the groups' sums of gamma dz and gamma dz (x - mean)
+        float acc[2][kG];
+        if constexpr (UNI) {
+            F2 u1 = mul2(gamma[0], s1[0]), u2 = mul2(gamma[0], s2[0]);
+#pragma unroll
+            for (int i = 1; i < NP; ++i) {
+                u1 = fma2(gamma[i], s1[i], u1);
+                u2 = fma2(gamma[i], s2[i], u2);
+            }
+            acc[0][0] = low(u1) + high(u1);
+            acc[1][0] = low(u2) + high(u2);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const F2 u1 = mul2(gamma[i], s1[i]), u2 = mul2(gamma[i], s2[i]);
+                acc[0][2 * i] = low(u1);
+                acc[0][2 * i + 1] = high(u1);
+                acc[1][2 * i] = low(u2);
+                acc[1][2 * i + 1] = high(u2);
+            }
+        }
+        if (s.cluster > 1 && a.y && threadIdx.x == 0) ex.expect(p.groups, s.cluster);
+        float *my_area = area + buf * 2 * kTH * kG, *now = ready + buf * 2 * gmax;
+        put_groups<2, VEC, UNI, kTH / 32>(acc, p, s.cg, my_area, sums);
+        // a thread per group joins the CTAs.  dx = rstd (gamma dz - m1 - xhat m2)
+        //   = (rstd gamma) dz - rstd^3 M2 (x - mean) - rstd m1,  M2 the mean of gamma dz (x - mean)
+        if (a.y && g < p.groups) {
+            float t1 = group_sum<2, UNI, kTH / 32>(0, g, p, my_area, sums), t2 = group_sum<2, UNI, kTH / 32>(1, g, p, my_area, sums);
+            if (s.cluster > 1) {
+                ex.tell(make_float2(t1, t2), p.rank, g, s.cluster, gmax);
+                ex.hear(a.status, a.wait_ns);
+                t1 = t2 = 0.f;
+                for (int r = 0; r < s.cluster; ++r) {
+                    const float2 v = *ex.at(r, g, s.cluster, gmax);
+                    t1 += v.x;
+                    t2 += v.y;
                 }
             }
+            now[g] = t1 * inv_all;
+            now[gmax + g] = t2 * inv_all;
         }
-        // the groups' sums of gamma dz and gamma dz xhat
-        float acc[2][kG];
-#pragma unroll
-        for (int i = 0; i < kG; ++i) acc[0][i] = acc[1][i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            acc[0][UNI ? 0 : 2 * i] = fmaf(gamma[i].x, s1[i].x, acc[0][UNI ? 0 : 2 * i]);
-            acc[0][UNI ? 0 : 2 * i + 1] = fmaf(gamma[i].y, s1[i].y, acc[0][UNI ? 0 : 2 * i + 1]);
-            acc[1][UNI ? 0 : 2 * i] = fmaf(gamma[i].x, s2[i].x, acc[1][UNI ? 0 : 2 * i]);
-            acc[1][UNI ? 0 : 2 * i + 1] = fmaf(gamma[i].y, s2[i].y, acc[1][UNI ? 0 : 2 * i + 1]);
-        }
-        sum_groups<2, VEC, UNI>(acc, p, s.cg, area + buf * kTH * (UNI ? 2 : VEC), sums);
-        if (sum1 || sum2) {     // sum_groups had a barrier: the entries are there
-            for (int c = (int)threadIdx.x; c < both; c += kTH) {
-                float t = 0.f;
-                const float *in = entries + buf * lines * both + c;
+        ++ex.turn;
+        if (sum1 || sum2) {     // put_groups had a barrier: the entries are there
+            if (whole) {
+                for (int c = (int)threadIdx.x; c < both; c += kTH) {
+                    float t = 0.f;
 #pragma unroll 8
-                for (int r = 0; r < lines; ++r) t += in[r * both];
-                float *out = c < p.width ? sum1 : sum2;
-                if (out) out[((int64_t)n * s.cluster + p.rank) * ld_sum + p.slab * s.sc + (c < p.width ? c : c - p.width)] = t;
+                    for (int r = 0; r < p.rt; ++r) t += my_entries[r * both + c];
+                    float *out = c < p.width ? sum1 : sum2;
+                    if (out) out[(int64_t)n * ld_sum + p.slab * s.sc + (c < p.width ? c : c - p.width)] = t;
+                }
+            } else {
+                for (int w = (int)threadIdx.x; w < kShares * both; w += kTH) {
+                    const int share = w / both, c = w - share * both;
+                    float t = 0.f;
+#pragma unroll 8
+                    for (int r = share * p.rt / kShares; r < (share + 1) * p.rt / kShares; ++r) t += my_entries[r * both + c];
+                    float *out = c < p.width ? sum1 : sum2;
+                    if (out)
+                        out[(((int64_t)n * s.cluster + p.rank) * kShares + share) * ld_sum + p.slab * s.sc + (c < p.width ? c : c - p.width)] = t;
+                }
             }
         }
         if (a.y) {
-            if (s.cluster > 1) {
-                float *box = peers + (size_t)buf * s.cluster * 2 * gmax;
+            __syncthreads();
+            float acc1[kG], acc2[kG], r1[kG];
 #pragma unroll
-                for (int i = 0; i < kG; ++i)
-                    if (p.j == 0 && (p.col * VEC + i) % s.cg == 0) {
-                        const int g = (p.col * VEC + i) / s.cg;
-                        hand_out(&box[p.rank * 2 * gmax + g], acc[0][i], s.cluster);
-                        hand_out(&box[(p.rank * 2 + 1) * gmax + g], acc[1][i], s.cluster);
-                    }
-                cluster_meet();
-#pragma unroll
-                for (int i = 0; i < kG; ++i) {
-                    const float *in = box + (p.col * VEC + i) / s.cg;
-                    float t1 = 0.f, t2 = 0.f;
-                    for (int r = 0; r < s.cluster; ++r) {
-                        t1 += in[r * 2 * gmax];
-                        t2 += in[(r * 2 + 1) * gmax];
-                    }
-                    acc[0][i] = t1;
-                    acc[1][i] = t2;
-                }
+            for (int i = 0; i < NP; ++i) {
+                if constexpr (UNI) r1[0] = low(spread[0]);
+                else { r1[2 * i] = low(spread[i]); r1[2 * i + 1] = high(spread[i]); }
             }
-            // dx = rstd (gamma dz - m1 - xhat m2) = (rstd gamma) dz - rstd^3 M2 (x - mean) - rstd m1,  M2 the mean of gamma dz (x - mean)
 #pragma unroll
             for (int i = 0; i < kG; ++i) {
-                const float r = rstd[i] * kept;
-                acc[0][i] = -r * (acc[0][i] / all);
-                acc[1][i] = -r * rstd[i] * rstd[i] * (acc[1][i] / all);
+                const float r = r1[i] * kept;
+                acc1[i] = -r * now[mine_g[i]];
+                acc2[i] = -r * r1[i] * r1[i] * now[gmax + mine_g[i]];
             }
-            T *dst = static_cast<T *>(a.y) + (row * a.ld_y + p.c0);
+            F2 c1[NP], c2[NP];
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (k < p.mine) {
-                    F2 f[NP];
-                    unpack2<T, VEC>(held<T>(at_x + k * (kTH * 16)), f);
+            for (int i = 0; i < NP; ++i) {
+                c1[i] = pair_of<UNI>(acc1, i);
+                c2[i] = pair_of<UNI>(acc2, i);
+                scaled[i] = mul2(scaled[i], f2(kept));
+            }
+            T *to = dst;
+            for_rows<NV>(p, [&](int k) {
+                F2 f[NP];
+                unpack2<T, VEC>(held<T>(at_x + k * kTH), f);
 #pragma unroll
-                    for (int i = 0; i < NP; ++i) {
-                        const F2 m = pair_of<UNI>(mean, i), centred = add2(f[i], {-m.x, -m.y});
-                        f[i] = fma2(mul2(scaled[i], f2(kept)), dz[k][i], fma2(pair_of<UNI>(acc[1], i), centred, pair_of<UNI>(acc[0], i)));
-                        if (one) f[i] = f2(0.f);
-                    }
-                    store_packed<T, VEC>(dst, pack2<T, VEC>(f));
-                    dst += step_y;
+                for (int i = 0; i < NP; ++i) {
+                    f[i] = fma2(scaled[i], dz[k][i], fma2(c2[i], add2(f[i], less[i]), c1[i]));
+                    if (one) f[i] = f2(0.f);
                 }
-        }
-#pragma unroll
-        for (int i = 0; i < kG; ++i) {
-            mean[i] = mean_next[i];
-            rstd[i] = rstd_next[i];
+                store_packed<T, VEC>(to, pack2<T, VEC>(f));
+                to += step_y;
+            });
+            dst += next * a.ld_y;
         }
     }
+    if (s.cluster > 1) cluster_meet();
 }
 
 template <int V> struct Int { static constexpr int value = V; };
 
 // The slab and the cluster of an item, and the vectors a thread holds: false where an item does not fit.
-bool choose(int elem, int channels, int groups, int64_t samples, int64_t positions, int max_nv, Slab &s, int &nv) {
+bool choose(int elem, int channels, int groups, int64_t samples, int64_t positions, int kTH, int max_nv, Slab &s, int &nv) {
     const int vec = 16 / elem_bytes(elem);
     if (channels % vec || samples > 0x3fffffff) return false;
     s.cg = channels / groups;
     s.channels = channels;
     s.positions = positions;
     s.samples = (int)samples;
-    const int unit = std::lcm(s.cg, vec), wanted = 128 / elem_bytes(elem);
+    const int unit = std::lcm(s.cg, vec), wanted = CR_GN_WIDE / elem_bytes(elem);
     for (int width = std::min(channels, unit * std::max(1, wanted / unit));; width = std::max(unit, width / 2 / unit * unit)) {
         if (width / vec <= kTH) {
             const int rt = kTH / (width / vec);
@@ -558,43 +684,42 @@ bool choose(int elem, int channels, int groups, int64_t samples, int64_t positio
     }
 }
 
-// Clusters that are resident together, asked of the runtime once per kernel and cluster size.
+// What a kernel needs to be told once per device, and the clusters that are resident together, asked of the runtime once
+// per kernel, device and cluster size.
+struct Known {
+    static constexpr int kDevices = 16;
+    std::atomic<int> resident[kDevices][4] = {};
+};
 template <typename K>
-int resident_clusters(K kernel, int cluster, size_t smem, std::atomic<int> *known) {
+cudaError_t resident_clusters(K kernel, Known &known, int device, const cudaLaunchConfig_t &cfg, int cluster, int &r) {
     int log = 0;
     while (1 << log < cluster) ++log;
-    int r = known[log].load(std::memory_order_relaxed);
-    if (r) return r;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)cluster);
-    cfg.blockDim = dim3(kTH);
-    cfg.dynamicSmemBytes = smem;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&r, kernel, &cfg) != cudaSuccess || r < 1) {
-        (void)cudaGetLastError();
-        r = 1;
+    std::atomic<int> *place = device < Known::kDevices ? &known.resident[device][log] : nullptr;
+    r = place ? place->load(std::memory_order_relaxed) : 0;
+    if (r) return cudaSuccess;
+    // the largest shared memory a block may have, so that the attribute need not follow the call's sizes
+    int most = 0;
+    cudaError_t e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, device);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == cudaSuccess && cluster > 1) {
+        e = cudaOccupancyMaxActiveClusters(&r, kernel, &cfg);
+    } else if (e == cudaSuccess) {
+        int sms = 0;
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r, kernel, (int)cfg.blockDim.x, cfg.dynamicSmemBytes);
+        r *= sms;
     }
-    known[log].store(r, std::memory_order_relaxed);
-    return r;
+    if (e != cudaSuccess) return e;
+    r = std::max(r, 1);
+    if (place) place->store(r, std::memory_order_relaxed);
+    return cudaSuccess;
 }
 
 template <typename K, typename... More>
-cudaError_t launch(K kernel, std::atomic<int> *known, Slab s, size_t smem, cudaStream_t stream, int64_t *launches, const GroupNormArgs &a, More... more) {
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
-    // as many clusters as fit, in equal numbers per slab; each walks over every walkers-th sample
-    const int64_t rounds = std::max(1, resident_clusters(kernel, s.cluster, smem, known) / s.slabs);
-    s.walkers = (int)std::min<int64_t>(s.samples, rounds);
+cudaError_t launch(K kernel, int threads, Known &known, Slab s, size_t smem, cudaStream_t stream, int64_t *launches, const GroupNormArgs &a, More... more) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)s.walkers * (unsigned)s.slabs * (unsigned)s.cluster);
-    cfg.blockDim = dim3(kTH);
+    cfg.gridDim = dim3((unsigned)s.cluster);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -603,12 +728,18 @@ cudaError_t launch(K kernel, std::atomic<int> *known, Slab s, size_t smem, cudaS
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = s.cluster > 1 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, s, more...);
+    int resident = 0;
+    cudaError_t e = resident_clusters(kernel, known, a.device, cfg, s.cluster, resident);
+    if (e != cudaSuccess) return e;
+    // as many clusters as fit, in equal numbers per slab; each walks over every walkers-th sample
+    s.walkers = (int)std::min<int64_t>(s.samples, std::max(1, resident / s.slabs));
+    cfg.gridDim = dim3((unsigned)s.walkers * (unsigned)s.slabs * (unsigned)s.cluster);
+    e = cudaLaunchKernelEx(&cfg, kernel, a, s, more...);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
 
-constexpr int kForwardNV = CR_GN_FNV, kBackwardNV = CR_GN_BNV;
+constexpr int kForwardNV = CR_GN_FNV, kBackwardNV = CR_GN_BNV, kForwardTH = CR_GN_FTH, kBackwardTH = CR_GN_BTH;
 
 template <int Low, int High, typename F>
 cudaError_t by_nv(int nv, F &&f) {
@@ -638,18 +769,18 @@ cudaError_t by_type_act(int elem, int act, F &&f) {
 bool group_norm_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem) {
     Slab s;
     int nv;
-    return choose(elem, channels, groups, samples, positions, kForwardNV, s, nv);
+    return choose(elem, channels, groups, samples, positions, kForwardTH, kForwardNV, s, nv);
 }
 int group_norm_backward_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem) {
     Slab s;
     int nv;
-    return choose(elem, channels, groups, samples, positions, kBackwardNV, s, nv) ? s.cluster : 0;
+    return choose(elem, channels, groups, samples, positions, kBackwardTH, kBackwardNV, s, nv) ? s.cluster * kShares : 0;
 }
 
 cudaError_t launch_group_norm_on_chip(const GroupNormArgs &a, cudaStream_t stream, int64_t *launches) {
     Slab s;
     int nv;
-    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, kForwardNV, s, nv)) return cudaErrorInvalidValue;
+    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, kForwardTH, kForwardNV, s, nv)) return cudaErrorInvalidValue;
     return by_type_act(a.elem, a.act, [&](auto t, auto act) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T), ACT = decltype(act)::value;
@@ -658,32 +789,33 @@ cudaError_t launch_group_norm_on_chip(const GroupNormArgs &a, cudaStream_t strea
             constexpr int NV = decltype(n)::value;
             auto go = [&](auto uni) {
                 constexpr bool UNI = decltype(uni)::value != 0;
-                static std::atomic<int> known[4];
-                const size_t smem = (size_t)2 * NV * kTH * 16 + ((size_t)2 * kTH * (UNI ? 1 : VEC) + gmax + (size_t)4 * s.cluster * gmax) * 4;
-                return launch(cr_group_norm_kernel<T, NV, UNI, ACT>, known, s, smem, stream, launches, a);
+                constexpr int kTH = kForwardTH;
+                static Known known;
+                const size_t smem = (size_t)2 * NV * kTH * 16 + ((size_t)4 * kTH * (UNI ? 1 : VEC) + 4 * gmax + 2) * 4 + exchange_bytes(s.cluster, gmax);
+                return launch(cr_group_norm_kernel<T, NV, kTH, UNI, ACT>, kTH, known, s, smem, stream, launches, a);
             };
             return s.cg % VEC == 0 ? go(Int<1>{}) : go(Int<0>{});
         });
     });
 }
 
-cudaError_t launch_group_norm_grad_on_chip(const GroupNormArgs &a, float *sum1, float *sum2, int64_t ld_sum, cudaStream_t stream, int64_t *launches) {
+cudaError_t launch_group_norm_grad_on_chip(const GroupNormArgs &a, float *sum1, float *sum2, int64_t ld_sum, bool whole, cudaStream_t stream,
+                                           int64_t *launches) {
     Slab s;
     int nv;
-    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, kBackwardNV, s, nv)) return cudaErrorInvalidValue;
+    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, kBackwardTH, kBackwardNV, s, nv)) return cudaErrorInvalidValue;
     return by_type_act(a.elem, a.act, [&](auto t, auto act) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T), ACT = decltype(act)::value;
         const int gmax = s.sc / s.cg;
-        const int last = s.channels - (s.slabs - 1) * s.sc;     // a narrow last slab may need what a full one does not
-        s.entries = 32 % (s.sc / VEC) == 0 && 32 % (last / VEC) == 0 ? kWarps * 2 * s.sc : kTH * 2 * VEC;
         return by_nv<2, kBackwardNV>(nv, [&](auto n) {
             constexpr int NV = decltype(n)::value;
             auto go = [&](auto uni) {
                 constexpr bool UNI = decltype(uni)::value != 0;
-                static std::atomic<int> known[4];
-                const size_t smem = (size_t)4 * NV * kTH * 16 + ((size_t)2 * kTH * (UNI ? 2 : VEC) + 2 * (size_t)s.entries + gmax + (size_t)4 * s.cluster * gmax) * 4;
-                return launch(cr_group_norm_grad_kernel<T, NV, UNI, ACT>, known, s, smem, stream, launches, a, sum1, sum2, ld_sum);
+                constexpr int kTH = kBackwardTH;
+                static Known known;
+                const size_t smem = (size_t)4 * NV * kTH * 16 + ((size_t)4 * kTH * VEC + (size_t)4 * kTH * (UNI ? 1 : VEC) + 6 * gmax) * 4 + exchange_bytes(s.cluster, gmax);
+                return launch(cr_group_norm_grad_kernel<T, NV, kTH, UNI, ACT>, kTH, known, s, smem, stream, launches, a, sum1, sum2, ld_sum, whole ? 1 : 0);
             };
             return s.cg % VEC == 0 ? go(Int<1>{}) : go(Int<0>{});
         });

@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "cr_elem.cuh"
@@ -365,8 +366,14 @@ cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &d
     if (encode_codes(encode, &map_w, p.w, p.inner, p.outer, p.ld_w, kRows) != CUDA_SUCCESS ||
         encode_codes(encode, &map_x, p.x, p.inner, p.tokens, p.ld_x, TN) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    cudaError_t e = cudaFuncSetAttribute(cr_int8_product_kernel<T, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+    // told once per device: the largest shared memory of a block, whatever this call needs
+    static std::atomic<uint64_t> told{0};
+    cudaError_t e;
+    if (p.device > 63 || !(told.load(std::memory_order_relaxed) >> p.device & 1)) {
+        e = cudaFuncSetAttribute(cr_int8_product_kernel<T, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem_optin);
+        if (e != cudaSuccess) return e;
+        if (p.device <= 63) told.fetch_or(1ull << p.device, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : std::min<int64_t>(tiles, dev.sm_count)));
     cfg.blockDim = dim3(192);
@@ -377,7 +384,7 @@ cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &d
     attr[0].val.clusterDim.x = (unsigned)splits;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = splits > 1 ? 1 : 0;
     e = cudaLaunchKernelEx(&cfg, cr_int8_product_kernel<T, TN>, map_w, map_x, a, splits);
     if (e == cudaSuccess) ++*launches;
     return e;

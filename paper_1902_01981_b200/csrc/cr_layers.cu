@@ -522,13 +522,13 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
     const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
     const bool params = a.dgamma || a.dbeta;
     cudaError_t e;
-    if (const int cluster = wide ? group_norm_backward_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem) : 0) {
+    if (const int rows = wide ? group_norm_backward_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem) : 0) {
         // a partition of one sample that one CTA holds has its sums where they belong
-        if (a.partitions == a.samples && cluster == 1) return launch_group_norm_grad_on_chip(a, a.dbeta, a.dgamma, a.ld_param, stream, launches);
-        sum2 = sum1 + plane * cluster;
-        e = launch_group_norm_grad_on_chip(a, params ? sum1 : nullptr, params ? sum2 : nullptr, a.channels, stream, launches);
+        if (a.partitions == a.samples && rows == 2) return launch_group_norm_grad_on_chip(a, a.dbeta, a.dgamma, a.ld_param, true, stream, launches);
+        sum2 = sum1 + plane * rows;
+        e = launch_group_norm_grad_on_chip(a, params ? sum1 : nullptr, params ? sum2 : nullptr, a.channels, false, stream, launches);
         if (e != cudaSuccess || !params) return e;
-        return launch_params(a, sum1, sum2, cluster, stream, launches);
+        return launch_params(a, sum1, sum2, rows, stream, launches);
     }
     auto run = [&](auto t, auto v, auto act) {
         using T = decltype(t);

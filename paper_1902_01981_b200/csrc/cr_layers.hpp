@@ -43,6 +43,9 @@ struct GroupNormArgs {
     float eps = 0.f;
     DropSpec drop;
     float *workspace = nullptr;
+    int *status = nullptr;            // the plan's status word and the bound of every device-side wait
+    unsigned long long wait_ns = 0;
+    int device = 0;
 };
 
 // Workspace in bytes, from the sizes alone.
@@ -52,12 +55,12 @@ cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &dev, cud
 cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 
 // The one-pass forms (cr_group_norm.cu), for vector rows: whether an item fits a cluster, for the backward pass with the
-// CTAs of that cluster (0: no).  The backward one leaves the sums of dz (sum1) and dz xhat (sum2) of each sample's
-// channels, a row of ld_sum for each CTA of the cluster.
+// rows of sums it leaves for a sample (0: no).  The backward one leaves the sums of dz (sum1) and dz xhat (sum2) of each
+// sample's channels in that many rows of ld_sum, or in one (`whole`, which takes an item that one CTA holds: two rows).
 bool group_norm_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem);
 int group_norm_backward_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem);
 cudaError_t launch_group_norm_on_chip(const GroupNormArgs &a, cudaStream_t stream, int64_t *launches);
-cudaError_t launch_group_norm_grad_on_chip(const GroupNormArgs &a, float *sum1, float *sum2, int64_t ld_sum, cudaStream_t stream,
+cudaError_t launch_group_norm_grad_on_chip(const GroupNormArgs &a, float *sum1, float *sum2, int64_t ld_sum, bool whole, cudaStream_t stream,
                                            int64_t *launches);
 
 // y = residual + dropout(x) over [rows][cols] with row strides; residual may be null.
@@ -79,6 +82,7 @@ struct Int8ProductArgs {
     int64_t tokens = 0, outer = 0, inner = 0;
     int64_t ld_x = 0, ld_w = 0, ld_y = 0;
     int elem = 0;
+    int device = 0;
 };
 cudaError_t launch_int8_product(const Int8ProductArgs &a, int *status, const DeviceInfo &dev, const Tuning &tune,
                                 EncodeTiledFn encode, cudaStream_t stream, int64_t *launches);
