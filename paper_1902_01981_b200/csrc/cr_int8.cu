@@ -183,13 +183,51 @@ __device__ __forceinline__ void store_output(const TcArgs &a, int token, int cha
     static_cast<T *>(a.y)[(long long)token * a.ld_y + channel] = from_float<T>(fmaf((float)sum, xs * ws, b));
 }
 
+// Warps that read accumulators out: with 8 of them two share a quarter of the lanes and halve the tokens, which keeps the
+// read-out of a 256-token tile under the MMAs of the next one (int to float conversion alone takes 2048 cycles a tile).
+__host__ __device__ constexpr int drain_warps(int tn) { return tn >= 128 ? 8 : 4; }
+
+// Scales and stores the accumulator columns [c0, c1) of a tile for this thread's lane (channel); `scales`: shared memory of
+// this warp for c1 - c0 floats.
+template <typename T, int COLS>
+__device__ __forceinline__ void drain(const TcArgs &a, uint32_t taddr, int token0, int channel, float *scales) {
+    const int lane = (int)threadIdx.x & 31;
+    const bool mine = channel < a.outer;
+    const float ws = mine ? __ldg(a.w_scale + channel) : 0.f;
+    const float b = mine && a.bias ? __ldg(a.bias + channel) : 0.f;
+    for (int c = lane; c < COLS; c += 32) scales[c] = token0 + c < a.tokens ? __ldg(a.x_scale + token0 + c) : 0.f;
+    __syncwarp();
+    T *out = static_cast<T *>(a.y) + ((long long)token0 * a.ld_y + channel);
+    const int count = min(COLS, a.tokens - token0);
+#pragma unroll 1
+    for (int c = 0; c < count; c += 16) {
+        int r[16];
+        i8::tmem_load_16(taddr + (uint32_t)c, r);
+        float xs[16];
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4 *>(&xs[j]) = *reinterpret_cast<const float4 *>(scales + c + j);
+        if (!mine) continue;
+        if (c + 16 <= count) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j, out += a.ld_y) *out = from_float<T>(fmaf((float)r[j], xs[j] * ws, b));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j, out += a.ld_y)
+                if (c + j < count) *out = from_float<T>(fmaf((float)r[j], xs[j] * ws, b));
+        }
+    }
+    __syncwarp();
+}
+
 template <typename T, int TN>
-__global__ void __launch_bounds__(192, 1)
+__global__ void __launch_bounds__(64 + 32 * drain_warps(TN), 1)
 cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const TcArgs a, const int splits) {
     using namespace i8;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     constexpr uint32_t kWBytes = kRows * kChunk, kStage = kWBytes + TN * kChunk;
+    constexpr int kDrain = drain_warps(TN), kThreads = 64 + 32 * kDrain, kCols1 = TN * 4 / kDrain;   // tokens a warp reads out
     constexpr uint32_t kCols = 2 * TN < 32 ? 32 : 2 * TN;
+    __shared__ __align__(16) float scales[kDrain][kCols1];
     const int S = a.stages;
     unsigned char *ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint64_t *full = reinterpret_cast<uint64_t *>(ring + (size_t)S * kStage);
@@ -206,7 +244,7 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
 
     if (tid == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], 4); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], kDrain); }
         flags[0] = 0; flags[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -267,42 +305,31 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
             if (!ok) { flags[0] = 1; atomicExch(a.status, 1); }
         }
     } else {
-        const int q = warp & 3;
-        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
+        const int q = warp & 3, c0 = (warp - 2) / 4 * kCols1;
+        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0;
         int use = 0;
         for (int t = first; t < tiles; t += step, ++use) {
             const int set = use & 1;
             int tm, tn;
             tile_at(a, t, tm, tn);
-            const int channel = tn * kRows + q * 32 + lane;
-            const bool mine = channel < a.outer;
-            const float ws = mine ? __ldg(a.w_scale + channel) : 0.f;
-            const float b = mine && a.bias ? __ldg(a.bias + channel) : 0.f;
             const bool ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[set], (uint32_t)((use >> 1) & 1), &flags[0], a.wait_ns) ? 1 : 0) != 0;
             if (!ok) {
                 if (lane == 0) { flags[0] = 1; atomicExch(a.status, 1); }
                 break;
             }
             tc_fence_after();
+            if (splits > 1) {
+                // every MMA that read the ring has finished: its memory takes the sums
+                int *sums = reinterpret_cast<int *>(ring) + c0 * kRows + q * 32 + lane;
 #pragma unroll 1
-            for (int c = 0; c < TN; c += 16) {
-                const int token0 = tm * TN + c;
-                if (token0 >= a.tokens && splits == 1) break;
-                int r[16];
-                tmem_load_16(lanes + (uint32_t)(set * TN + c), r);
-                if (splits > 1) {
-                    // every MMA that read the ring has finished: its memory takes the sums
-                    int *sums = reinterpret_cast<int *>(ring);
+                for (int c = 0; c < kCols1; c += 16) {
+                    int r[16];
+                    tmem_load_16(lanes + (uint32_t)(set * TN + c), r);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sums[(c + j) * kRows + q * 32 + lane] = r[j];
-                } else {
-                    const float xs_mine = token0 + (lane & 15) < a.tokens ? __ldg(a.x_scale + token0 + (lane & 15)) : 0.f;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float xs = __shfl_sync(0xffffffffu, xs_mine, j);
-                        if (mine && token0 + j < a.tokens) store_output<T>(a, token0 + j, channel, r[j], xs, ws, b);
-                    }
+                    for (int j = 0; j < 16; ++j) sums[(c + j) * kRows] = r[j];
                 }
+            } else {
+                drain<T, kCols1>(a, lanes + (uint32_t)(set * TN), tm * TN + c0, tn * kRows + q * 32 + lane, scales[warp - 2]);
             }
             tc_fence_before();
             __syncwarp();
@@ -319,7 +346,7 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         int tm, tn;
         tile_at(a, first, tm, tn);
         const int c0 = TN * rank / splits, c1 = TN * (rank + 1) / splits;
-        for (int e = tid; e < (c1 - c0) * kRows; e += 192) {
+        for (int e = tid; e < (c1 - c0) * kRows; e += kThreads) {
             const int c = c0 + e / kRows, l = e % kRows;
             const int token = tm * TN + c, channel = tn * kRows + l;
             if (token >= a.tokens || channel >= a.outer) continue;
@@ -332,6 +359,127 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     }
 }
 
+// Large products: two CTAs on neighbouring SMs share a tile of 256 channels x 256 tokens (cta_group::2).  Each brings its
+// half of the channels and its half of the tokens, so a byte that crosses from L2 serves twice the products that it
+// serves in the kernel above, which L2 paces there (13.8 TB/s at 58 % of the tensor cores' cycles on 8192 x 4096 x 8192).
+// The even CTA's thread issues the MMAs for both; its barriers count both CTAs' copies, its commits free both CTAs'
+// stages, and each CTA reads its own 128 channels out of its own tensor memory.
+constexpr int kPairStages = 6, kPairDrain = 8, kPairThreads = 64 + 32 * kPairDrain;
+
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+cr_int8_product_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const TcArgs a) {
+    using namespace i8;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    constexpr uint32_t kWBytes = kRows * kChunk, kXBytes = 128 * kChunk, kStage = kWBytes + kXBytes;
+    constexpr int S = kPairStages, TN = 256, kCols1 = TN * 4 / kPairDrain;
+    __shared__ __align__(16) float scales[kPairDrain][kCols1];
+    unsigned char *ring = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint64_t *full = reinterpret_cast<uint64_t *>(ring + (size_t)S * kStage);   // used in the even CTA
+    uint64_t *empty = full + S;
+    uint64_t *acc_full = empty + S, *acc_empty = acc_full + 2;                  // acc_empty: used in the even CTA
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    volatile int *flags = reinterpret_cast<volatile int *>(tmem_slot + 1);      // [0] someone gave up, [1] never set
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = (int)cluster_rank();
+    const int first = (int)blockIdx.x >> 1, step = (int)gridDim.x >> 1;
+    const int tiles = a.tiles_m * a.tiles_n;
+    if (tid == 0) {
+        for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], 2 * kPairDrain); }
+        flags[0] = 0; flags[1] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc_pair(tmem_slot, 2 * TN);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();          // both CTAs' barriers and tensor memory are there
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0, issued = 0;
+            uint32_t phase = 1;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step) {
+                int tm, tn;
+                tile_at(a, t, tm, tn);
+                for (int k = 0; k < a.chunks; ++k) {
+                    if (!mbar_wait(&empty[s], phase, &flags[0], a.wait_ns)) { ok = false; break; }
+                    unsigned char *st = ring + (size_t)s * kStage;
+                    if (rank == 0) mbar_expect_tx(&full[s], 2 * kStage);
+                    const uint32_t bar = map_to_rank(smem_u32(&full[s]), 0);
+                    tma_load_2d_pair(st, &map_w, k * kChunk, tn * 2 * kRows + rank * kRows, bar);
+                    tma_load_2d_pair(st + kWBytes, &map_x, k * kChunk, tm * TN + rank * 128, bar);
+                    ++issued;
+                    if (++s == S) { s = 0; phase ^= 1; }
+                }
+            }
+            if (!ok) {
+                flags[0] = 1;
+                atomicExch(a.status, 1);
+                if (rank == 0)
+                    for (int i = issued > S ? issued - S : 0; i < issued; ++i)
+                        mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), &flags[1], a.wait_ns);
+            } else {
+                // the commits of the last stages have arrived before this CTA may end
+                for (int i = issued > S ? issued - S : 0; i < issued; ++i)
+                    mbar_wait(&empty[i % S], (uint32_t)((i / S) & 1), &flags[1], a.wait_ns);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = instr_desc(2 * kRows, TN);
+            int s = 0, use = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step, ++use) {
+                const int set = use & 1;
+                if (!mbar_wait(&acc_empty[set], (uint32_t)(((use >> 1) & 1) ^ 1), &flags[0], a.wait_ns)) { ok = false; break; }
+                tc_fence_after();
+                for (int k = 0; k < a.chunks; ++k) {
+                    if (!mbar_wait(&full[s], phase, &flags[0], a.wait_ns)) { ok = false; break; }
+                    tc_fence_after();
+                    const unsigned char *st = ring + (size_t)s * kStage;
+#pragma unroll
+                    for (int q = 0; q < kChunk / 32; ++q)
+                        mma_i8_pair(tmem + (uint32_t)(set * TN), smem_desc(st + q * 32), smem_desc(st + kWBytes + q * 32), idesc, (k > 0 || q > 0) ? 1u : 0u);
+                    mma_commit_pair(&empty[s]);
+                    if (++s == S) { s = 0; phase ^= 1; }
+                }
+                if (ok) mma_commit_pair(&acc_full[set]);
+            }
+            if (!ok) { flags[0] = 1; atomicExch(a.status, 1); }
+        }
+    } else {
+        const int q = warp & 3, c0 = (warp - 2) / 4 * kCols1;
+        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0;
+        int use = 0;
+        for (int t = first; t < tiles; t += step, ++use) {
+            const int set = use & 1;
+            int tm, tn;
+            tile_at(a, t, tm, tn);
+            const bool ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[set], (uint32_t)((use >> 1) & 1), &flags[0], a.wait_ns) ? 1 : 0) != 0;
+            if (!ok) {
+                if (lane == 0) { flags[0] = 1; atomicExch(a.status, 1); }
+                break;
+            }
+            tc_fence_after();
+            drain<T, kCols1>(a, lanes + (uint32_t)(set * TN), tm * TN + c0, tn * 2 * kRows + rank * kRows + q * 32 + lane, scales[warp - 2]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&acc_empty[set]), 0));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();          // neither CTA ends while the other one's MMAs or commits may reach it
+    if (warp == 1) tmem_free_pair(tmem, 2 * TN);
+}
+
 CUresult encode_codes(EncodeTiledFn encode, CUtensorMap *map, const void *base, int64_t cols, int64_t rows, int64_t ld, int box_rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)ld};
@@ -340,43 +488,76 @@ CUresult encode_codes(EncodeTiledFn encode, CUtensorMap *map, const void *base, 
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-template <typename T, int TN>
-cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &dev, const Tuning &tune, EncodeTiledFn encode,
-                      cudaStream_t stream, int64_t *launches) {
+constexpr int kStaticSmem = 8 * 128 * 4;   // at most: the scales of eight read-out warps
+
+cudaError_t allow_most_smem(const void *kernel, std::atomic<uint64_t> &told, int device, const DeviceInfo &dev) {
+    // told once per device: the largest dynamic shared memory of a block, whatever this call needs
+    if (device <= 63 && (told.load(std::memory_order_relaxed) >> device & 1)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem_optin - kStaticSmem);
+    if (e == cudaSuccess && device <= 63) told.fetch_or(1ull << device, std::memory_order_relaxed);
+    return e;
+}
+
+TcArgs tc_args(const Int8ProductArgs &p, int tile_tokens, int tile_channels, int *status, const Tuning &tune) {
     TcArgs a;
     a.x_scale = p.x_scale; a.w_scale = p.w_scale; a.bias = p.bias; a.y = p.y; a.ld_y = p.ld_y;
     a.tokens = (int)p.tokens; a.outer = (int)p.outer;
-    a.tiles_m = (int)((p.tokens + TN - 1) / TN); a.tiles_n = (int)((p.outer + kRows - 1) / kRows);
+    a.tiles_m = (int)((p.tokens + tile_tokens - 1) / tile_tokens);
+    a.tiles_n = (int)((p.outer + tile_channels - 1) / tile_channels);
     a.chunks = (int)((p.inner + kChunk - 1) / kChunk);
+    a.stages = 0;
     a.status = status; a.wait_ns = tune.wait_limit_ns;
+    return a;
+}
+
+template <typename T>
+cudaError_t launch_pair(const Int8ProductArgs &p, int *status, const DeviceInfo &dev, const Tuning &tune, EncodeTiledFn encode,
+                        cudaStream_t stream, int64_t *launches) {
+    const TcArgs a = tc_args(p, 256, 2 * kRows, status, tune);
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+    if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
+    CUtensorMap map_w, map_x;
+    if (encode_codes(encode, &map_w, p.w, p.inner, p.outer, p.ld_w, kRows) != CUDA_SUCCESS ||
+        encode_codes(encode, &map_x, p.x, p.inner, p.tokens, p.ld_x, 128) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+    static std::atomic<uint64_t> told{0};
+    cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_int8_product_pair_kernel<T>), told, p.device, dev);
+    if (e != cudaSuccess) return e;
+    const size_t smem = (size_t)kPairStages * (kRows + 128) * kChunk + (2 * kPairStages + 4) * 8 + 16 + 1024;
+    const unsigned pairs = (unsigned)std::min<int64_t>(tiles, dev.sm_count / 2);
+    cr_int8_product_pair_kernel<T><<<2 * pairs, kPairThreads, smem, stream>>>(map_w, map_x, a);
+    e = cudaGetLastError();
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+template <typename T, int TN>
+cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &dev, const Tuning &tune, EncodeTiledFn encode,
+                      cudaStream_t stream, int64_t *launches) {
+    TcArgs a = tc_args(p, TN, kRows, status, tune);
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
     if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
     int splits = 1;
     while (splits < 8 && tiles * splits * 2 <= dev.sm_count && a.chunks >= 2 * splits * 2) splits *= 2;
     constexpr size_t kStage = (kRows + TN) * kChunk;
-    const size_t tail = 1024 + 256;
+    const size_t tail = 1024 + 256 + kStaticSmem;   // alignment, barriers, scales
     const size_t room = (size_t)dev.smem_optin - tail;
     int stages = (int)std::min<size_t>(8, room / kStage);
     const int per_cta = (a.chunks + splits - 1) / splits;
     // a ring no deeper than the CTA's work, but large enough for the sums of a split tile
-    if (tiles * splits <= dev.sm_count) stages = std::max(std::min(stages, per_cta), (int)((TN * kRows * 4 + kStage - 1) / kStage));
+    if (tiles * splits <= dev.sm_count) stages = std::min(stages, std::max(per_cta, (int)((TN * kRows * 4 + kStage - 1) / kStage)));
     a.stages = stages;
     const size_t smem = stages * kStage + (2 * stages + 4) * 8 + 16 + 1024;
     CUtensorMap map_w, map_x;
     if (encode_codes(encode, &map_w, p.w, p.inner, p.outer, p.ld_w, kRows) != CUDA_SUCCESS ||
         encode_codes(encode, &map_x, p.x, p.inner, p.tokens, p.ld_x, TN) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    // told once per device: the largest shared memory of a block, whatever this call needs
     static std::atomic<uint64_t> told{0};
-    cudaError_t e;
-    if (p.device > 63 || !(told.load(std::memory_order_relaxed) >> p.device & 1)) {
-        e = cudaFuncSetAttribute(cr_int8_product_kernel<T, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem_optin);
-        if (e != cudaSuccess) return e;
-        if (p.device <= 63) told.fetch_or(1ull << p.device, std::memory_order_relaxed);
-    }
+    cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_int8_product_kernel<T, TN>), told, p.device, dev);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : std::min<int64_t>(tiles, dev.sm_count)));
-    cfg.blockDim = dim3(192);
+    cfg.blockDim = dim3(64 + 32 * drain_warps(TN));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -430,7 +611,13 @@ cudaError_t launch_int8_product(const Int8ProductArgs &a, int *status, const Dev
             if (a.tokens <= 32) return launch_tc<T, 32>(a, status, dev, tune, encode, stream, launches);
             if (a.tokens <= 64) return launch_tc<T, 64>(a, status, dev, tune, encode, stream, launches);
             if (a.tokens <= 128) return launch_tc<T, 128>(a, status, dev, tune, encode, stream, launches);
-            return launch_tc<T, 256>(a, status, dev, tune, encode, stream, launches);
+            // rounds of tiles times what L2 lets a round take, in its unit of 32 KB a chunk: 128 x 128 on one SM, 256 x 256 on two
+            const int64_t tn = (a.outer + 127) / 128, sms = dev.sm_count;
+            const int64_t single = ((a.tokens + 127) / 128 * tn + sms - 1) / sms;
+            const int64_t pair = ((a.tokens + 255) / 256 * ((tn + 1) / 2) + sms / 2 - 1) / (sms / 2);
+            // one round of small tiles has L2 to itself and takes half the MMA cycles of one of large tiles
+            if (single < pair || single == 1) return launch_tc<T, 128>(a, status, dev, tune, encode, stream, launches);
+            return launch_pair<T>(a, status, dev, tune, encode, stream, launches);
         });
     }
     const int64_t blocks = ((a.tokens + 63) / 64) * ((a.outer + 63) / 64);
