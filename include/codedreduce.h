@@ -408,7 +408,8 @@ typedef struct {
 /* y = dropout(act(gamma_c (x - mean) rstd + beta_c)), mean and rstd = 1 / sqrt(var + eps) over the positions and
  * channels of each (sample, group), var the mean square distance from the mean.  gamma, beta: fp32 [channels] or NULL
  * (ones, zeros).  mean, rstd: fp32 [samples][groups], written for the backward pass; both NULL if not wanted.  y may
- * be x itself (same stride).  workspace: device scratch of cr_group_norm_workspace_bytes (CR_ERR_OOM if smaller). */
+ * be x itself (same stride).  workspace: device scratch of cr_group_norm_workspace_bytes (CR_ERR_OOM if
+ * smaller), 16-byte aligned. */
 size_t cr_group_norm_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc);
 cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const void *x, int64_t ld_x, const float *gamma,
                           const float *beta, void *y, int64_t ld_y, float *mean, float *rstd, void *workspace,

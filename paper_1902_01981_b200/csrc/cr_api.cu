@@ -1278,6 +1278,7 @@ cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const vo
     if (!on_element(x, desc->elem) || !on_element(y, desc->elem)) return CR_ERR_INVALID_ARG;
     const size_t need = cr_group_norm_workspace_bytes(plan, desc);
     if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
     cr::GroupNormArgs a = group_norm_args(*plan, *desc);
     a.x = x; a.ld_x = ld_x; a.y = y; a.ld_y = ld_y; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
     a.workspace = static_cast<float *>(workspace);
@@ -1312,6 +1313,7 @@ cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc,
     if (!dx && !dgamma && !dbeta) return CR_OK;
     const size_t need = cr_group_norm_backward_workspace_bytes(plan, desc);
     if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
     cr::GroupNormArgs a = group_norm_args(*plan, *desc);
     a.x = x; a.ld_x = ld_x; a.dy = dy; a.ld_dy = ld_dy; a.y = dx; a.ld_y = ld_dx; a.gamma = gamma; a.beta = beta;
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);

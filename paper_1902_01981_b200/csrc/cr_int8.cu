@@ -29,8 +29,35 @@ __device__ __forceinline__ RowScale row_scale(uint32_t largest_bits) {
     if (largest < 0x1p-120f) return {0.f, 0.f};
     return {__fdiv_rn(127.f, largest), __fdiv_rn(largest, 127.f)};
 }
-__device__ __forceinline__ int code(float x, float mult) {
-    return mult == 0.f ? 0 : max(-127, min(127, __float2int_rn(x * mult)));
+// rint(x * mult) in two's complement in the low byte: 1.5 * 2^23 pushes the fraction out of the significand, and the sum
+// rounds to even.  |x * mult| <= 127 (1 + 2^-23), so no code leaves the range.
+__device__ __forceinline__ uint32_t code(float x, float mult) { return __float_as_uint(__fadd_rn(__fmul_rn(x, mult), 12582912.f)); }
+
+// The largest magnitude of a vector, as the bits of a float.  Magnitudes are compared as integers: the order is the same,
+// and a NaN is larger than everything.  16-bit elements are compared two at a time.
+template <typename T, int VEC>
+__device__ __forceinline__ uint32_t largest(const Packed<T, VEC> &pv, uint32_t top) {
+    if constexpr (VEC == 1) {
+        return max(top, __float_as_uint(to_float(pv.e)) & 0x7fffffffu);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) top = max(top, pv.w[i] & 0x7fffffffu);
+        return top;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) top = __vmaxu2(top, pv.w[i] & 0x7fff7fffu);
+        return top;
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ uint32_t float_bits(uint32_t top) {
+    if constexpr (VEC == 1 || sizeof(T) == 4) {
+        return top;
+    } else {
+        const unsigned short h = (unsigned short)max(top & 0xffffu, top >> 16);
+        if constexpr (__is_same(T, __nv_bfloat16)) return (uint32_t)h << 16;
+        else return __float_as_uint(__half2float(__ushort_as_half(h)));
+    }
 }
 
 // One block per row.  The row's first kHeld vectors of each thread stay in registers between the search for the
@@ -45,41 +72,37 @@ __global__ void __launch_bounds__(512) cr_quantize_rows_kernel(const T *x, int64
     const int nt = (int)blockDim.x, tid = (int)threadIdx.x;
     Packed<T, VEC> held[kHeld];
     uint32_t top = 0;
-    // magnitudes are compared as integers: the order is the same, and a NaN is larger than everything
-    auto look = [&](const Packed<T, VEC> &pv) {
-        float v[VEC];
-        unpack<T, VEC>(pv, v);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-    };
 #pragma unroll
     for (int u = 0; u < kHeld; ++u)
         if (tid + u * nt < nvec) held[u] = load_packed<T, VEC>(row + (int64_t)(tid + u * nt) * VEC);
 #pragma unroll
     for (int u = 0; u < kHeld; ++u)
-        if (tid + u * nt < nvec) look(held[u]);
-    for (int64_t v = tid + kHeld * nt; v < nvec; v += nt) look(load_packed<T, VEC>(row + v * VEC));
+        if (tid + u * nt < nvec) top = largest<T, VEC>(held[u], top);
+    for (int64_t v = tid + kHeld * nt; v < nvec; v += nt) top = largest<T, VEC>(load_packed<T, VEC>(row + v * VEC), top);
+    top = float_bits<T, VEC>(top);
     for (int64_t c = nvec * VEC + tid; c < cols; c += nt) top = max(top, __float_as_uint(to_float(row[c])) & 0x7fffffffu);
     top = __reduce_max_sync(0xffffffffu, top);
-    if ((tid & 31) == 0) sm[tid >> 5] = top;
-    __syncthreads();
-    top = sm[0];
-    for (int w = 1; w < nt / 32; ++w) top = max(top, sm[w]);
+    if (nt > 32) {
+        if ((tid & 31) == 0) sm[tid >> 5] = top;
+        __syncthreads();
+        top = sm[0];
+        for (int w = 1; w < nt / 32; ++w) top = max(top, sm[w]);
+    }
     const RowScale rs = row_scale(top);
+    const bool dead = top >= 0x7f800000u;     // an infinity or a NaN: codes 0
     if (tid == 0) scale[blockIdx.x] = rs.scale;
     auto put = [&](const Packed<T, VEC> &pv, int64_t v) {
         float f[VEC];
         unpack<T, VEC>(pv, f);
         if constexpr (VEC == 1) {
-            out[v] = (int8_t)code(f[0], rs.mult);
+            out[v] = dead ? (int8_t)0 : (int8_t)code(f[0], rs.mult);
         } else {
             uint32_t w[VEC / 4];
 #pragma unroll
             for (int i = 0; i < VEC / 4; ++i) {
-                uint32_t b = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) b |= ((uint32_t)code(f[4 * i + k], rs.mult) & 0xffu) << (8 * k);
-                w[i] = b;
+                const uint32_t a = __byte_perm(code(f[4 * i], rs.mult), code(f[4 * i + 1], rs.mult), 0x0040);
+                const uint32_t b = __byte_perm(code(f[4 * i + 2], rs.mult), code(f[4 * i + 3], rs.mult), 0x0040);
+                w[i] = dead ? 0u : __byte_perm(a, b, 0x5410);
             }
             if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(out + v * 8) = make_uint2(w[0], w[1]);
             else *reinterpret_cast<uint32_t *>(out + v * 4) = w[0];
@@ -89,7 +112,7 @@ __global__ void __launch_bounds__(512) cr_quantize_rows_kernel(const T *x, int64
     for (int u = 0; u < kHeld; ++u)
         if (tid + u * nt < nvec) put(held[u], tid + u * nt);
     for (int64_t v = tid + kHeld * nt; v < nvec; v += nt) put(load_packed<T, VEC>(row + v * VEC), v);
-    for (int64_t c = nvec * VEC + tid; c < cols; c += nt) out[c] = (int8_t)code(to_float(row[c]), rs.mult);
+    for (int64_t c = nvec * VEC + tid; c < cols; c += nt) out[c] = dead ? (int8_t)0 : (int8_t)code(to_float(row[c]), rs.mult);
 }
 
 // ---- product, any alignment --------------------------------------------------------------------------------------------

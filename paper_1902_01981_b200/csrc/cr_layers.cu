@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <numeric>
 
 #include "cr_elem.cuh"
 
@@ -32,17 +33,17 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Which part of the tensor a block of the streaming kernels has: sample, tile of up to 256 vectors of channels,
-// chunk of positions.  A thread keeps its vector of channels and walks every rt-th row of the chunk.
+// Which part of the tensor a block of the streaming kernels has: sample, tile of channels, chunk of positions.  A tile
+// is a run of whole groups of up to 256 vectors, or one of `parts` pieces of a group that is wider than that.  A thread
+// keeps its vector of channels and walks every rt-th row of the chunk.
 struct Split {
-    int64_t positions;
-    int channels, cg, nvec, tiles, chunks;
-    int64_t rows_per_chunk;
+    int64_t positions, rows_per_chunk;
+    int channels, groups, cg, width, tiles, parts, chunks;
 };
 struct Place {
     int64_t n, row0;
-    int rows, tile, chunk, vecs, rt, col, j;   // j: this thread's first row of the chunk; -1: no work
-    int c0;                                    // its first channel
+    int rows, chunk, part, c_start, width, vecs, rt, col, j;   // j: this thread's first row of the chunk; -1: no work
+    int c0, g0, groups;                                        // its first channel; the tile's groups
 };
 template <int VEC>
 __device__ __forceinline__ Place place(const Split &s) {
@@ -50,40 +51,91 @@ __device__ __forceinline__ Place place(const Split &s) {
     const uint32_t b = blockIdx.x;
     p.chunk = (int)(b % (uint32_t)s.chunks);
     const uint32_t r = b / (uint32_t)s.chunks;
-    p.tile = (int)(r % (uint32_t)s.tiles);
+    const int tile = (int)(r % (uint32_t)s.tiles);
     p.n = r / (uint32_t)s.tiles;
     p.row0 = (int64_t)p.chunk * s.rows_per_chunk;
     p.rows = (int)min(s.rows_per_chunk, s.positions - p.row0);
-    p.vecs = min(kThreads, s.nvec - p.tile * kThreads);
+    p.part = tile % s.parts;
+    if (s.parts > 1) {
+        p.g0 = tile / s.parts;
+        p.groups = 1;
+        p.c_start = p.g0 * s.cg + p.part * s.width;
+        p.width = min(s.width, s.cg - p.part * s.width);
+    } else {
+        p.c_start = tile * s.width;
+        p.width = min(s.width, s.channels - p.c_start);
+        p.g0 = p.c_start / s.cg;
+        p.groups = p.width / s.cg;
+    }
+    p.vecs = p.width / VEC;
     p.rt = kThreads / p.vecs;
     p.col = (int)threadIdx.x % p.vecs;
     const int j = (int)threadIdx.x / p.vecs;
     p.j = j < p.rt ? j : -1;
-    p.c0 = (p.tile * kThreads + p.col) * VEC;
+    p.c0 = p.c_start + p.col * VEC;
     return p;
 }
-__device__ __forceinline__ int rows_of(const Place &p, int j) { return j < p.rows ? (p.rows - j + p.rt - 1) / p.rt : 0; }
+// The partial results of (sample, group): one per chunk and piece, next to each other.
+__device__ __forceinline__ int64_t entries_of(const Split &s, int64_t n, int g) { return (n * s.groups + g) * s.chunks * s.parts; }
 
-// ---- forward, streaming: statistics of each channel over a chunk ----------------------------------------------
+// Sums sm[j * width + c] over j < rt into sm[c], for c < width, both planes; `plane` floats apart.  Up to 16 threads share
+// a channel, so that a narrow tile does not leave its sums to a few threads.
+__device__ __forceinline__ void fold_rows(float *sm, int plane, int width, int rt) {
+    int share = 1;
+    while (share < 16 && share * 2 <= rt && share * 2 * width <= kThreads) share *= 2;
+    __syncthreads();
+    if (share > 1) {
+        const int c = (int)threadIdx.x % width, q = (int)threadIdx.x / width;
+        if (q < share) {
+            float t1 = 0.f, t2 = 0.f;
+            for (int j = q; j < rt; j += share) {
+                t1 += sm[j * width + c];
+                t2 += sm[plane + j * width + c];
+            }
+            sm[q * width + c] = t1;            // row q is this thread's own
+            sm[plane + q * width + c] = t2;
+        }
+        __syncthreads();
+        rt = share;
+    }
+    for (int c = threadIdx.x; c < width; c += kThreads) {
+        float t1 = 0.f, t2 = 0.f;
+        for (int j = 0; j < rt; ++j) {
+            t1 += sm[j * width + c];
+            t2 += sm[plane + j * width + c];
+        }
+        sm[c] = t1;
+        sm[plane + c] = t2;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// ---- forward, streaming: mean and centred square sum of each group over a chunk -------------------------------------
 //
-// Sums are taken of x - k, k the thread's first value of the channel: the squares then carry the spread and not the
-// mean.  Threads and chunks are joined by mean and centred square sum.
+// Sums are taken of x - k, k the channel's value in the chunk's first row: the squares then carry the spread and not the
+// mean.  Channels, chunks and pieces are joined by mean and centred square sum.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_stats_kernel(const T *x, int64_t ld, const Split s, float *part_mean, float *part_m2) {
-    __shared__ float sm[2][kThreads * VEC];
+__global__ void __launch_bounds__(kThreads) cr_group_norm_stats_kernel(const T *x, int64_t ld, const Split s, float2 *partial) {
+    __shared__ float sm[2 * kThreads * VEC];
+    constexpr int kPlane = kThreads * VEC;
     const Place p = place<VEC>(s);
+    const T *first = x + ((p.n * s.positions + p.row0) * ld + p.c0);
     if (p.j >= 0) {
         float k[VEC], s1[VEC], s2[VEC];
-        const int cnt = rows_of(p, p.j);
-        const T *src = x + ((p.n * s.positions + p.row0 + p.j) * ld + p.c0);
+        unpack<T, VEC>(load_packed<T, VEC>(first), k);
+        const T *src = first + p.j * ld;
         const int64_t step = (int64_t)p.rt * ld;
-        if (cnt > 0) unpack<T, VEC>(load_packed<T, VEC>(src), k);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.f;
 #pragma unroll 4
-        for (int r = 1; r < cnt; ++r) {
+        for (int r = p.j; r < p.rows; r += p.rt, src += step) {
             float v[VEC];
-            unpack<T, VEC>(load_packed<T, VEC>(src + r * step), v);
+            unpack<T, VEC>(load_packed<T, VEC>(src), v);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const float dlt = v[i] - k[i];
@@ -91,68 +143,32 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_stats_kernel(const T *
                 s2[i] = fmaf(dlt, dlt, s2[i]);
             }
         }
-        const float inv = cnt > 0 ? 1.f / (float)cnt : 0.f;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const int at = (p.j * p.vecs + p.col) * VEC + i;
-            sm[0][at] = cnt > 0 ? fmaf(s1[i], inv, k[i]) : 0.f;
-            sm[1][at] = cnt > 0 ? fmaxf(s2[i] - s1[i] * s1[i] * inv, 0.f) : 0.f;
+            sm[at] = s1[i];
+            sm[kPlane + at] = s2[i];
         }
     }
+    fold_rows(sm, kPlane, p.width, p.rt);
+    const float rows = (float)p.rows, inv = 1.f / rows;
+    for (int c = threadIdx.x; c < p.width; c += kThreads) {
+        const float t1 = sm[c];
+        sm[kPlane + c] = fmaxf(sm[kPlane + c] - t1 * t1 * inv, 0.f);
+        sm[c] = to_float(x[(p.n * s.positions + p.row0) * ld + p.c_start + c]) + t1 * inv;
+    }
     __syncthreads();
-    const int width = p.vecs * VEC;
-    for (int c = threadIdx.x; c < width; c += kThreads) {
-        float sum = 0.f;
-        for (int j = 0; j < p.rt; ++j) sum += (float)rows_of(p, j) * sm[0][j * width + c];
-        const float mean = sum / (float)p.rows;
-        float m2 = 0.f;
-        for (int j = 0; j < p.rt; ++j) {
-            const float dlt = sm[0][j * width + c] - mean;
-            m2 += sm[1][j * width + c] + (float)rows_of(p, j) * dlt * dlt;
+    const int lane = threadIdx.x & 31, per = p.width / p.groups;
+    for (int g = threadIdx.x >> 5; g < p.groups; g += kThreads / 32) {
+        float sum = 0.f, m2 = 0.f;
+        for (int c = g * per + lane; c < (g + 1) * per; c += 32) sum += sm[c];
+        const float mean = warp_sum(sum) / (float)per;
+        for (int c = g * per + lane; c < (g + 1) * per; c += 32) {
+            const float d = sm[c] - mean;
+            m2 += sm[kPlane + c] + rows * d * d;
         }
-        const int64_t at = (p.n * s.chunks + p.chunk) * s.channels + p.tile * kThreads * VEC + c;
-        part_mean[at] = mean;
-        part_m2[at] = m2;
-    }
-}
-
-__device__ __forceinline__ float block_sum_128(float v, float *sm) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return (sm[0] + sm[1]) + (sm[2] + sm[3]);
-}
-
-// One block of 128 threads per (sample, group) joins the chunks' statistics.
-__global__ void __launch_bounds__(128) cr_group_norm_join_kernel(const float *part_mean, const float *part_m2, const Split s, int groups,
-                                                                 float eps, float *mean_out, float *rstd_out) {
-    __shared__ float sm[4];
-    const int64_t n = blockIdx.x / (unsigned)groups;
-    const int g = (int)(blockIdx.x % (unsigned)groups);
-    const int64_t base = n * s.chunks * (int64_t)s.channels + (int64_t)g * s.cg;
-    const int entries = s.chunks * s.cg;
-    float sum = 0.f;
-    for (int e = threadIdx.x; e < entries; e += 128) {
-        const int k = e / s.cg;
-        const float rows = (float)min(s.rows_per_chunk, s.positions - k * s.rows_per_chunk);
-        sum = fmaf(rows, part_mean[base + (int64_t)k * s.channels + e % s.cg], sum);
-    }
-    const float total = (float)s.positions * (float)s.cg;
-    const float mean = block_sum_128(sum, sm) / total;
-    float m2 = 0.f;
-    for (int e = threadIdx.x; e < entries; e += 128) {
-        const int k = e / s.cg;
-        const float rows = (float)min(s.rows_per_chunk, s.positions - k * s.rows_per_chunk);
-        const int64_t at = base + (int64_t)k * s.channels + e % s.cg;
-        const float dlt = part_mean[at] - mean;
-        m2 += part_m2[at] + rows * dlt * dlt;
-    }
-    m2 = block_sum_128(m2, sm);
-    if (threadIdx.x == 0) {
-        mean_out[blockIdx.x] = mean;
-        rstd_out[blockIdx.x] = 1.f / sqrtf(m2 / total + eps);
+        m2 = warp_sum(m2);
+        if (lane == 0) partial[entries_of(s, p.n, p.g0 + g) + p.chunk * s.parts + p.part] = make_float2(mean, m2);
     }
 }
 
@@ -160,16 +176,11 @@ __global__ void __launch_bounds__(128) cr_group_norm_join_kernel(const float *pa
 template <int VEC>
 struct Affine {
     float mean[VEC], rstd[VEC], gamma[VEC], beta[VEC];
-    __device__ __forceinline__ void load(const Place &p, const Split &s, int groups, const float *mean_in, const float *rstd_in,
-                                         const float *gamma_in, const float *beta_in) {
+    __device__ __forceinline__ void parameters(const Place &p, const float *gamma_in, const float *beta_in) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int c = p.c0 + i;
-            const int64_t at = p.n * groups + c / s.cg;
-            mean[i] = mean_in[at];
-            rstd[i] = rstd_in[at];
-            gamma[i] = gamma_in ? __ldg(gamma_in + c) : 1.f;
-            beta[i] = beta_in ? __ldg(beta_in + c) : 0.f;
+            gamma[i] = gamma_in ? __ldg(gamma_in + p.c0 + i) : 1.f;
+            beta[i] = beta_in ? __ldg(beta_in + p.c0 + i) : 0.f;
         }
     }
     __device__ __forceinline__ float xhat(float x, int i) const { return __fmul_rn(x - mean[i], rstd[i]); }
@@ -177,11 +188,49 @@ struct Affine {
 };
 
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_apply_kernel(const GroupNormArgs a, const Split s) {
+__global__ void __launch_bounds__(kThreads) cr_group_norm_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
+    __shared__ float2 ready[kThreads * VEC];     // mean and rstd of the tile's groups
     const Place p = place<VEC>(s);
-    if (p.j < 0) return;
     Affine<VEC> f;
-    f.load(p, s, a.groups, a.mean, a.rstd, a.gamma, a.beta);
+    if (p.j >= 0) f.parameters(p, a.gamma, a.beta);
+    // every block joins the chunks of its groups for itself: a warp per group, in one order
+    const int lane = threadIdx.x & 31, entries = s.chunks * s.parts;
+    const float total = (float)s.positions * (float)s.cg;
+    for (int g = threadIdx.x >> 5; g < p.groups; g += kThreads / 32) {
+        const float2 *in = partial + entries_of(s, p.n, p.g0 + g);
+        auto count = [&](int e) {
+            const int chunk = e / s.parts, part = e - chunk * s.parts;
+            const float rows = (float)min(s.rows_per_chunk, s.positions - chunk * s.rows_per_chunk);
+            return rows * (float)(s.parts > 1 ? min(s.width, s.cg - part * s.width) : s.cg);
+        };
+        float sum = 0.f, m2 = 0.f;
+#pragma unroll 8
+        for (int e = lane; e < entries; e += 32) sum = fmaf(count(e), in[e].x, sum);
+        const float mean = warp_sum(sum) / total;
+#pragma unroll 8
+        for (int e = lane; e < entries; e += 32) {
+            const float2 v = in[e];
+            const float d = v.x - mean;
+            m2 += fmaf(count(e) * d, d, v.y);
+        }
+        m2 = warp_sum(m2);
+        if (lane == 0) {
+            const float rstd = 1.f / sqrtf(m2 / total + a.eps);
+            ready[g] = make_float2(mean, rstd);
+            if (a.mean && p.chunk == 0 && p.part == 0) {
+                a.mean[p.n * s.groups + p.g0 + g] = mean;
+                a.rstd[p.n * s.groups + p.g0 + g] = rstd;
+            }
+        }
+    }
+    __syncthreads();
+    if (p.j < 0) return;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const float2 v = ready[(p.c0 + i) / s.cg - p.g0];
+        f.mean[i] = v.x;
+        f.rstd[i] = v.y;
+    }
     const int64_t first = p.n * s.positions + p.row0;
 #pragma unroll 2
     for (int r = p.j; r < p.rows; r += p.rt) {
@@ -195,6 +244,17 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_apply_kernel(const Gro
 }
 
 // ---- backward, streaming -----------------------------------------------------------------------------------------
+
+template <int VEC>
+__device__ __forceinline__ void statistics(Affine<VEC> &f, const Place &p, const Split &s, const GroupNormArgs &a) {
+    f.parameters(p, a.gamma, a.beta);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const int64_t at = p.n * s.groups + (p.c0 + i) / s.cg;
+        f.mean[i] = a.mean[at];
+        f.rstd[i] = a.rstd[at];
+    }
+}
 
 // dz of a vector of elements, and their xhat.
 template <typename T, int VEC, int ACT>
@@ -210,13 +270,16 @@ __device__ __forceinline__ void slopes(const GroupNormArgs &a, const Affine<VEC>
     }
 }
 
+// The channels' sums of dz (part1) and dz xhat (part2) over a chunk, [samples][chunks] rows of `channels`, and the
+// groups' sums of gamma dz and gamma dz xhat.
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_grad_sums_kernel(const GroupNormArgs a, const Split s, float *part1, float *part2) {
-    __shared__ float sm[2][kThreads * VEC];
+__global__ void __launch_bounds__(kThreads) cr_group_norm_grad_sums_kernel(const GroupNormArgs a, const Split s, float *part1, float *part2, float2 *partial) {
+    __shared__ float sm[2 * kThreads * VEC];
+    constexpr int kPlane = kThreads * VEC;
     const Place p = place<VEC>(s);
     if (p.j >= 0) {
         Affine<VEC> f;
-        f.load(p, s, a.groups, a.mean, a.rstd, a.gamma, a.beta);
+        statistics<VEC>(f, p, s, a);
         float s1[VEC], s2[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.f;
@@ -233,72 +296,59 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_grad_sums_kernel(const
         }
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            sm[0][(p.j * p.vecs + p.col) * VEC + i] = s1[i];
-            sm[1][(p.j * p.vecs + p.col) * VEC + i] = s2[i];
+            sm[(p.j * p.vecs + p.col) * VEC + i] = s1[i];
+            sm[kPlane + (p.j * p.vecs + p.col) * VEC + i] = s2[i];
         }
     }
-    __syncthreads();
-    const int width = p.vecs * VEC;
-    for (int c = threadIdx.x; c < width; c += kThreads) {
-        float t1 = 0.f, t2 = 0.f;
-        for (int j = 0; j < p.rt; ++j) {
-            t1 += sm[0][j * width + c];
-            t2 += sm[1][j * width + c];
-        }
-        const int64_t at = (p.n * s.chunks + p.chunk) * s.channels + p.tile * kThreads * VEC + c;
-        part1[at] = t1;
-        part2[at] = t2;
+    fold_rows(sm, kPlane, p.width, p.rt);
+    for (int c = threadIdx.x; c < p.width; c += kThreads) {
+        const int64_t at = (p.n * s.chunks + p.chunk) * s.channels + p.c_start + c;
+        part1[at] = sm[c];
+        part2[at] = sm[kPlane + c];
     }
-}
-
-// One block per sample: the channels' sums over the chunks, then m1 and m2 of its groups.
-__global__ void __launch_bounds__(kThreads) cr_group_norm_grad_join_kernel(const float *part1, const float *part2, const Split s, int groups,
-                                                                           const float *gamma, float *sum1, float *sum2,
-                                                                           float *m1, float *m2) {
-    const int64_t n = blockIdx.x;
-    for (int c = threadIdx.x; c < s.channels; c += kThreads) {
+    const int lane = threadIdx.x & 31, per = p.width / p.groups;
+    for (int g = threadIdx.x >> 5; g < p.groups; g += kThreads / 32) {
         float t1 = 0.f, t2 = 0.f;
-        for (int k = 0; k < s.chunks; ++k) {
-            t1 += part1[(n * s.chunks + k) * s.channels + c];
-            t2 += part2[(n * s.chunks + k) * s.channels + c];
+        for (int c = g * per + lane; c < (g + 1) * per; c += 32) {
+            const float w = a.gamma ? __ldg(a.gamma + p.c_start + c) : 1.f;
+            t1 = fmaf(w, sm[c], t1);
+            t2 = fmaf(w, sm[kPlane + c], t2);
         }
-        sum1[n * s.channels + c] = t1;
-        sum2[n * s.channels + c] = t2;
-    }
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    const float total = (float)s.positions * (float)s.cg;
-    for (int g = threadIdx.x >> 5; g < groups; g += kThreads / 32) {
-        float t1 = 0.f, t2 = 0.f;
-        for (int c = g * s.cg + lane; c < (g + 1) * s.cg; c += 32) {
-            const float w = gamma ? gamma[c] : 1.f;
-            t1 = fmaf(w, sum1[n * s.channels + c], t1);
-            t2 = fmaf(w, sum2[n * s.channels + c], t2);
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            t1 += __shfl_xor_sync(0xffffffffu, t1, o);
-            t2 += __shfl_xor_sync(0xffffffffu, t2, o);
-        }
-        if (lane == 0) {
-            m1[n * groups + g] = t1 / total;
-            m2[n * groups + g] = t2 / total;
-        }
+        t1 = warp_sum(t1);
+        t2 = warp_sum(t2);
+        if (lane == 0) partial[entries_of(s, p.n, p.g0 + g) + p.chunk * s.parts + p.part] = make_float2(t1, t2);
     }
 }
 
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_grad_apply_kernel(const GroupNormArgs a, const Split s, const float *m1, const float *m2) {
+__global__ void __launch_bounds__(kThreads) cr_group_norm_grad_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
+    __shared__ float2 ready[kThreads * VEC];     // m1 and m2 of the tile's groups
     const Place p = place<VEC>(s);
+    const int lane = threadIdx.x & 31, entries = s.chunks * s.parts;
+    const float total = (float)s.positions * (float)s.cg;
+    for (int g = threadIdx.x >> 5; g < p.groups; g += kThreads / 32) {
+        float t1 = 0.f, t2 = 0.f;
+        const float2 *in = partial + entries_of(s, p.n, p.g0 + g);
+#pragma unroll 8
+        for (int e = lane; e < entries; e += 32) {
+            const float2 v = in[e];
+            t1 += v.x;
+            t2 += v.y;
+        }
+        t1 = warp_sum(t1);
+        t2 = warp_sum(t2);
+        if (lane == 0) ready[g] = make_float2(t1 / total, t2 / total);
+    }
+    __syncthreads();
     if (p.j < 0) return;
     Affine<VEC> f;
-    f.load(p, s, a.groups, a.mean, a.rstd, a.gamma, a.beta);
+    statistics<VEC>(f, p, s, a);
     float b1[VEC], b2[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        const int64_t at = p.n * a.groups + (p.c0 + i) / s.cg;
-        b1[i] = m1[at];
-        b2[i] = m2[at];
+        const float2 v = ready[(p.c0 + i) / s.cg - p.g0];
+        b1[i] = v.x;
+        b2[i] = v.y;
     }
     const int64_t first = p.n * s.positions + p.row0;
     for (int r = p.j; r < p.rows; r += p.rt) {
@@ -352,11 +402,26 @@ __global__ void cr_zero_params_kernel(int64_t count, int channels, int64_t ld, f
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------
 
-// The elements of a row-major [rows][cols] tensor as vectors; a thread takes kUnroll of them, a block apart.  Where the
-// row strides are the width, the caller passes one long row and no division is made.
+// Division by an invariant number (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994),
+// for 32-bit dividends.
+struct Divide {
+    uint32_t by, mul, shift;
+    explicit Divide(uint32_t d) : by(d), mul(0), shift(0) {
+        while (shift < 32 && (1ull << shift) < d) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+        if (shift == 0) return n;
+        const uint32_t t = __umulhi(mul, n);
+        return (t + ((n - t) >> 1)) >> (shift - 1);
+    }
+};
+
+// The elements of a row-major [rows][cols] tensor as 16-byte vectors; a thread takes kUnroll of them, a block apart.
+// Where the row strides are the width, the caller passes one long row and no division is made.
 template <typename T, int VEC, typename I>
-__global__ void __launch_bounds__(kThreads) cr_dropout_kernel(const T *x, const T *residual, T *y, I nvec, I vecs_per_row, int64_t ld_x,
-                                                              int64_t ld_r, int64_t ld_y, const DropSpec d) {
+__global__ void __launch_bounds__(kThreads) cr_dropout_kernel(const T *x, const T *residual, T *y, I nvec, I vecs_per_row, const Divide divide,
+                                                              int64_t ld_x, int64_t ld_r, int64_t ld_y, const DropSpec d) {
     constexpr int kUnroll = 4;
     const I v0 = (I)blockIdx.x * (kThreads * kUnroll) + threadIdx.x;
     Packed<T, VEC> px[kUnroll], pr[kUnroll];
@@ -364,7 +429,8 @@ __global__ void __launch_bounds__(kThreads) cr_dropout_kernel(const T *x, const 
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
         const I v = v0 + u * kThreads;
-        const I r = vecs_per_row == nvec ? 0 : v / vecs_per_row;
+        I r = 0;
+        if (vecs_per_row != nvec) r = sizeof(I) == 4 ? (I)divide((uint32_t)v) : v / vecs_per_row;
         row[u] = (int64_t)r;
         col[u] = (int64_t)(v - r * vecs_per_row) * VEC;
         if (v < nvec) {
@@ -389,25 +455,70 @@ __global__ void __launch_bounds__(kThreads) cr_dropout_kernel(const T *x, const 
     }
 }
 
+// Element by element, for rows that no vector fits.  A warp has 128 consecutive elements, the first one's index a multiple
+// of four: lane l makes the output of elements 4 l .. 4 l + 3, and every lane fetches its 16 bits from the lane that made
+// them, so that neighbouring lanes still read and write neighbouring elements.
+template <typename T, typename I>
+__global__ void __launch_bounds__(kThreads) cr_dropout_elements_kernel(const T *x, const T *residual, T *y, I count, I cols, const Divide divide,
+                                                                       int64_t ld_x, int64_t ld_r, int64_t ld_y, const DropSpec d) {
+    const int lane = threadIdx.x & 31;
+    const I ahead = (I)(d.offset & 3);                     // elements of the first four that lie before the tensor
+    const I start = ((I)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * 128;    // counted with those
+    const unsigned long long w = drop_word(d.key, (d.offset >> 2) + (unsigned long long)(start >> 2) + (unsigned)lane);
+    const uint32_t lo = (uint32_t)w, hi = (uint32_t)(w >> 32);
+    const bool all_go = d.scale == 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int from = q * 8 + (lane >> 2);
+        const uint32_t a = __shfl_sync(0xffffffffu, lo, from), b = __shfl_sync(0xffffffffu, hi, from);
+        const uint32_t half = lane & 2 ? b : a, number = lane & 1 ? half >> 16 : half & 0xffffu;
+        const I counted = start + (I)(q * 32 + lane);
+        if (counted < ahead || counted - ahead >= count) continue;
+        const I i = counted - ahead;
+        I r = 0;
+        if (cols != count) r = sizeof(I) == 4 ? (I)divide((uint32_t)i) : i / cols;
+        const int64_t row = (int64_t)r, col = (int64_t)(i - r * cols);
+        float v = to_float(x[row * ld_x + col]);
+        if (d.threshold) v = all_go || number < d.threshold ? 0.f : v * d.scale;
+        if (residual) v += to_float(residual[row * ld_r + col]);
+        y[row * ld_y + col] = from_float<T>(v);
+    }
+}
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 Split make_split(int64_t samples, int64_t positions, int channels, int groups, int vec) {
     Split s;
     s.positions = positions;
     s.channels = channels;
+    s.groups = groups;
     s.cg = channels / groups;
-    s.nvec = channels / vec;
-    s.tiles = (s.nvec + kThreads - 1) / kThreads;
-    // chunks of at least 32 rows a thread-row, about 2048 blocks in all
-    const int vecs = std::min(kThreads, s.nvec);
-    const int64_t least = 32ll * (kThreads / vecs);
-    int64_t chunks = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, samples * s.tiles));
+    const int most = kThreads * vec, unit = std::lcm(s.cg, vec);
+    if (unit <= most) {
+        s.parts = 1;
+        s.width = std::min(channels, most / unit * unit);
+        s.tiles = (channels + s.width - 1) / s.width;
+    } else {
+        s.parts = (s.cg + most - 1) / most;
+        s.width = most;
+        s.tiles = groups * s.parts;
+    }
+    // Chunks of at least four rows a thread, about four blocks an SM in all: fewer leave SMs idle (one sample of 52066
+    // positions of 4 channels: 74 us in 6 chunks), more spend their time on the joins.
+    const int64_t least = 4ll * (kThreads / std::min(kThreads, s.width / vec));
+    int64_t chunks = std::max<int64_t>(1, 592 / std::max<int64_t>(1, samples * s.tiles));
     chunks = std::min(chunks, std::max<int64_t>(1, positions / least));
     s.rows_per_chunk = (positions + chunks - 1) / chunks;
     // a block counts its rows in 32 bits, and a float holds the count of a group without rounding far beyond this
     s.rows_per_chunk = std::min<int64_t>(s.rows_per_chunk, 1 << 24);
     s.chunks = (int)((positions + s.rows_per_chunk - 1) / s.rows_per_chunk);
     return s;
+}
+// Elements of a vector of the streaming kernels: 16 bytes where the rows allow it and no group wider than a tile is cut
+// inside a vector.
+int split_vec(bool wide, int elem, int channels, int groups) {
+    const int vec = 16 / elem_bytes(elem), cg = channels / groups;
+    return wide && (cg % vec == 0 || std::lcm(cg, vec) <= kThreads * vec) ? vec : 1;
 }
 
 template <typename F>
@@ -444,10 +555,11 @@ bool vector_rows(int elem, int64_t channels, std::initializer_list<const void *>
 size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem) {
     if (samples < 1) return 0;
     size_t most = 0;
-    for (int vec : {1, 16 / elem_bytes(elem)}) {
+    for (bool wide : {false, true}) {
+        const int vec = split_vec(wide, elem, channels, groups);
         if (channels % vec) continue;
         const Split s = make_split(samples, positions, channels, groups, vec);
-        most = std::max(most, ((size_t)s.chunks * channels + groups) * (size_t)samples * 8);
+        most = std::max(most, (size_t)s.chunks * groups * s.parts * (size_t)samples * 8);
     }
     return most;
 }
@@ -455,43 +567,38 @@ size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channe
 size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem) {
     if (samples < 1) return 0;
     size_t most = 0;
-    for (int vec : {1, 16 / elem_bytes(elem)}) {
+    for (bool wide : {false, true}) {
+        const int vec = split_vec(wide, elem, channels, groups);
         if (channels % vec) continue;
         const Split s = make_split(samples, positions, channels, groups, vec);
-        most = std::max(most, ((size_t)(s.chunks + 1) * channels + groups) * (size_t)samples * 8);
+        most = std::max(most, (size_t)s.chunks * (channels + (size_t)groups * s.parts) * (size_t)samples * 8);
     }
     // the one-pass form's rows of sums
     return std::max(most, (size_t)group_norm_backward_on_chip(samples, positions, channels, groups, elem) * channels * (size_t)samples * 8);
 }
 
-cudaError_t launch_group_norm(const GroupNormArgs &in, const DeviceInfo &, cudaStream_t stream, int64_t *launches) {
-    if (in.samples == 0) return cudaSuccess;
-    GroupNormArgs a = in;
+cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &, cudaStream_t stream, int64_t *launches) {
+    if (a.samples == 0) return cudaSuccess;
     const bool wide = vector_rows(a.elem, a.channels, {a.x, a.y}, {a.ld_x, a.ld_y});
     if (wide && group_norm_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem)) return launch_group_norm_on_chip(a, stream, launches);
-    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, wide ? 16 / elem_bytes(a.elem) : 1);
-    float *part_mean = a.workspace;
-    float *part_m2 = part_mean + (size_t)a.samples * s.chunks * a.channels;
-    if (!a.mean) a.mean = part_m2 + (size_t)a.samples * s.chunks * a.channels;
-    if (!a.rstd) a.rstd = part_m2 + (size_t)a.samples * s.chunks * a.channels + (size_t)a.samples * a.groups;
+    const int vec = split_vec(wide, a.elem, a.channels, a.groups);
+    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec);
+    float2 *partial = reinterpret_cast<float2 *>(a.workspace);
     const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
     auto run = [&](auto t, auto v) {
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value;
-        cr_group_norm_stats_kernel<T, VEC><<<blocks, kThreads, 0, stream>>>(static_cast<const T *>(a.x), a.ld_x, s, part_mean, part_m2);
+        cr_group_norm_stats_kernel<T, VEC><<<blocks, kThreads, 0, stream>>>(static_cast<const T *>(a.x), a.ld_x, s, partial);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
-        cr_group_norm_join_kernel<<<(unsigned)(a.samples * a.groups), 128, 0, stream>>>(part_mean, part_m2, s, a.groups, a.eps, a.mean, a.rstd);
-        e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
         e = by_act(a.act, [&](auto act) {
-            cr_group_norm_apply_kernel<T, VEC, decltype(act)::value><<<blocks, kThreads, 0, stream>>>(a, s);
+            cr_group_norm_apply_kernel<T, VEC, decltype(act)::value><<<blocks, kThreads, 0, stream>>>(a, s, partial);
             return cudaGetLastError();
         });
-        if (e == cudaSuccess) *launches += 3;
+        if (e == cudaSuccess) *launches += 2;
         return e;
     };
-    return by_type(a.elem, [&](auto t) { return wide ? run(t, Int<16 / (int)sizeof(t)>{}) : run(t, Int<1>{}); });
+    return by_type(a.elem, [&](auto t) { return vec > 1 ? run(t, Int<16 / (int)sizeof(t)>{}) : run(t, Int<1>{}); });
 }
 
 static cudaError_t launch_params(const GroupNormArgs &a, const float *sum1, const float *sum2, int rows_per_sample, cudaStream_t stream,
@@ -514,34 +621,32 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         return e;
     }
     const bool wide = vector_rows(a.elem, a.channels, {a.x, a.dy, a.y}, {a.ld_x, a.ld_dy, a.y ? a.ld_y : 0});
-    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, wide ? 16 / elem_bytes(a.elem) : 1);
-    const size_t plane = (size_t)a.samples * a.channels;
-    float *sum1 = a.workspace, *sum2 = sum1 + plane;
-    float *part1 = sum2 + plane, *part2 = part1 + plane * s.chunks;
-    float *m1 = part2 + plane * s.chunks, *m2 = m1 + (size_t)a.samples * a.groups;
-    const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
     const bool params = a.dgamma || a.dbeta;
+    const size_t plane = (size_t)a.samples * a.channels;
+    float *sum1 = a.workspace;
     cudaError_t e;
     if (const int rows = wide ? group_norm_backward_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem) : 0) {
         // a partition of one sample that one CTA holds has its sums where they belong
         if (a.partitions == a.samples && rows == 2) return launch_group_norm_grad_on_chip(a, a.dbeta, a.dgamma, a.ld_param, true, stream, launches);
-        sum2 = sum1 + plane * rows;
+        float *sum2 = sum1 + plane * rows;
         e = launch_group_norm_grad_on_chip(a, params ? sum1 : nullptr, params ? sum2 : nullptr, a.channels, false, stream, launches);
         if (e != cudaSuccess || !params) return e;
         return launch_params(a, sum1, sum2, rows, stream, launches);
     }
+    const int vec = split_vec(wide, a.elem, a.channels, a.groups);
+    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec);
+    float *sum2 = sum1 + plane * s.chunks;
+    float2 *partial = reinterpret_cast<float2 *>(sum2 + plane * s.chunks);
+    const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
     auto run = [&](auto t, auto v, auto act) {
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value, ACT = decltype(act)::value;
-        cr_group_norm_grad_sums_kernel<T, VEC, ACT><<<blocks, kThreads, 0, stream>>>(a, s, part1, part2);
+        cr_group_norm_grad_sums_kernel<T, VEC, ACT><<<blocks, kThreads, 0, stream>>>(a, s, sum1, sum2, partial);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
-        cr_group_norm_grad_join_kernel<<<(unsigned)a.samples, kThreads, 0, stream>>>(part1, part2, s, a.groups, a.gamma, sum1, sum2, m1, m2);
-        e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-        *launches += 2;
+        ++*launches;
         if (a.y) {
-            cr_group_norm_grad_apply_kernel<T, VEC, ACT><<<blocks, kThreads, 0, stream>>>(a, s, m1, m2);
+            cr_group_norm_grad_apply_kernel<T, VEC, ACT><<<blocks, kThreads, 0, stream>>>(a, s, partial);
             e = cudaGetLastError();
             if (e != cudaSuccess) return e;
             ++*launches;
@@ -549,10 +654,10 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         return cudaSuccess;
     };
     e = by_type(a.elem, [&](auto t) {
-        return by_act(a.act, [&](auto act) { return wide ? run(t, Int<16 / (int)sizeof(t)>{}, act) : run(t, Int<1>{}, act); });
+        return by_act(a.act, [&](auto act) { return vec > 1 ? run(t, Int<16 / (int)sizeof(t)>{}, act) : run(t, Int<1>{}, act); });
     });
     if (e != cudaSuccess || !params) return e;
-    return launch_params(a, sum1, sum2, 1, stream, launches);
+    return launch_params(a, sum1, sum2, s.chunks, stream, launches);
 }
 
 cudaError_t launch_dropout(const void *x, const void *residual, void *y, int64_t rows, int64_t cols, int64_t ld_x,
@@ -565,28 +670,29 @@ cudaError_t launch_dropout(const void *x, const void *residual, void *y, int64_t
         rows = 1;
         ld_x = ld_r = ld_y = cols;
     }
-    auto run = [&](auto t, auto v) {
+    return by_type(elem, [&](auto t) {
         using T = decltype(t);
-        constexpr int VEC = decltype(v)::value;
-        const int64_t per_row = cols / VEC, nvec = rows * per_row;
-        const int64_t blocks = (nvec + kThreads * 4 - 1) / (kThreads * 4);
+        constexpr int VEC = 16 / (int)sizeof(T);
+        const T *px = static_cast<const T *>(x), *pr = static_cast<const T *>(residual);
+        T *py = static_cast<T *>(y);
+        const bool one = rows == 1;   // a long row's stride does not count
+        const bool vectors = vector_rows(elem, cols, {x, residual, y}, {one ? 0 : ld_x, one ? 0 : ld_r, one ? 0 : ld_y});
+        const int64_t units = vectors ? rows * (cols / VEC) : rows * cols, per_row = vectors ? cols / VEC : cols;
+        const int64_t blocks = (units + 3 + kThreads * 4 - 1) / (kThreads * 4);    // + 3: elements counted before the first
         if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+        const Divide divide((uint32_t)std::min<int64_t>(per_row, 0x7fffffff));
         auto go = [&](auto i) {
             using I = decltype(i);
-            cr_dropout_kernel<T, VEC, I><<<(unsigned)blocks, kThreads, 0, stream>>>(
-                static_cast<const T *>(x), static_cast<const T *>(residual), static_cast<T *>(y), (I)nvec, (I)per_row, ld_x, ld_r, ld_y, drop);
+            if (vectors)
+                cr_dropout_kernel<T, VEC, I><<<(unsigned)blocks, kThreads, 0, stream>>>(px, pr, py, (I)units, (I)per_row, divide, ld_x, ld_r, ld_y, drop);
+            else
+                cr_dropout_elements_kernel<T, I><<<(unsigned)blocks, kThreads, 0, stream>>>(px, pr, py, (I)units, (I)per_row, divide, ld_x, ld_r, ld_y, drop);
         };
-        if (nvec < (1ll << 31)) go(uint32_t{});
+        if (units < (1ll << 31) - 8192) go(uint32_t{});
         else go(uint64_t{});
         const cudaError_t e = cudaGetLastError();
         if (e == cudaSuccess) ++*launches;
         return e;
-    };
-    return by_type(elem, [&](auto t) {
-        // one long row may end inside a vector: the scalar form takes it whole
-        constexpr int VEC = 16 / (int)sizeof(t);
-        const bool one = rows == 1;
-        return vector_rows(elem, cols, {x, residual, y}, {one ? 0 : ld_x, one ? 0 : ld_r, one ? 0 : ld_y}) ? run(t, Int<VEC>{}) : run(t, Int<1>{});
     });
 }
 
