@@ -17,24 +17,25 @@
 #include "cr_elem.cuh"
 #include "cr_tcgen05.cuh"
 
-#ifndef CR_GN_FMIN
-#define CR_GN_FMIN 6
-#define CR_GN_BMIN 4
-#define CR_GN_FNV 8
-#define CR_GN_BNV 4
-#endif
-#ifndef CR_GN_WIDE
-#define CR_GN_WIDE 64
-#endif
-#ifndef CR_GN_FTH
-#define CR_GN_FTH 128
-#define CR_GN_BTH 128
-#endif
-
 namespace cr {
 namespace {
 
 constexpr int kMaxCluster = 8;
+
+// Threads of a CTA, vectors a thread holds at most, and the CTAs an SM is to hold.  A thread's work per vector has to
+// carry what it does once per sample (sums, exchange, addresses: about 300 instructions), and the CTAs of an SM have to
+// cover each other's barriers, so small CTAs with many vectors a thread win, as far as shared memory (two samples in
+// flight) and registers (dz) go.  Measured on 256 samples of 1024 x 256 (forward) and 192 (backward), bf16, us:
+// forward 256 threads 3 CTAs 71, 128 threads 6 CTAs 67, 5 CTAs 73; 4 vectors 82; backward 256 threads 2 CTAs 117,
+// 128 threads 4 CTAs 114, 5 CTAs 166 (spills).  fp32 has half the elements in a vector and wants twice the vectors in
+// the backward pass: 165 with 4, 125 with 8.
+constexpr int kTH = 128, kForwardNV = 8, kForwardCTAs = 6;
+constexpr int backward_nv(int elem_size) { return elem_size == 4 ? 8 : 4; }
+constexpr int backward_ctas(int elem_size) { return elem_size == 4 ? 3 : 4; }
+// Bytes of channels of a slab, where the groups allow it.  Wide slabs need more CTAs for an item, narrow ones more
+// sectors for a row: forward 74 / 67 / 74 us at 128 / 64 / 32 bytes; fp32 backward 125 at 128 bytes, 136 at 64.
+constexpr int kForwardBytes = 64;
+constexpr int backward_bytes(int elem_size) { return elem_size == 4 ? 128 : 64; }
 
 struct Slab {
     int sc;              // channels of a slab (the last one of a row may have fewer)
@@ -51,11 +52,11 @@ struct Slab {
 // Where a thread stands in the items of its cluster.
 struct Spot {
     int slab, rank, first_sample, rows, width, vpr, rt, col, j, c0, mine;   // j < 0: idle; mine: rows of this thread
-    int groups, cv;                                                       // groups of the slab; vectors per group
+    int groups, cv, cv_log;                                               // groups of the slab; vectors per group, its logarithm
     int lanes;           // bit o: lanes that differ in bit o hold rows or columns of the same group; -1: not that simple
     bool full;           // every thread has all its rows
 };
-template <int VEC, int NV, int kTH>
+template <int VEC, int NV>
 __device__ __forceinline__ Spot spot(const Slab &s) {
     Spot p;
     const uint32_t cluster = blockIdx.x / (uint32_t)s.cluster;
@@ -73,6 +74,7 @@ __device__ __forceinline__ Spot spot(const Slab &s) {
     p.mine = p.j < 0 || p.j >= p.rows ? 0 : (p.rows - p.j + p.rt - 1) / p.rt;
     p.groups = p.width / s.cg;
     p.cv = s.cg / VEC;
+    p.cv_log = 31 - __clz(max(p.cv, 1));
     // whole rows in a warp and a power of two of vectors in a group: column bits below cv, row bits from vpr on
     p.lanes = 32 % p.vpr == 0 && s.cg % VEC == 0 && (p.cv & (p.cv - 1)) == 0 ? (p.cv - 1) | (31 & ~(p.vpr - 1)) : -1;
     p.full = kTH % p.vpr == 0 && p.rows == NV * p.rt;
@@ -92,34 +94,26 @@ __device__ __forceinline__ void fold(const float *in, float *out, int count, int
     }
 }
 
-// Adds v over the lanes of the warp that hold the same column: lane, lane + vpr, .. (vpr divides 32).
-template <int N>
-__device__ __forceinline__ void sum_rows_of_warp(float (&v)[N], int vpr) {
-    for (int o = 16; o >= vpr; o >>= 1) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    }
-}
-
 // Sums over the CTA, by group, of N numbers a thread has for each of its groups (one group where a vector lies inside
 // it, else one per channel of the vector).  After the barrier in it, group_sum gives any thread any group's sum.
 // Where a warp holds whole rows and the groups a power of two of vectors, lanes add up the warp and one number a warp and
-// group goes through shared memory; otherwise every entry does.  `area`: kTH * N * kG floats.
+// group goes through shared memory; otherwise every entry does.  `lanes`: the lane bits to add over (-1: not that
+// simple), `group`: the thread's group.  `area`: kTH * N * kG floats.
 template <int N, int VEC, bool UNI, int kWarps>
-__device__ __forceinline__ void put_groups(float (&acc)[N][UNI ? 1 : VEC], const Spot &p, int cg, float *area, float *sums) {
+__device__ __forceinline__ void put_groups(float (&acc)[N][UNI ? 1 : VEC], const Spot &p, int lanes, int group, int cg, float *area, float *sums) {
     constexpr int kG = UNI ? 1 : VEC;
-    if (UNI && p.lanes >= 0) {
+    if (UNI && lanes >= 0) {
         float t[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) t[n] = acc[n][0];
 #pragma unroll
         for (int b = 0; b < 5; ++b)
-            if (p.lanes >> b & 1) {
+            if (lanes >> b & 1) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) t[n] += __shfl_xor_sync(0xffffffffu, t[n], 1 << b);
             }
-        if (((int)threadIdx.x & 31 & p.lanes) == 0) {
-            float *mine = area + (p.col / p.cv) * (N * kWarps) + ((int)threadIdx.x >> 5);
+        if (((int)threadIdx.x & 31 & lanes) == 0) {
+            float *mine = area + group * (N * kWarps) + ((int)threadIdx.x >> 5);
 #pragma unroll
             for (int n = 0; n < N; ++n) mine[n * kWarps] = t[n];
         }
@@ -161,48 +155,54 @@ __device__ __forceinline__ void cluster_meet() {
 // and nothing is fenced; a barrier of the cluster would wait for the stores of the previous sample as well.  Two boxes
 // by turns: a CTA writes into a box again only after it has heard from everybody about the exchange in between, which
 // they take part in after they have read this one.
+template <int KM>   // KM: most groups of a slab
 struct Exchange {
-    float2 *box;          // [2][cluster][gmax]
-    uint64_t *bars;       // [2]
-    volatile int *given_up;
+    struct Memory {
+        float2 box[2][kMaxCluster][KM];
+        uint64_t bars[2];
+        int given_up, unused;
+    };
+    Memory *m;
     int turn = 0;
 
-    __device__ __forceinline__ float2 *at(int rank, int g, int cluster, int gmax) const {
-        return box + ((turn & 1) * cluster + rank) * gmax + g;
+    // Sets the barriers up; the cluster meets once, since a CTA's memory may be written from outside only once it runs.
+    __device__ __forceinline__ void open(Memory *memory, int cluster) {
+        m = memory;
+        if (cluster > 1) {
+            if (threadIdx.x == 0) {
+                i8::mbar_init(&m->bars[0], 1);
+                i8::mbar_init(&m->bars[1], 1);
+                m->given_up = 0;
+                asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            }
+            cluster_meet();
+        }
     }
     // by one thread, before the others' numbers are waited for
     __device__ __forceinline__ void expect(int groups, int cluster) const {
-        i8::mbar_expect_tx(&bars[turn & 1], (uint32_t)(groups * cluster * 8));
+        i8::mbar_expect_tx(&m->bars[turn & 1], (uint32_t)(groups * cluster * 8));
     }
-    __device__ __forceinline__ void tell(float2 v, int rank, int g, int cluster, int gmax) const {
-        const uint32_t to = i8::smem_u32(at(rank, g, cluster, gmax)), bar = i8::smem_u32(&bars[turn & 1]);
+    __device__ __forceinline__ void tell(float2 v, int rank, int g, int cluster) const {
+        const uint32_t to = i8::smem_u32(&m->box[turn & 1][rank][g]), bar = i8::smem_u32(&m->bars[turn & 1]);
         for (int r = 0; r < cluster; ++r)
             asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
                          ::"r"(i8::map_to_rank(to, (uint32_t)r)), "f"(v.x), "f"(v.y), "r"(i8::map_to_rank(bar, (uint32_t)r)) : "memory");
     }
-    __device__ __forceinline__ void hear(int *status, unsigned long long wait_ns) const {
-        if (!i8::mbar_wait(&bars[turn & 1], (uint32_t)((turn >> 1) & 1), given_up, wait_ns)) {
-            *given_up = 1;
+    // The sums over the cluster of group g, in the order of the ranks.
+    __device__ __forceinline__ float2 hear(int g, int cluster, int *status, unsigned long long wait_ns) const {
+        if (!i8::mbar_wait(&m->bars[turn & 1], (uint32_t)((turn >> 1) & 1), &m->given_up, wait_ns)) {
+            m->given_up = 1;
             atomicExch(status, 1);
         }
+        float2 t = make_float2(0.f, 0.f);
+        for (int r = 0; r < cluster; ++r) {
+            const float2 v = m->box[turn & 1][r][g];
+            t.x += v.x;
+            t.y += v.y;
+        }
+        return t;
     }
 };
-// Sets the barriers up; the cluster meets once, since a CTA's memory may be written from outside only once it runs.
-__device__ __forceinline__ void open_exchange(Exchange &x, float *memory, int cluster, int gmax) {
-    x.box = reinterpret_cast<float2 *>(memory);
-    x.bars = reinterpret_cast<uint64_t *>(x.box + 2 * cluster * gmax);
-    x.given_up = reinterpret_cast<volatile int *>(x.bars + 2);
-    if (cluster > 1) {
-        if (threadIdx.x == 0) {
-            i8::mbar_init(&x.bars[0], 1);
-            i8::mbar_init(&x.bars[1], 1);
-            *x.given_up = 0;
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        cluster_meet();
-    }
-}
-inline size_t exchange_bytes(int cluster, int gmax) { return (size_t)2 * cluster * gmax * 8 + 2 * 8 + 8; }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -239,6 +239,28 @@ __device__ __forceinline__ F2 pair_of(const float (&v)[N], int i) {
     else return f2(v[2 * i], v[2 * i + 1]);
 }
 
+// Most groups of a slab: a slab is at most 32 channels wide, or one run of groups that no shorter run aligns (at most
+// as many as a vector has elements).  Where vectors lie inside groups these have 4 (fp32) or 8 channels at least.
+template <bool UNI>
+__host__ __device__ constexpr int most_groups() { return UNI ? 8 : 32; }
+// Shared memory of the two kernels behind the vectors; every array at a fixed place, which costs no register.
+template <int VEC, bool UNI>
+struct ForwardMemory {
+    float area[2][kTH * 2 * (UNI ? 1 : VEC)];                // by turns
+    float ready[2][most_groups<UNI>()];                      // mean, rstd
+    float sums[2 * most_groups<UNI>()];
+    int again[2];                                            // by turns
+    typename Exchange<most_groups<UNI>()>::Memory exchange;
+};
+template <int VEC, bool UNI>
+struct BackwardMemory {
+    float entries[2 * kTH * VEC];                            // [rt][2 * width]: channel sums of the thread rows
+    float area[2][kTH * 2 * (UNI ? 1 : VEC)];                // by turns
+    float ready[2][2][most_groups<UNI>()];                   // by turns
+    float sums[2 * most_groups<UNI>()];
+    typename Exchange<most_groups<UNI>()>::Memory exchange;
+};
+
 // The vectors of a thread: all NV of them where the CTA's share is full (no branches), else the first `mine`.
 template <int NV, typename F>
 __device__ __forceinline__ void for_rows(const Spot &p, F &&f) {
@@ -252,23 +274,37 @@ __device__ __forceinline__ void for_rows(const Spot &p, F &&f) {
     }
 }
 
-// Forward.  Sums and squares are taken of x - pivot, the pivot being the group's very first value: one pass over the
-// vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
+// Sums and squares of 16-bit elements on the tensor cores, four elements of every lane an instruction and no conversion:
+// with the lanes' registers r0, r1 as rows 0..7 of A and at the same time as B, entry (i, i) of A B is the sum of the
+// squares of what the four lanes of quad i hold, and with ones in rows 8..15 every entry (8 + ., i) is their plain sum.
+// (The other entries are not used.)  Products of 16-bit elements are exact in fp32; the accumulator is fp32.
+template <typename T>
+__device__ __forceinline__ void add_moments(float (&d)[4], uint32_t r0, uint32_t r1) {
+    if constexpr (__is_same(T, __nv_bfloat16)) {
+        constexpr uint32_t kOnes = 0x3f803f80u;
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %6, %5, %6}, {%4, %5}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(r0), "r"(r1), "r"(kOnes));
+    } else {
+        constexpr uint32_t kOnes = 0x3c003c00u;
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %6, %5, %6}, {%4, %5}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(r0), "r"(r1), "r"(kOnes));
+    }
+}
+
+// Forward.  Sums and squares are taken of x - pivot, the pivot being the group's very first value (zero where the tensor
+// cores take them: 16-bit elements, up to 8 vectors a row): one pass over the vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
 // squares have lost digits to it, and the item is summed once more around the mean itself (all CTAs of the cluster see
 // the same numbers and decide alike).
 // UNI: every vector lies inside one group.
-template <typename T, int NV, int kTH, bool UNI, int ACT>
-__global__ void __launch_bounds__(kTH, NV <= 8 ? CR_GN_FMIN : 1) cr_group_norm_kernel(const GroupNormArgs a, const Slab s) {
+template <typename T, int NV, bool UNI, int ACT>
+__global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const GroupNormArgs a, const Slab s) {
     constexpr int VEC = 16 / (int)sizeof(T), NP = VEC / 2, kG = UNI ? 1 : VEC;   // kG: groups a thread may touch
     extern __shared__ __align__(16) float sm[];
-    const Spot p = spot<VEC, NV, kTH>(s);
-    const int gmax = s.sc / s.cg;
-    float *area = sm + 2 * NV * kTH * 4;       // [2][kTH * 2 * kG], by turns
-    float *ready = area + 4 * kTH * kG;        // [2][gmax]: mean, rstd
-    float *sums = ready + 2 * gmax;            // [2][gmax]
-    volatile int *again = reinterpret_cast<volatile int *>(sums + 2 * gmax);   // [2]: by turns
-    Exchange ex;
-    open_exchange(ex, sums + 2 * gmax + 2, s.cluster, gmax);
+    const Spot p = spot<VEC, NV>(s);
+    constexpr int KM = most_groups<UNI>();
+    ForwardMemory<VEC, UNI> &mem = *reinterpret_cast<ForwardMemory<VEC, UNI> *>(sm + 2 * NV * kTH * 4);
+    Exchange<KM> ex;
+    ex.open(&mem.exchange, s.cluster);
     const uint32_t mine_at = i8::smem_u32(sm) + threadIdx.x * 16;
     const int64_t row0 = (int64_t)p.first_sample * s.positions + (int64_t)p.rank * s.rows_per_cta + max(p.j, 0);
     const T *src = static_cast<const T *>(a.x) + (row0 * a.ld_x + p.c0);
@@ -298,7 +334,22 @@ __global__ void __launch_bounds__(kTH, NV <= 8 ? CR_GN_FMIN : 1) cr_group_norm_k
     // first values of the thread's groups, and of the group it joins
     const T *firsts = static_cast<const T *>(a.x) + ((int64_t)p.first_sample * s.positions * a.ld_x + p.slab * s.sc);
     T pivots[kG], pivot_g;
+    constexpr bool kMoments = UNI && sizeof(T) == 2;
+    // Quad i of a warp takes the moments of column i % vpr, the rows 4 (i / vpr) + 0..3 of the warp: the slots of other
+    // lanes of the same warp.  (Copying in that order would cost a sector a lane.)
+    const bool moments = kMoments && p.vpr <= 8 && p.lanes >= 0;
+    const int lane = (int)threadIdx.x & 31, quad = lane >> 2;
+    const int quad_col = quad % p.vpr, quad_row = quad / p.vpr * 4 + (lane & 3);
+    const int quad_slot = (int)threadIdx.x - lane + quad_row * p.vpr + quad_col;
+    const int quad_j = ((int)threadIdx.x >> 5) * (32 / p.vpr) + quad_row;
+    const int quad_mine = quad_j < p.rows ? (p.rows - quad_j + p.rt - 1) / p.rt : 0;
+    const int quad_group = kMoments ? quad_col * VEC / s.cg : 0;
+    const int quad_lanes = 31 & ~(4 * (p.vpr - 1)) | 4 * (p.cv - 1);
     auto look_ahead = [&]() {
+        if (moments) {
+            pivots[0] = pivot_g = from_float<T>(0.f);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kG; ++i) pivots[i] = firsts[mine_g[i] * s.cg];
         pivot_g = firsts[(g < p.groups ? g : 0) * s.cg];
@@ -323,79 +374,95 @@ __global__ void __launch_bounds__(kTH, NV <= 8 ? CR_GN_FMIN : 1) cr_group_norm_k
 #pragma unroll
         for (int i = 0; i < NP; ++i) less[i] = pair_of<UNI>(m, i);
         for (int pass = 0;; ++pass) {
-            F2 t1[NP], t2[NP];
-#pragma unroll
-            for (int i = 0; i < NP; ++i) t1[i] = t2[i] = f2(0.f);
-            for_rows<NV>(p, [&](int k) {
-                F2 f[NP];
-                unpack2<T, VEC>(held<T>(at + k * kTH), f);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const F2 d = add2(f[i], less[i]);
-                    t1[i] = add2(t1[i], d);
-                    t2[i] = fma2(d, d, t2[i]);
-                }
-            });
             float acc[2][kG];
-            if constexpr (UNI) {
+            const bool by_quads = kMoments && moments && pass == 0;
+            if (by_quads) {
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint4 *from = reinterpret_cast<const uint4 *>(sm) + buf * NV * kTH + quad_slot;
+                __syncwarp();                  // the lanes' copies have landed, for all lanes
 #pragma unroll
-                for (int i = 1; i < NP; ++i) {
-                    t1[0] = add2(t1[0], t1[i]);
-                    t2[0] = add2(t2[0], t2[i]);
-                }
-                acc[0][0] = low(t1[0]) + high(t1[0]);
-                acc[1][0] = low(t2[0]) + high(t2[0]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    acc[0][2 * i] = low(t1[i]);
-                    acc[0][2 * i + 1] = high(t1[i]);
-                    acc[1][2 * i] = low(t2[i]);
-                    acc[1][2 * i + 1] = high(t2[i]);
-                }
-            }
-            float *my_area = area + (ex.turn & 1) * 2 * kTH * kG;
-            if (threadIdx.x == 0) {
-                again[ex.turn & 1] = 0;
-                if (s.cluster > 1) ex.expect(p.groups, s.cluster);
-            }
-            put_groups<2, VEC, UNI, kTH / 32>(acc, p, s.cg, my_area, sums);
-            if (g < p.groups) {
-                float total = group_sum<2, UNI, kTH / 32>(0, g, p, my_area, sums), squares = group_sum<2, UNI, kTH / 32>(1, g, p, my_area, sums);
-                if (s.cluster > 1) {
-                    ex.tell(make_float2(total, squares), p.rank, g, s.cluster, gmax);
-                    ex.hear(a.status, a.wait_ns);
-                    total = squares = 0.f;
-                    for (int r = 0; r < s.cluster; ++r) {
-                        const float2 v = *ex.at(r, g, s.cluster, gmax);
-                        total += v.x;
-                        squares += v.y;
+                for (int k = 0; k < NV; ++k) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (p.full || k < quad_mine) v = from[k * kTH];
+                    if constexpr (kMoments) {
+                        add_moments<T>(d, v.x, v.y);
+                        add_moments<T>(d, v.z, v.w);
                     }
                 }
+                // lane 4 i + i / 2 holds what belongs to quad i
+                const bool holds = (lane & 3) == quad >> 1;
+                acc[0][0] = holds ? (quad & 1 ? d[3] : d[2]) : 0.f;
+                acc[1][0] = holds ? (quad & 1 ? d[1] : d[0]) : 0.f;
+            } else {
+                F2 t1[NP], t2[NP];
+#pragma unroll
+                for (int i = 0; i < NP; ++i) t1[i] = t2[i] = f2(0.f);
+                for_rows<NV>(p, [&](int k) {
+                    F2 f[NP];
+                    unpack2<T, VEC>(held<T>(at + k * kTH), f);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        const F2 d = add2(f[i], less[i]);
+                        t1[i] = add2(t1[i], d);
+                        t2[i] = fma2(d, d, t2[i]);
+                    }
+                });
+                if constexpr (UNI) {
+#pragma unroll
+                    for (int i = 1; i < NP; ++i) {
+                        t1[0] = add2(t1[0], t1[i]);
+                        t2[0] = add2(t2[0], t2[i]);
+                    }
+                    acc[0][0] = low(t1[0]) + high(t1[0]);
+                    acc[1][0] = low(t2[0]) + high(t2[0]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        acc[0][2 * i] = low(t1[i]);
+                        acc[0][2 * i + 1] = high(t1[i]);
+                        acc[1][2 * i] = low(t2[i]);
+                        acc[1][2 * i + 1] = high(t2[i]);
+                    }
+                }
+            }
+            float *my_area = mem.area[ex.turn & 1];
+            if (threadIdx.x == 0) {
+                mem.again[ex.turn & 1] = 0;
+                if (s.cluster > 1) ex.expect(p.groups, s.cluster);
+            }
+            put_groups<2, VEC, UNI, kTH / 32>(acc, p, by_quads ? quad_lanes : p.lanes, by_quads ? quad_group : p.col >> p.cv_log, s.cg, my_area, mem.sums);
+            if (g < p.groups) {
+                float total = group_sum<2, UNI, kTH / 32>(0, g, p, my_area, mem.sums), squares = group_sum<2, UNI, kTH / 32>(1, g, p, my_area, mem.sums);
+                if (s.cluster > 1) {
+                    ex.tell(make_float2(total, squares), p.rank, g, s.cluster);
+                    const float2 all = ex.hear(g, s.cluster, a.status, a.wait_ns);
+                    total = all.x;
+                    squares = all.y;
+                }
                 const float off = total * inv_all, m2 = fmaxf(fmaf(-total, off, squares), 0.f);
-                if (pass == 0 && m2 * 16.f < squares) again[ex.turn & 1] = 1;
+                if (pass == 0 && m2 * 16.f < squares) mem.again[ex.turn & 1] = 1;
                 const float mean = pivot + off, rstd = 1.f / sqrtf(fmaf(m2, inv_all, a.eps));
                 pivot = mean;
-                ready[g] = mean;
-                ready[gmax + g] = rstd;
+                mem.ready[0][g] = mean;
+                mem.ready[1][g] = rstd;
                 if (a.mean && p.rank == 0) {
-                    const int64_t to = (int64_t)n * a.groups + p.slab * gmax + g;
+                    const int64_t to = (int64_t)n * a.groups + p.slab * (s.sc / s.cg) + g;
                     a.mean[to] = mean;
                     a.rstd[to] = rstd;
                 }
             }
             __syncthreads();
-            const int more = again[ex.turn & 1];
+            const int more = *const_cast<volatile int *>(&mem.again[ex.turn & 1]);
             ++ex.turn;
 #pragma unroll
-            for (int i = 0; i < kG; ++i) m[i] = -ready[mine_g[i]];
+            for (int i = 0; i < kG; ++i) m[i] = -mem.ready[0][mine_g[i]];
 #pragma unroll
             for (int i = 0; i < NP; ++i) less[i] = pair_of<UNI>(m, i);
             if (!more) break;
         }
         F2 scaled[NP], spread[NP];
 #pragma unroll
-        for (int i = 0; i < kG; ++i) m[i] = ready[gmax + mine_g[i]];
+        for (int i = 0; i < kG; ++i) m[i] = mem.ready[1][mine_g[i]];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             spread[i] = pair_of<UNI>(m, i);
@@ -432,18 +499,15 @@ constexpr int kShares = 2;
 // Backward: x and dy are read once; dz takes the place of dy, in registers.  sum1, sum2 (may be null): the sums of dz and
 // of dz xhat of each channel over a share of this CTA's rows of a sample, [samples][cluster][shares] rows of ld_sum;
 // `whole`: one row per sample, cluster = 1.
-template <typename T, int NV, int kTH, bool UNI, int ACT>
-__global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_grad_kernel(const GroupNormArgs a, const Slab s, float *sum1, float *sum2, int64_t ld_sum, int whole) {
+template <typename T, int NV, bool UNI, int ACT>
+__global__ void __launch_bounds__(kTH, backward_ctas(sizeof(T))) cr_group_norm_grad_kernel(const GroupNormArgs a, const Slab s, float *sum1, float *sum2, int64_t ld_sum, int whole) {
     constexpr int VEC = 16 / (int)sizeof(T), NP = VEC / 2, kG = UNI ? 1 : VEC;
     extern __shared__ __align__(16) float sm[];
-    const Spot p = spot<VEC, NV, kTH>(s);
-    const int gmax = s.sc / s.cg;
-    float *entries = sm + 4 * NV * kTH * 4;    // [2][rt][2 * width]: channel sums of the thread rows, by turns
-    float *area = entries + 4 * kTH * VEC;     // [2][kTH * 2 * kG]: by turns
-    float *ready = area + 4 * kTH * kG;        // [2][2][gmax]: by turns
-    float *sums = ready + 4 * gmax;            // [2][gmax]
-    Exchange ex;
-    open_exchange(ex, sums + 2 * gmax, s.cluster, gmax);
+    const Spot p = spot<VEC, NV>(s);
+    constexpr int KM = most_groups<UNI>();
+    BackwardMemory<VEC, UNI> &mem = *reinterpret_cast<BackwardMemory<VEC, UNI> *>(sm + 4 * NV * kTH * 4);
+    Exchange<KM> ex;
+    ex.open(&mem.exchange, s.cluster);
     const int both = 2 * p.width;
     const uint32_t mine_at = i8::smem_u32(sm) + threadIdx.x * 16;
     const int64_t row0 = (int64_t)p.first_sample * s.positions + (int64_t)p.rank * s.rows_per_cta + max(p.j, 0);
@@ -463,27 +527,21 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
     };
     fetch(0);
     copies_issued();
-    F2 gamma[NP], beta[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        gamma[i] = a.gamma ? f2(__ldg(a.gamma + p.c0 + 2 * i), __ldg(a.gamma + p.c0 + 2 * i + 1)) : f2(1.f);
-        beta[i] = a.beta ? f2(__ldg(a.beta + p.c0 + 2 * i), __ldg(a.beta + p.c0 + 2 * i + 1)) : f2(0.f);
-    }
     const float inv_all = 1.f / ((float)s.positions * (float)s.cg);
     const bool one = s.positions * s.cg == 1;  // groups of one value have m1 = gamma dz and no gradient at all
     const float kept = a.drop.threshold ? a.drop.scale : 1.f;
     const int g = (int)threadIdx.x;            // the group this thread joins, if g < p.groups
-    int mine_g[kG];
-#pragma unroll
-    for (int i = 0; i < kG; ++i) mine_g[i] = (p.col * VEC + i) / s.cg;
-    const float *mean_in = a.mean + (int64_t)p.first_sample * a.groups + p.slab * gmax;
-    const float *rstd_in = a.rstd + (int64_t)p.first_sample * a.groups + p.slab * gmax;
+    // the group of a channel of the thread: formed anew where it is needed, registers are what this kernel lacks (keeping
+    // it: 114 -> 127 us on 192 samples of 1024 x 256, bf16)
+    auto group_of = [&](int i) { return (p.col * VEC + i) / s.cg; };
+    const float *mean_in = a.mean + (int64_t)p.first_sample * a.groups + p.slab * (s.sc / s.cg);
+    const float *rstd_in = a.rstd + (int64_t)p.first_sample * a.groups + p.slab * (s.sc / s.cg);
     float mean[kG], rstd[kG];
     auto look_ahead = [&]() {
 #pragma unroll
         for (int i = 0; i < kG; ++i) {
-            mean[i] = mean_in[mine_g[i]];
-            rstd[i] = rstd_in[mine_g[i]];
+            mean[i] = mean_in[group_of(i)];
+            rstd[i] = rstd_in[group_of(i)];
         }
         mean_in += (int64_t)s.walkers * a.groups;
         rstd_in += (int64_t)s.walkers * a.groups;
@@ -491,7 +549,7 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
     look_ahead();
     int buf = 0;
     for (int n = p.first_sample; n < s.samples; n += s.walkers, buf ^= 1) {
-        F2 dz[NV][NP], s1[NP], s2[NP], scaled[NP], less[NP], spread[NP];
+        F2 dz[NV][NP], s1[NP], s2[NP], scaled[NP], gamma[ACT == kActRelu ? NP : 1], beta[NP], less[NP], spread[NP];
         {
             float m[kG];
 #pragma unroll
@@ -501,7 +559,11 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
                 s1[i] = s2[i] = f2(0.f);
                 less[i] = pair_of<UNI>(m, i);
                 spread[i] = pair_of<UNI>(rstd, i);
-                scaled[i] = mul2(gamma[i], spread[i]);
+                // the parameters are fetched for each sample (from L1): kept, they cost registers that this kernel lacks
+                const F2 weight = a.gamma ? f2(__ldg(a.gamma + p.c0 + 2 * i), __ldg(a.gamma + p.c0 + 2 * i + 1)) : f2(1.f);
+                if constexpr (ACT == kActRelu) gamma[i] = weight;
+                beta[i] = a.beta ? f2(__ldg(a.beta + p.c0 + 2 * i), __ldg(a.beta + p.c0 + 2 * i + 1)) : f2(0.f);
+                scaled[i] = mul2(weight, spread[i]);
             }
         }
         if (n + s.walkers < s.samples) {
@@ -527,7 +589,7 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
             for (int i = 0; i < NP; ++i) {
                 const F2 centred = add2(f[i], less[i]);
                 if constexpr (ACT != kActNone) {
-                    const F2 z = z_of<ACT>(centred, spread[i], gamma[i], scaled[i], beta[i]);
+                    const F2 z = z_of<ACT>(centred, spread[i], gamma[ACT == kActRelu ? i : 0], scaled[i], beta[i]);
                     if constexpr (ACT == kActSilu) {
                         const F2 sg = sigmoid2(z);
                         dz[k][i] = mul2(dz[k][i], mul2(sg, fma2(z, fma2(sg, f2(-1.f), f2(1.f)), f2(1.f))));
@@ -540,7 +602,7 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
             }
         });
         // the channels' sums, on their way while the groups are joined
-        float *my_entries = entries + buf * 2 * kTH * VEC;
+        float *my_entries = mem.entries;
         if ((sum1 || sum2) && p.j >= 0) {
             float *mine = my_entries + p.j * both + p.col * VEC;
 #pragma unroll
@@ -551,21 +613,21 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
                 *reinterpret_cast<float4 *>(mine + p.width + 2 * i) = make_float4(low(u2), high(u2), low(v2), high(v2));
             }
         }
-        // the groups' sums of gamma dz and gamma dz (x - mean)
+        // the groups' sums of rstd gamma dz and rstd gamma dz (x - mean)
         float acc[2][kG];
         if constexpr (UNI) {
-            F2 u1 = mul2(gamma[0], s1[0]), u2 = mul2(gamma[0], s2[0]);
+            F2 u1 = mul2(scaled[0], s1[0]), u2 = mul2(scaled[0], s2[0]);
 #pragma unroll
             for (int i = 1; i < NP; ++i) {
-                u1 = fma2(gamma[i], s1[i], u1);
-                u2 = fma2(gamma[i], s2[i], u2);
+                u1 = fma2(scaled[i], s1[i], u1);
+                u2 = fma2(scaled[i], s2[i], u2);
             }
             acc[0][0] = low(u1) + high(u1);
             acc[1][0] = low(u2) + high(u2);
         } else {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const F2 u1 = mul2(gamma[i], s1[i]), u2 = mul2(gamma[i], s2[i]);
+                const F2 u1 = mul2(scaled[i], s1[i]), u2 = mul2(scaled[i], s2[i]);
                 acc[0][2 * i] = low(u1);
                 acc[0][2 * i + 1] = high(u1);
                 acc[1][2 * i] = low(u2);
@@ -573,24 +635,20 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
             }
         }
         if (s.cluster > 1 && a.y && threadIdx.x == 0) ex.expect(p.groups, s.cluster);
-        float *my_area = area + buf * 2 * kTH * kG, *now = ready + buf * 2 * gmax;
-        put_groups<2, VEC, UNI, kTH / 32>(acc, p, s.cg, my_area, sums);
+        float *my_area = mem.area[buf];
+        put_groups<2, VEC, UNI, kTH / 32>(acc, p, p.lanes, p.col >> p.cv_log, s.cg, my_area, mem.sums);
         // a thread per group joins the CTAs.  dx = rstd (gamma dz - m1 - xhat m2)
-        //   = (rstd gamma) dz - rstd^3 M2 (x - mean) - rstd m1,  M2 the mean of gamma dz (x - mean)
+        //   = (rstd gamma) dz - M1 - rstd^2 M2 (x - mean),  M1, M2 the means of rstd gamma dz and rstd gamma dz (x - mean)
         if (a.y && g < p.groups) {
-            float t1 = group_sum<2, UNI, kTH / 32>(0, g, p, my_area, sums), t2 = group_sum<2, UNI, kTH / 32>(1, g, p, my_area, sums);
+            float t1 = group_sum<2, UNI, kTH / 32>(0, g, p, my_area, mem.sums), t2 = group_sum<2, UNI, kTH / 32>(1, g, p, my_area, mem.sums);
             if (s.cluster > 1) {
-                ex.tell(make_float2(t1, t2), p.rank, g, s.cluster, gmax);
-                ex.hear(a.status, a.wait_ns);
-                t1 = t2 = 0.f;
-                for (int r = 0; r < s.cluster; ++r) {
-                    const float2 v = *ex.at(r, g, s.cluster, gmax);
-                    t1 += v.x;
-                    t2 += v.y;
-                }
+                ex.tell(make_float2(t1, t2), p.rank, g, s.cluster);
+                const float2 all = ex.hear(g, s.cluster, a.status, a.wait_ns);
+                t1 = all.x;
+                t2 = all.y;
             }
-            now[g] = t1 * inv_all;
-            now[gmax + g] = t2 * inv_all;
+            mem.ready[buf][0][g] = t1 * inv_all;
+            mem.ready[buf][1][g] = t2 * inv_all;
         }
         ++ex.turn;
         if (sum1 || sum2) {     // put_groups had a barrier: the entries are there
@@ -616,17 +674,12 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
         }
         if (a.y) {
             __syncthreads();
-            float acc1[kG], acc2[kG], r1[kG];
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                if constexpr (UNI) r1[0] = low(spread[0]);
-                else { r1[2 * i] = low(spread[i]); r1[2 * i + 1] = high(spread[i]); }
-            }
+            float acc1[kG], acc2[kG];
 #pragma unroll
             for (int i = 0; i < kG; ++i) {
-                const float r = r1[i] * kept;
-                acc1[i] = -r * now[mine_g[i]];
-                acc2[i] = -r * r1[i] * r1[i] * now[gmax + mine_g[i]];
+                const float r = UNI ? low(spread[0]) : (i & 1 ? high(spread[i / 2]) : low(spread[i / 2]));
+                acc1[i] = -kept * mem.ready[buf][0][group_of(i)];
+                acc2[i] = -kept * r * r * mem.ready[buf][1][group_of(i)];
             }
             F2 c1[NP], c2[NP];
 #pragma unroll
@@ -648,6 +701,8 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
                 to += step_y;
             });
             dst += next * a.ld_y;
+        } else {
+            __syncthreads();    // the entries are free again
         }
     }
     if (s.cluster > 1) cluster_meet();
@@ -656,14 +711,14 @@ __global__ void __launch_bounds__(kTH, NV <= 4 ? CR_GN_BMIN : 1) cr_group_norm_g
 template <int V> struct Int { static constexpr int value = V; };
 
 // The slab and the cluster of an item, and the vectors a thread holds: false where an item does not fit.
-bool choose(int elem, int channels, int groups, int64_t samples, int64_t positions, int kTH, int max_nv, Slab &s, int &nv) {
+bool choose(int elem, int channels, int groups, int64_t samples, int64_t positions, int bytes, int max_nv, Slab &s, int &nv) {
     const int vec = 16 / elem_bytes(elem);
     if (channels % vec || samples > 0x3fffffff) return false;
     s.cg = channels / groups;
     s.channels = channels;
     s.positions = positions;
     s.samples = (int)samples;
-    const int unit = std::lcm(s.cg, vec), wanted = CR_GN_WIDE / elem_bytes(elem);
+    const int unit = std::lcm(s.cg, vec), wanted = bytes / elem_bytes(elem);
     for (int width = std::min(channels, unit * std::max(1, wanted / unit));; width = std::max(unit, width / 2 / unit * unit)) {
         if (width / vec <= kTH) {
             const int rt = kTH / (width / vec);
@@ -716,10 +771,10 @@ cudaError_t resident_clusters(K kernel, Known &known, int device, const cudaLaun
 }
 
 template <typename K, typename... More>
-cudaError_t launch(K kernel, int threads, Known &known, Slab s, size_t smem, cudaStream_t stream, int64_t *launches, const GroupNormArgs &a, More... more) {
+cudaError_t launch(K kernel, Known &known, Slab s, size_t smem, cudaStream_t stream, int64_t *launches, const GroupNormArgs &a, More... more) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)s.cluster);
-    cfg.blockDim = dim3((unsigned)threads);
+    cfg.blockDim = dim3(kTH);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -738,8 +793,6 @@ cudaError_t launch(K kernel, int threads, Known &known, Slab s, size_t smem, cud
     if (e == cudaSuccess) ++*launches;
     return e;
 }
-
-constexpr int kForwardNV = CR_GN_FNV, kBackwardNV = CR_GN_BNV, kForwardTH = CR_GN_FTH, kBackwardTH = CR_GN_BTH;
 
 template <int Low, int High, typename F>
 cudaError_t by_nv(int nv, F &&f) {
@@ -769,30 +822,28 @@ cudaError_t by_type_act(int elem, int act, F &&f) {
 bool group_norm_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem) {
     Slab s;
     int nv;
-    return choose(elem, channels, groups, samples, positions, kForwardTH, kForwardNV, s, nv);
+    return choose(elem, channels, groups, samples, positions, kForwardBytes, kForwardNV, s, nv);
 }
 int group_norm_backward_on_chip(int64_t samples, int64_t positions, int channels, int groups, int elem) {
     Slab s;
     int nv;
-    return choose(elem, channels, groups, samples, positions, kBackwardTH, kBackwardNV, s, nv) ? s.cluster * kShares : 0;
+    return choose(elem, channels, groups, samples, positions, backward_bytes(elem_bytes(elem)), backward_nv(elem_bytes(elem)), s, nv) ? s.cluster * kShares : 0;
 }
 
 cudaError_t launch_group_norm_on_chip(const GroupNormArgs &a, cudaStream_t stream, int64_t *launches) {
     Slab s;
     int nv;
-    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, kForwardTH, kForwardNV, s, nv)) return cudaErrorInvalidValue;
+    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, kForwardBytes, kForwardNV, s, nv)) return cudaErrorInvalidValue;
     return by_type_act(a.elem, a.act, [&](auto t, auto act) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T), ACT = decltype(act)::value;
-        const int gmax = s.sc / s.cg;
         return by_nv<2, kForwardNV>(nv, [&](auto n) {
             constexpr int NV = decltype(n)::value;
             auto go = [&](auto uni) {
                 constexpr bool UNI = decltype(uni)::value != 0;
-                constexpr int kTH = kForwardTH;
                 static Known known;
-                const size_t smem = (size_t)2 * NV * kTH * 16 + ((size_t)4 * kTH * (UNI ? 1 : VEC) + 4 * gmax + 2) * 4 + exchange_bytes(s.cluster, gmax);
-                return launch(cr_group_norm_kernel<T, NV, kTH, UNI, ACT>, kTH, known, s, smem, stream, launches, a);
+                constexpr size_t smem = (size_t)2 * NV * kTH * 16 + sizeof(ForwardMemory<VEC, UNI>);
+                return launch(cr_group_norm_kernel<T, NV, UNI, ACT>, known, s, smem, stream, launches, a);
             };
             return s.cg % VEC == 0 ? go(Int<1>{}) : go(Int<0>{});
         });
@@ -803,19 +854,17 @@ cudaError_t launch_group_norm_grad_on_chip(const GroupNormArgs &a, float *sum1, 
                                            int64_t *launches) {
     Slab s;
     int nv;
-    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, kBackwardTH, kBackwardNV, s, nv)) return cudaErrorInvalidValue;
+    if (!choose(a.elem, a.channels, a.groups, a.samples, a.positions, backward_bytes(elem_bytes(a.elem)), backward_nv(elem_bytes(a.elem)), s, nv)) return cudaErrorInvalidValue;
     return by_type_act(a.elem, a.act, [&](auto t, auto act) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T), ACT = decltype(act)::value;
-        const int gmax = s.sc / s.cg;
-        return by_nv<2, kBackwardNV>(nv, [&](auto n) {
+        return by_nv<2, backward_nv(sizeof(T))>(nv, [&](auto n) {
             constexpr int NV = decltype(n)::value;
             auto go = [&](auto uni) {
                 constexpr bool UNI = decltype(uni)::value != 0;
-                constexpr int kTH = kBackwardTH;
                 static Known known;
-                const size_t smem = (size_t)4 * NV * kTH * 16 + ((size_t)4 * kTH * VEC + (size_t)4 * kTH * (UNI ? 1 : VEC) + 6 * gmax) * 4 + exchange_bytes(s.cluster, gmax);
-                return launch(cr_group_norm_grad_kernel<T, NV, kTH, UNI, ACT>, kTH, known, s, smem, stream, launches, a, sum1, sum2, ld_sum, whole ? 1 : 0);
+                constexpr size_t smem = (size_t)4 * NV * kTH * 16 + sizeof(BackwardMemory<VEC, UNI>);
+                return launch(cr_group_norm_grad_kernel<T, NV, UNI, ACT>, known, s, smem, stream, launches, a, sum1, sum2, ld_sum, whole ? 1 : 0);
             };
             return s.cg % VEC == 0 ? go(Int<1>{}) : go(Int<0>{});
         });
