@@ -291,8 +291,8 @@ __device__ __forceinline__ void add_moments(float (&d)[4], uint32_t r0, uint32_t
     }
 }
 
-// Forward.  Sums and squares are taken of x - pivot, the pivot being the group's very first value (zero where the tensor
-// cores take them: 16-bit elements, up to 8 vectors a row): one pass over the vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
+// Forward.  Sums and squares are taken of x - pivot, the pivot being the mean of the group's very first values, one vector of
+// them (zero where the tensor cores take the sums: 16-bit elements, up to 8 vectors a row): one pass over the vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
 // squares have lost digits to it, and the item is summed once more around the mean itself (all CTAs of the cluster see
 // the same numbers and decide alike).
 // UNI: every vector lies inside one group.
@@ -333,7 +333,15 @@ __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const 
     for (int i = 0; i < kG; ++i) mine_g[i] = (p.col * VEC + i) / s.cg;
     // first values of the thread's groups, and of the group it joins
     const T *firsts = static_cast<const T *>(a.x) + ((int64_t)p.first_sample * s.positions * a.ld_x + p.slab * s.sc);
-    T pivots[kG], pivot_g;
+    constexpr int kFirst = UNI ? VEC : 1;
+    Packed<T, kFirst> pivots[kG], pivot_g;
+    auto pivot_of = [](const Packed<T, kFirst> &first) {
+        float f[kFirst], t = 0.f;
+        unpack<T, kFirst>(first, f);
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) t += f[i];
+        return t * (1.f / kFirst);
+    };
     constexpr bool kMoments = UNI && sizeof(T) == 2;
     // Quad i of a warp takes the moments of column i % vpr, the rows 4 (i / vpr) + 0..3 of the warp: the slots of other
     // lanes of the same warp.  (Copying in that order would cost a sector a lane.)
@@ -346,13 +354,10 @@ __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const 
     const int quad_group = kMoments ? quad_col * VEC / s.cg : 0;
     const int quad_lanes = 31 & ~(4 * (p.vpr - 1)) | 4 * (p.cv - 1);
     auto look_ahead = [&]() {
-        if (moments) {
-            pivots[0] = pivot_g = from_float<T>(0.f);
-            return;
-        }
+        if (moments) return;
 #pragma unroll
-        for (int i = 0; i < kG; ++i) pivots[i] = firsts[mine_g[i] * s.cg];
-        pivot_g = firsts[(g < p.groups ? g : 0) * s.cg];
+        for (int i = 0; i < kG; ++i) pivots[i] = load_packed<T, kFirst>(firsts + mine_g[i] * s.cg);
+        pivot_g = load_packed<T, kFirst>(firsts + (g < p.groups ? g : 0) * s.cg);
         firsts += next_x;
     };
     look_ahead();
@@ -360,8 +365,8 @@ __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const 
     for (int n = p.first_sample; n < s.samples; n += s.walkers, buf ^= 1) {
         float m[kG];
 #pragma unroll
-        for (int i = 0; i < kG; ++i) m[i] = -to_float(pivots[i]);
-        float pivot = to_float(pivot_g);
+        for (int i = 0; i < kG; ++i) m[i] = moments ? 0.f : -pivot_of(pivots[i]);
+        float pivot = moments ? 0.f : pivot_of(pivot_g);
         src += next_x;
         if (n + s.walkers < s.samples) {
             fetch(buf ^ 1);

@@ -33,6 +33,10 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Blocks of the streaming kernels that an SM holds, by the registers that a thread's channels take (elements of its
+// vector, arrays it reads); the chunks are cut so that one round of blocks covers the tensor.
+__host__ __device__ constexpr int blocks_per_sm(int vec, int arrays) { return vec < 8 ? 4 : arrays == 1 ? 3 : 2; }
+
 // Which part of the tensor a block of the streaming kernels has: sample, tile of channels, chunk of positions.  A tile
 // is a run of whole groups of up to 256 vectors, or one of `parts` pieces of a group that is wider than that.  A thread
 // keeps its vector of channels and walks every rt-th row of the chunk.
@@ -109,6 +113,26 @@ __device__ __forceinline__ void fold_rows(float *sm, int plane, int width, int r
     }
     __syncthreads();
 }
+// Vectors that a thread requests before it works on the first of them.  An
+// output may be the input's own buffer, so the compiler does not move a load over a store and the batches are made here.
+__host__ __device__ constexpr int in_flight(int vec, int arrays) { return (vec == 1 ? 8 : 4) / arrays; }
+
+// f(vector, k) for the thread's k-th row of the chunk, whose first lies at `src`, `step` elements apart.
+template <typename T, int VEC, typename F>
+__device__ __forceinline__ void walk_one(const Place &p, const T *src, int64_t step, F &&f) {
+    constexpr int U = in_flight(VEC, 1);
+    const int mine = p.j < p.rows ? (p.rows - p.j + p.rt - 1) / p.rt : 0;
+    int k = 0;
+    for (; k + U <= mine; k += U, src += U * step) {
+        Packed<T, VEC> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = load_packed<T, VEC>(src + u * step);
+#pragma unroll
+        for (int u = 0; u < U; ++u) f(raw[u], k + u);
+    }
+    for (; k < mine; ++k, src += step) f(load_packed<T, VEC>(src), k);
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -120,7 +144,7 @@ __device__ __forceinline__ float warp_sum(float v) {
 // Sums are taken of x - k, k the channel's value in the chunk's first row: the squares then carry the spread and not the
 // mean.  Channels, chunks and pieces are joined by mean and centred square sum.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_stats_kernel(const T *x, int64_t ld, const Split s, float2 *partial) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 1)) cr_group_norm_stats_kernel(const T *x, int64_t ld, const Split s, float2 *partial) {
     __shared__ float sm[2 * kThreads * VEC];
     constexpr int kPlane = kThreads * VEC;
     const Place p = place<VEC>(s);
@@ -132,17 +156,16 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_stats_kernel(const T *
         const int64_t step = (int64_t)p.rt * ld;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.f;
-#pragma unroll 4
-        for (int r = p.j; r < p.rows; r += p.rt, src += step) {
+        walk_one<T, VEC>(p, src, step, [&](const Packed<T, VEC> &raw, int) {
             float v[VEC];
-            unpack<T, VEC>(load_packed<T, VEC>(src), v);
+            unpack<T, VEC>(raw, v);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const float dlt = v[i] - k[i];
                 s1[i] += dlt;
                 s2[i] = fmaf(dlt, dlt, s2[i]);
             }
-        }
+        });
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const int at = (p.j * p.vecs + p.col) * VEC + i;
@@ -188,7 +211,7 @@ struct Affine {
 };
 
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 1)) cr_group_norm_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
     __shared__ float2 ready[kThreads * VEC];     // mean and rstd of the tile's groups
     const Place p = place<VEC>(s);
     Affine<VEC> f;
@@ -231,16 +254,22 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_apply_kernel(const Gro
         f.mean[i] = v.x;
         f.rstd[i] = v.y;
     }
-    const int64_t first = p.n * s.positions + p.row0;
-#pragma unroll 2
-    for (int r = p.j; r < p.rows; r += p.rt) {
+    const int64_t first = p.n * s.positions + p.row0 + p.j;
+    T *y = static_cast<T *>(a.y) + (first * a.ld_y + p.c0);
+    const int64_t step_y = (int64_t)p.rt * a.ld_y;
+    unsigned long long e = a.drop.offset + (unsigned long long)(first * s.channels + p.c0);
+    walk_one<T, VEC>(p, static_cast<const T *>(a.x) + (first * a.ld_x + p.c0), (int64_t)p.rt * a.ld_x, [&](const Packed<T, VEC> &raw, int) {
         float v[VEC];
-        unpack<T, VEC>(load_packed<T, VEC>(static_cast<const T *>(a.x) + ((first + r) * a.ld_x + p.c0)), v);
+        unpack<T, VEC>(raw, v);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) v[i] = act_value<ACT>(f.z(f.xhat(v[i], i), i));
-        if (a.drop.threshold) drop<VEC>(v, a.drop, a.drop.offset + (unsigned long long)((first + r) * s.channels + p.c0));
-        store_packed<T, VEC>(static_cast<T *>(a.y) + ((first + r) * a.ld_y + p.c0), pack<T, VEC>(v));
-    }
+        if (a.drop.threshold) {
+            drop<VEC>(v, a.drop, e);
+            e += (unsigned long long)p.rt * s.channels;
+        }
+        store_packed<T, VEC>(y, pack<T, VEC>(v));
+        y += step_y;
+    });
 }
 
 // ---- backward, streaming -----------------------------------------------------------------------------------------
@@ -256,13 +285,13 @@ __device__ __forceinline__ void statistics(Affine<VEC> &f, const Place &p, const
     }
 }
 
-// dz of a vector of elements, and their xhat.
+// dz of a vector of elements, and their xhat; `e`: index of the first element.
 template <typename T, int VEC, int ACT>
-__device__ __forceinline__ void slopes(const GroupNormArgs &a, const Affine<VEC> &f, int64_t row, int c0, int channels,
+__device__ __forceinline__ void slopes(const GroupNormArgs &a, const Affine<VEC> &f, const Packed<T, VEC> &x, const Packed<T, VEC> &dy, int64_t e,
                                        float (&dz)[VEC], float (&xh)[VEC]) {
-    unpack<T, VEC>(load_packed<T, VEC>(static_cast<const T *>(a.x) + (row * a.ld_x + c0)), xh);
-    unpack<T, VEC>(load_packed<T, VEC>(static_cast<const T *>(a.dy) + (row * a.ld_dy + c0)), dz);
-    if (a.drop.threshold) drop<VEC>(dz, a.drop, a.drop.offset + (unsigned long long)(row * channels + c0));
+    unpack<T, VEC>(x, xh);
+    unpack<T, VEC>(dy, dz);
+    if (a.drop.threshold) drop<VEC>(dz, a.drop, a.drop.offset + (unsigned long long)e);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
         xh[i] = f.xhat(xh[i], i);
@@ -270,10 +299,40 @@ __device__ __forceinline__ void slopes(const GroupNormArgs &a, const Affine<VEC>
     }
 }
 
+// Walks the thread's rows of the chunk in batches: f(dz, xhat).
+template <typename T, int VEC, int ACT, typename F>
+__device__ __forceinline__ void walk(const GroupNormArgs &a, const Split &s, const Place &p, const Affine<VEC> &aff, F &&f) {
+    const int64_t first = p.n * s.positions + p.row0 + p.j;
+    const T *x = static_cast<const T *>(a.x) + (first * a.ld_x + p.c0);
+    const T *dy = static_cast<const T *>(a.dy) + (first * a.ld_dy + p.c0);
+    const int64_t step_x = (int64_t)p.rt * a.ld_x, step_dy = (int64_t)p.rt * a.ld_dy, step_e = (int64_t)p.rt * s.channels;
+    int64_t e = first * s.channels + p.c0;
+    constexpr int U = in_flight(VEC, 2);
+    const int mine = p.j < p.rows ? (p.rows - p.j + p.rt - 1) / p.rt : 0;
+    auto one = [&](const Packed<T, VEC> &raw_x, const Packed<T, VEC> &raw_dy) {
+        float dz[VEC], xh[VEC];
+        slopes<T, VEC, ACT>(a, aff, raw_x, raw_dy, e, dz, xh);
+        e += step_e;
+        f(dz, xh);
+    };
+    int k = 0;
+    for (; k + U <= mine; k += U, x += U * step_x, dy += U * step_dy) {
+        Packed<T, VEC> raw_x[U], raw_dy[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            raw_x[u] = load_packed<T, VEC>(x + u * step_x);
+            raw_dy[u] = load_packed<T, VEC>(dy + u * step_dy);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) one(raw_x[u], raw_dy[u]);
+    }
+    for (; k < mine; ++k, x += step_x, dy += step_dy) one(load_packed<T, VEC>(x), load_packed<T, VEC>(dy));
+}
+
 // The channels' sums of dz (part1) and dz xhat (part2) over a chunk, [samples][chunks] rows of `channels`, and the
 // groups' sums of gamma dz and gamma dz xhat.
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_grad_sums_kernel(const GroupNormArgs a, const Split s, float *part1, float *part2, float2 *partial) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 2)) cr_group_norm_grad_sums_kernel(const GroupNormArgs a, const Split s, float *part1, float *part2, float2 *partial) {
     __shared__ float sm[2 * kThreads * VEC];
     constexpr int kPlane = kThreads * VEC;
     const Place p = place<VEC>(s);
@@ -283,17 +342,13 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_grad_sums_kernel(const
         float s1[VEC], s2[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s1[i] = s2[i] = 0.f;
-        const int64_t first = p.n * s.positions + p.row0;
-#pragma unroll 2
-        for (int r = p.j; r < p.rows; r += p.rt) {
-            float dz[VEC], xh[VEC];
-            slopes<T, VEC, ACT>(a, f, first + r, p.c0, s.channels, dz, xh);
+        walk<T, VEC, ACT>(a, s, p, f, [&](const float (&dz)[VEC], const float (&xh)[VEC]) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 s1[i] += dz[i];
                 s2[i] = fmaf(dz[i], xh[i], s2[i]);
             }
-        }
+        });
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             sm[(p.j * p.vecs + p.col) * VEC + i] = s1[i];
@@ -321,7 +376,7 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_grad_sums_kernel(const
 }
 
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads) cr_group_norm_grad_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 2)) cr_group_norm_grad_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
     __shared__ float2 ready[kThreads * VEC];     // m1 and m2 of the tile's groups
     const Place p = place<VEC>(s);
     const int lane = threadIdx.x & 31, entries = s.chunks * s.parts;
@@ -350,15 +405,15 @@ __global__ void __launch_bounds__(kThreads) cr_group_norm_grad_apply_kernel(cons
         b1[i] = v.x;
         b2[i] = v.y;
     }
-    const int64_t first = p.n * s.positions + p.row0;
-    for (int r = p.j; r < p.rows; r += p.rt) {
-        float dz[VEC], xh[VEC];
-        slopes<T, VEC, ACT>(a, f, first + r, p.c0, s.channels, dz, xh);
+    const int64_t row = p.n * s.positions + p.row0 + p.j, step_y = (int64_t)p.rt * a.ld_y;
+    T *y = static_cast<T *>(a.y) + (row * a.ld_y + p.c0);
+    walk<T, VEC, ACT>(a, s, p, f, [&](float (&dz)[VEC], const float (&xh)[VEC]) {
         // gamma dz is rounded before m1 leaves it: a group of one value has m1 = gamma dz and so a gradient of zero
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dz[i] = f.rstd[i] * fmaf(-xh[i], b2[i], __fmul_rn(f.gamma[i], dz[i]) - b1[i]);
-        store_packed<T, VEC>(static_cast<T *>(a.y) + ((first + r) * a.ld_y + p.c0), pack<T, VEC>(dz));
-    }
+        store_packed<T, VEC>(y, pack<T, VEC>(dz));
+        y += step_y;
+    });
 }
 
 // Parameter gradients of a partition: the sums over the rows (one or more a sample) of its samples, 32 channels a block, eight threads to a channel.
@@ -487,7 +542,7 @@ __global__ void __launch_bounds__(kThreads) cr_dropout_elements_kernel(const T *
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-Split make_split(int64_t samples, int64_t positions, int channels, int groups, int vec) {
+Split make_split(int64_t samples, int64_t positions, int channels, int groups, int vec, int arrays) {
     Split s;
     s.positions = positions;
     s.channels = channels;
@@ -503,10 +558,10 @@ Split make_split(int64_t samples, int64_t positions, int channels, int groups, i
         s.width = most;
         s.tiles = groups * s.parts;
     }
-    // Chunks of at least four rows a thread, about four blocks an SM in all: fewer leave SMs idle (one sample of 52066
-    // positions of 4 channels: 74 us in 6 chunks), more spend their time on the joins.
+    // Chunks of at least four rows a thread, one round of blocks on 148 SMs: fewer leave SMs idle (one sample of 52066
+    // positions of 4 channels: 74 us in 6 chunks, 24 so), more spend their time on the joins.
     const int64_t least = 4ll * (kThreads / std::min(kThreads, s.width / vec));
-    int64_t chunks = std::max<int64_t>(1, 592 / std::max<int64_t>(1, samples * s.tiles));
+    int64_t chunks = std::max<int64_t>(1, 148 * blocks_per_sm(vec, arrays) / std::max<int64_t>(1, samples * s.tiles));
     chunks = std::min(chunks, std::max<int64_t>(1, positions / least));
     s.rows_per_chunk = (positions + chunks - 1) / chunks;
     // a block counts its rows in 32 bits, and a float holds the count of a group without rounding far beyond this
@@ -558,7 +613,7 @@ size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channe
     for (bool wide : {false, true}) {
         const int vec = split_vec(wide, elem, channels, groups);
         if (channels % vec) continue;
-        const Split s = make_split(samples, positions, channels, groups, vec);
+        const Split s = make_split(samples, positions, channels, groups, vec, 1);
         most = std::max(most, (size_t)s.chunks * groups * s.parts * (size_t)samples * 8);
     }
     return most;
@@ -570,7 +625,7 @@ size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, i
     for (bool wide : {false, true}) {
         const int vec = split_vec(wide, elem, channels, groups);
         if (channels % vec) continue;
-        const Split s = make_split(samples, positions, channels, groups, vec);
+        const Split s = make_split(samples, positions, channels, groups, vec, 2);
         most = std::max(most, (size_t)s.chunks * (channels + (size_t)groups * s.parts) * (size_t)samples * 8);
     }
     // the one-pass form's rows of sums
@@ -582,7 +637,7 @@ cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &, cudaSt
     const bool wide = vector_rows(a.elem, a.channels, {a.x, a.y}, {a.ld_x, a.ld_y});
     if (wide && group_norm_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem)) return launch_group_norm_on_chip(a, stream, launches);
     const int vec = split_vec(wide, a.elem, a.channels, a.groups);
-    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec);
+    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec, 1);
     float2 *partial = reinterpret_cast<float2 *>(a.workspace);
     const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
     auto run = [&](auto t, auto v) {
@@ -634,7 +689,7 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         return launch_params(a, sum1, sum2, rows, stream, launches);
     }
     const int vec = split_vec(wide, a.elem, a.channels, a.groups);
-    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec);
+    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec, 2);
     float *sum2 = sum1 + plane * s.chunks;
     float2 *partial = reinterpret_cast<float2 *>(sum2 + plane * s.chunks);
     const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
