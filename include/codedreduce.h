@@ -409,8 +409,9 @@ typedef struct {
  * channels of each (sample, group), var the mean square distance from the mean.  gamma, beta: fp32 [channels] or NULL
  * (ones, zeros).  mean, rstd: fp32 [samples][groups], written for the backward pass; both NULL if not wanted.  y may
  * be x itself (same stride).  workspace: device scratch of cr_group_norm_workspace_bytes (CR_ERR_OOM if
- * smaller), 16-byte aligned. */
-size_t cr_group_norm_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc);
+ * smaller), 16-byte aligned; vector_rows: whether every tensor of the call has a 16-byte aligned base and row stride
+ * (then it is often 0: items that fit the chip are read once and need none). */
+size_t cr_group_norm_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc, int32_t vector_rows);
 cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const void *x, int64_t ld_x, const float *gamma,
                           const float *beta, void *y, int64_t ld_y, float *mean, float *rstd, void *workspace,
                           size_t workspace_bytes, void *stream);
@@ -420,7 +421,8 @@ cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const vo
  * consecutive samples (partitions >= 1 divides samples) -- the partial gradients of the partitions, which can be
  * written straight into longer rows of gradients; either may be NULL.  dx may be dy itself (same stride).
  * workspace as above, of cr_group_norm_backward_workspace_bytes. */
-size_t cr_group_norm_backward_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc);
+size_t cr_group_norm_backward_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc,
+                                              int32_t vector_rows);
 cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc, const void *dy, int64_t ld_dy,
                                    const void *x, int64_t ld_x, const float *gamma, const float *beta,
                                    const float *mean, const float *rstd, void *dx, int64_t ld_dx, float *dgamma,

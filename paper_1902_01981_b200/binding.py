@@ -108,10 +108,10 @@ _SIGNATURES = {
     "cr_plan_tune_items": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32]),
     "cr_dropout": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
                              C.c_int64, C.c_int32, C.c_double, C.c_uint64, C.c_int64, C.c_void_p]),
-    "cr_group_norm_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(cr_group_norm_t)]),
+    "cr_group_norm_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(cr_group_norm_t), C.c_int32]),
     "cr_group_norm": (C.c_int, [C.c_void_p, C.POINTER(cr_group_norm_t), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
                                 C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
-    "cr_group_norm_backward_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(cr_group_norm_t)]),
+    "cr_group_norm_backward_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(cr_group_norm_t), C.c_int32]),
     "cr_group_norm_backward": (C.c_int, [C.c_void_p, C.POINTER(cr_group_norm_t), C.c_void_p, C.c_int64, C.c_void_p,
                                          C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                          C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
@@ -539,18 +539,26 @@ def _group_norm_desc(x, groups, eps, act, p, seed, offset):
 
 
 @functools.lru_cache(maxsize=256)
-def _group_norm_workspace(backward: bool, plan: int, shape, groups: int, elem: int) -> int:
-    """The workspace is a function of these sizes (the plan's device included), so a loop asks once."""
+def _group_norm_workspace(backward: bool, plan: int, shape, groups: int, elem: int, vector_rows: int) -> int:
+    """The workspace is a function of these (the plan's device included), so a loop asks once."""
     fn = lib().cr_group_norm_backward_workspace_bytes if backward else lib().cr_group_norm_workspace_bytes
-    return fn(plan, cr_group_norm_t(*shape, groups, elem, CR_ACT_NONE, 0.0, 0.0, 0, 0))
+    return fn(plan, cr_group_norm_t(*shape, groups, elem, CR_ACT_NONE, 0.0, 0.0, 0, 0), vector_rows)
+
+
+def _vector_rows(x) -> int:
+    ptr, ld = _row_ptr(x, x.shape)
+    return int(ptr % 16 == 0 and ld * x.element_size() % 16 == 0)
 
 
 def cr_group_norm_workspace_bytes(plan: int, x, groups: int) -> int:
-    return _group_norm_workspace(False, plan, x.shape, groups, _elem(x))
+    """For tensors that all lie in memory as x does (alignment and row stride); a call whose other tensors are less
+    aligned than x says CR_ERR_OOM when it needs more."""
+    return _group_norm_workspace(False, plan, x.shape, groups, _elem(x), _vector_rows(x))
 
 
 def cr_group_norm_backward_workspace_bytes(plan: int, x, groups: int) -> int:
-    return _group_norm_workspace(True, plan, x.shape, groups, _elem(x))
+    """As cr_group_norm_workspace_bytes, for cr_group_norm_backward."""
+    return _group_norm_workspace(True, plan, x.shape, groups, _elem(x), _vector_rows(x))
 
 
 def cr_group_norm(plan: int, x, gamma, beta, groups: int, y, mean=None, rstd=None, eps: float = 1e-5,

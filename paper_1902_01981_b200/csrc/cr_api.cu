@@ -1260,9 +1260,10 @@ cr_status_t cr_dropout(cr_plan_t *plan, const void *x, int64_t ld_x, const void 
     return CR_OK;
 }
 
-size_t cr_group_norm_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc) {
+size_t cr_group_norm_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc, int32_t vector_rows) {
     if (!plan || !good_desc(desc)) return 0;
-    return cr::group_norm_workspace_bytes(desc->samples, desc->positions, desc->channels, desc->groups, desc->elem);
+    const bool vectors = vector_rows && desc->channels % (16 / cr::elem_bytes(desc->elem)) == 0;
+    return cr::group_norm_workspace_bytes(desc->samples, desc->positions, desc->channels, desc->groups, desc->elem, vectors);
 }
 
 cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const void *x, int64_t ld_x, const float *gamma,
@@ -1276,20 +1277,21 @@ cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const vo
     const int64_t rows = desc->samples * desc->positions;
     if (!good_rows(rows, desc->channels, ld_x) || !good_rows(rows, desc->channels, ld_y)) return CR_ERR_INVALID_ARG;
     if (!on_element(x, desc->elem) || !on_element(y, desc->elem)) return CR_ERR_INVALID_ARG;
-    const size_t need = cr_group_norm_workspace_bytes(plan, desc);
-    if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
-    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
     cr::GroupNormArgs a = group_norm_args(*plan, *desc);
     a.x = x; a.ld_x = ld_x; a.y = y; a.ld_y = ld_y; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
     a.workspace = static_cast<float *>(workspace);
+    const size_t need = cr_group_norm_workspace_bytes(plan, desc, cr::group_norm_vector_rows(a));
+    if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
     cudaError_t e = cr::launch_group_norm(a, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
     if (e != cudaSuccess) { note_cuda(e, "cr_group_norm"); return CR_ERR_CUDA; }
     return CR_OK;
 }
 
-size_t cr_group_norm_backward_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc) {
+size_t cr_group_norm_backward_workspace_bytes(const cr_plan_t *plan, const cr_group_norm_t *desc, int32_t vector_rows) {
     if (!plan || !good_desc(desc)) return 0;
-    return cr::group_norm_backward_workspace_bytes(desc->samples, desc->positions, desc->channels, desc->groups, desc->elem);
+    const bool vectors = vector_rows && desc->channels % (16 / cr::elem_bytes(desc->elem)) == 0;
+    return cr::group_norm_backward_workspace_bytes(desc->samples, desc->positions, desc->channels, desc->groups, desc->elem, vectors);
 }
 
 cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc, const void *dy, int64_t ld_dy,
@@ -1311,14 +1313,14 @@ cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc,
         if (!on_element(x, desc->elem) || !on_element(dy, desc->elem) || !on_element(dx, desc->elem)) return CR_ERR_INVALID_ARG;
     }
     if (!dx && !dgamma && !dbeta) return CR_OK;
-    const size_t need = cr_group_norm_backward_workspace_bytes(plan, desc);
-    if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
-    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
     cr::GroupNormArgs a = group_norm_args(*plan, *desc);
     a.x = x; a.ld_x = ld_x; a.dy = dy; a.ld_dy = ld_dy; a.y = dx; a.ld_y = ld_dx; a.gamma = gamma; a.beta = beta;
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
     a.dgamma = dgamma; a.dbeta = dbeta; a.ld_param = ld_param; a.partitions = partitions;
     a.workspace = static_cast<float *>(workspace);
+    const size_t need = cr_group_norm_backward_workspace_bytes(plan, desc, cr::group_norm_vector_rows(a));
+    if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
     cudaError_t e = cr::launch_group_norm_backward(a, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
     if (e != cudaSuccess) { note_cuda(e, "cr_group_norm_backward"); return CR_ERR_CUDA; }
     return CR_OK;

@@ -291,8 +291,8 @@ __device__ __forceinline__ void add_moments(float (&d)[4], uint32_t r0, uint32_t
     }
 }
 
-// Forward.  Sums and squares are taken of x - pivot, the pivot being the mean of the group's very first values, one vector of
-// them (zero where the tensor cores take the sums: 16-bit elements, up to 8 vectors a row): one pass over the vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
+// Forward.  Sums and squares are taken of x - pivot, the pivot being the mean of the group's very first vector (16-bit
+// elements: its first value; zero where the tensor cores take the sums: 16-bit elements, up to 8 vectors a row): one pass over the vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
 // squares have lost digits to it, and the item is summed once more around the mean itself (all CTAs of the cluster see
 // the same numbers and decide alike).
 // UNI: every vector lies inside one group.
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const 
     for (int i = 0; i < kG; ++i) mine_g[i] = (p.col * VEC + i) / s.cg;
     // first values of the thread's groups, and of the group it joins
     const T *firsts = static_cast<const T *>(a.x) + ((int64_t)p.first_sample * s.positions * a.ld_x + p.slab * s.sc);
-    constexpr int kFirst = UNI ? VEC : 1;
+    constexpr int kFirst = UNI && sizeof(T) == 4 ? VEC : 1;   // (16-bit elements hardly come here, and registers are short)
     Packed<T, kFirst> pivots[kG], pivot_g;
     auto pivot_of = [](const Packed<T, kFirst> &first) {
         float f[kFirst], t = 0.f;

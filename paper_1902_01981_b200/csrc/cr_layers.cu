@@ -607,34 +607,27 @@ bool vector_rows(int elem, int64_t channels, std::initializer_list<const void *>
 
 }  // namespace
 
-size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem) {
-    if (samples < 1) return 0;
-    size_t most = 0;
-    for (bool wide : {false, true}) {
-        const int vec = split_vec(wide, elem, channels, groups);
-        if (channels % vec) continue;
-        const Split s = make_split(samples, positions, channels, groups, vec, 1);
-        most = std::max(most, (size_t)s.chunks * groups * s.parts * (size_t)samples * 8);
-    }
-    return most;
+bool group_norm_vector_rows(const GroupNormArgs &a) {
+    return vector_rows(a.elem, a.channels, {a.x, a.dy, a.y}, {a.ld_x, a.dy ? a.ld_dy : 0, a.y ? a.ld_y : 0});
 }
 
-size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem) {
+size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem, bool vectors) {
+    if (samples < 1 || (vectors && group_norm_on_chip(samples, positions, channels, groups, elem))) return 0;
+    const Split s = make_split(samples, positions, channels, groups, split_vec(vectors, elem, channels, groups), 1);
+    return (size_t)s.chunks * groups * s.parts * (size_t)samples * 8;
+}
+
+size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem, bool vectors) {
     if (samples < 1) return 0;
-    size_t most = 0;
-    for (bool wide : {false, true}) {
-        const int vec = split_vec(wide, elem, channels, groups);
-        if (channels % vec) continue;
-        const Split s = make_split(samples, positions, channels, groups, vec, 2);
-        most = std::max(most, (size_t)s.chunks * (channels + (size_t)groups * s.parts) * (size_t)samples * 8);
-    }
-    // the one-pass form's rows of sums
-    return std::max(most, (size_t)group_norm_backward_on_chip(samples, positions, channels, groups, elem) * channels * (size_t)samples * 8);
+    if (const int rows = vectors ? group_norm_backward_on_chip(samples, positions, channels, groups, elem) : 0)
+        return (size_t)rows * channels * (size_t)samples * 8;
+    const Split s = make_split(samples, positions, channels, groups, split_vec(vectors, elem, channels, groups), 2);
+    return (size_t)s.chunks * (channels + (size_t)groups * s.parts) * (size_t)samples * 8;
 }
 
 cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &, cudaStream_t stream, int64_t *launches) {
     if (a.samples == 0) return cudaSuccess;
-    const bool wide = vector_rows(a.elem, a.channels, {a.x, a.y}, {a.ld_x, a.ld_y});
+    const bool wide = group_norm_vector_rows(a);
     if (wide && group_norm_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem)) return launch_group_norm_on_chip(a, stream, launches);
     const int vec = split_vec(wide, a.elem, a.channels, a.groups);
     const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec, 1);
@@ -675,7 +668,7 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         if (e == cudaSuccess) ++*launches;
         return e;
     }
-    const bool wide = vector_rows(a.elem, a.channels, {a.x, a.dy, a.y}, {a.ld_x, a.ld_dy, a.y ? a.ld_y : 0});
+    const bool wide = group_norm_vector_rows(a);
     const bool params = a.dgamma || a.dbeta;
     const size_t plane = (size_t)a.samples * a.channels;
     float *sum1 = a.workspace;

@@ -48,9 +48,11 @@ struct GroupNormArgs {
     int device = 0;
 };
 
-// Workspace in bytes, from the sizes alone.
-size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem);
-size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem);
+// Whether all rows of the tensors are whole 16-byte vectors (dy, y may be null).
+bool group_norm_vector_rows(const GroupNormArgs &a);
+// Workspace in bytes, from the sizes and from whether the rows are such vectors.
+size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem, bool vectors);
+size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem, bool vectors);
 cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 

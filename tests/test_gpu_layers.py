@@ -78,6 +78,12 @@ SHAPES = [
     (1, 20000, 40, 1, 0, 0),       # one group over everything
     (70, 9, 32, 8, 0, 0),
     (1, 70001, 32, 4, 0, 0),       # a sample of several megabytes
+    (3, 130, 88, 11, 0, 0),        # the last slab is narrower than the others
+    (2, 200, 80, 5, 0, 0),         # sixteen channels a group, a slab of 48 and one of 32 (or 16s)
+    (2000, 4, 32, 8, 0, 0),        # more samples than CTAs: each walks over several
+    (300, 260, 64, 8, 0, 0),       # the same in clusters
+    (2, 50, 5000, 1, 0, 0),        # a group wider than a tile
+    (2, 50, 2310, 2, 0, 0),
 ]
 
 
@@ -235,6 +241,24 @@ def test_a_nan_stays_in_its_group_and_statistics_survive_a_large_mean(plan):
     assert np.max(np.abs(f64(mean) - mean64)) <= 2.0 ** -11
     assert np.max(np.abs(f64(rstd) / rstd64 - 1)) <= 1e-5
     assert np.max(np.abs(f64(y) - want)) <= 2.0 ** -10
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape", [(3, 300, 32, 4), (2, 40, 30, 3), (1, 1100, 64, 8)])
+def test_statistics_whatever_comes_first(plan, shape, dtype):
+    """The first values of every group are a hundred standard deviations off, and so is the mean of one sample: one-pass
+    sums around either would lose four of seven digits of the variance."""
+    n, s, c, groups = shape
+    xv, gv, bv, dyv = norm_data((n, s, c), 21)
+    xv[:, 0, :] += 100.0
+    xv[0] += 50.0
+    x, gamma, beta = place(xv, dtype), dev32(gv), dev32(bv)
+    y, mean, rstd = forward(plan, x, gamma, beta, groups, dtype, act=B.CR_ACT_SILU)
+    want, mean64, rstd64, _ = O.group_norm(f64(x), f64(gamma), f64(beta), groups, 1e-5, "silu")
+    # sums of values up to 150, each rounded to 2^-24 of the running sum
+    assert np.max(np.abs(f64(mean) - mean64)) <= 150 * 2e-6
+    assert np.max(np.abs(f64(rstd) / rstd64 - 1)) <= 2e-5
+    check(y, want, dtype, extra=np.max(rstd64) * 150 * 2e-6)
 
 
 def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
@@ -481,7 +505,7 @@ def test_refusals_launch_nothing(plan):
     for kw in (dict(samples=-1), dict(positions=0), dict(channels=0), dict(groups=0), dict(groups=3), dict(elem=3), dict(elem=-1), dict(act=3),
                dict(eps=-1.0), dict(eps=float("nan")), dict(p=-0.1), dict(p=1.1), dict(p=float("nan")), dict(offset=-1)):
         assert lib.cr_group_norm(plan, desc(**kw), p(x), 8, 0, 0, p(y), 8, 0, 0, p(ws), 1 << 20, stream) == bad, kw
-        assert lib.cr_group_norm_workspace_bytes(plan, desc(**kw)) == 0
+        assert lib.cr_group_norm_workspace_bytes(plan, desc(**kw), 1) == 0
         assert lib.cr_group_norm_backward(plan, desc(**kw), p(x), 8, p(x), 8, 0, 0, p(stats), p(stats), p(y), 8, 0, 0, 8, 1, p(ws),
                                           1 << 20, stream) == bad, kw
     d = desc()
@@ -493,8 +517,11 @@ def test_refusals_launch_nothing(plan):
     back = lambda parts, ldp, nbytes, rstd=stats: lib.cr_group_norm_backward(  # noqa: E731
         plan, d, p(x), 8, p(x), 8, 0, 0, p(stats), 0 if rstd is None else p(rstd), p(y), 8, p(params), 0, ldp, parts, p(ws), nbytes, stream)
     assert back(3, 8, 1 << 20) == bad and back(0, 8, 1 << 20) == bad and back(4, 7, 1 << 20) == bad and back(4, 8, 1 << 20, None) == bad
-    need = lib.cr_group_norm_backward_workspace_bytes(plan, d)
+    need = lib.cr_group_norm_backward_workspace_bytes(plan, d, 1)
     assert need and back(4, 8, need - 1) == B.CR_ERR_OOM
+    need = lib.cr_group_norm_workspace_bytes(plan, d, 0)     # rows off their vectors: the streaming form
+    assert need and lib.cr_group_norm(plan, d, p(x) + 4, 8, 0, 0, p(y), 8, 0, 0, p(ws), need - 1, stream) == B.CR_ERR_OOM
+    assert lib.cr_group_norm(plan, d, p(x) + 4, 8, 0, 0, p(y), 8, 0, 0, p(ws) + 4, need, stream) == bad
     drop = lambda ld=8, rows=40, elem=0, pr=0.5, off=0: lib.cr_dropout(plan, p(x), ld, 0, 0, p(y), 8, rows, 8, elem, pr, 1, off, stream)  # noqa: E731
     assert [drop(ld=7), drop(rows=-1), drop(elem=9), drop(pr=2.0), drop(pr=float("nan")), drop(off=-4)] == [bad] * 6
     quant = lambda rows=4, cols=8, ldq=8, elem=0: lib.cr_quantize_rows(plan, p(x), 8, rows, cols, elem, p(codes), ldq, p(one), stream)  # noqa: E731
