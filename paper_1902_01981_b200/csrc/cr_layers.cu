@@ -34,7 +34,7 @@ namespace {
 constexpr int kThreads = 256;
 
 // Blocks of the streaming kernels that an SM holds, by the registers that a thread's channels take (elements of its
-// vector, arrays it reads); the chunks are cut so that one round of blocks covers the tensor.
+// vector, arrays it reads).
 __host__ __device__ constexpr int blocks_per_sm(int vec, int arrays) { return vec < 8 ? 4 : arrays == 1 ? 3 : 2; }
 
 // Which part of the tensor a block of the streaming kernels has: sample, tile of channels, chunk of positions.  A tile
@@ -211,9 +211,9 @@ struct Affine {
 };
 
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 1)) cr_group_norm_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 1)) cr_group_norm_apply_kernel(const GroupNormArgs a, const Split s, const Split own, const float2 *partial) {
     __shared__ float2 ready[kThreads * VEC];     // mean and rstd of the tile's groups
-    const Place p = place<VEC>(s);
+    const Place p = place<VEC>(own);             // `s`: how the partial results were cut
     Affine<VEC> f;
     if (p.j >= 0) f.parameters(p, a.gamma, a.beta);
     // every block joins the chunks of its groups for itself: a warp per group, in one order
@@ -376,9 +376,9 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 2)) cr_group_norm
 }
 
 template <typename T, int VEC, int ACT>
-__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 2)) cr_group_norm_grad_apply_kernel(const GroupNormArgs a, const Split s, const float2 *partial) {
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 2)) cr_group_norm_grad_apply_kernel(const GroupNormArgs a, const Split s, const Split own, const float2 *partial) {
     __shared__ float2 ready[kThreads * VEC];     // m1 and m2 of the tile's groups
-    const Place p = place<VEC>(s);
+    const Place p = place<VEC>(own);             // `s`: how the partial results were cut
     const int lane = threadIdx.x & 31, entries = s.chunks * s.parts;
     const float total = (float)s.positions * (float)s.cg;
     for (int g = threadIdx.x >> 5; g < p.groups; g += kThreads / 32) {
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kThreads) cr_dropout_elements_kernel(const T *
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-Split make_split(int64_t samples, int64_t positions, int channels, int groups, int vec, int arrays) {
+Split make_split(int64_t positions, int channels, int groups, int vec) {
     Split s;
     s.positions = positions;
     s.channels = channels;
@@ -558,15 +558,25 @@ Split make_split(int64_t samples, int64_t positions, int channels, int groups, i
         s.width = most;
         s.tiles = groups * s.parts;
     }
-    // Chunks of at least four rows a thread, one round of blocks on 148 SMs: fewer leave SMs idle (one sample of 52066
-    // positions of 4 channels: 74 us in 6 chunks, 24 so), more spend their time on the joins.
-    const int64_t least = 4ll * (kThreads / std::min(kThreads, s.width / vec));
-    int64_t chunks = std::max<int64_t>(1, 148 * blocks_per_sm(vec, arrays) / std::max<int64_t>(1, samples * s.tiles));
-    chunks = std::min(chunks, std::max<int64_t>(1, positions / least));
+    // Chunks of 32 vectors (64 single elements) a thread, at most one an SM for a sample.  The number of samples must not
+    // count: the chunks set the order of the sums, and a worker that holds a partition alone has to get the bits of the
+    // whole batch.  Forward, us, at 16 / 32 / 64 a thread: 8 samples of 65536 x 64 in vectors 72 / 64 / -, 64 samples of
+    // 1024 x 256 in odd rows 76 / 59 / 49; two samples of 65536 x 64 spend 9.3 / 10.9 / - on the sums.
+    const int64_t least = (vec == 1 ? 64ll : 32ll) * (kThreads / std::min(kThreads, s.width / vec));
+    const int64_t chunks = std::min<int64_t>(148, std::max<int64_t>(1, positions / least));
     s.rows_per_chunk = (positions + chunks - 1) / chunks;
     // a block counts its rows in 32 bits, and a float holds the count of a group without rounding far beyond this
     s.rows_per_chunk = std::min<int64_t>(s.rows_per_chunk, 1 << 24);
     s.chunks = (int)((positions + s.rows_per_chunk - 1) / s.rows_per_chunk);
+    return s;
+}
+// The same tiles in chunks for a pass without sums of its own, whose order does not matter: one round of blocks.
+Split recut(Split s, int64_t samples, int vec, int arrays) {
+    const int64_t least = 4ll * (kThreads / std::min(kThreads, s.width / vec));
+    int64_t chunks = std::max<int64_t>(1, 148 * blocks_per_sm(vec, arrays) / std::max<int64_t>(1, samples * s.tiles));
+    chunks = std::min(chunks, std::max<int64_t>(1, s.positions / least));
+    s.rows_per_chunk = std::min<int64_t>((s.positions + chunks - 1) / chunks, 1 << 24);
+    s.chunks = (int)((s.positions + s.rows_per_chunk - 1) / s.rows_per_chunk);
     return s;
 }
 // Elements of a vector of the streaming kernels: 16 bytes where the rows allow it and no group wider than a tile is cut
@@ -613,7 +623,7 @@ bool group_norm_vector_rows(const GroupNormArgs &a) {
 
 size_t group_norm_workspace_bytes(int64_t samples, int64_t positions, int channels, int groups, int elem, bool vectors) {
     if (samples < 1 || (vectors && group_norm_on_chip(samples, positions, channels, groups, elem))) return 0;
-    const Split s = make_split(samples, positions, channels, groups, split_vec(vectors, elem, channels, groups), 1);
+    const Split s = make_split(positions, channels, groups, split_vec(vectors, elem, channels, groups));
     return (size_t)s.chunks * groups * s.parts * (size_t)samples * 8;
 }
 
@@ -621,7 +631,7 @@ size_t group_norm_backward_workspace_bytes(int64_t samples, int64_t positions, i
     if (samples < 1) return 0;
     if (const int rows = vectors ? group_norm_backward_on_chip(samples, positions, channels, groups, elem) : 0)
         return (size_t)rows * channels * (size_t)samples * 8;
-    const Split s = make_split(samples, positions, channels, groups, split_vec(vectors, elem, channels, groups), 2);
+    const Split s = make_split(positions, channels, groups, split_vec(vectors, elem, channels, groups));
     return (size_t)s.chunks * (channels + (size_t)groups * s.parts) * (size_t)samples * 8;
 }
 
@@ -630,9 +640,10 @@ cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &, cudaSt
     const bool wide = group_norm_vector_rows(a);
     if (wide && group_norm_on_chip(a.samples, a.positions, a.channels, a.groups, a.elem)) return launch_group_norm_on_chip(a, stream, launches);
     const int vec = split_vec(wide, a.elem, a.channels, a.groups);
-    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec, 1);
+    const Split s = make_split(a.positions, a.channels, a.groups, vec);
     float2 *partial = reinterpret_cast<float2 *>(a.workspace);
-    const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
+    const Split own = recut(s, a.samples, vec, 1);
+    const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks), own_blocks = (unsigned)(a.samples * own.tiles * own.chunks);
     auto run = [&](auto t, auto v) {
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value;
@@ -640,7 +651,7 @@ cudaError_t launch_group_norm(const GroupNormArgs &a, const DeviceInfo &, cudaSt
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
         e = by_act(a.act, [&](auto act) {
-            cr_group_norm_apply_kernel<T, VEC, decltype(act)::value><<<blocks, kThreads, 0, stream>>>(a, s, partial);
+            cr_group_norm_apply_kernel<T, VEC, decltype(act)::value><<<own_blocks, kThreads, 0, stream>>>(a, s, own, partial);
             return cudaGetLastError();
         });
         if (e == cudaSuccess) *launches += 2;
@@ -682,10 +693,11 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         return launch_params(a, sum1, sum2, rows, stream, launches);
     }
     const int vec = split_vec(wide, a.elem, a.channels, a.groups);
-    const Split s = make_split(a.samples, a.positions, a.channels, a.groups, vec, 2);
+    const Split s = make_split(a.positions, a.channels, a.groups, vec);
     float *sum2 = sum1 + plane * s.chunks;
     float2 *partial = reinterpret_cast<float2 *>(sum2 + plane * s.chunks);
-    const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks);
+    const Split own = recut(s, a.samples, vec, 2);
+    const unsigned blocks = (unsigned)(a.samples * s.tiles * s.chunks), own_blocks = (unsigned)(a.samples * own.tiles * own.chunks);
     auto run = [&](auto t, auto v, auto act) {
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value, ACT = decltype(act)::value;
@@ -694,7 +706,7 @@ cudaError_t launch_group_norm_backward(const GroupNormArgs &a, const DeviceInfo 
         if (e != cudaSuccess) return e;
         ++*launches;
         if (a.y) {
-            cr_group_norm_grad_apply_kernel<T, VEC, ACT><<<blocks, kThreads, 0, stream>>>(a, s, partial);
+            cr_group_norm_grad_apply_kernel<T, VEC, ACT><<<own_blocks, kThreads, 0, stream>>>(a, s, own, partial);
             e = cudaGetLastError();
             if (e != cudaSuccess) return e;
             ++*launches;

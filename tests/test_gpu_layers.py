@@ -199,15 +199,18 @@ def test_group_norm_gradient_against_differences(plan, shape, act):
         assert abs(slope - want) <= 1e-3 * (abs(want) + size) + 1e-5 * np.sqrt(x.numel())
 
 
-def test_partitions_add_up_and_do_not_see_each_other(plan):
+@pytest.mark.parametrize("shape,dtype", [((12, 40, 64, 8), "bf16"), ((12, 40, 64, 8), "f32"), ((8, 700, 30, 5), "f32"),
+                                         ((8, 700, 30, 5), "f16"), ((4, 9000, 48, 1), "bf16"), ((200, 1030, 64, 8), "f16")])
+def test_partitions_add_up_and_do_not_see_each_other(plan, shape, dtype):
     """Per-partition gradients are what a worker that holds the partition alone computes, bit for bit: the same
-    samples, the index of its first element as offset."""
-    n, s, c, groups, parts = 12, 40, 64, 8, 4
+    samples, the index of its first element as offset.  Items of one CTA, of clusters, and of the streaming form."""
+    n, s, c, groups = shape
+    parts = 4
     xv, gv, bv, dyv = norm_data((n, s, c), 5)
-    x, dy = place(xv, "bf16"), place(dyv, "bf16")
+    x, dy = place(xv, dtype), place(dyv, dtype)
     gamma, beta = dev32(gv), dev32(bv)
     kw = dict(act=B.CR_ACT_SILU, p=0.2, seed=11)
-    y, mean, rstd = forward(plan, x, gamma, beta, groups, "bf16", offset=7, **kw)
+    y, mean, rstd = forward(plan, x, gamma, beta, groups, dtype, offset=7, **kw)
     dx, dg, db = torch.empty_like(x), torch.empty((parts, c), device="cuda"), torch.empty((parts, c), device="cuda")
     ws = scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups))
     B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, dg, db, workspace=ws, offset=7, **kw)
@@ -215,7 +218,7 @@ def test_partitions_add_up_and_do_not_see_each_other(plan):
     for q in range(parts):
         mine = slice(q * per, (q + 1) * per)
         offset = 7 + q * per * s * c
-        y1, mean1, rstd1 = forward(plan, x[mine], gamma, beta, groups, "bf16", offset=offset, **kw)
+        y1, mean1, rstd1 = forward(plan, x[mine], gamma, beta, groups, dtype, offset=offset, **kw)
         assert torch.equal(y1, y[mine]) and torch.equal(mean1, mean[mine]) and torch.equal(rstd1, rstd[mine])
         dx1, dg1, db1 = torch.empty_like(x[mine]), torch.empty((1, c), device="cuda"), torch.empty((1, c), device="cuda")
         B.cr_group_norm_backward(plan, dy[mine], x[mine], gamma, beta, mean1, rstd1, groups, dx1, dg1, db1, workspace=ws,
