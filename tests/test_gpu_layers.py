@@ -486,6 +486,55 @@ def test_int8_product_of_nothing_and_repeats_itself(plan):
         assert torch.equal(part, full[a:b])
 
 
+# ------------------------------------------------------------------------------------------------ beyond 32 bits
+
+def test_dropout_of_more_than_2_to_31_elements(plan):
+    for count in ((1 << 31) + 4096, (1 << 31) + 4097):      # in vectors, and element by element
+        x = torch.empty(count, dtype=torch.float16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+        y = torch.empty_like(x)
+        B.cr_dropout(plan, x, y, 0.25, 77, offset=3)
+        for a in (0, (1 << 31) - 500, count - 1000):
+            factors = O.dropout_factors((1000,), 0.25, 77, 3 + a)
+            got, want = f64(y[a:a + 1000]), f64(x[a:a + 1000]) * factors
+            assert np.array_equal(got == 0, want == 0) and np.all(np.abs(got - want) <= ROUND["f16"] * np.abs(want) + TINY["f16"])
+        del x, y
+
+
+def test_group_norm_of_more_than_2_to_31_elements(plan):
+    n, s, c, groups = 520, 4096, 1024, 32
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.empty((n, s, c), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    dy = torch.empty_like(x).normal_(generator=g)
+    gamma, beta = torch.rand(c, generator=g, device="cuda") + 0.5, torch.rand(c, generator=g, device="cuda")
+    kw = dict(act=B.CR_ACT_SILU, p=0.25, seed=5)
+    y, mean, rstd = torch.empty_like(x), torch.empty((n, groups), device="cuda"), torch.empty((n, groups), device="cuda")
+    B.cr_group_norm(plan, x, gamma, beta, groups, y, mean, rstd, workspace=scratch(B.cr_group_norm_workspace_bytes(plan, x, groups)), **kw)
+    dx, dg, db = torch.empty_like(x), torch.empty((n, c), device="cuda"), torch.empty((n, c), device="cuda")
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, dg, db,
+                             workspace=scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups)), **kw)
+    k = n - 1                                               # the last sample lies beyond 2^31 elements
+    factors = O.dropout_factors((1, s, c), 0.25, 5, k * s * c)
+    want, mean64, _, _ = O.group_norm(f64(x[k:]), f64(gamma), f64(beta), groups, 1e-5, "silu", factors)
+    check(y[k:], want, "bf16")
+    assert np.max(np.abs(f64(mean[k:]) - mean64)) <= 1e-6
+    dx64, dg64, db64, _, ag, ab = O.group_norm_backward(f64(dy[k:]), f64(x[k:]), f64(gamma), f64(beta), groups, 1e-5, "silu", factors)
+    check(dx[k:], dx64, "bf16")
+    assert np.all(np.abs(f64(dg[k:]) - dg64) <= 1e-5 * ag) and np.all(np.abs(f64(db[k:]) - db64) <= 1e-5 * ab)
+
+
+def test_int8_product_of_weights_beyond_2_to_31_bytes(plan):
+    outer, inner = 600000, 4096
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = torch.randint(-127, 128, (outer, inner), generator=g, device="cuda", dtype=torch.int8)
+    for tokens in (2, 300):
+        x = torch.randint(-127, 128, (tokens, inner), generator=g, device="cuda", dtype=torch.int8)
+        y = torch.empty((tokens, outer), device="cuda")
+        B.cr_int8_product(plan, x, torch.ones(tokens, device="cuda"), w, torch.ones(outer, device="cuda"), y)
+        for a in (0, outer - 200):
+            want, _ = O.int8_product(x.cpu().numpy(), w[a:a + 200].cpu().numpy(), np.ones(tokens), np.ones(200))
+            assert np.max(np.abs(f64(y[:, a:a + 200]) - want) / (1 + np.abs(want))) <= 2.0 ** -23
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 
 def test_refusals_launch_nothing(plan):
