@@ -496,16 +496,16 @@ def _row_ptr(t, shape):
     width, st = shape[-1], t.stride()
     if width > 1 and st[-1] != 1:
         raise ValueError("the elements of a row must be next to each other")
-    ld = 0
+    ld = None
     spaced = 1           # rows spanned by the dimensions seen so far, innermost first
     for k in range(len(shape) - 2, -1, -1):
         if shape[k] > 1:
-            if not ld:
-                ld = st[k] // spaced if st[k] % spaced == 0 else -1
-            if st[k] != ld * spaced:
-                raise ValueError("the rows must be equally spaced")
+            if ld is None:
+                ld = st[k] // spaced
+            if ld < width or st[k] != ld * spaced:     # an expanded dimension has stride 0: its rows are one row
+                raise ValueError("the rows must be equally spaced and must not overlap")
         spaced *= shape[k]
-    return t.data_ptr(), ld or width
+    return t.data_ptr(), width if ld is None else ld
 
 
 def _vector_ptr(t, count: int) -> int:

@@ -1,7 +1,7 @@
 // Group norm in one pass: a sample's slab of channels stays on chip between its statistics and its output.
 //
-// The work item is (sample, slab), a slab being neighbouring whole groups, 128 bytes of channels wide where the groups
-// allow it, over all positions.  A cluster of K CTAs holds it in shared memory, each CTA an equal share of the positions,
+// The work item is (sample, slab), a slab being neighbouring whole groups, 64 or 128 bytes of channels wide where the
+// groups allow it, over all positions.  A cluster of K CTAs holds it in shared memory, each CTA an equal share of the positions,
 // each thread up to NV vectors of 16 bytes of one column: x is read once from HBM and y written once, which is the floor
 // of the operation.  The clusters are persistent: each keeps one slab and walks over samples, so that what depends on
 // the channels is set up once, and while it works on one sample the copies of the next are under way.  A thread copies

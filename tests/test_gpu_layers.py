@@ -590,6 +590,9 @@ def test_refusals_launch_nothing(plan):
                  lambda: B.cr_dropout(plan, x.double(), y, 0.5, 1), lambda: B.cr_dropout(plan, x.cpu(), y, 0.5, 1),
                  lambda: B.cr_dropout(plan, x.transpose(0, 1), y.transpose(0, 1), 0.5, 1),
                  lambda: B.cr_dropout(plan, x[..., ::2], y[..., ::2], 0.5, 1),
+                 lambda: B.cr_dropout(plan, x[0, 0].expand(40, 8), y.view(40, 8), 0.5, 1),          # one row, forty times
+                 lambda: B.cr_dropout(plan, x[:1].expand(4, 10, 8), y, 0.5, 1),
+                 lambda: B.cr_group_norm_backward(plan, one[0].expand(4, 10, 8), x, None, None, stats, stats, 2, y, workspace=ws),
                  lambda: B.cr_group_norm(plan, x, one, None, 2, y, workspace=ws),
                  lambda: B.cr_group_norm(plan, x[0], None, None, 2, y[0], workspace=ws),
                  lambda: B.cr_int8_product(plan, x[0], one, q, one, out), lambda: B.cr_int8_product(plan, q[:, :32], one, q, one, out),
