@@ -439,7 +439,7 @@ cr_status_t cr_quantize_rows(cr_plan_t *plan, const void *x, int64_t ld_x, int64
 /* y[t][n] = (sum_k x[t][k] w[n][k]) * (x_scale[t] * w_scale[n]) + bias[n]: x [tokens][inner] and w [outer][inner]
  * codes of 8 bits at row strides ld_x, ld_w (bytes), fp32 scales, bias fp32 [outer] or NULL, y [tokens][outer] of type
  * `elem` at row stride ld_y.  The sum is exact (32-bit integers; 1 <= inner <= 131071 keeps it in range for every
- * code), tokens and outer >= 0.  16-byte aligned x, w and strides that are multiples of 16 enable the tensor-core
+ * code), 0 <= tokens, outer <= 2^31 - 512.  16-byte aligned x, w and strides that are multiples of 16 enable the tensor-core
  * form.  The layer sits on the data: no gradient is taken through it. */
 cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w,
                             int64_t ld_w, const float *w_scale, const float *bias, void *y, int64_t ld_y, int64_t tokens,

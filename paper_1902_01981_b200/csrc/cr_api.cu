@@ -1346,7 +1346,8 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
     if (st != CR_OK) return st;
     // 2^14 * 131071 < 2^31: the largest inner length whose sum stays in 32 bits for every code
     if (tokens < 0 || outer < 0 || inner < 1 || inner > 131071 || !known_elem(elem)) return CR_ERR_INVALID_ARG;
-    if (tokens > 0x7fffffffll || outer > 0x7fffffffll) return CR_ERR_INVALID_ARG;
+    // tiles run up to 255 past the end, counted in 31 bits
+    if (tokens > 0x7ffffe00ll || outer > 0x7ffffe00ll) return CR_ERR_INVALID_ARG;
     if (tokens == 0 || outer == 0) return CR_OK;
     if (!x || !w || !x_scale || !w_scale || !y || !on_element(y, elem)) return CR_ERR_INVALID_ARG;
     if (!good_rows(tokens, inner, ld_x) || !good_rows(outer, inner, ld_w) || !good_rows(tokens, outer, ld_y)) return CR_ERR_INVALID_ARG;

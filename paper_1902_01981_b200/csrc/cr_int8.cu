@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(256) cr_int8_product_bytes_kernel(const Int8Pr
 // tensor memory, so one token needs a tile of 16 columns and not of 128 rows, and a warp that reads a column out holds
 // 32 neighbouring channels of one token, which it stores as they lie in y.
 // Warp 0 streams boxes of 128 bytes of k (128 weight rows, TN token rows, 128-byte swizzle) into a ring; one thread of
-// warp 1 issues four tcgen05.mma (kind::i8, 32 bytes of k each) per box into one of two accumulators; warps 2..5 read
+// warp 1 issues four tcgen05.mma (kind::i8, 32 bytes of k each) per box into one of two accumulators; the others read
 // the other one, scale it and store it.  CTAs are persistent over the tiles.
 // One token through 4096 x 32768 weights, 134 MB: 28.7 us cold (4.7 TB/s); 4096 x 4096: 10 us, the latency of launch, copies
 // and the cluster's two meetings.
@@ -229,6 +229,7 @@ __device__ __forceinline__ void drain(const TcArgs &a, uint32_t taddr, int token
 #pragma unroll 1
     for (int c = 0; c < count; c += 16) {
         int r[16];
+        __syncwarp();
         i8::tmem_load_16(taddr + (uint32_t)c, r);
         float xs[16];
 #pragma unroll

@@ -580,7 +580,7 @@ def test_refusals_launch_nothing(plan):
     assert [quant(rows=-1), quant(cols=0), quant(ldq=7), quant(elem=5)] == [bad] * 4
     prod = lambda k=64, ld=64, elem=0, m=4, sc=one: lib.cr_int8_product(  # noqa: E731
         plan, p(q), ld, p(sc) if sc is not None else 0, p(q), 64, p(one), 0, p(out), 4, m, 4, k, elem, stream)
-    assert [prod(k=0), prod(k=131072), prod(ld=63), prod(elem=3), prod(m=-1), prod(sc=None)] == [bad] * 6
+    assert [prod(k=0), prod(k=131072), prod(ld=63), prod(elem=3), prod(m=-1), prod(sc=None), prod(m=(1 << 31) - 300)] == [bad] * 7
     host = B.cr_plan_create(4, 2, 1, 24, 1024, device=-1)
     assert lib.cr_dropout(host, p(x), 8, 0, 0, p(y), 8, 40, 8, 0, 0.5, 1, 0, stream) == B.CR_ERR_CUDA
     B.cr_plan_destroy(host)
