@@ -296,8 +296,8 @@ __device__ __forceinline__ void add_moments(float (&d)[4], uint32_t r0, uint32_t
 
 // Forward.  Sums and squares are taken of x - pivot, the pivot being the mean of the group's very first vector (16-bit
 // elements: its first value; zero where the tensor cores take the sums: 16-bit elements, up to 8 vectors a row): one pass over the vectors and one exchange.  Where the pivot turns out to lie more than four standard deviations off the mean, the
-// squares have lost digits to it, and the item is summed once more around the mean itself (all CTAs of the cluster see
-// the same numbers and decide alike).
+// squares have lost digits to it, and where their sum has left the range of a float they have lost everything: the item is
+// then summed once more around the mean itself (all CTAs of the cluster see the same numbers and decide alike).
 // UNI: every vector lies inside one group.
 template <typename T, int NV, bool UNI, int ACT>
 __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const GroupNormArgs a, const Slab s) {
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const 
                     squares = all.y;
                 }
                 const float off = total * inv_all, m2 = fmaxf(fmaf(-total, off, squares), 0.f);
-                if (pass == 0 && m2 * 16.f < squares) mem.again[ex.turn & 1] = 1;
+                if (pass == 0 && (m2 * 16.f < squares || isinf(squares))) mem.again[ex.turn & 1] = 1;
                 const float mean = pivot + off, rstd = 1.f / sqrtf(fmaf(m2, inv_all, a.eps));
                 pivot = mean;
                 mem.ready[0][g] = mean;

@@ -264,6 +264,22 @@ def test_statistics_whatever_comes_first(plan, shape, dtype):
     check(y, want, dtype, extra=np.max(rstd64) * 150 * 2e-6)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_values_with_a_small_spread(plan, dtype):
+    """1e18 with a spread of 2 %: the squares of 8192 values leave the range of a float, those around the mean do not.
+    The second sample starts with a row of zeros, so that no value of its first row is near the mean."""
+    n, s, c, groups = 2, 256, 64, 2
+    xv = 1e18 * (1 + 0.02 * np.random.default_rng(31).standard_normal((n, s, c)))
+    xv[1, 0] = 0.0
+    x = place(xv, dtype)
+    y, mean, rstd = forward(plan, x, None, None, groups, dtype)
+    want, mean64, rstd64, _ = O.group_norm(f64(x), None, None, groups, 1e-5)
+    # as below: sums of values up to 1.1e18, each rounded to 2^-24 of the running sum
+    assert np.max(np.abs(f64(mean) - mean64)) <= 1.1e18 * 2e-6
+    assert np.max(np.abs(f64(rstd) / rstd64 - 1)) <= 2e-5
+    check(y, want, dtype, extra=np.max(rstd64) * 1.1e18 * 2e-6)
+
+
 def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
     xv, gv, bv, dyv = norm_data((6, 300, 64), 9)
     gamma, beta = dev32(gv), dev32(bv)
