@@ -30,6 +30,9 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
+// A difference that cannot be negative but for rounding.  A NaN stays one (a maximum with zero would hide it).
+__device__ __forceinline__ float not_below_zero(float v) { return v < 0.f ? 0.f : v; }
+
 // Ordinary accesses, which the compiler may move past one another: an output may be the input's own buffer, so nothing
 // goes through the read-only path.
 template <typename T, int VEC>

@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const 
                     total = all.x;
                     squares = all.y;
                 }
-                const float off = total * inv_all, m2 = fmaxf(fmaf(-total, off, squares), 0.f);
+                const float off = total * inv_all, m2 = not_below_zero(fmaf(-total, off, squares));
                 if (pass == 0 && (m2 * 16.f < squares || isinf(squares))) mem.again[ex.turn & 1] = 1;
                 const float mean = pivot + off, rstd = 1.f / sqrtf(fmaf(m2, inv_all, a.eps));
                 pivot = mean;

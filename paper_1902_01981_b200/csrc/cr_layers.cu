@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 1)) cr_group_norm
     const float rows = (float)p.rows, inv = 1.f / rows;
     for (int c = threadIdx.x; c < p.width; c += kThreads) {
         const float t1 = sm[c];
-        sm[kPlane + c] = fmaxf(sm[kPlane + c] - t1 * t1 * inv, 0.f);
+        sm[kPlane + c] = not_below_zero(sm[kPlane + c] - t1 * t1 * inv);
         sm[c] = to_float(x[(p.n * s.positions + p.row0) * ld + p.c_start + c]) + t1 * inv;
     }
     __syncthreads();

@@ -280,6 +280,37 @@ def test_large_values_with_a_small_spread(plan, dtype):
     check(y, want, dtype, extra=np.max(rstd64) * 1.1e18 * 2e-6)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape,shift", [((3, 100, 32, 4), 0), ((3, 100, 32, 4), 1), ((3, 700, 64, 4), 0), ((2, 9000, 32, 4), 0),
+                                         ((3, 40, 24, 8), 0)])
+def test_nan_and_infinities_reach_the_statistics(plan, shape, shift, dtype):
+    """A group that holds one has no finite mean, rstd, output or gradient; the others are as without it."""
+    n, s, c, groups = shape
+    xv, gv, bv, dyv = norm_data((n, s, c), 6)
+    inf = float("inf")
+    dead = np.zeros((n, groups), bool)
+    for i, j, k, v in ((0, 0, 0, float("nan")), (0, s - 1, c - 1, inf), (1, s // 2, c // groups, -inf), (1, 0, c - 1, inf), (1, 1, c - 1, -inf)):
+        xv[i, j, k] = v
+        dead[i, k * groups // c] = True
+    x, dy, gamma, beta = place(xv, dtype, 0, shift), place(dyv, dtype, 0, shift), dev32(gv), dev32(bv)
+    y, mean, rstd = forward(plan, x, gamma, beta, groups, dtype, shift=shift, act=B.CR_ACT_SILU)
+    assert np.array_equal(np.isnan(f64(rstd)), dead) and np.array_equal(~np.isfinite(f64(mean)), dead)
+    gone = np.repeat(dead, c // groups, axis=1)
+    every = np.broadcast_to(gone[:, None, :], (n, s, c))
+    assert np.isnan(f64(y)[every]).all()
+    finite = np.where(np.isfinite(f64(x)), f64(x), 0.0)
+    want, mean64, rstd64, _ = O.group_norm(finite, f64(gamma), f64(beta), groups, 1e-5, "silu")
+    check(torch.from_numpy(np.where(every, 0, f64(y))), np.where(every, 0, want), dtype)
+    check(torch.from_numpy(np.where(dead, 0, f64(rstd))), np.where(dead, 0, rstd64), "f32")
+    dx, dg, db = place(np.zeros(xv.shape), dtype, 0, shift), torch.empty((n, c), device="cuda"), torch.empty((n, c), device="cuda")
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, dg, db, act=B.CR_ACT_SILU,
+                             workspace=scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups)))
+    assert np.isnan(f64(dx)[every]).all() and np.isnan(f64(dg)[gone]).all() and np.isnan(f64(db)[gone]).all()
+    dx64, dg64, db64, _, ag, ab = O.group_norm_backward(f64(dy), finite, f64(gamma), f64(beta), groups, 1e-5, "silu", None, n)
+    check(torch.from_numpy(np.where(every, 0, f64(dx))), np.where(every, 0, dx64), dtype)
+    assert np.all(np.abs(f64(dg) - dg64)[~gone] <= 1e-5 * ag[~gone]) and np.all(np.abs(f64(db) - db64)[~gone] <= 1e-5 * ab[~gone])
+
+
 def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
     xv, gv, bv, dyv = norm_data((6, 300, 64), 9)
     gamma, beta = dev32(gv), dev32(bv)
