@@ -142,18 +142,23 @@ __device__ __forceinline__ float warp_sum(float v) {
 // ---- forward, streaming: mean and centred square sum of each group over a chunk -------------------------------------
 //
 // Sums are taken of x - k, k the channel's value in the chunk's first row: the squares then carry the spread and not the
-// mean.  Channels, chunks and pieces are joined by mean and centred square sum.  This form serves what the one-pass form
-// does not take: odd rows, and items beyond a cluster's shared memory, whose second read comes from L2 where the tensor
-// fits it.  Two samples of 65536 x 64 f16 (floor 5.2 us): 11 us here and 13 us in the apply pass.
+// mean.  Where that value lies more than eight standard deviations off the channel's mean over the chunk (first rows of
+// zeros, say), the squares have lost digits to it, or their sum has left the range of a float, and the block walks its
+// chunk once more around the means: what is lost otherwise stays below 64 x 2^-24 of the variance, and ordinary data, whose
+// values do not lie that far out, are walked once.  Channels, chunks and pieces are joined by mean and centred square sum.
+// This form serves what the one-pass form does not take: odd rows, and items beyond a cluster's shared memory, whose
+// second read comes from L2 where the tensor fits it.  Two samples of 65536 x 64 f16 (floor 5.2 us): 11 us here and 13 us
+// in the apply pass.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 1)) cr_group_norm_stats_kernel(const T *x, int64_t ld, const Split s, float2 *partial) {
     __shared__ float sm[2 * kThreads * VEC];
+    __shared__ float around[kThreads * VEC];     // the channels' means, where the chunk is walked again
     constexpr int kPlane = kThreads * VEC;
     const Place p = place<VEC>(s);
     const T *first = x + ((p.n * s.positions + p.row0) * ld + p.c0);
-    if (p.j >= 0) {
-        float k[VEC], s1[VEC], s2[VEC];
-        unpack<T, VEC>(load_packed<T, VEC>(first), k);
+    // The sums around k, by channel, in `sm`.
+    auto sums_around = [&](const float (&k)[VEC]) {
+        float s1[VEC], s2[VEC];
         const T *src = first + p.j * ld;
         const int64_t step = (int64_t)p.rt * ld;
 #pragma unroll
@@ -174,15 +179,38 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(VEC, 1)) cr_group_norm
             sm[at] = s1[i];
             sm[kPlane + at] = s2[i];
         }
+    };
+    if (p.j >= 0) {
+        float k[VEC];
+        unpack<T, VEC>(load_packed<T, VEC>(first), k);
+        sums_around(k);
     }
     fold_rows(sm, kPlane, p.width, p.rt);
     const float rows = (float)p.rows, inv = 1.f / rows;
+    bool far = false;
     for (int c = threadIdx.x; c < p.width; c += kThreads) {
-        const float t1 = sm[c];
-        sm[kPlane + c] = not_below_zero(sm[kPlane + c] - t1 * t1 * inv);
-        sm[c] = to_float(x[(p.n * s.positions + p.row0) * ld + p.c_start + c]) + t1 * inv;
+        const float t1 = sm[c], t2 = sm[kPlane + c], off = t1 * inv, m2 = not_below_zero(fmaf(-t1, off, t2));
+        far = far || m2 * 64.f < t2 || isinf(t2);
+        sm[kPlane + c] = m2;
+        sm[c] = to_float(x[(p.n * s.positions + p.row0) * ld + p.c_start + c]) + off;
     }
-    __syncthreads();
+    if (__syncthreads_or(far)) {
+        float k[VEC];
+        if (p.j >= 0) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) k[i] = sm[p.col * VEC + i];
+        }
+        for (int c = threadIdx.x; c < p.width; c += kThreads) around[c] = sm[c];
+        __syncthreads();
+        if (p.j >= 0) sums_around(k);
+        fold_rows(sm, kPlane, p.width, p.rt);
+        for (int c = threadIdx.x; c < p.width; c += kThreads) {
+            const float t1 = sm[c], off = t1 * inv;
+            sm[kPlane + c] = not_below_zero(fmaf(-t1, off, sm[kPlane + c]));
+            sm[c] = around[c] + off;
+        }
+        __syncthreads();
+    }
     const int lane = threadIdx.x & 31, per = p.width / p.groups;
     for (int g = threadIdx.x >> 5; g < p.groups; g += kThreads / 32) {
         float sum = 0.f, m2 = 0.f;

@@ -311,6 +311,36 @@ def test_nan_and_infinities_reach_the_statistics(plan, shape, shift, dtype):
     assert np.all(np.abs(f64(dg) - dg64)[~gone] <= 1e-5 * ag[~gone]) and np.all(np.abs(f64(db) - db64)[~gone] <= 1e-5 * ab[~gone])
 
 
+@pytest.mark.parametrize("far", [100.0, 300.0, 1000.0])
+@pytest.mark.parametrize("shape", [(1, 16384, 1, 1), (1, 65536, 4, 1), (1, 70001, 3, 1), (2, 3000, 30, 3)])
+def test_streaming_statistics_whatever_comes_first(plan, shape, far):
+    """The first row far off, in front of hundreds to thousands of rows that are summed around it."""
+    n, s, c, groups = shape
+    xv = np.random.default_rng(22).standard_normal((n, s, c))
+    xv[:, 0, :] += far
+    x = place(xv, "f32")
+    y, mean, rstd = forward(plan, x, None, None, groups, "f32")
+    want, mean64, rstd64, _ = O.group_norm(f64(x), None, None, groups, 1e-5)
+    # sums of values up to far + 5, each rounded to 2^-24 of the running sum
+    assert np.max(np.abs(f64(mean) - mean64)) <= (far + 5) * 2e-6
+    assert np.max(np.abs(f64(rstd) / rstd64 - 1)) <= 2e-5
+    check(y, want, "f32", extra=np.max(rstd64) * (far + 5) * 2e-6)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_values_with_a_small_spread_in_odd_rows(plan, dtype):
+    """As test_large_values_with_a_small_spread, in the streaming form: a first row of zeros before values of 1e18."""
+    n, s, c, groups = 2, 256, 64, 2
+    xv = 1e18 * (1 + 0.02 * np.random.default_rng(31).standard_normal((n, s, c)))
+    xv[1, 0] = 0.0
+    x = place(xv, dtype, 0, 1)
+    y, mean, rstd = forward(plan, x, None, None, groups, dtype, shift=1)
+    want, mean64, rstd64, _ = O.group_norm(f64(x), None, None, groups, 1e-5)
+    assert np.max(np.abs(f64(mean) - mean64)) <= 1.1e18 * 2e-6
+    assert np.max(np.abs(f64(rstd) / rstd64 - 1)) <= 2e-5
+    check(y, want, dtype, extra=np.max(rstd64) * 1.1e18 * 2e-6)
+
+
 def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
     xv, gv, bv, dyv = norm_data((6, 300, 64), 9)
     gamma, beta = dev32(gv), dev32(bv)
