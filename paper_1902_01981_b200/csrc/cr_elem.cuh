@@ -246,15 +246,16 @@ __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == kActSilu) return z * sigmoid(z);
     return z;
 }
-// Derivative of the activation at z.
+// dy times the derivative of the activation at z.  Where relu is off the gradient is selected away, not multiplied by zero:
+// an infinity or a NaN in dy there leaves a zero.
 template <int ACT>
-__device__ __forceinline__ float act_slope(float z) {
-    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : 0.f;
+__device__ __forceinline__ float act_gradient(float dy, float z) {
+    if constexpr (ACT == kActRelu) return z > 0.f ? dy : 0.f;
     if constexpr (ACT == kActSilu) {
         const float s = sigmoid(z);
-        return s * fmaf(z, 1.f - s, 1.f);
+        return dy * (s * fmaf(z, 1.f - s, 1.f));
     }
-    return 1.f;
+    return dy;
 }
 
 }  // namespace cr

@@ -325,7 +325,7 @@ __device__ __forceinline__ void slopes(const GroupNormArgs &a, const Affine<VEC>
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
         xh[i] = f.xhat(xh[i], i);
-        if constexpr (ACT != kActNone) dz[i] *= act_slope<ACT>(f.z(xh[i], i));
+        if constexpr (ACT != kActNone) dz[i] = act_gradient<ACT>(dz[i], f.z(xh[i], i));
     }
 }
 

@@ -341,6 +341,30 @@ def test_large_values_with_a_small_spread_in_odd_rows(plan, dtype):
     check(y, want, dtype, extra=np.max(rstd64) * 1.1e18 * 2e-6)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape,shift", [((4, 50, 64, 8), 0), ((4, 50, 64, 8), 1), ((2, 9000, 32, 4), 0), ((4, 50, 30, 5), 0)])
+def test_gradients_from_above_where_relu_is_off_do_not_count(plan, shape, shift, dtype):
+    """Infinities and NaN there give the very gradients that zeros give."""
+    n, s, c, groups = shape
+    xv, gv, bv, dyv = norm_data((n, s, c), 41)
+    x, gamma, beta = place(xv, dtype, 0, shift), dev32(gv), dev32(bv)
+    _, mean, rstd = forward(plan, x, gamma, beta, groups, dtype, shift=shift, act=B.CR_ACT_RELU)
+    z = O.group_norm(f64(x), f64(gamma), f64(beta), groups, 1e-5)[3]
+    off = np.argwhere(z < -0.5)
+    off = off[:: max(1, len(off) // 7)]
+    out = []
+    for values in ([0.0], [float("inf"), float("-inf"), float("nan")]):
+        for k, at in enumerate(off):
+            dyv[tuple(at)] = values[k % len(values)]
+        dy, dx = place(dyv, dtype, 0, shift), place(np.zeros(xv.shape), dtype, 0, shift)
+        dg, db = torch.empty((n, c), device="cuda"), torch.empty((n, c), device="cuda")
+        B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, dg, db, act=B.CR_ACT_RELU,
+                                 workspace=scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups)))
+        out.append((dx, dg, db))
+    for zeros, others in zip(*out):
+        assert torch.isfinite(others).all() and torch.equal(zeros, others)
+
+
 def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
     xv, gv, bv, dyv = norm_data((6, 300, 64), 9)
     gamma, beta = dev32(gv), dev32(bv)
