@@ -440,7 +440,8 @@ cr_status_t cr_quantize_rows(cr_plan_t *plan, const void *x, int64_t ld_x, int64
  * codes of 8 bits at row strides ld_x, ld_w (bytes), fp32 scales, bias fp32 [outer] or NULL, y [tokens][outer] of type
  * `elem` at row stride ld_y.  The sum is exact (32-bit integers; 1 <= inner <= 131071 keeps it in range for every
  * code), 0 <= tokens, outer <= 2^31 - 512.  16-byte aligned x, w and strides that are multiples of 16 enable the tensor-core
- * form.  The layer sits on the data: no gradient is taken through it. */
+ * form (the stride of a single token or a single channel does not count).  The layer sits on the data: no gradient is taken
+ * through it. */
 cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w,
                             int64_t ld_w, const float *w_scale, const float *bias, void *y, int64_t ld_y, int64_t tokens,
                             int64_t outer, int64_t inner, int32_t elem, void *stream);

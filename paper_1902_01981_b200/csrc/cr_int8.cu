@@ -510,9 +510,12 @@ cr_int8_product_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __g
     if (warp == 1) tmem_free_pair(tmem, 2 * TN);
 }
 
+// Whether rows of codes start on 16-byte boundaries; one row by itself has no stride to ask for.
+bool rows_on_16(const void *p, int64_t rows, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows == 1 || ld % 16 == 0); }
+
 CUresult encode_codes(EncodeTiledFn encode, CUtensorMap *map, const void *base, int64_t cols, int64_t rows, int64_t ld, int box_rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint64_t strides[1] = {(cuuint64_t)(rows == 1 ? (cols + 15) / 16 * 16 : ld)};
     const cuuint32_t box[2] = {kChunk, (cuuint32_t)box_rows}, estr[2] = {1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -618,8 +621,8 @@ cudaError_t launch_quantize_rows(const void *x, int64_t rows, int64_t cols, int6
     return by_type(elem, [&](auto t) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T);
-        const bool wide = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ld_x % VEC == 0 && (reinterpret_cast<uintptr_t>(q) & (VEC - 1)) == 0 &&
-                          ld_q % VEC == 0;
+        const bool wide = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (reinterpret_cast<uintptr_t>(q) & (VEC - 1)) == 0 &&
+                          (rows == 1 || (ld_x % VEC == 0 && ld_q % VEC == 0));
         const int64_t nvec = wide ? (cols + VEC - 1) / VEC : cols;
         const int threads = (int)std::min<int64_t>(512, std::max<int64_t>(32, (nvec + 127) / 128 * 32));   // about four vectors a thread
         if (wide) cr_quantize_rows_kernel<T, VEC><<<(unsigned)rows, threads, 0, stream>>>(static_cast<const T *>(x), cols, ld_x, q, ld_q, scale);
@@ -633,8 +636,7 @@ cudaError_t launch_quantize_rows(const void *x, int64_t rows, int64_t cols, int6
 cudaError_t launch_int8_product(const Int8ProductArgs &a, int *status, const DeviceInfo &dev, const Tuning &tune, EncodeTiledFn encode,
                                 cudaStream_t stream, int64_t *launches) {
     if (a.tokens == 0 || a.outer == 0) return cudaSuccess;
-    auto on16 = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 16 == 0; };
-    if (encode && on16(a.x, a.ld_x) && on16(a.w, a.ld_w)) {
+    if (encode && rows_on_16(a.x, a.tokens, a.ld_x) && rows_on_16(a.w, a.outer, a.ld_w)) {
         return by_type(a.elem, [&](auto t) {
             using T = decltype(t);
             if (a.tokens <= 16) return launch_tc<T, 16>(a, status, dev, tune, encode, stream, launches);

@@ -557,6 +557,48 @@ def test_int8_product(plan, tokens, inner, outer, elem):
         assert np.all(np.abs(got - want) <= 4 * 2.0 ** -24 * size + ROUND[elem] * 1.01 * np.abs(want) + TINY[elem])
 
 
+def kernels_of(call):
+    """Names of the kernels that `call` launches, from a graph that captures it."""
+    from cuda.bindings import driver
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    raw = driver.CUgraph(graph.raw_cuda_graph())
+    _, _, count = driver.cuGraphGetNodes(raw, 0)
+    _, nodes, _ = driver.cuGraphGetNodes(raw, count)
+    names = []
+    for node in nodes[:count]:
+        err, params = driver.cuGraphKernelNodeGetParams(node)
+        assert err == driver.CUresult.CUDA_SUCCESS
+        err, name = driver.cuFuncGetName(params.func)
+        assert err == driver.CUresult.CUDA_SUCCESS
+        names.append(name.decode())
+    return names
+
+
+@pytest.mark.parametrize("tokens,inner,outer", [(1, 5004, 1001), (1, 77, 130), (1, 77, 1), (5, 77, 1), (300, 1000, 1)])
+def test_one_row_of_codes_takes_the_tensor_cores(plan, tokens, inner, outer):
+    """torch calls a view of one row contiguous and its stride is lost; it does not count."""
+    rng = np.random.default_rng(tokens + inner)
+    up = (inner + 15) // 16 * 16
+    values = rng.standard_normal((tokens, inner))
+    xf = place(values, "bf16", (inner + 7) // 8 * 8 - inner)
+    q, scale = strided_codes(np.full((tokens, inner), 55), up), torch.empty(tokens, device="cuda")
+    names = kernels_of(lambda: B.cr_quantize_rows(plan, xf, q, scale))
+    assert len(names) == 1 and "cr_quantize_rows_kernel" in names[0] and "Li8E" in names[0]
+    codes, want_scale = O.quantize_rows(f64(xf))
+    assert np.array_equal(q.cpu().numpy().astype(np.int64), codes) and np.array_equal(scale.cpu().numpy(), want_scale)
+    wc = rng.integers(-128, 128, (outer, inner))
+    w, ws = strided_codes(wc, up), np.exp(rng.standard_normal(outer)).astype(np.float32) / 900
+    y, ws_dev = torch.empty((tokens, outer), device="cuda"), dev32(ws)
+    names = kernels_of(lambda: B.cr_int8_product(plan, q, scale, w, ws_dev, y))
+    assert len(names) == 1 and "cr_int8_product_kernel" in names[0]
+    want, sums = O.int8_product(codes, wc, want_scale, ws)
+    assert np.all(np.abs(f64(y) - want) <= 4 * 2.0 ** -24 * np.abs(want) + 2.0 ** -23 * np.abs(want))
+
+
 def test_int8_product_longest_sum_and_nan_scales(plan):
     inner = 131071
     x = torch.full((2, 131072), -128, dtype=torch.int8, device="cuda")[:, :inner]
