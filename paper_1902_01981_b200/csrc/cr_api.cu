@@ -1217,6 +1217,9 @@ bool known_elem(int32_t elem) { return elem == CR_ELEM_F32 || elem == CR_ELEM_BF
 bool on_element(const void *p, int32_t elem) {
     return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(cr::elem_bytes(elem) - 1)) == 0;
 }
+// fp32 operands (parameters, statistics, scales); null is on every boundary.
+template <typename... P>
+bool on_float(const P *...p) { return ((... | reinterpret_cast<uintptr_t>(p)) & 3u) == 0; }
 // Row strides up to 2^40 elements and extents up to 2^46 elements keep every offset in 64 bits.
 bool good_rows(int64_t rows, int64_t cols, int64_t ld) {
     return ld >= cols && ld <= (1ll << 40) && (rows == 0 || ld == 0 || rows <= (1ll << 46) / ld);
@@ -1276,7 +1279,7 @@ cr_status_t cr_group_norm(cr_plan_t *plan, const cr_group_norm_t *desc, const vo
     if (!x || !y || desc->positions > (1ll << 46) / desc->samples) return CR_ERR_INVALID_ARG;
     const int64_t rows = desc->samples * desc->positions;
     if (!good_rows(rows, desc->channels, ld_x) || !good_rows(rows, desc->channels, ld_y)) return CR_ERR_INVALID_ARG;
-    if (!on_element(x, desc->elem) || !on_element(y, desc->elem)) return CR_ERR_INVALID_ARG;
+    if (!on_element(x, desc->elem) || !on_element(y, desc->elem) || !on_float(gamma, beta, mean, rstd)) return CR_ERR_INVALID_ARG;
     cr::GroupNormArgs a = group_norm_args(*plan, *desc);
     a.x = x; a.ld_x = ld_x; a.y = y; a.ld_y = ld_y; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
     a.workspace = static_cast<float *>(workspace);
@@ -1305,6 +1308,7 @@ cr_status_t cr_group_norm_backward(cr_plan_t *plan, const cr_group_norm_t *desc,
     if ((dgamma || dbeta) && (!good_rows(partitions, desc->channels, ld_param) ||
                               partitions > 0x7fffffffll / ((desc->channels + 31) / 32)))
         return CR_ERR_INVALID_ARG;
+    if (!on_float(gamma, beta, mean, rstd, dgamma, dbeta)) return CR_ERR_INVALID_ARG;
     if (desc->samples > 0) {
         if (!dy || !x || !mean || !rstd || desc->positions > (1ll << 46) / desc->samples) return CR_ERR_INVALID_ARG;
         const int64_t rows = desc->samples * desc->positions;
@@ -1332,7 +1336,7 @@ cr_status_t cr_quantize_rows(cr_plan_t *plan, const void *x, int64_t ld_x, int64
     if (st != CR_OK) return st;
     if (rows < 0 || rows > 0x7fffffffll || cols < 1 || !known_elem(elem)) return CR_ERR_INVALID_ARG;
     if (rows == 0) return CR_OK;
-    if (!x || !q || !scale || !good_rows(rows, cols, ld_x) || !good_rows(rows, cols, ld_q) || !on_element(x, elem)) return CR_ERR_INVALID_ARG;
+    if (!x || !q || !scale || !good_rows(rows, cols, ld_x) || !good_rows(rows, cols, ld_q) || !on_element(x, elem) || !on_float(scale)) return CR_ERR_INVALID_ARG;
     cudaError_t e = cr::launch_quantize_rows(x, rows, cols, ld_x, elem, q, ld_q, scale, plan->dev,
                                              reinterpret_cast<cudaStream_t>(stream), &plan->launches);
     if (e != cudaSuccess) { note_cuda(e, "cr_quantize_rows"); return CR_ERR_CUDA; }
@@ -1349,7 +1353,7 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
     // tiles run up to 255 past the end, counted in 31 bits
     if (tokens > 0x7ffffe00ll || outer > 0x7ffffe00ll) return CR_ERR_INVALID_ARG;
     if (tokens == 0 || outer == 0) return CR_OK;
-    if (!x || !w || !x_scale || !w_scale || !y || !on_element(y, elem)) return CR_ERR_INVALID_ARG;
+    if (!x || !w || !x_scale || !w_scale || !y || !on_element(y, elem) || !on_float(x_scale, w_scale, bias)) return CR_ERR_INVALID_ARG;
     if (!good_rows(tokens, inner, ld_x) || !good_rows(outer, inner, ld_w) || !good_rows(tokens, outer, ld_y)) return CR_ERR_INVALID_ARG;
     cr::Int8ProductArgs a;
     a.x = x; a.ld_x = ld_x; a.x_scale = x_scale; a.w = w; a.ld_w = ld_w; a.w_scale = w_scale; a.bias = bias;

@@ -743,3 +743,29 @@ def test_refusals_launch_nothing(plan):
         with pytest.raises(ValueError):
             call()
     assert B.cr_plan_launch_count(plan) == before
+
+
+def test_fp32_operands_off_their_elements_are_refused(plan):
+    x = torch.zeros(4, 10, 8, device="cuda")
+    y, stats, params = torch.empty_like(x), torch.zeros((4, 2), device="cuda"), torch.zeros((5, 8), device="cuda")
+    codes, one, out, ws = torch.zeros((4, 64), dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda"), torch.empty((4, 4), device="cuda"), scratch(1 << 20)
+    lib, before, bad = B.lib(), B.cr_plan_launch_count(plan), B.CR_ERR_INVALID_ARG
+    p = lambda t: t.data_ptr()  # noqa: E731
+    stream = torch.cuda.current_stream().cuda_stream
+    desc = B.cr_group_norm_t(4, 10, 8, 2, B.CR_ELEM_F32, 0, 1e-5, 0.0, 0, 0)
+    for off in (1, 2, 3):
+        for k in range(4):      # gamma, beta, mean, rstd
+            a = [p(one) if k < 2 else 0, p(one) if k < 2 else 0, p(stats), p(stats)]
+            a[k] += off
+            assert lib.cr_group_norm(plan, desc, p(x), 8, a[0], a[1], p(y), 8, a[2], a[3], p(ws), 1 << 20, stream) == bad
+        for k in range(6):      # gamma, beta, mean, rstd, dgamma, dbeta
+            a = [p(one), p(one), p(stats), p(stats), p(params), p(params)]
+            a[k] += off
+            assert lib.cr_group_norm_backward(plan, desc, p(x), 8, p(x), 8, a[0], a[1], a[2], a[3], p(y), 8, a[4], a[5], 8, 4, p(ws),
+                                              1 << 20, stream) == bad
+        assert lib.cr_quantize_rows(plan, p(x), 8, 4, 8, B.CR_ELEM_F32, p(codes), 16, p(one) + off, stream) == bad
+        for k in range(3):      # x_scale, w_scale, bias
+            a = [p(one), p(one), p(one)]
+            a[k] += off
+            assert lib.cr_int8_product(plan, p(codes), 64, a[0], p(codes), 64, a[1], a[2], p(out), 4, 4, 4, 64, B.CR_ELEM_F32, stream) == bad
+    assert B.cr_plan_launch_count(plan) == before
