@@ -517,6 +517,12 @@ def _vector_ptr(t, count: int) -> int:
     return t.data_ptr()
 
 
+def _generator_numbers(seed: int, offset: int) -> None:
+    """Refuses what the 64-bit arguments would cut off in silence (a negative seed is its two's complement)."""
+    if not (-(1 << 63) <= seed < 1 << 64 and -(1 << 63) <= offset < 1 << 63):
+        raise ValueError("seed and offset are numbers of 64 bits")
+
+
 def cr_dropout(plan: int, x, y, p: float, seed: int, offset: int = 0, residual=None, stream=None) -> None:
     """y = residual + dropout(x) for row-major tensors of one shape; the mask depends on (seed, offset + index of the
     element) only.  The backward pass is the same call on dy."""
@@ -526,15 +532,26 @@ def cr_dropout(plan: int, x, y, p: float, seed: int, offset: int = 0, residual=N
     rp, ldr = (0, 0) if residual is None else _row_ptr(residual, shape)
     if y.dtype != x.dtype or (residual is not None and residual.dtype != x.dtype):
         raise ValueError("x, residual and y must have one element type")
+    _generator_numbers(seed, offset)
     cols = shape[-1] if len(shape) else 1
     _check(lib().cr_dropout(plan, xp, ldx, rp, ldr, yp, ldy, x.numel() // cols if cols else 0, cols, e, p,
                             seed, offset, _stream_ptr(stream)), "cr_dropout")
 
 
-def _group_norm_desc(x, groups, eps, act, p, seed, offset):
+def _group_norm_sizes(x, groups: int):
+    """Shape of x; refuses numbers that the descriptor's 32-bit fields would cut off in silence."""
     if x.dim() != 3:
         raise ValueError("expected [samples, positions, channels]")
-    n, s, c = x.shape
+    if x.shape[2] >= 1 << 31 or not -(1 << 31) <= groups < 1 << 31:
+        raise ValueError("channels and groups are numbers of 32 bits")
+    return x.shape
+
+
+def _group_norm_desc(x, groups, eps, act, p, seed, offset):
+    n, s, c = _group_norm_sizes(x, groups)
+    _generator_numbers(seed, offset)
+    if not -(1 << 31) <= act < 1 << 31:
+        raise ValueError("act is one of CR_ACT_NONE, CR_ACT_RELU and CR_ACT_SILU")
     return cr_group_norm_t(n, s, c, groups, _elem(x), act, eps, p, seed, offset)
 
 
@@ -553,12 +570,12 @@ def _vector_rows(x) -> int:
 def cr_group_norm_workspace_bytes(plan: int, x, groups: int) -> int:
     """For tensors that all lie in memory as x does (alignment and row stride); a call whose other tensors are less
     aligned than x says CR_ERR_OOM when it needs more."""
-    return _group_norm_workspace(False, plan, x.shape, groups, _elem(x), _vector_rows(x))
+    return _group_norm_workspace(False, plan, _group_norm_sizes(x, groups), groups, _elem(x), _vector_rows(x))
 
 
 def cr_group_norm_backward_workspace_bytes(plan: int, x, groups: int) -> int:
     """As cr_group_norm_workspace_bytes, for cr_group_norm_backward."""
-    return _group_norm_workspace(True, plan, x.shape, groups, _elem(x), _vector_rows(x))
+    return _group_norm_workspace(True, plan, _group_norm_sizes(x, groups), groups, _elem(x), _vector_rows(x))
 
 
 def cr_group_norm(plan: int, x, gamma, beta, groups: int, y, mean=None, rstd=None, eps: float = 1e-5,

@@ -769,3 +769,27 @@ def test_fp32_operands_off_their_elements_are_refused(plan):
             a[k] += off
             assert lib.cr_int8_product(plan, p(codes), 64, a[0], p(codes), 64, a[1], a[2], p(out), 4, 4, 4, 64, B.CR_ELEM_F32, stream) == bad
     assert B.cr_plan_launch_count(plan) == before
+
+
+def test_numbers_that_a_field_would_cut_are_refused(plan):
+    x = torch.zeros(4, 10, 8, device="cuda")
+    y, stats, ws = torch.empty_like(x), torch.zeros((4, 2), device="cuda"), scratch(1 << 20)
+    wide = x[0, 0, :1].expand(1, 1, (1 << 32) + 8)
+    before = B.cr_plan_launch_count(plan)
+    for kw in (dict(groups=(1 << 32) + 2), dict(act=1 << 32), dict(offset=1 << 64), dict(offset=(1 << 63) + 1), dict(seed=1 << 64)):
+        args = dict(dict(groups=2, workspace=ws), **kw)
+        with pytest.raises(ValueError):
+            B.cr_group_norm(plan, x, None, None, y=y, **args)
+        with pytest.raises(ValueError):
+            B.cr_group_norm_backward(plan, x, x, None, None, stats, stats, dx=y, **args)
+        if "seed" in kw or "offset" in kw:
+            with pytest.raises(ValueError):
+                B.cr_dropout(plan, x, y, 0.5, kw.get("seed", 1), offset=kw.get("offset", 0))
+    for query in (B.cr_group_norm_workspace_bytes, B.cr_group_norm_backward_workspace_bytes):
+        for t, groups in ((x, (1 << 32) + 2), (wide, 2), (x[0], 2), (x[None], 2)):
+            with pytest.raises(ValueError):
+                query(plan, t, groups)
+    assert B.cr_plan_launch_count(plan) == before
+    B.cr_dropout(plan, x, y, 0.5, -1)
+    B.cr_dropout(plan, x, x, 0.5, (1 << 64) - 1)
+    assert torch.equal(x, y)
