@@ -492,7 +492,7 @@ def _row_ptr(t, shape):
     if t.shape != shape:
         raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.is_contiguous():
-        return t.data_ptr(), shape[-1]
+        return t.data_ptr(), shape[-1] if len(shape) else 1      # no dimension: a row of one element
     width, st = shape[-1], t.stride()
     if width > 1 and st[-1] != 1:
         raise ValueError("the elements of a row must be next to each other")

@@ -486,6 +486,14 @@ def test_dropout_ends_of_p_and_dropped_infinities(plan):
     B.cr_dropout(plan, torch.empty((0, 5), device="cuda"), torch.empty((0, 5), device="cuda"), 0.5, 1)
 
 
+def test_dropout_of_a_tensor_without_dimensions(plan):
+    for offset in range(12):
+        x = torch.tensor(3.0, device="cuda")
+        y = torch.empty_like(x)
+        B.cr_dropout(plan, x, y, 0.5, 7, offset=offset)
+        assert float(y) == 3.0 * float(O.dropout_factors((1,), 0.5, 7, offset)[0])
+
+
 # ------------------------------------------------------------------------------------------------ 8-bit products
 
 def strided_codes(codes, ld, shift=0):
