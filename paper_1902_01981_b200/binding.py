@@ -562,20 +562,25 @@ def _group_norm_workspace(backward: bool, plan: int, shape, groups: int, elem: i
     return fn(plan, cr_group_norm_t(*shape, groups, elem, CR_ACT_NONE, 0.0, 0.0, 0, 0), vector_rows)
 
 
-def _vector_rows(x) -> int:
-    ptr, ld = _row_ptr(x, x.shape)
-    return int(ptr % 16 == 0 and ld * x.element_size() % 16 == 0)
+def _vector_rows(x, others) -> int:
+    """Whether every tensor of a call has a 16-byte aligned base and row stride."""
+    for t in (x, *others):
+        if t is not None:
+            ptr, ld = _row_ptr(t, x.shape)
+            if ptr % 16 or ld * t.element_size() % 16:
+                return 0
+    return 1
 
 
-def cr_group_norm_workspace_bytes(plan: int, x, groups: int) -> int:
-    """For tensors that all lie in memory as x does (alignment and row stride); a call whose other tensors are less
-    aligned than x says CR_ERR_OOM when it needs more."""
-    return _group_norm_workspace(False, plan, _group_norm_sizes(x, groups), groups, _elem(x), _vector_rows(x))
+def cr_group_norm_workspace_bytes(plan: int, x, groups: int, *others) -> int:
+    """Scratch of cr_group_norm.  `others`: the call's y, if it may be less aligned than x (base or row stride off 16
+    bytes); without it y is taken to lie in memory as x does, and a call that needs more says CR_ERR_OOM."""
+    return _group_norm_workspace(False, plan, _group_norm_sizes(x, groups), groups, _elem(x), _vector_rows(x, others))
 
 
-def cr_group_norm_backward_workspace_bytes(plan: int, x, groups: int) -> int:
-    """As cr_group_norm_workspace_bytes, for cr_group_norm_backward."""
-    return _group_norm_workspace(True, plan, _group_norm_sizes(x, groups), groups, _elem(x), _vector_rows(x))
+def cr_group_norm_backward_workspace_bytes(plan: int, x, groups: int, *others) -> int:
+    """As cr_group_norm_workspace_bytes, for cr_group_norm_backward; `others`: its dy and dx."""
+    return _group_norm_workspace(True, plan, _group_norm_sizes(x, groups), groups, _elem(x), _vector_rows(x, others))
 
 
 def cr_group_norm(plan: int, x, gamma, beta, groups: int, y, mean=None, rstd=None, eps: float = 1e-5,

@@ -389,6 +389,34 @@ def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
     assert torch.equal(dy, dx)
 
 
+@pytest.mark.parametrize("which", ["y", "dy", "dx"])
+def test_workspace_of_tensors_that_are_less_aligned_than_x(plan, which):
+    n, s, c, groups = 4, 300, 64, 8
+    xv, gv, bv, dyv = norm_data((n, s, c), 51)
+    gamma, beta = dev32(gv), dev32(bv)
+    off = {which: 1}
+    x, y = place(xv, "f32"), place(np.zeros(xv.shape), "f32", 0, off.get("y", 0))
+    dy, dx = place(dyv, "f32", 0, off.get("dy", 0)), place(np.zeros(xv.shape), "f32", off.get("dx", 0), 0)
+    mean, rstd = torch.empty((n, groups), device="cuda"), torch.empty((n, groups), device="cuda")
+    B.cr_group_norm(plan, x, gamma, beta, groups, y, mean, rstd,
+                    workspace=scratch(B.cr_group_norm_workspace_bytes(plan, x, groups, y)))
+    want = O.group_norm(f64(x), f64(gamma), f64(beta), groups, 1e-5)
+    check(y, want[0], "f32")
+    need = B.cr_group_norm_backward_workspace_bytes(plan, x, groups, dy, dx)
+    B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, workspace=scratch(need))
+    check(dx, O.group_norm_backward(f64(dy), f64(x), f64(gamma), f64(beta), groups, 1e-5)[0], "f32")
+    # what the call itself asks for: one byte less is refused
+    stats = (mean, rstd)
+    ends = {"y": lambda ws: B.cr_group_norm(plan, x, gamma, beta, groups, y, *stats, workspace=ws)}
+    ends["dy"] = ends["dx"] = lambda ws: B.cr_group_norm_backward(plan, dy, x, gamma, beta, *stats, groups, dx, workspace=ws)
+    if which == "y":
+        need = B.cr_group_norm_workspace_bytes(plan, x, groups, y)
+        assert need > B.cr_group_norm_workspace_bytes(plan, x, groups, None) == 0
+    with pytest.raises(B.CodedReduceError) as e:
+        ends[which](scratch(need)[:need - 1])
+    assert e.value.status == B.CR_ERR_OOM
+
+
 def test_group_norm_of_no_samples(plan):
     x = torch.empty((0, 5, 8), device="cuda")
     B.cr_group_norm(plan, x, None, None, 2, torch.empty_like(x), torch.empty((0, 2), device="cuda"), torch.empty((0, 2), device="cuda"))
