@@ -261,7 +261,8 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     uint64_t *full = reinterpret_cast<uint64_t *>(ring + (size_t)S * kStage);
     uint64_t *empty = full + S;
     uint64_t *acc_full = empty + S, *acc_empty = acc_full + 2;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    uint64_t *settled = acc_empty + 2;                                       // used after a wait has run out
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(settled + 1);
     volatile int *flags = reinterpret_cast<volatile int *>(tmem_slot + 1);   // [0] someone gave up, [1] never set
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -273,6 +274,7 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     if (tid == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], kDrain); }
+        mbar_init(settled, 1);
         flags[0] = 0; flags[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -282,10 +284,11 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    int issued = 0;                          // boxes that thread 0 has asked for
 
     if (warp == 0) {
         if (lane == 0) {
-            int issued = 0, s = 0;
+            int s = 0;
             uint32_t phase = 1;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
@@ -301,12 +304,7 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
                     if (++s == S) { s = 0; phase ^= 1; }
                 }
             }
-            if (!ok) {
-                flags[0] = 1;
-                atomicExch(a.status, 1);
-                for (int i = issued > S ? issued - S : 0; i < issued; ++i)
-                    mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), &flags[1], a.wait_ns);
-            }
+            if (!ok) { flags[0] = 1; atomicExch(a.status, 1); }
         }
     } else if (warp == 1) {
         if (lane == 0) {
@@ -364,9 +362,19 @@ cr_int8_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
             if (lane == 0) mbar_arrive(&acc_empty[set]);
         }
     }
-    // tensor memory goes back before the cluster meets: a CTA that holds some never waits for another CTA
     tc_fence_before();
     __syncthreads();
+    if (flags[0]) {
+        // somebody gave up (whoever it was): boxes and MMAs may be under way that nobody has waited for
+        if (tid == 0)
+            for (int i = issued > S ? issued - S : 0; i < issued; ++i) mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), &flags[1], kSettleNs);
+        if (tid == 32) {                     // the thread that issued the MMAs
+            mma_commit(settled);
+            mbar_wait(settled, 0, &flags[1], kSettleNs);
+        }
+        __syncthreads();
+    }
+    // tensor memory goes back before the cluster meets: a CTA that holds some never waits for another CTA
     if (warp == 1) tmem_free(tmem, kCols);
     __syncthreads();
     if (splits > 1) {
@@ -408,8 +416,9 @@ cr_int8_product_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __g
     uint64_t *full = reinterpret_cast<uint64_t *>(ring + (size_t)S * kStage);   // used in the even CTA
     uint64_t *empty = full + S;
     uint64_t *acc_full = empty + S, *acc_empty = acc_full + 2;                  // acc_empty: used in the even CTA
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
-    volatile int *flags = reinterpret_cast<volatile int *>(tmem_slot + 1);      // [0] someone gave up, [1] never set
+    uint64_t *settled = acc_empty + 2;                                          // used after a wait has run out
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(settled + 1);
+    volatile int *flags = reinterpret_cast<volatile int *>(tmem_slot + 1);      // [0] someone gave up, [1] never set, [2] boxes of the odd CTA
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = (int)cluster_rank();
@@ -418,7 +427,8 @@ cr_int8_product_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __g
     if (tid == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], 2 * kPairDrain); }
-        flags[0] = 0; flags[1] = 0;
+        mbar_init(settled, 1);
+        flags[0] = 0; flags[1] = 0; flags[2] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -428,10 +438,11 @@ cr_int8_product_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __g
     cluster_sync();          // both CTAs' barriers and tensor memory are there
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    int issued = 0;                          // boxes that thread 0 has asked for
 
     if (warp == 0) {
         if (lane == 0) {
-            int s = 0, issued = 0;
+            int s = 0;
             uint32_t phase = 1;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += step) {
@@ -448,17 +459,9 @@ cr_int8_product_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __g
                     if (++s == S) { s = 0; phase ^= 1; }
                 }
             }
-            if (!ok) {
-                flags[0] = 1;
-                atomicExch(a.status, 1);
-                if (rank == 0)
-                    for (int i = issued > S ? issued - S : 0; i < issued; ++i)
-                        mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), &flags[1], a.wait_ns);
-            } else {
-                // the commits of the last stages have arrived before this CTA may end
-                for (int i = issued > S ? issued - S : 0; i < issued; ++i)
-                    mbar_wait(&empty[i % S], (uint32_t)((i / S) & 1), &flags[1], a.wait_ns);
-            }
+            // the commits of the last stages have arrived before this CTA may end
+            for (int i = issued > S ? issued - S : 0; i < issued && ok; ++i) ok = mbar_wait(&empty[i % S], (uint32_t)((i / S) & 1), &flags[0], a.wait_ns);
+            if (!ok) { flags[0] = 1; atomicExch(a.status, 1); }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
@@ -506,7 +509,29 @@ cr_int8_product_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __g
     }
     tc_fence_before();
     __syncthreads();
+    if (tid == 0 && flags[0]) store_cluster(map_to_rank(smem_u32(const_cast<int *>(flags)), (uint32_t)(rank ^ 1)), 1);
     cluster_sync();          // neither CTA ends while the other one's MMAs or commits may reach it
+    if (flags[0]) {
+        // One of the two gave up: boxes and MMAs may be under way that nobody has waited for.  Both CTAs' boxes count on the
+        // even CTA's barriers, which expect two halves a stage; the CTAs may have stopped up to a ring apart.
+        if (tid == 0 && rank == 1) store_cluster(map_to_rank(smem_u32(const_cast<int *>(flags + 2)), 0), issued);
+        __syncthreads();
+        cluster_sync();
+        if (tid == 0 && rank == 0) {
+            const int other = flags[2], last = max(issued, other);
+            for (int i = min(issued, other); i < last; ++i) {
+                if (i >= issued) mbar_expect_tx(&full[i % S], kStage);      // the odd CTA's half comes alone
+                else mbar_complete_tx(&full[i % S], kStage);                // the odd CTA's half does not come
+            }
+            for (int i = last > S ? last - S : 0; i < last; ++i) mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), &flags[1], kSettleNs);
+        }
+        if (tid == 32) {
+            if (rank == 0) mma_commit_pair(settled);                        // the thread that issued the MMAs
+            mbar_wait(settled, 0, &flags[1], kSettleNs);
+        }
+        __syncthreads();
+        cluster_sync();
+    }
     if (warp == 1) tmem_free_pair(tmem, 2 * TN);
 }
 
@@ -556,7 +581,7 @@ cudaError_t launch_pair(const Int8ProductArgs &p, int *status, const DeviceInfo 
     static std::atomic<uint64_t> told{0};
     cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_int8_product_pair_kernel<T>), told, p.device, dev);
     if (e != cudaSuccess) return e;
-    const size_t smem = (size_t)kPairStages * (kRows + 128) * kChunk + (2 * kPairStages + 4) * 8 + 16 + 1024;
+    const size_t smem = (size_t)kPairStages * (kRows + 128) * kChunk + (2 * kPairStages + 5) * 8 + 16 + 1024;
     const unsigned pairs = (unsigned)std::min<int64_t>(tiles, dev.sm_count / 2);
     cr_int8_product_pair_kernel<T><<<2 * pairs, kPairThreads, smem, stream>>>(map_w, map_x, a);
     e = cudaGetLastError();
@@ -580,7 +605,7 @@ cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &d
     // a ring no deeper than the CTA's work, but large enough for the sums of a split tile
     if (tiles * splits <= dev.sm_count) stages = std::min(stages, std::max(per_cta, (int)((TN * kRows * 4 + kStage - 1) / kStage)));
     a.stages = stages;
-    const size_t smem = stages * kStage + (2 * stages + 4) * 8 + 16 + 1024;
+    const size_t smem = stages * kStage + (2 * stages + 5) * 8 + 16 + 1024;
     CUtensorMap map_w, map_x;
     if (encode_codes(encode, &map_w, p.w, p.inner, p.outer, p.ld_w, kRows) != CUDA_SUCCESS ||
         encode_codes(encode, &map_x, p.x, p.inner, p.tokens, p.ld_x, TN) != CUDA_SUCCESS)

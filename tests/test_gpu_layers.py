@@ -665,6 +665,36 @@ def test_int8_product_of_nothing_and_repeats_itself(plan):
         assert torch.equal(part, full[a:b])
 
 
+@pytest.mark.parametrize("tokens,inner,outer", [(1, 131056, 300), (40, 131056, 300), (200, 8192, 16384), (2048, 131056, 512), (4096, 8192, 4096)])
+def test_products_under_the_shortest_wait_limit(tokens, inner, outer):
+    """A limit of a microsecond may or may not run out.  Where it does the status says so; either way the call ends, writes
+    nothing beside its output, and the next call with an ordinary limit is right."""
+    plan = B.cr_plan_create(4, 2, 1, 24, 1024, device=0)
+    try:
+        g = torch.Generator(device="cuda").manual_seed(tokens)
+        x = torch.randint(-127, 128, (tokens, inner), generator=g, device="cuda", dtype=torch.int8)
+        w = torch.randint(-127, 128, (outer, inner), generator=g, device="cuda", dtype=torch.int8)
+        xs, ws = torch.rand(tokens, generator=g, device="cuda"), torch.rand(outer, generator=g, device="cuda")
+        want = torch.empty((tokens, outer), device="cuda")
+        B.cr_int8_product(plan, x, xs, w, ws, want)
+        for _ in range(20):
+            B.cr_plan_set_wait_limit(plan, 1000)
+            wide = torch.full((tokens + 2, outer + 8), 7.0, device="cuda")
+            y = wide[1:-1, 4:-4]
+            B.cr_int8_product(plan, x, xs, w, ws, y)
+            status = B.cr_plan_device_status(plan)
+            assert status in (B.CR_OK, B.CR_ERR_TIMEOUT)
+            assert status == B.CR_ERR_TIMEOUT or torch.equal(y, want)
+            y.zero_()
+            assert (wide[0] == 7).all() and (wide[-1] == 7).all() and (wide[:, :4] == 7).all() and (wide[:, -4:] == 7).all()
+            B.cr_plan_clear_status(plan)
+            B.cr_plan_set_wait_limit(plan, 2_000_000_000)
+            B.cr_int8_product(plan, x, xs, w, ws, y)
+            assert B.cr_plan_device_status(plan) == B.CR_OK and torch.equal(y, want)
+    finally:
+        B.cr_plan_destroy(plan)
+
+
 # ------------------------------------------------------------------------------------------------ beyond 32 bits
 
 def test_dropout_of_more_than_2_to_31_elements(plan):
