@@ -174,7 +174,8 @@ cr_status_t cr_latency_masks(const cr_plan_t *plan, const double *compute_time, 
 cr_status_t cr_plan_device_status(cr_plan_t *plan);
 cr_status_t cr_plan_clear_status(cr_plan_t *plan);
 /* Bound of every device-side wait of this plan's kernels, in nanoseconds (default 2e9; accepted range
- * 1e3 .. 6e10).  It travels to the kernels as an argument of each launch. */
+ * 1e3 .. 6e10).  It travels to the kernels as an argument of each launch.  A kernel that has given up then waits, at most
+ * two seconds a wait, for what it has in flight. */
 cr_status_t cr_plan_set_wait_limit(cr_plan_t *plan, uint64_t limit_ns);
 /* Shows the give-up path without harming anything: enqueues one small kernel whose single thread waits
  * limit_ns (1e3 .. 1e8) on a barrier that nobody completes, through the same bounded wait as the

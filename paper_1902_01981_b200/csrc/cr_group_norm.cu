@@ -191,11 +191,16 @@ struct Exchange {
             asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
                          ::"r"(i8::map_to_rank(to, (uint32_t)r)), "f"(v.x), "f"(v.y), "r"(i8::map_to_rank(bar, (uint32_t)r)) : "memory");
     }
-    // The sums over the cluster of group g, in the order of the ranks.
+    // The sums over the cluster of group g, in the order of the ranks.  A wait that runs out is reported, and the numbers are
+    // then waited for with a limit of their own: every CTA of the cluster runs and tells its numbers whatever it hears, so they
+    // come, and a CTA that went on without them would arrive on a barrier whose phase is not over, decide unlike its
+    // peers about a second sum, and might end while a peer's numbers are on their way into its memory.
     __device__ __forceinline__ float2 hear(int g, int cluster, int *status, unsigned long long wait_ns) const {
-        if (!i8::mbar_wait(&m->bars[turn & 1], (uint32_t)((turn >> 1) & 1), &m->given_up, wait_ns)) {
-            m->given_up = 1;
+        uint64_t *bar = &m->bars[turn & 1];
+        const uint32_t parity = (uint32_t)((turn >> 1) & 1);
+        if (!i8::mbar_wait(bar, parity, &m->given_up, wait_ns)) {
             atomicExch(status, 1);
+            if (!i8::mbar_wait(bar, parity, &m->given_up, i8::kSettleNs)) m->given_up = 1;
         }
         float2 t = make_float2(0.f, 0.f);
         for (int r = 0; r < cluster; ++r) {

@@ -454,6 +454,46 @@ def test_group_norm_step_in_a_graph(plan):
     del graph
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 700, 64, 8), (600, 1024, 64, 8), (40, 1100, 48, 8)])
+def test_group_norm_under_the_shortest_wait_limit(shape, dtype):
+    """Items in clusters, whose CTAs wait for each other.  A limit of a microsecond may or may not run out: where it does the
+    status says so; either way the call ends, writes nothing beside its outputs, and the next call is right."""
+    n, s, c, groups = shape
+    plan = B.cr_plan_create(4, 2, 1, 24, 1024, device=0)
+    try:
+        g = torch.Generator(device="cuda").manual_seed(n)
+        rand = lambda: torch.randn((n, s, c), generator=g, device="cuda").to(TYPES[dtype])  # noqa: E731
+        x, dy = rand(), rand()
+
+        def step():
+            wide = torch.full((2, n * s + 2, c), 7.0, dtype=TYPES[dtype], device="cuda")
+            y, dx = wide[0, 1:-1].view(n, s, c), wide[1, 1:-1].view(n, s, c)
+            mean, rstd = torch.empty((n, groups), device="cuda"), torch.empty((n, groups), device="cuda")
+            dg, db = torch.empty((n, c), device="cuda"), torch.empty((n, c), device="cuda")
+            B.cr_group_norm(plan, x, None, None, groups, y, mean, rstd, act=B.CR_ACT_SILU)
+            forward_status = B.cr_plan_device_status(plan)
+            B.cr_group_norm_backward(plan, dy, x, None, None, mean, rstd, groups, dx, dg, db, act=B.CR_ACT_SILU,
+                                     workspace=scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups)))
+            status = B.cr_plan_device_status(plan)
+            assert {status, forward_status} <= {B.CR_OK, B.CR_ERR_TIMEOUT}
+            assert (wide[:, 0] == 7).all() and (wide[:, -1] == 7).all()
+            return status, [t.clone() for t in (y, mean, rstd, dx, dg, db)]
+
+        status, want = step()
+        assert status == B.CR_OK
+        for _ in range(10):
+            B.cr_plan_set_wait_limit(plan, 1000)
+            status, got = step()
+            assert status == B.CR_ERR_TIMEOUT or all(torch.equal(a, b) for a, b in zip(got, want))
+            B.cr_plan_clear_status(plan)
+            B.cr_plan_set_wait_limit(plan, 2_000_000_000)
+            status, got = step()
+            assert status == B.CR_OK and all(torch.equal(a, b) for a, b in zip(got, want))
+    finally:
+        B.cr_plan_destroy(plan)
+
+
 # ------------------------------------------------------------------------------------------------ dropout
 
 @pytest.mark.parametrize("dtype", list(TYPES))
