@@ -472,7 +472,12 @@ def slot_partitions(plan: int) -> np.ndarray:
 # ------------------------------------------------------------------ layers in front of the workers' model
 
 _elems = {}
-_I31, _I63 = 1 << 31, 1 << 63
+
+
+def _fitting(numbers32, numbers64) -> None:
+    """Refuses what ctypes would cut off in silence; a seed above 2^63 is its two's complement."""
+    if any(not -(1 << 31) <= v < 1 << 31 for v in numbers32) or any(not -(1 << 63) <= v < end for v, end in numbers64):
+        raise ValueError("channels, groups and act are numbers of 32 bits, seed and offset of 64")
 
 
 def _elem(t) -> int:
@@ -527,8 +532,8 @@ def cr_dropout(plan: int, x, y, p: float, seed: int, offset: int = 0, residual=N
     rp, ldr = (0, 0) if residual is None else _row_ptr(residual, shape)
     if y.dtype != x.dtype or (residual is not None and residual.dtype != x.dtype):
         raise ValueError("x, residual and y must have one element type")
-    if not (-_I63 <= seed < 2 * _I63 and -_I63 <= offset < _I63):
-        raise ValueError("seed and offset are numbers of 64 bits")
+    if (seed | offset) >> 63:
+        _fitting((), ((seed, 1 << 64), (offset, 1 << 63)))
     cols = shape[-1] if len(shape) else 1
     _check(lib().cr_dropout(plan, xp, ldx, rp, ldr, yp, ldy, x.numel() // cols if cols else 0, cols, e, p,
                             seed, offset, _stream_ptr(stream)), "cr_dropout")
@@ -538,44 +543,41 @@ def _group_norm_desc(x, groups, eps, act, p, seed, offset):
     if x.dim() != 3:
         raise ValueError("expected [samples, positions, channels]")
     n, s, c = x.shape
-    # the descriptor would cut off in silence what does not fit its fields
-    if not (-_I31 <= groups < _I31 and -_I31 <= act < _I31 and c < _I31 and -_I63 <= seed < 2 * _I63 and -_I63 <= offset < _I63):
-        raise ValueError("channels, groups and act are numbers of 32 bits, seed and offset of 64")
+    if (c | groups | act) >> 31 or (seed | offset) >> 63:
+        _fitting((c, groups, act), ((seed, 1 << 64), (offset, 1 << 63)))
     return cr_group_norm_t(n, s, c, groups, _elem(x), act, eps, p, seed, offset)
 
 
 @functools.lru_cache(maxsize=256)
 def _group_norm_workspace(backward: bool, plan: int, shape, groups: int, elem: int, vector_rows: int) -> int:
     """The workspace is a function of these (the plan's device included), so a loop asks once."""
-    if len(shape) != 3 or shape[2] >= _I31 or not -_I31 <= groups < _I31:
-        raise ValueError("expected [samples, positions, channels], channels and groups of 32 bits")
+    if len(shape) != 3:
+        raise ValueError("expected [samples, positions, channels]")
+    _fitting((shape[2], groups), ())
     fn = lib().cr_group_norm_backward_workspace_bytes if backward else lib().cr_group_norm_workspace_bytes
     return fn(plan, cr_group_norm_t(*shape, groups, elem, CR_ACT_NONE, 0.0, 0.0, 0, 0), vector_rows)
 
 
-def _vector_rows(t, shape) -> int:
-    ptr, ld = _row_ptr(t, shape)
-    return int(ptr % 16 == 0 and ld * t.element_size() % 16 == 0)
-
-
-def _workspace_of(backward: bool, plan: int, x, groups: int, others) -> int:
-    shape = x.shape
-    wide = _vector_rows(x, shape)
+def _vector_rows(x, shape, others) -> int:
+    """Whether every tensor of a call has a 16-byte aligned base and row stride."""
+    ptr, ld = _row_ptr(x, shape)
+    wide = ptr % 16 == 0 and ld * x.element_size() % 16 == 0
     for t in others:
-        if t is not None:
-            wide &= _vector_rows(t, shape)
-    return _group_norm_workspace(backward, plan, shape, groups, _elem(x), wide)
+        wide = wide and (t is None or _vector_rows(t, shape, ()))
+    return int(wide)
 
 
 def cr_group_norm_workspace_bytes(plan: int, x, groups: int, *others) -> int:
     """Scratch of cr_group_norm.  `others`: the call's y, if it may be less aligned than x (base or row stride off 16
     bytes); without it y is taken to lie in memory as x does, and a call that needs more says CR_ERR_OOM."""
-    return _workspace_of(False, plan, x, groups, others)
+    shape = x.shape
+    return _group_norm_workspace(False, plan, shape, groups, _elem(x), _vector_rows(x, shape, others))
 
 
 def cr_group_norm_backward_workspace_bytes(plan: int, x, groups: int, *others) -> int:
     """As cr_group_norm_workspace_bytes, for cr_group_norm_backward; `others`: its dy and dx."""
-    return _workspace_of(True, plan, x, groups, others)
+    shape = x.shape
+    return _group_norm_workspace(True, plan, shape, groups, _elem(x), _vector_rows(x, shape, others))
 
 
 def cr_group_norm(plan: int, x, gamma, beta, groups: int, y, mean=None, rstd=None, eps: float = 1e-5,
