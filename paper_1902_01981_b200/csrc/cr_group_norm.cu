@@ -447,6 +447,9 @@ __global__ void __launch_bounds__(kTH, kForwardCTAs) cr_group_norm_kernel(const 
             if (g < p.groups) {
                 float total = group_sum<2, UNI, kTH / 32>(0, g, p, my_area, mem.sums), squares = group_sum<2, UNI, kTH / 32>(1, g, p, my_area, mem.sums);
                 if (s.cluster > 1) {
+                    // y may be x: the peer that holds the first row writes over it once it has heard from this thread, so the
+                    // pivot is here before that (the other threads' pivots have gone into the sums)
+                    asm volatile("" ::"f"(pivot) : "memory");
                     ex.tell(make_float2(total, squares), p.rank, g, s.cluster);
                     const float2 all = ex.hear(g, s.cluster, a.status, a.wait_ns);
                     total = all.x;

@@ -389,6 +389,21 @@ def test_group_norm_in_place_on_another_stream_and_without_statistics(plan):
     assert torch.equal(dy, dx)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape", [(3, 700, 64, 8), (1500, 512, 64, 8), (700, 512, 32, 32), (40, 9, 32, 8), (2, 9000, 32, 4), (5, 300, 30, 5)])
+def test_group_norm_in_place_in_every_form(plan, shape, dtype):
+    """y = x gives the bits of y elsewhere: items of one CTA, of clusters (one and several a cluster), and of the streaming form."""
+    n, s, c, groups = shape
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn((n, s, c), generator=g, device="cuda").add_(3.0).to(TYPES[dtype])
+    y, mean, rstd = forward(plan, x, None, None, groups, dtype, act=B.CR_ACT_SILU)
+    ws = scratch(B.cr_group_norm_workspace_bytes(plan, x, groups))
+    for _ in range(5):
+        x2, mean2, rstd2 = x.clone(), torch.empty_like(mean), torch.empty_like(rstd)
+        B.cr_group_norm(plan, x2, None, None, groups, x2, mean2, rstd2, act=B.CR_ACT_SILU, workspace=ws)
+        assert torch.equal(x2, y) and torch.equal(mean2, mean) and torch.equal(rstd2, rstd)
+
+
 @pytest.mark.parametrize("which", ["y", "dy", "dx"])
 def test_workspace_of_tensors_that_are_less_aligned_than_x(plan, which):
     n, s, c, groups = 4, 300, 64, 8
