@@ -368,8 +368,10 @@ cr_status_t cr_plan_tune_items(cr_plan_t *plan, int32_t item_order, int32_t mult
  * its layers.  The gradients of the partitions must ADD UP to the gradient of the whole data set, so no layer may
  * couple the samples of different partitions: the normalisation is per sample (group norm).  And every worker that
  * holds a partition must compute THE SAME partial gradient, or the decode of a redundant copy is not exact: dropout
- * masks are functions of the element's index alone, sums have one fixed order (no atomics), integer products have no
- * rounding at all.
+ * masks are functions of the element's index alone, integer products have no rounding at all, and sums have one order
+ * (no atomics) that follows from the sizes, the element type and whether ALL tensors of the call (for the backward pass dx
+ * too, if wanted) have 16-byte aligned bases and row strides.  The samples beside a partition, the strides themselves and
+ * the machine do not count; workers that are to agree to the last bit agree on that one thing, and otherwise to rounding.
  *   - Tensors are channels last: rows of `channels` consecutive elements, one row per position, `ld` elements from
  *     row to row (>= channels), the positions of a sample one after the other.  Element types are cr_elem_t; the
  *     arithmetic is fp32 throughout, rounded once to the element type.  Buffers must be aligned to their element;

@@ -6,10 +6,13 @@
 //   dz = drop(dy) act'(z),  dbeta_c = sum dz,  dgamma_c = sum dz xhat  (over a partition's samples),
 //   dx = rstd (gamma_c dz - m1 - xhat m2),  m1 = sum gamma_c dz / K,  m2 = sum gamma_c dz xhat / K.
 // Statistics and sums are held in 32 bits whatever the elements' type; a value is rounded to it once, when it is
-// stored.  No atomics: every sum has one order, so every worker that holds a partition gets the same bits.
+// stored.  No atomics: every sum has one order.  The order follows the sizes, the element type and whether all tensors of
+// the call lie in 16-byte vectors (which decides between the forms), not the samples beside it, the strides themselves or
+// the machine: every worker that holds a partition in such a layout gets the same bits.
 //
-// z is formed as ((x - mean) * rstd) * gamma + beta with each step rounded, in the forward and the backward pass
-// alike: where the activation has a kink its slope then belongs to the very z that the forward pass used.
+// z is formed as ((x - mean) * rstd) * gamma + beta: in this file, and for relu everywhere, with each step rounded, in the
+// forward and the backward pass alike.  Where the activation has a kink its slope then belongs to the very z that the
+// forward pass used.
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -226,6 +226,35 @@ def test_partitions_add_up_and_do_not_see_each_other(plan, shape, dtype):
         assert torch.equal(dx1, dx[mine]) and torch.equal(dg1[0], dg[q]) and torch.equal(db1[0], db[q])
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape", [(6, 40, 64, 8), (3, 700, 64, 8), (2, 9000, 48, 4), (2, 50, 4096, 1), (4, 60, 24, 8)])
+def test_bits_depend_on_the_layout_only_by_its_alignment(plan, shape, dtype):
+    """Packed rows and rows inside wider ones, both in 16-byte vectors: the same bits.  So for two layouts that are off them.
+    From one to the other the sums are taken in another order."""
+    n, s, c, groups = shape
+    xv, gv, bv, dyv = norm_data((n, s, c), 61)
+    gamma, beta = dev32(gv), dev32(bv)
+    kw = dict(act=B.CR_ACT_SILU, p=0.2, seed=5, offset=3)
+
+    def step(*layouts):                              # (pad, shift) of x, y, dy, dx
+        (x, dy), (y, dx) = ((place(a, dtype, *layouts[k]), place(b, dtype, *layouts[k + 2])) for k, a, b in ((0, xv, dyv), (1, 0 * xv, 0 * xv)))
+        mean, rstd = torch.empty((n, groups), device="cuda"), torch.empty((n, groups), device="cuda")
+        dg, db = torch.empty((n, c), device="cuda"), torch.empty((n, c), device="cuda")
+        B.cr_group_norm(plan, x, gamma, beta, groups, y, mean, rstd, workspace=scratch(B.cr_group_norm_workspace_bytes(plan, x, groups, y)), **kw)
+        B.cr_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, groups, dx, dg, db,
+                                 workspace=scratch(B.cr_group_norm_backward_workspace_bytes(plan, x, groups, dy, dx)), **kw)
+        return [t.contiguous() for t in (y, mean, rstd, dx, dg, db)]
+
+    packed, wider, moved = (0, 0), (16, 0), (0, 16)
+    on = step(packed, packed, packed, packed)
+    for layouts in ((wider,) * 4, (packed, wider, moved, packed), (moved, packed, wider, wider)):
+        assert all(torch.equal(a, b) for a, b in zip(on, step(*layouts)))
+    odd, off = (1, 0), (0, 1)
+    others = step(odd, odd, odd, odd)
+    for layouts in ((off,) * 4, (packed, off, packed, odd), (off, packed, wider, off)):
+        assert all(torch.equal(a, b) for a, b in zip(others, step(*layouts)))
+
+
 def test_a_nan_stays_in_its_group_and_statistics_survive_a_large_mean(plan):
     n, s, c, groups = 3, 100, 32, 4
     xv, gv, bv, _ = norm_data((n, s, c), 6)
