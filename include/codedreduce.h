@@ -409,7 +409,8 @@ typedef struct {
 } cr_group_norm_t;
 
 /* y = dropout(act(gamma_c (x - mean) rstd + beta_c)), mean and rstd = 1 / sqrt(var + eps) over the positions and
- * channels of each (sample, group), var the mean square distance from the mean.  gamma, beta: fp32 [channels] or NULL
+ * channels of each (sample, group), var the mean square distance from the mean (sums in fp32: a group whose sum or whose
+ * summed square distances leave its range, 3.4e38, has no result).  gamma, beta: fp32 [channels] or NULL
  * (ones, zeros).  mean, rstd: fp32 [samples][groups], written for the backward pass; both NULL if not wanted.  y may
  * be x itself (same stride).  workspace: device scratch of cr_group_norm_workspace_bytes (CR_ERR_OOM if
  * smaller), 16-byte aligned; vector_rows: whether every tensor of the call has a 16-byte aligned base and row stride

@@ -8,8 +8,10 @@
 // (cp.async) exactly the vectors that it reads itself, so the pipeline needs no barrier and no wait on another thread.
 // What a CTA knows of its groups goes to its peers through distributed shared memory, joined in the order of the ranks.
 // Measured (floor at the copy bandwidth): forward, 256 samples of 1024 x 256, fp32 98 us (83), bf16 62 (42), bf16 with
-// dropout 90; backward, 192 of them, fp32 124 (94), bf16 112 (47), with dropout 134.  fp32 is near the memory; 16-bit
-// elements are bound by instructions, about 15 an element forward and 8.5 more for the dropout mask.
+// dropout 90; backward, 192 of them, fp32 124 (94), bf16 112 (47), with dropout 134.  fp32 is near the memory.  16-bit
+// elements are bound by latency at low occupancy: 20 (forward) and 13 warps an SM fill 2.1 and 1.8 of 4 issue slots a cycle with
+// DRAM at a fifth of its peak, and wait for their own previous results and at the two barriers and the exchange of a sample.
+// What is issued is about 15 instructions an element forward and 8.5 more for the dropout mask.
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -594,9 +594,9 @@ Split make_split(int64_t positions, int channels, int groups, int vec) {
         s.width = most;
         s.tiles = groups * s.parts;
     }
-    // Chunks of 32 vectors (64 single elements) a thread, at most one an SM for a sample.  The number of samples must not
-    // count: the chunks set the order of the sums, and a worker that holds a partition alone has to get the bits of the
-    // whole batch.  Forward, us, at 16 / 32 / 64 a thread: 8 samples of 65536 x 64 in vectors 72 / 64 / -, 64 samples of
+    // Chunks of 32 vectors (64 single elements) a thread, at most 148 (this machine's SMs) for a sample.  Neither the number
+    // of samples nor the device's own count may enter: the chunks set the order of the sums, and a worker that holds a
+    // partition alone, wherever, has to get the bits of the whole batch.  Forward, us, at 16 / 32 / 64 a thread: 8 samples of 65536 x 64 in vectors 72 / 64 / -, 64 samples of
     // 1024 x 256 in odd rows 76 / 59 / 49; two samples of 65536 x 64 spend 9.3 / 10.9 / - on the sums.
     const int64_t least = (vec == 1 ? 64ll : 32ll) * (kThreads / std::min(kThreads, s.width / vec));
     const int64_t chunks = std::min<int64_t>(148, std::max<int64_t>(1, positions / least));
