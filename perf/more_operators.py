@@ -114,9 +114,9 @@ def work(case):
                 "flops": 9 * count}
     count, ids = case["rows"] * case["vocab"], ID_SIZE[case["ids"]]
     if op == "probs":
-        return {"bytes": count * size + case["rows"] * (ids + 12 + case["top"] * (4 + ids)), "flops": 6 * count}
+        return {"bytes": count * size + case["rows"] * (ids + 16 + case["top"] * (4 + ids)), "flops": 6 * count}
     if op == "probs_grad":
-        return {"bytes": 2 * count * size + case["rows"] * (ids + 16), "flops": 8 * count}
+        return {"bytes": 2 * count * size + case["rows"] * (ids + 20), "flops": 8 * count}
     return {"bytes": count * size * (2 if case["grad"] else 1) + case["rows"] * (8 + case["top"] * (4 + ids)),
             "flops": count * (8 if case["grad"] else 4)}
 
@@ -196,10 +196,13 @@ def _inputs(case, seed):
     s["logits"] = logits.to(dtype)
     if op == "probs_grad":
         s["dlogp"], s["dentropy"] = rand(case["rows"]), 0.1 * rand(case["rows"])
-        z = s["logits"].double() / case["temperature"]
-        lse = torch.logsumexp(z, 1)
-        p = torch.exp(z - lse[:, None])
-        s["lse"], s["entropy"] = lse.float(), (lse - (p * torch.where(p > 0, z, 0.0)).sum(1)).float()
+        # what the forward pass has left: each row's largest logit, the logarithm of the sum relative to it, the entropy
+        largest = s["logits"].double().amax(1)
+        z = (s["logits"].double() - largest[:, None]) / case["temperature"]
+        log_sum = torch.logsumexp(z, 1)
+        p = torch.exp(z - log_sum[:, None])
+        s["stats"] = torch.stack([largest, log_sum], 1).float()
+        s["entropy"] = (log_sum - (p * torch.where(p > 0, z, 0.0)).sum(1)).float()
     return s
 
 
@@ -277,12 +280,13 @@ def _own_norm_grad(s):
 
 def _own_probs(s):
     B, c, x = s["binding"], s["case"], s["logits"]
-    logp, lse, entropy = (torch.empty(c["rows"], device="cuda") for _ in range(3))
-    out = {"logp": logp, "lse": lse, "entropy": entropy}
+    logp, entropy = torch.empty(c["rows"], device="cuda"), torch.empty(c["rows"], device="cuda")
+    stats = torch.empty((c["rows"], 2), device="cuda")
+    out = {"logp": logp, "stats": stats, "entropy": entropy}
     if c["top"]:
         out["top_logp"] = torch.empty((c["rows"], c["top"]), device="cuda")
         out["top_ids"] = torch.empty((c["rows"], c["top"]), dtype=s["ids"].dtype, device="cuda")
-    B.cr_token_log_probs(s["plan"], x, s["ids"], logp, lse=lse, entropy=entropy, top_logp=out.get("top_logp"),
+    B.cr_token_log_probs(s["plan"], x, s["ids"], logp, stats=stats, entropy=entropy, top_logp=out.get("top_logp"),
                          top_ids=out.get("top_ids"), temperature=c["temperature"])
     return out
 
@@ -290,8 +294,8 @@ def _own_probs(s):
 def _own_probs_grad(s):
     B, x = s["binding"], s["logits"]
     dlogits = torch.empty_like(x)
-    B.cr_token_log_probs_backward(s["plan"], x, s["ids"], s["lse"], s["entropy"], s["dlogp"], s["dentropy"], dlogits,
-                                  temperature=s["case"]["temperature"])
+    B.cr_token_log_probs_backward(s["plan"], x, s["ids"], s["stats"], s["entropy"], s["dlogp"], s["dentropy"],
+                                  dlogits, temperature=s["case"]["temperature"])
     return dlogits
 
 
@@ -359,26 +363,27 @@ def _plain_norm_grad(s):
 def _plain_probs(s):
     c = s["case"]
     x = s["logits"].float()
-    z = x * (1.0 / c["temperature"])
-    top = z.amax(1, keepdim=True)
-    e = torch.exp(z - top)
+    largest = x.amax(1, keepdim=True)
+    z = (x - largest) * (1.0 / c["temperature"])
+    e = torch.exp(z)
     total = e.sum(1)
-    lse = top[:, 0] + torch.log(total)
+    log_sum = torch.log(total)
     mean = (e * torch.where(e > 0, z, 0.0)).sum(1) / total
-    out = {"logp": z.gather(1, s["ids"].long()[:, None])[:, 0] - lse, "lse": lse, "entropy": lse - mean}
+    out = {"logp": z.gather(1, s["ids"].long()[:, None])[:, 0] - log_sum, "entropy": log_sum - mean,
+           "stats": torch.stack([largest[:, 0], log_sum], 1)}
     if c["top"]:
         bits = (x + 0.0).view(torch.int32).long()
         order = torch.where(bits >= 0, bits, -(bits & 0x7FFFFFFF))     # whole numbers in the values' order
         order = (order << 32) + (0x7FFFFFFF - torch.arange(c["vocab"], device="cuda"))    # equal values: the lowest index first
         best = torch.topk(order, c["top"], dim=1).indices
-        out["top_logp"] = z.gather(1, best) - lse[:, None]
+        out["top_logp"] = z.gather(1, best) - log_sum[:, None]
         out["top_ids"] = best.to(s["ids"].dtype)
     return out
 
 
 def _plain_probs_grad(s):
     inverse = 1.0 / s["case"]["temperature"]
-    log_p = s["logits"].float() * inverse - s["lse"][:, None]
+    log_p = (s["logits"].float() - s["stats"][:, :1]) * inverse - s["stats"][:, 1:]
     p = torch.exp(log_p)
     a, b = s["dlogp"][:, None], s["dentropy"][:, None]
     d = -p * (a + b * (torch.where(p > 0, log_p, 0.0) + s["entropy"][:, None]))
@@ -470,8 +475,9 @@ def _exact_norm_grad(case, s):
 def _exact_probs(case, s):
     z = s["logits"].double() / case["temperature"]
     log_p = torch.log_softmax(z, 1)
-    out = {"logp": log_p.gather(1, s["ids"].long()[:, None]).squeeze(1), "lse": torch.logsumexp(z, 1),
-           "entropy": torch.special.entr(torch.softmax(z, 1)).sum(1)}
+    largest, where = s["logits"].double().max(1)
+    out = {"logp": log_p.gather(1, s["ids"].long()[:, None]).squeeze(1),
+           "stats": torch.stack([largest, -log_p.gather(1, where[:, None]).squeeze(1)], 1), "entropy": torch.special.entr(torch.softmax(z, 1)).sum(1)}
     if case["top"]:
         values, ids = torch.sort(s["logits"].double(), dim=1, descending=True, stable=True)
         out["top_ids"] = ids[:, :case["top"]].to(s["ids"].dtype)
