@@ -450,6 +450,96 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
                             int64_t ld_w, const float *w_scale, const float *bias, void *y, int64_t ld_y, int64_t tokens,
                             int64_t outer, int64_t inner, int32_t elem, void *stream);
 
+/* ---- token layers ------------------------------------------------------------------------------------
+ * A model over tokens: the lookup of their rows in a table (a linear model on one-hot features is the same thing), a norm
+ * that couples no samples, the loss over a vocabulary and the scores of given tokens.  The conventions are those of the
+ * layers above: rows of consecutive elements at a row stride `ld` (>= their length), cr_elem_t elements, fp32 arithmetic
+ * rounded once, gradients of parameters per partition in fp32, no atomics in a sum, and an order of every sum that follows
+ * from the row's length (for a parameter's gradient the partition's sizes too), the element type and whether ALL tensors of
+ * the call have 16-byte aligned bases and row strides and whole 16-byte vectors in a row.
+ *   - Token numbers are 32- or 64-bit integers, `id_bytes` 4 or 8, aligned to their size and next to each other.  A number
+ *     outside [0, vocab) names no token (padding): that is not an error.
+ *   - Like the other device calls these only enqueue kernels and can be captured in a CUDA graph. */
+
+/* y[t][:] = scale * table[ids[t]][:] (a zero row where ids[t] names no token).  table [vocab][width], y [tokens][width], one
+ * element type.  0 <= tokens <= 2^31 - 1, 0 <= vocab <= 2^31 - 1, 0 <= width <= 2^24. */
+cr_status_t cr_embedding(cr_plan_t *plan, const void *ids, int32_t id_bytes, const void *table, int64_t ld_table, void *y,
+                         int64_t ld_y, int64_t tokens, int64_t vocab, int64_t width, int32_t elem, double scale, void *stream);
+
+/* Gradients of the table, one for each of `partitions` groups of `tokens` consecutive tokens:
+ *   dtable[p][v][:] = scale * sum over the tokens t of partition p with ids[p][t] = v of dy[p][t][:]
+ * ids [partitions][tokens], dy [partitions * tokens][width] at row stride ld_dy, dtable fp32 [partitions][vocab][width] at
+ * row stride ld_row and partition stride ld_partition (>= vocab * ld_row), written whole: rows that no token names become
+ * zero.  Tokens of number `padding` take no part (-1: all do; for a table whose padding row is looked up and not trained).
+ * A row's tokens are added in the order of their positions, in pieces whose ends depend on the partition's own tokens.
+ * workspace: device scratch of cr_embedding_backward_workspace_bytes (CR_ERR_OOM if smaller), 16-byte aligned. */
+size_t cr_embedding_backward_workspace_bytes(const cr_plan_t *plan, int64_t tokens, int64_t partitions, int64_t vocab, int64_t width);
+cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_bytes, const void *dy, int64_t ld_dy,
+                                  float *dtable, int64_t ld_row, int64_t ld_partition, int64_t tokens, int64_t partitions,
+                                  int64_t vocab, int64_t width, int32_t elem, double scale, int64_t padding, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/* Root-mean-square norm of rows with the residual's addition in front:
+ *   h = x + residual (residual NULL: h = x),  rstd = 1 / sqrt(mean of h^2 + eps),  y = h rstd gamma
+ * The norm is taken of the fp32 sum; h (NULL: not wanted) is that sum rounded once, the residual stream that goes on and
+ * what the backward pass takes.  gamma fp32 [cols] or NULL (ones); rstd fp32 [rows] or NULL.  y or h may be x or residual
+ * itself (same stride).  rows of zeros need eps > 0; a row whose sum of squares leaves the range of a float has no result.
+ * 0 <= rows <= 2^31 - 1, 1 <= cols <= 2^31 - 1, eps >= 0. */
+cr_status_t cr_rms_norm(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r, const float *gamma,
+                        void *h, int64_t ld_h, void *y, int64_t ld_y, float *rstd, int64_t rows, int64_t cols, int32_t elem,
+                        double eps, void *stream);
+
+/* The same with y as 8-bit codes and a scale for each row, as cr_quantize_rows would give them for the fp32 y (which is
+ * never rounded to 16 bits), ready for cr_int8_product.  q: [rows] at stride ld_q bytes; h may be x or residual itself. */
+cr_status_t cr_rms_norm_codes(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r,
+                              const float *gamma, void *h, int64_t ld_h, int8_t *q, int64_t ld_q, float *scale, float *rstd,
+                              int64_t rows, int64_t cols, int32_t elem, double eps, void *stream);
+
+/* Gradients of cr_rms_norm from dy, with the forward pass's h, rstd and gamma: dx (type of h; NULL: not wanted), which is
+ * the gradient of x and of residual alike, plus dh, the gradient that reaches h by the residual stream (NULL: none).
+ * dgamma fp32 [partitions][cols] at row stride ld_gamma, one row for every rows / partitions consecutive rows (NULL: not
+ * wanted).  dx may be dy, h or dh itself (same stride).  workspace as above. */
+size_t cr_rms_norm_backward_workspace_bytes(const cr_plan_t *plan, int64_t rows, int64_t cols, int64_t partitions);
+cr_status_t cr_rms_norm_backward(cr_plan_t *plan, const void *dy, int64_t ld_dy, const void *h, int64_t ld_h,
+                                 const float *gamma, const float *rstd, const void *dh, int64_t ld_dh, void *dx, int64_t ld_dx,
+                                 float *dgamma, int64_t ld_gamma, int64_t partitions, int64_t rows, int64_t cols, int32_t elem,
+                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* Scores over logits [rows][vocab] at temperature T > 0.  With m the row's largest logit and
+ * log_sum = log sum_v e^{(x_v - m) / T}, log p_v = (x_v - m) / T - log_sum:
+ *   logp[r] = log p of token ids[r] (0 where it names none),  entropy[r] = -sum_v p_v log p_v,
+ *   stats[r] = {m, log_sum} (what the backward pass takes; the log of the partition function is m / T + log_sum),
+ *   top_ids, top_logp [rows][top]: the `top` largest logits in descending order, equal ones by ascending index, and their
+ *   log p.  top_ids are of id_bytes.
+ * All outputs fp32; each of logp, stats, entropy may be NULL, the last two are there if top > 0 (0 <= top <= 32, <= vocab).
+ * Logits of -infinity are masked out.  A row that is -infinity throughout has no distribution: log p = -infinity, entropy 0,
+ * its alternatives are the lowest indices.  A NaN makes all of its row's numbers NaN, and is the best alternative; a row with
+ * +infinity has log p = -infinity for its finite logits and NaN for the infinite ones and the entropy.
+ * 0 <= rows <= 2^31 - 1, 1 <= vocab <= 2^31 - 1. */
+cr_status_t cr_token_log_probs(cr_plan_t *plan, const void *logits, int64_t ld, const void *ids, int32_t id_bytes,
+                               int64_t rows, int64_t vocab, int32_t elem, double temperature, float *logp, float *stats,
+                               float *entropy, int32_t top, float *top_logp, void *top_ids, void *stream);
+
+/* dlogits = gradient of sum_r (dlogp[r] logp[r] + dentropy[r] entropy[r]) from the forward pass's stats and entropy.  dlogp
+ * or dentropy may be NULL (zeros; ids and entropy are then not read).  A row without a distribution, or whose numbers from
+ * above are both zero (padding), has gradient zero whatever its logits hold.  dlogits may be logits itself. */
+cr_status_t cr_token_log_probs_backward(cr_plan_t *plan, const void *logits, int64_t ld, const void *ids, int32_t id_bytes,
+                                        const float *stats, const float *entropy, const float *dlogp, const float *dentropy,
+                                        void *dlogits, int64_t ld_d, int64_t rows, int64_t vocab, int32_t elem,
+                                        double temperature, void *stream);
+
+/* Distillation from a teacher's `top` best logits per row (1 <= top <= 1024): teacher_ids [rows][top] of id_bytes and
+ * teacher fp32 [rows][top] (logits, or log probabilities: a constant per row drops out), both contiguous.  With
+ * t = softmax(teacher / T) over the row's named tokens and p = softmax(logits / T) over the vocabulary:
+ *   loss[r] = T^2 sum_j t_j (log t_j - log p_{id_j}),   dlogits[r][v] = weight[r] T (p_v - sum_{j: id_j = v} t_j)
+ * loss fp32 [rows] or NULL; dlogits of the logits' type or NULL, may be logits itself; weight fp32 [rows] (the loss's
+ * gradient from above) or NULL (ones).  Teacher logits of -infinity count as not named; a token named twice counts twice.
+ * A row whose teacher names nothing has loss and gradient zero, one of weight zero the gradient zero, whatever its logits
+ * hold.  Student logits of -infinity are masked out: p = 0 there, and the loss is infinite if the teacher wants them. */
+cr_status_t cr_distill(cr_plan_t *plan, const void *logits, int64_t ld, const void *teacher_ids, int32_t id_bytes,
+                       const float *teacher, int32_t top, const float *weight, float *loss, void *dlogits, int64_t ld_d,
+                       int64_t rows, int64_t vocab, int32_t elem, double temperature, void *stream);
+
 /* Kernel launches enqueued by this plan's device calls so far. */
 int64_t cr_plan_launch_count(const cr_plan_t *plan);
 

@@ -121,6 +121,29 @@ _SIGNATURES = {
     "cr_int8_product": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
                                   C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32,
                                   C.c_void_p]),
+    "cr_embedding": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                               C.c_int64, C.c_int64, C.c_int32, C.c_double, C.c_void_p]),
+    "cr_embedding_backward_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64]),
+    "cr_embedding_backward": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                        C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_double,
+                                        C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "cr_rms_norm": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                              C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_double, C.c_void_p]),
+    "cr_rms_norm_codes": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                    C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64,
+                                    C.c_int32, C.c_double, C.c_void_p]),
+    "cr_rms_norm_backward_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int64, C.c_int64, C.c_int64]),
+    "cr_rms_norm_backward": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                                       C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "cr_token_log_probs": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_int64,
+                                     C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                     C.c_void_p, C.c_void_p]),
+    "cr_token_log_probs_backward": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p,
+                                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64,
+                                              C.c_int64, C.c_int32, C.c_double, C.c_void_p]),
+    "cr_distill": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p,
+                             C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_double, C.c_void_p]),
     "cr_plan_launch_count": (C.c_int64, [C.c_void_p]),
     "cr_plan_last_kernel": (C.c_char_p, [C.c_void_p]),
 }
@@ -657,3 +680,202 @@ def cr_int8_product(plan: int, x, x_scale, w, w_scale, y, bias=None, stream=None
     _check(lib().cr_int8_product(plan, xp, ldx, _vector_ptr(x_scale, m), wp, ldw, _vector_ptr(w_scale, n),
                                  _vector_ptr(bias, n), yp, ldy, m, n, k, _elem(y), _stream_ptr(stream)),
            "cr_int8_product")
+
+
+# ------------------------------------------------------------------ token layers
+
+_id_bytes = {}
+
+
+def _ids_ptr(t, shape):
+    """(address, id_bytes) of contiguous token numbers on the device."""
+    if not _id_bytes:
+        import torch
+        _id_bytes.update({torch.int32: 4, torch.int64: 8})
+    n = _id_bytes.get(t.dtype)
+    if n is None:
+        raise ValueError(f"expected int32 or int64 token numbers, got {t.dtype}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected contiguous token numbers on the device")
+    if t.shape != shape:
+        raise ValueError(f"expected token numbers of shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr(), n
+
+
+def _one_type(*tensors) -> int:
+    """cr_elem_t of tensors that must share it (None: left out)."""
+    kept = [t for t in tensors if t is not None]
+    if any(t.dtype != kept[0].dtype for t in kept):
+        raise ValueError("the tensors must have one element type")
+    return _elem(kept[0])
+
+
+def cr_embedding(plan: int, ids, table, y, scale: float = 1.0, stream=None) -> None:
+    """y [..., width] = scale * table [vocab, width] at ids [...]; a number outside the table gives a zero row."""
+    if table.dim() != 2 or y.dim() < 1:
+        raise ValueError("expected table [vocab, width] and y [..., width]")
+    vocab, width = table.shape
+    e = _one_type(table, y)
+    ip, ib = _ids_ptr(ids, y.shape[:-1])
+    tp, ldt = _row_ptr(table, table.shape)
+    yp, ldy = _row_ptr(y, (*ids.shape, width))
+    _check(lib().cr_embedding(plan, ip, ib, tp, ldt, yp, ldy, ids.numel(), vocab, width, e, scale, _stream_ptr(stream)),
+           "cr_embedding")
+
+
+def _table_gradient(ids, dtable):
+    """(partitions, tokens of each, vocab, width) of ids [tokens] with dtable [vocab, width], or ids [partitions, ...] with
+    dtable [partitions, vocab, width]."""
+    if dtable.dim() == 2:
+        return 1, ids.numel(), *dtable.shape
+    if dtable.dim() != 3 or ids.dim() < 1 or ids.shape[0] != dtable.shape[0]:
+        raise ValueError("expected ids [partitions, ...] and dtable [partitions, vocab, width]")
+    parts = ids.shape[0]
+    return parts, ids.numel() // parts if parts else 0, *dtable.shape[1:]
+
+
+def cr_embedding_backward_workspace_bytes(plan: int, ids, dtable) -> int:
+    """Scratch of cr_embedding_backward for these tensors."""
+    parts, tokens, vocab, width = _table_gradient(ids, dtable)
+    return lib().cr_embedding_backward_workspace_bytes(plan, tokens, parts, vocab, width)
+
+
+def cr_embedding_backward(plan: int, ids, dy, dtable, scale: float = 1.0, padding: int = -1, workspace=None,
+                          stream=None) -> None:
+    """dtable [vocab, width] or [partitions, vocab, width] (float32, written whole) = gradients of the table from dy
+    [*ids.shape, width]; tokens of number `padding` take no part."""
+    parts, tokens, vocab, width = _table_gradient(ids, dtable)
+    if padding >> 63 not in (0, -1):
+        raise ValueError("padding is a number of 64 bits")
+    ip, ib = _ids_ptr(ids, ids.shape)
+    dp, ldd = _row_ptr(dy, (*ids.shape, width))
+    if _elem(dtable) != CR_ELEM_F32 or not dtable.is_cuda:
+        raise ValueError("expected a float32 dtable on the device")
+    if dtable.is_contiguous():
+        ldr, ldp = width, vocab * width
+    else:
+        st = dtable.stride()
+        ldr = st[-2] if vocab > 1 else width
+        ldp = st[0] if parts > 1 else vocab * ldr
+        if (width > 1 and st[-1] != 1) or ldr < width or ldp < vocab * ldr:
+            raise ValueError("the rows and partitions of dtable must not overlap, the elements of a row be next to each other")
+    wp, wb = _ptr_and_bytes(workspace)
+    _check(lib().cr_embedding_backward(plan, ip, ib, dp, ldd, dtable.data_ptr(), ldr, ldp, tokens, parts, vocab, width,
+                                       _elem(dy), scale, padding, wp, wb, _stream_ptr(stream)), "cr_embedding_backward")
+
+
+def _rows_and_cols(x):
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("expected rows of at least one element")
+    return x.numel() // x.shape[-1], x.shape[-1]
+
+
+def cr_rms_norm(plan: int, x, gamma, y, residual=None, h=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
+    """h = x + residual, y = h / sqrt(mean h^2 + eps) * gamma over the last dimension of x; h (the residual stream) and
+    rstd (one number a row, contiguous) are what the backward pass takes."""
+    rows, cols = _rows_and_cols(x)
+    e, shape = _one_type(x, residual, h, y), x.shape
+    xp, ldx = _row_ptr(x, shape)
+    rp, ldr = (0, 0) if residual is None else _row_ptr(residual, shape)
+    hp, ldh = (0, 0) if h is None else _row_ptr(h, shape)
+    yp, ldy = _row_ptr(y, shape)
+    _check(lib().cr_rms_norm(plan, xp, ldx, rp, ldr, _vector_ptr(gamma, cols), hp, ldh, yp, ldy, _vector_ptr(rstd, rows), rows,
+                             cols, e, eps, _stream_ptr(stream)), "cr_rms_norm")
+
+
+def cr_rms_norm_codes(plan: int, x, gamma, q, scale, residual=None, h=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
+    """cr_rms_norm with y as int8 codes q (shape of x) and a scale for each row, as cr_int8_product takes them; a row stride
+    of q that is a multiple of 16 lets it take its tensor-core form."""
+    rows, cols = _rows_and_cols(x)
+    e, shape = _one_type(x, residual, h), x.shape
+    xp, ldx = _row_ptr(x, shape)
+    rp, ldr = (0, 0) if residual is None else _row_ptr(residual, shape)
+    hp, ldh = (0, 0) if h is None else _row_ptr(h, shape)
+    qp, ldq = _codes_ptr(q, shape)
+    _check(lib().cr_rms_norm_codes(plan, xp, ldx, rp, ldr, _vector_ptr(gamma, cols), hp, ldh, qp, ldq, _vector_ptr(scale, rows),
+                                   _vector_ptr(rstd, rows), rows, cols, e, eps, _stream_ptr(stream)), "cr_rms_norm_codes")
+
+
+def cr_rms_norm_backward_workspace_bytes(plan: int, h, partitions: int = 1) -> int:
+    """Scratch of cr_rms_norm_backward for rows like h's."""
+    rows, cols = _rows_and_cols(h)
+    return lib().cr_rms_norm_backward_workspace_bytes(plan, rows, cols, partitions)
+
+
+def cr_rms_norm_backward(plan: int, dy, h, gamma, rstd, dx=None, dgamma=None, dh=None, workspace=None, stream=None) -> None:
+    """dx = gradient of x and residual from dy and, by the residual stream, dh (None: none); dgamma [partitions, cols] (rows
+    may lie inside wider rows) for equal runs of rows."""
+    rows, cols = _rows_and_cols(h)
+    e, shape = _one_type(h, dy, dh, dx), h.shape
+    gp, ldg = _row_ptr(dy, shape)
+    hp, ldh = _row_ptr(h, shape)
+    sp, lds = (0, 0) if dh is None else _row_ptr(dh, shape)
+    dp, ldd = (0, 0) if dx is None else _row_ptr(dx, shape)
+    parts, pp, ldp = 1, 0, cols
+    if dgamma is not None:
+        if dgamma.dim() != 2 or dgamma.shape[1] != cols or _elem(dgamma) != CR_ELEM_F32:
+            raise ValueError("dgamma is float32 [partitions, cols]")
+        parts = dgamma.shape[0]
+        pp, ldp = _row_ptr(dgamma, dgamma.shape)
+    wp, wb = _ptr_and_bytes(workspace)
+    _check(lib().cr_rms_norm_backward(plan, gp, ldg, hp, ldh, _vector_ptr(gamma, cols), _vector_ptr(rstd, rows), sp, lds, dp, ldd,
+                                      pp, ldp, parts, rows, cols, e, wp, wb, _stream_ptr(stream)), "cr_rms_norm_backward")
+
+
+def _logits(x):
+    if x.dim() != 2 or x.shape[1] < 1:
+        raise ValueError("expected logits [rows, vocab]")
+    return (*x.shape, *_row_ptr(x, x.shape), _elem(x))
+
+
+def cr_token_log_probs(plan: int, logits, ids, logp=None, stats=None, entropy=None, top_logp=None, top_ids=None,
+                       temperature: float = 1.0, stream=None) -> None:
+    """For logits [rows, vocab]: log probabilities of ids [rows] (None with logp None), entropy [rows], stats [rows, 2] for
+    the backward pass, and the best alternatives top_ids, top_logp [rows, top] (both or neither)."""
+    rows, vocab, xp, ld, e = _logits(logits)
+    ip, ib = (0, 8) if ids is None else _ids_ptr(ids, (rows,))
+    if logp is not None and ids is None:
+        raise ValueError("logp needs ids")
+    if (top_ids is None) != (top_logp is None):
+        raise ValueError("top_ids and top_logp go together")
+    top, tp = 0, 0
+    if top_ids is not None:
+        top = top_ids.shape[-1]
+        tp, tb = _ids_ptr(top_ids, (rows, top))
+        if ids is not None and tb != ib:
+            raise ValueError("ids and top_ids must have one type")
+        ib = tb
+    _check(lib().cr_token_log_probs(plan, xp, ld, ip, ib, rows, vocab, e, temperature, _vector_ptr(logp, rows),
+                                    _vector_ptr(stats, 2 * rows), _vector_ptr(entropy, rows), top,
+                                    _vector_ptr(top_logp, rows * top), tp, _stream_ptr(stream)), "cr_token_log_probs")
+
+
+def cr_token_log_probs_backward(plan: int, logits, ids, stats, entropy, dlogp, dentropy, dlogits, temperature: float = 1.0,
+                                stream=None) -> None:
+    """dlogits = gradient of sum(dlogp * logp + dentropy * entropy); dlogp (with ids) or dentropy (with entropy) may be None."""
+    rows, vocab, xp, ld, e = _logits(logits)
+    ip, ib = (0, 8) if ids is None else _ids_ptr(ids, (rows,))
+    if (dlogp is not None and ids is None) or (dentropy is not None and entropy is None) or stats is None:
+        raise ValueError("dlogp needs ids, dentropy needs entropy, both need stats")
+    _one_type(logits, dlogits)
+    dp, ldd = _row_ptr(dlogits, logits.shape)
+    _check(lib().cr_token_log_probs_backward(plan, xp, ld, ip, ib, _vector_ptr(stats, 2 * rows), _vector_ptr(entropy, rows),
+                                             _vector_ptr(dlogp, rows), _vector_ptr(dentropy, rows), dp, ldd, rows, vocab, e,
+                                             temperature, _stream_ptr(stream)), "cr_token_log_probs_backward")
+
+
+def cr_distill(plan: int, logits, teacher_ids, teacher, loss=None, dlogits=None, weight=None, temperature: float = 1.0,
+               stream=None) -> None:
+    """Loss [rows] of logits [rows, vocab] against a teacher's logits `teacher` (float32) of its best tokens teacher_ids, both
+    [rows, top], and dlogits = the gradient of sum(weight * loss) (weight None: ones); either may be None."""
+    rows, vocab, xp, ld, e = _logits(logits)
+    if teacher_ids.dim() != 2:
+        raise ValueError("expected teacher_ids [rows, top]")
+    top = teacher_ids.shape[1]
+    ip, ib = _ids_ptr(teacher_ids, (rows, top))
+    dp, ldd = 0, vocab
+    if dlogits is not None:
+        _one_type(logits, dlogits)
+        dp, ldd = _row_ptr(dlogits, logits.shape)
+    _check(lib().cr_distill(plan, xp, ld, ip, ib, _vector_ptr(teacher, rows * top), top, _vector_ptr(weight, rows),
+                            _vector_ptr(loss, rows), dp, ldd, rows, vocab, e, temperature, _stream_ptr(stream)), "cr_distill")

@@ -10,7 +10,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcodedreduce.so")
-SOURCES = ["cr_plan.cpp", "cr_kernels.cu", "cr_tc.cu", "cr_layers.cu", "cr_group_norm.cu", "cr_int8.cu", "cr_api.cu"]
+SOURCES = ["cr_plan.cpp", "cr_kernels.cu", "cr_tc.cu", "cr_layers.cu", "cr_group_norm.cu", "cr_int8.cu", "cr_embedding.cu",
+           "cr_rms_norm.cu", "cr_vocab.cu", "cr_api.cu"]
 HEADERS = ["cr_plan.hpp", "cr_kernels.hpp", "cr_layers.hpp", "cr_elem.cuh", "cr_tcgen05.cuh"]
 
 

@@ -1365,3 +1365,205 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
 }
 
 }  // extern "C"
+
+// ---- token layers ----------------------------------------------------------------------------------
+
+namespace {
+
+constexpr int64_t kMost31 = 0x7fffffffll;
+bool good_ids(const void *ids, int32_t id_bytes) {
+    return (id_bytes == 4 || id_bytes == 8) && (reinterpret_cast<uintptr_t>(ids) & (uintptr_t)(id_bytes - 1)) == 0;
+}
+// A factor that stays a number in fp32; a NaN fails.
+bool good_factor(double f) { return f >= -3.4e38 && f <= 3.4e38; }
+// Its square, its reciprocal and the logarithm's factor stay in range.
+bool good_temperature(double t) { return t >= 1e-18 && t <= 1e18; }
+bool good_extents(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kMost31 && cols >= 1 && cols <= kMost31; }
+
+bool good_embedding(int64_t tokens, int64_t partitions, int64_t vocab, int64_t width) {
+    return tokens >= 0 && tokens <= kMost31 && vocab >= 0 && vocab <= kMost31 && width >= 0 && width <= (1 << 24) && partitions >= 0 &&
+           partitions <= (1 << 24) && (tokens == 0 || partitions <= (1ll << 40) / tokens);
+}
+
+cr::VocabArgs vocab_args(const void *logits, int64_t ld, const void *ids, int32_t id_bytes, int64_t rows, int64_t vocab, int32_t elem, double t) {
+    cr::VocabArgs a;
+    a.logits = logits; a.ld = ld; a.ids = ids; a.id_bytes = id_bytes; a.rows = rows; a.vocab = vocab; a.elem = elem;
+    a.inverse = (float)(1.0 / t);
+    a.temperature = (float)t;
+    return a;
+}
+
+cr_status_t rms_norm(cr_plan_t *plan, cr::RmsNormArgs &a, int32_t elem, double eps, void *stream, const char *name) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_extents(a.rows, a.cols) || !known_elem(elem) || !(eps >= 0.0)) return CR_ERR_INVALID_ARG;
+    if (a.rows == 0) return CR_OK;
+    if (!a.x || !good_rows(a.rows, a.cols, a.ld_x) || (a.residual && !good_rows(a.rows, a.cols, a.ld_residual)) ||
+        (a.h && !good_rows(a.rows, a.cols, a.ld_h)) || !on_element(a.x, elem) || !on_element(a.residual, elem) || !on_element(a.h, elem) ||
+        !on_element(a.y, elem) || !on_float(a.gamma, a.rstd, a.scale))
+        return CR_ERR_INVALID_ARG;
+    a.elem = elem;
+    a.eps = (float)eps;
+    cudaError_t e = cr::launch_rms_norm(a, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, name); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cr_status_t cr_embedding(cr_plan_t *plan, const void *ids, int32_t id_bytes, const void *table, int64_t ld_table, void *y,
+                         int64_t ld_y, int64_t tokens, int64_t vocab, int64_t width, int32_t elem, double scale, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_embedding(tokens, 1, vocab, width) || !known_elem(elem) || !good_ids(ids, id_bytes) || !good_factor(scale)) return CR_ERR_INVALID_ARG;
+    if (tokens == 0 || width == 0) return CR_OK;
+    if (!ids || (!table && vocab > 0) || !y || !good_rows(vocab, width, ld_table) || !good_rows(tokens, width, ld_y) || !on_element(table, elem) ||
+        !on_element(y, elem))
+        return CR_ERR_INVALID_ARG;
+    cr::EmbeddingArgs a;
+    a.ids = ids; a.id_bytes = id_bytes; a.table = table; a.ld_table = ld_table; a.y = y; a.ld_y = ld_y; a.tokens = tokens; a.vocab = vocab;
+    a.width = width; a.elem = elem; a.scale = (float)scale;
+    cudaError_t e = cr::launch_embedding(a, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_embedding"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+size_t cr_embedding_backward_workspace_bytes(const cr_plan_t *plan, int64_t tokens, int64_t partitions, int64_t vocab, int64_t width) {
+    if (!plan || !good_embedding(tokens, partitions, vocab, width) || partitions == 0 || vocab == 0 || width == 0) return 0;
+    return cr::embedding_backward_workspace_bytes(tokens, partitions, width);
+}
+
+cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_bytes, const void *dy, int64_t ld_dy,
+                                  float *dtable, int64_t ld_row, int64_t ld_partition, int64_t tokens, int64_t partitions,
+                                  int64_t vocab, int64_t width, int32_t elem, double scale, int64_t padding, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_embedding(tokens, partitions, vocab, width) || !known_elem(elem) || !good_ids(ids, id_bytes) || !good_factor(scale)) return CR_ERR_INVALID_ARG;
+    if (partitions == 0 || vocab == 0 || width == 0) return CR_OK;
+    if (!dtable || !on_float(dtable) || !good_rows(vocab, width, ld_row) || !good_rows(partitions, vocab * ld_row, ld_partition)) return CR_ERR_INVALID_ARG;
+    if (tokens > 0 && (!ids || !dy || !good_rows(tokens * partitions, width, ld_dy) || !on_element(dy, elem))) return CR_ERR_INVALID_ARG;
+    const size_t need = cr::embedding_backward_workspace_bytes(tokens, partitions, width);
+    if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
+    cr::EmbeddingArgs a;
+    a.ids = ids; a.id_bytes = id_bytes; a.dy = dy; a.ld_dy = ld_dy; a.dtable = dtable; a.ld_row = ld_row; a.ld_partition = ld_partition;
+    a.tokens = tokens; a.partitions = partitions; a.vocab = vocab; a.width = width; a.elem = elem; a.scale = (float)scale; a.padding = padding;
+    cudaError_t e = cr::launch_embedding_backward(a, workspace, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_embedding_backward"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+cr_status_t cr_rms_norm(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r, const float *gamma,
+                        void *h, int64_t ld_h, void *y, int64_t ld_y, float *rstd, int64_t rows, int64_t cols, int32_t elem,
+                        double eps, void *stream) {
+    if (rows > 0 && (!y || !good_rows(rows, cols, ld_y))) return CR_ERR_INVALID_ARG;
+    cr::RmsNormArgs a;
+    a.x = x; a.ld_x = ld_x; a.residual = residual; a.ld_residual = ld_r; a.gamma = gamma; a.h = h; a.ld_h = ld_h; a.y = y; a.ld_y = ld_y;
+    a.rstd = rstd; a.rows = rows; a.cols = cols;
+    return rms_norm(plan, a, elem, eps, stream, "cr_rms_norm");
+}
+
+cr_status_t cr_rms_norm_codes(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r,
+                              const float *gamma, void *h, int64_t ld_h, int8_t *q, int64_t ld_q, float *scale, float *rstd,
+                              int64_t rows, int64_t cols, int32_t elem, double eps, void *stream) {
+    if (rows > 0 && (!q || !scale || !good_rows(rows, cols, ld_q))) return CR_ERR_INVALID_ARG;
+    cr::RmsNormArgs a;
+    a.x = x; a.ld_x = ld_x; a.residual = residual; a.ld_residual = ld_r; a.gamma = gamma; a.h = h; a.ld_h = ld_h; a.q = q; a.ld_q = ld_q;
+    a.scale = scale; a.rstd = rstd; a.rows = rows; a.cols = cols;
+    return rms_norm(plan, a, elem, eps, stream, "cr_rms_norm_codes");
+}
+
+size_t cr_rms_norm_backward_workspace_bytes(const cr_plan_t *plan, int64_t rows, int64_t cols, int64_t partitions) {
+    if (!plan || !good_extents(rows, cols) || partitions < 1 || rows % partitions != 0) return 0;
+    return cr::rms_norm_backward_workspace_bytes(rows, cols, partitions);
+}
+
+cr_status_t cr_rms_norm_backward(cr_plan_t *plan, const void *dy, int64_t ld_dy, const void *h, int64_t ld_h,
+                                 const float *gamma, const float *rstd, const void *dh, int64_t ld_dh, void *dx, int64_t ld_dx,
+                                 float *dgamma, int64_t ld_gamma, int64_t partitions, int64_t rows, int64_t cols, int32_t elem,
+                                 void *workspace, size_t workspace_bytes, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_extents(rows, cols) || !known_elem(elem) || partitions < 1 || partitions > kMost31 || rows % partitions != 0) return CR_ERR_INVALID_ARG;
+    if (!on_float(gamma, rstd, dgamma) || (dgamma && !good_rows(partitions, cols, ld_gamma))) return CR_ERR_INVALID_ARG;
+    if (!dx && !dgamma) return CR_OK;
+    if (rows > 0) {
+        if (!dy || !h || !rstd || !good_rows(rows, cols, ld_dy) || !good_rows(rows, cols, ld_h) || (dx && dh && !good_rows(rows, cols, ld_dh)) ||
+            (dx && !good_rows(rows, cols, ld_dx)) || !on_element(dy, elem) || !on_element(h, elem) || !on_element(dh, elem) || !on_element(dx, elem))
+            return CR_ERR_INVALID_ARG;
+        // without dgamma there are no chunks to join: a number a row
+        const size_t need = cr::rms_norm_backward_workspace_bytes(rows, cols, dgamma ? partitions : rows);
+        if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
+    }
+    cr::RmsNormArgs a;
+    a.dy = dy; a.ld_dy = ld_dy; a.h = const_cast<void *>(h); a.ld_h = ld_h; a.gamma = gamma; a.rstd = const_cast<float *>(rstd);
+    a.dh = dx ? dh : nullptr; a.ld_dh = ld_dh; a.y = dx; a.ld_y = ld_dx; a.dgamma = dgamma; a.ld_gamma = ld_gamma;
+    a.partitions = partitions; a.rows = rows; a.cols = cols; a.elem = elem;
+    cudaError_t e = cr::launch_rms_norm_backward(a, static_cast<float *>(workspace), reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_rms_norm_backward"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+cr_status_t cr_token_log_probs(cr_plan_t *plan, const void *logits, int64_t ld, const void *ids, int32_t id_bytes,
+                               int64_t rows, int64_t vocab, int32_t elem, double temperature, float *logp, float *stats,
+                               float *entropy, int32_t top, float *top_logp, void *top_ids, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_extents(rows, vocab) || !known_elem(elem) || !good_temperature(temperature) || top < 0 || top > 32 || top > vocab) return CR_ERR_INVALID_ARG;
+    if ((logp || top > 0) && !good_ids(ids, id_bytes)) return CR_ERR_INVALID_ARG;
+    if (top > 0 && (!top_logp || !top_ids || !good_ids(top_ids, id_bytes) || !on_float(top_logp)) && rows > 0) return CR_ERR_INVALID_ARG;
+    if (rows == 0) return CR_OK;
+    if (!logits || (logp && !ids) || !good_rows(rows, vocab, ld) || !on_element(logits, elem) || !on_float(logp, stats, entropy) ||
+        (reinterpret_cast<uintptr_t>(stats) & 7u) != 0)
+        return CR_ERR_INVALID_ARG;
+    if (!logp && !stats && !entropy && top == 0) return CR_OK;
+    cr::VocabArgs a = vocab_args(logits, ld, ids, id_bytes, rows, vocab, elem, temperature);
+    a.logp = logp; a.stats = stats; a.entropy = entropy; a.top = top; a.top_logp = top_logp; a.top_ids = top_ids;
+    cudaError_t e = cr::launch_token_log_probs(a, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_token_log_probs"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+cr_status_t cr_token_log_probs_backward(cr_plan_t *plan, const void *logits, int64_t ld, const void *ids, int32_t id_bytes,
+                                        const float *stats, const float *entropy, const float *dlogp, const float *dentropy,
+                                        void *dlogits, int64_t ld_d, int64_t rows, int64_t vocab, int32_t elem,
+                                        double temperature, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_extents(rows, vocab) || !known_elem(elem) || !good_temperature(temperature) || (dlogp && !good_ids(ids, id_bytes))) return CR_ERR_INVALID_ARG;
+    if (rows == 0) return CR_OK;
+    if (!logits || !dlogits || !stats || (dlogp && !ids) || (dentropy && !entropy) || !good_rows(rows, vocab, ld) || !good_rows(rows, vocab, ld_d) ||
+        !on_element(logits, elem) || !on_element(dlogits, elem) || !on_float(stats, entropy, dlogp, dentropy) ||
+        (reinterpret_cast<uintptr_t>(stats) & 7u) != 0)
+        return CR_ERR_INVALID_ARG;
+    cr::VocabArgs a = vocab_args(logits, ld, ids, id_bytes, rows, vocab, elem, temperature);
+    a.stats = const_cast<float *>(stats); a.entropy = const_cast<float *>(entropy); a.dlogp = dlogp; a.dentropy = dentropy;
+    a.dlogits = dlogits; a.ld_d = ld_d;
+    cudaError_t e = cr::launch_token_log_probs_backward(a, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_token_log_probs_backward"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+cr_status_t cr_distill(cr_plan_t *plan, const void *logits, int64_t ld, const void *teacher_ids, int32_t id_bytes,
+                       const float *teacher, int32_t top, const float *weight, float *loss, void *dlogits, int64_t ld_d,
+                       int64_t rows, int64_t vocab, int32_t elem, double temperature, void *stream) {
+    cr_status_t st = check_device_plan(plan);
+    if (st != CR_OK) return st;
+    if (!good_extents(rows, vocab) || !known_elem(elem) || !good_temperature(temperature) || top < 1 || top > 1024 || !good_ids(teacher_ids, id_bytes))
+        return CR_ERR_INVALID_ARG;
+    if (rows == 0 || (!loss && !dlogits)) return CR_OK;
+    if (!logits || !teacher_ids || !teacher || !good_rows(rows, vocab, ld) || (dlogits && !good_rows(rows, vocab, ld_d)) || !on_element(logits, elem) ||
+        !on_element(dlogits, elem) || !on_float(teacher, weight, loss))
+        return CR_ERR_INVALID_ARG;
+    cr::VocabArgs a = vocab_args(logits, ld, teacher_ids, id_bytes, rows, vocab, elem, temperature);
+    a.teacher = teacher; a.top = top; a.weight = weight; a.loss = loss; a.dlogits = dlogits; a.ld_d = ld_d;
+    cudaError_t e = cr::launch_distill(a, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    if (e != cudaSuccess) { note_cuda(e, "cr_distill"); return CR_ERR_CUDA; }
+    return CR_OK;
+}
+
+}  // extern "C"

@@ -1,4 +1,5 @@
-// Vectors of 32-, bf16- and f16-elements, and the counter-based generator of the dropout masks.
+// What the layer kernels share: vectors of 32-, bf16- and f16-elements, the counter-based generator of the dropout masks,
+// pairs of fp32 operations, activations, 8-bit codes; dispatch by element type.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -6,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "cr_layers.hpp"
 
@@ -258,6 +260,47 @@ __device__ __forceinline__ float act_gradient(float dy, float z) {
         return dy * (s * fmaf(z, 1.f - s, 1.f));
     }
     return dy;
+}
+
+// ---- 8-bit codes -----------------------------------------------------------------------------------
+//
+// Rows whose largest magnitude is below 2^-120 count as zero (127 / max would leave the range of a float); a row with an
+// infinity or a NaN gets the scale NaN, which its outputs then show.
+struct RowScale {
+    float mult, scale;
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t largest_bits) {
+    const float largest = __uint_as_float(largest_bits);
+    if (largest_bits >= 0x7f800000u) return {0.f, __uint_as_float(0x7fc00000u)};
+    if (largest < 0x1p-120f) return {0.f, 0.f};
+    return {__fdiv_rn(127.f, largest), __fdiv_rn(largest, 127.f)};
+}
+// rint(x * mult) in two's complement in the low byte: 1.5 * 2^23 pushes the fraction out of the significand, and the sum
+// rounds to even.  |x * mult| <= 127 (1 + 2^-23), so no code leaves the range.
+__device__ __forceinline__ uint32_t code(float x, float mult) { return __float_as_uint(__fadd_rn(__fmul_rn(x, mult), 12582912.f)); }
+
+// ---- what the launch wrappers share ---------------------------------------------------------------
+
+template <typename F>
+inline cudaError_t by_type(int elem, F &&f) {
+    switch (elem) {
+        case kElemF32: return f(float{});
+        case kElemBF16: return f(__nv_bfloat16{});
+        default: return f(__half{});
+    }
+}
+template <int V> struct Int { static constexpr int value = V; };
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// The vector form needs whole 16-byte vectors in every row.
+inline bool vector_rows(int elem, int64_t channels, std::initializer_list<const void *> ptrs, std::initializer_list<int64_t> lds) {
+    const int vec = 16 / elem_bytes(elem);
+    if (channels % vec) return false;
+    for (const void *p : ptrs)
+        if (p && !aligned16(p)) return false;
+    for (int64_t ld : lds)
+        if (ld % vec) return false;
+    return true;
 }
 
 }  // namespace cr

@@ -726,7 +726,6 @@ __global__ void __launch_bounds__(kTH, backward_ctas(sizeof(T))) cr_group_norm_g
     if (s.cluster > 1) cluster_meet();
 }
 
-template <int V> struct Int { static constexpr int value = V; };
 
 // The slab and the cluster of an item, and the vectors a thread holds: false where an item does not fit.
 bool choose(int elem, int channels, int groups, int64_t samples, int64_t positions, int bytes, int max_nv, Slab &s, int &nv) {

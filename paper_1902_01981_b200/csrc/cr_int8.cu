@@ -18,21 +18,6 @@ namespace {
 
 // ---- quantiser ------------------------------------------------------------------------------------------------------
 
-// Rows whose largest magnitude is below 2^-120 count as zero (127 / max would leave the range of a float); a row with an
-// infinity or a NaN gets the scale NaN, which its outputs then show.
-struct RowScale {
-    float mult, scale;
-};
-__device__ __forceinline__ RowScale row_scale(uint32_t largest_bits) {
-    const float largest = __uint_as_float(largest_bits);
-    if (largest_bits >= 0x7f800000u) return {0.f, __uint_as_float(0x7fc00000u)};
-    if (largest < 0x1p-120f) return {0.f, 0.f};
-    return {__fdiv_rn(127.f, largest), __fdiv_rn(largest, 127.f)};
-}
-// rint(x * mult) in two's complement in the low byte: 1.5 * 2^23 pushes the fraction out of the significand, and the sum
-// rounds to even.  |x * mult| <= 127 (1 + 2^-23), so no code leaves the range.
-__device__ __forceinline__ uint32_t code(float x, float mult) { return __float_as_uint(__fadd_rn(__fmul_rn(x, mult), 12582912.f)); }
-
 // The largest magnitude of a vector, as the bits of a float.  Magnitudes are compared as integers: the order is the same,
 // and a NaN is larger than everything.  16-bit elements are compared two at a time.
 template <typename T, int VEC>
@@ -627,15 +612,6 @@ cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &d
     e = cudaLaunchKernelEx(&cfg, cr_int8_product_kernel<T, TN>, map_w, map_x, a, splits);
     if (e == cudaSuccess) ++*launches;
     return e;
-}
-
-template <typename F>
-cudaError_t by_type(int elem, F &&f) {
-    switch (elem) {
-        case kElemF32: return f(float{});
-        case kElemBF16: return f(__nv_bfloat16{});
-        default: return f(__half{});
-    }
 }
 
 }  // namespace

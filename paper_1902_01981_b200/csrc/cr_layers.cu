@@ -576,8 +576,6 @@ __global__ void __launch_bounds__(kThreads) cr_dropout_elements_kernel(const T *
     }
 }
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 Split make_split(int64_t positions, int channels, int groups, int vec) {
     Split s;
     s.positions = positions;
@@ -623,32 +621,12 @@ int split_vec(bool wide, int elem, int channels, int groups) {
 }
 
 template <typename F>
-cudaError_t by_type(int elem, F &&f) {
-    switch (elem) {
-        case kElemF32: return f(float{});
-        case kElemBF16: return f(__nv_bfloat16{});
-        default: return f(__half{});
-    }
-}
-template <int V> struct Int { static constexpr int value = V; };
-template <typename F>
 cudaError_t by_act(int act, F &&f) {
     switch (act) {
         case kActNone: return f(Int<kActNone>{});
         case kActRelu: return f(Int<kActRelu>{});
         default: return f(Int<kActSilu>{});
     }
-}
-
-// The vector form needs whole 16-byte vectors in every row.
-bool vector_rows(int elem, int64_t channels, std::initializer_list<const void *> ptrs, std::initializer_list<int64_t> lds) {
-    const int vec = 16 / elem_bytes(elem);
-    if (channels % vec) return false;
-    for (const void *p : ptrs)
-        if (p && !aligned16(p)) return false;
-    for (int64_t ld : lds)
-        if (ld % vec) return false;
-    return true;
 }
 
 }  // namespace

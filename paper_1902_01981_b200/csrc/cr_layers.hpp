@@ -1,4 +1,5 @@
-// Launch wrappers of the layer kernels: group norm and dropout (cr_layers.cu), 8-bit integer product (cr_int8.cu).
+// Launch wrappers of the layer kernels: group norm and dropout (cr_layers.cu), 8-bit integer product (cr_int8.cu), embedding
+// (cr_embedding.cu), root-mean-square norm (cr_rms_norm.cu), log probabilities and distillation (cr_vocab.cu).
 #pragma once
 
 #include <cuda.h>
@@ -88,5 +89,61 @@ struct Int8ProductArgs {
 };
 cudaError_t launch_int8_product(const Int8ProductArgs &a, int *status, const DeviceInfo &dev, const Tuning &tune,
                                 EncodeTiledFn encode, cudaStream_t stream, int64_t *launches);
+
+// ---- token layers ----
+
+struct EmbeddingArgs {
+    const void *ids = nullptr;       // [partitions][tokens] numbers of id_bytes (4 or 8)
+    const void *table = nullptr;     // [vocab][ld_table]
+    const void *dy = nullptr;        // [partitions][tokens][ld_dy]
+    void *y = nullptr;               // [tokens][ld_y]
+    float *dtable = nullptr;         // [partitions] at ld_partition, [vocab] at ld_row
+    int64_t tokens = 0, partitions = 1, vocab = 0, width = 0;
+    int64_t ld_table = 0, ld_y = 0, ld_dy = 0, ld_row = 0, ld_partition = 0;
+    int64_t padding = -1;
+    int id_bytes = 8, elem = 0;
+    float scale = 1.f;
+};
+cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream, int64_t *launches);
+size_t embedding_backward_workspace_bytes(int64_t tokens, int64_t partitions, int64_t width);
+cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, cudaStream_t stream, int64_t *launches);
+
+struct RmsNormArgs {
+    const void *x = nullptr, *residual = nullptr;   // [rows]; residual may be null
+    const void *dy = nullptr, *dh = nullptr;        // backward; dh may be null
+    void *h = nullptr;                              // x + residual: written by the forward pass (may be null), read by the backward pass
+    void *y = nullptr;                              // y, or dx
+    int8_t *q = nullptr;                            // codes in place of y
+    float *scale = nullptr;                         // [rows] with q
+    float *rstd = nullptr;                          // [rows]: written by the forward pass (may be null), read by the backward pass
+    const float *gamma = nullptr;                   // [cols] or null: ones
+    float *dgamma = nullptr;                        // [partitions] at ld_gamma, may be null
+    int64_t rows = 0, cols = 0, partitions = 1;
+    int64_t ld_x = 0, ld_residual = 0, ld_dy = 0, ld_dh = 0, ld_h = 0, ld_y = 0, ld_q = 0, ld_gamma = 0;
+    int elem = 0;
+    float eps = 0.f;
+};
+cudaError_t launch_rms_norm(const RmsNormArgs &a, cudaStream_t stream, int64_t *launches);
+size_t rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t partitions);
+cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cudaStream_t stream, int64_t *launches);
+
+struct VocabArgs {
+    const void *logits = nullptr;    // [rows][ld]
+    const void *ids = nullptr;       // [rows], or [rows][top] of the teacher
+    const float *teacher = nullptr;  // [rows][top]
+    const float *weight = nullptr;   // [rows] or null: ones
+    const float *dlogp = nullptr, *dentropy = nullptr;   // [rows] or null: zeros
+    float *logp = nullptr, *entropy = nullptr, *loss = nullptr;   // [rows], each may be null
+    float *stats = nullptr;          // [rows][2]: the largest logit m and log sum e^{(x - m) / T}; may be null (forward)
+    float *top_logp = nullptr;       // [rows][top]
+    void *top_ids = nullptr;         // [rows][top]
+    void *dlogits = nullptr;         // [rows][ld_d]
+    int64_t rows = 0, vocab = 0, ld = 0, ld_d = 0;
+    int top = 0, id_bytes = 8, elem = 0;
+    float inverse = 1.f, temperature = 1.f;   // 1 / temperature
+};
+cudaError_t launch_token_log_probs(const VocabArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
+cudaError_t launch_token_log_probs_backward(const VocabArgs &a, cudaStream_t stream, int64_t *launches);
+cudaError_t launch_distill(const VocabArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 
 }  // namespace cr
