@@ -18,125 +18,398 @@
 namespace cr {
 namespace {
 
-constexpr int kThreads = 256;
+
 constexpr float kLn2 = 0.6931471805599453f;
 // Exponents below this are zero in fp32; the clamp keeps 0 * -infinity out of the entropy.
 constexpr float kLeast = -160.f;
+constexpr int kMaxCluster = 8, kScoreWarps = 8, kDistillWarps = 8;
 
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-
-template <typename F>
-__device__ __forceinline__ float block_reduce(float v, float *sm, F f) {
+__device__ __forceinline__ float warp_max_nan(float v) {
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
-    if (threadIdx.x % 32 == 0) sm[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = sm[0];
-    for (int w = 1; w < kThreads / 32; ++w) v = f(v, sm[w]);
+    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-__device__ __forceinline__ float add(float a, float b) { return a + b; }
+__device__ __forceinline__ float finite_base(float m) { return isinf(m) ? 0.f : m; }
 
-// Position in the order of the alternatives: the larger value first, then the lower index; a NaN above everything.
-__device__ __forceinline__ unsigned long long rank_key(float x, uint32_t index) {
-    const uint32_t b = __float_as_uint(x + 0.f);     // -0 counts as 0
-    const uint32_t order = x != x ? 0xffffffffu : (b >> 31) ? ~b : b | 0x80000000u;
-    return (unsigned long long)order << 32 | (0xffffffffu - index);
+// ---- a cluster of CTAs on a row --------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void arrive(int cluster) {
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float key_value(unsigned long long key) {
-    const uint32_t order = (uint32_t)(key >> 32);
-    return __uint_as_float((order >> 31) ? order & 0x7fffffffu : ~order);
+__device__ __forceinline__ void wait(int cluster) {
+    if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void meet(int cluster) {
+    if (cluster > 1) {
+        arrive(cluster);
+        wait(cluster);
+    } else {
+        __syncthreads();
+    }
+}
+__device__ __forceinline__ uint32_t address_at(const void *p, int rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return a;
+}
+
+// ---- pieces of a row ---------------------------------------------------------------------------------------------------------
+//
+// A row is cut into chunks that a warp takes at once, all loads first: kUnroll vectors (or elements, where rows do not lie in
+// vectors) a lane, 4 KB of 16-byte vectors.  A chunk yields its largest logit m, sum 2^u and sum 2^u u with u = (x - m) c; they
+// go into slots (chunk modulo kSlots, in ascending order where a row is longer than that) and are joined over the slots in
+// a fixed order.  So the result depends on the row's length alone, and any number of warps and CTAs may share a row.
+constexpr int kSlots = 1024;
+
+template <typename T, int VEC>
+struct Chunk {
+    static constexpr int kUnroll = VEC == 1 ? 32 : 8;
+    static constexpr int kElements = 32 * kUnroll * VEC;
+    static constexpr int kLane = kUnroll * VEC;      // elements of a lane
+    Packed<T, VEC> r[kUnroll];
+
+    // The index of element i of vector u of a lane.
+    static __device__ __forceinline__ int64_t index(int64_t chunk, int lane, int u, int i) { return ((chunk * kUnroll + u) * 32 + lane) * VEC + i; }
+
+    __device__ __forceinline__ void load(const T *x, int64_t vocab, int64_t chunk) {
+        const int lane = (int)threadIdx.x % 32;
+        const T *p = x + index(chunk, lane, 0, 0);
+        if ((chunk + 1) * kElements <= vocab) {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) r[u] = load_packed<T, VEC>(p + u * 32 * VEC);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                float none[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) none[i] = -INFINITY;
+                r[u] = index(chunk, lane, u, 0) < vocab ? load_packed<T, VEC>(p + u * 32 * VEC) : pack<T, VEC>(none);
+            }
+        }
+    }
+    // The lane's largest logit (NaN if it has one).
+    __device__ __forceinline__ float largest() const {
+        if constexpr (VEC == 1 || sizeof(T) == 4) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                float f[VEC];
+                unpack<T, VEC>(r[u], f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) m = max_nan(m, f[i]);
+            }
+            return m;
+        } else if constexpr (__is_same(T, __nv_bfloat16)) {
+            __nv_bfloat162 m = *reinterpret_cast<const __nv_bfloat162 *>(&r[0].w[0]);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+                for (int i = 0; i < VEC / 2; ++i) m = __hmax2_nan(m, *reinterpret_cast<const __nv_bfloat162 *>(&r[u].w[i]));
+            return max_nan(__low2float(m), __high2float(m));
+        } else {
+            __half2 m = *reinterpret_cast<const __half2 *>(&r[0].w[0]);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+                for (int i = 0; i < VEC / 2; ++i) m = __hmax2_nan(m, *reinterpret_cast<const __half2 *>(&r[u].w[i]));
+            return max_nan(__low2float(m), __high2float(m));
+        }
+    }
+    // The lane's sum of 2^u, and of 2^u u where it is wanted.
+    template <bool TURN>
+    __device__ __forceinline__ float2 sums(float base, float c) const {
+        if constexpr (VEC == 1) {
+            float s[2] = {}, t[2] = {};
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                float w = (to_float(r[u].e) - base) * c;
+                if constexpr (TURN) w = max_nan(w, kLeast);
+                const float e = exp2_approx(w);
+                s[u & 1] += e;
+                if constexpr (TURN) t[u & 1] = fmaf(e, w, t[u & 1]);
+            }
+            return make_float2(s[0] + s[1], t[0] + t[1]);
+        } else {
+            const F2 shift = f2(-base), factor = f2(c);
+            F2 s = f2(0.f), t = f2(0.f);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                F2 v[VEC / 2];
+                unpack2<T, VEC>(r[u], v);
+#pragma unroll
+                for (int i = 0; i < VEC / 2; ++i) {
+                    F2 w = mul2(add2(v[i], shift), factor);
+                    if constexpr (TURN) w = f2(max_nan(low(w), kLeast), max_nan(high(w), kLeast));
+                    const F2 e = f2(exp2_approx(low(w)), exp2_approx(high(w)));
+                    s = add2(s, e);
+                    if constexpr (TURN) t = fma2(e, w, t);
+                }
+            }
+            return make_float2(low(s) + high(s), low(t) + high(t));
+        }
+    }
+    // 2^u factor of vector k.
+    __device__ __forceinline__ Packed<T, VEC> scaled(int k, float base, float c, float factor) const {
+        if constexpr (VEC == 1) {
+            const float f[1] = {exp2_approx((to_float(r[k].e) - base) * c) * factor};
+            return pack<T, 1>(f);
+        } else {
+            F2 v[VEC / 2];
+            unpack2<T, VEC>(r[k], v);
+#pragma unroll
+            for (int i = 0; i < VEC / 2; ++i) {
+                const F2 w = mul2(add2(v[i], f2(-base)), f2(c));
+                v[i] = mul2(f2(exp2_approx(low(w)), exp2_approx(high(w))), f2(factor));
+            }
+            return pack2<T, VEC>(v);
+        }
+    }
+};
+
+struct Piece {
+    float m, sum, turn, unused;
+};
+// b's numbers, taken relative to m, added to `a` (which is relative to m as well).
+__device__ __forceinline__ void add_piece(Piece &a, const Piece &b, float c) {
+    if (b.m == -INFINITY) return;
+    const float d = max_nan((finite_base(b.m) - finite_base(a.m)) * c, kLeast), f = exp2_approx(d);
+    a.sum = fmaf(b.sum, f, a.sum);
+    a.turn = fmaf(fmaf(b.sum, d, b.turn), f, a.turn);
+}
+// Joins the slots; every lane gets the result.
+__device__ __forceinline__ Piece join(const Piece *slots, int count, float c) {
+    const int lane = (int)threadIdx.x % 32;
+    float m = -INFINITY;
+    for (int j = lane; j < count; j += 32) m = max_nan(m, slots[j].m);
+    Piece a = {warp_max_nan(m), 0.f, 0.f, 0.f};
+    for (int j = lane; j < count; j += 32) add_piece(a, slots[j], c);
+    a.sum = warp_sum(a.sum);
+    a.turn = warp_sum(a.turn);
+    return a;
 }
 
 __device__ __forceinline__ int64_t id_at(const void *ids, int id_bytes, int64_t i) {
     return id_bytes == 4 ? (int64_t)static_cast<const int32_t *>(ids)[i] : (int64_t)static_cast<const long long *>(ids)[i];
 }
 
-struct RowStats {
-    float m, base, sum, turn;    // the largest logit; the same, 0 for an infinity; sum of 2^u, u = (x - base) c; sum of 2^u u
-};
+// ---- the best alternatives ------------------------------------------------------------------------------------------------
 
-template <typename T, int VEC>
-__device__ __forceinline__ RowStats row_stats(const T *x, int64_t vocab, float c, float *sm) {
-    const int64_t nvec = vocab / VEC;
-    float m = -INFINITY;
-    for (int64_t v = threadIdx.x; v < nvec; v += kThreads) {
-        float f[VEC];
-        unpack<T, VEC>(load_packed<T, VEC>(x + v * VEC), f);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) m = max_nan(m, f[i]);
-    }
-    m = block_reduce(m, sm, max_nan);
-    RowStats r;
-    r.m = m;
-    r.base = isinf(m) ? 0.f : m;
-    float s = 0.f, t = 0.f;
-    for (int64_t v = threadIdx.x; v < nvec; v += kThreads) {
-        float f[VEC];
-        unpack<T, VEC>(load_packed<T, VEC>(x + v * VEC), f);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float u = max_nan((f[i] - r.base) * c, kLeast), e = exp2_approx(u);
-            s += e;
-            t = fmaf(e, u, t);
-        }
-    }
-    r.sum = block_reduce(s, sm, add);
-    r.turn = block_reduce(t, sm, add);
-    return r;
+// Position in the order of the alternatives: the larger value first, then the lower index; a NaN above everything.
+// No logit has the place 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f);     // -0 counts as 0
+    return x != x ? 0xffffffffu : (b >> 31) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ unsigned long long rank_key(uint32_t order, uint32_t index) { return (unsigned long long)order << 32 | (0xffffffffu - index); }
+__device__ __forceinline__ float key_value(unsigned long long key) {
+    const uint32_t order = (uint32_t)(key >> 32);
+    return __uint_as_float((order >> 31) ? order & 0x7fffffffu : ~order);
 }
 
+// Lists of 32 values in descending order, one a lane.
+__device__ __forceinline__ uint32_t sort_list(uint32_t v) {
+    const int lane = (int)threadIdx.x % 32;
+#pragma unroll
+    for (int k = 2; k <= 32; k *= 2)
+#pragma unroll
+        for (int j = k / 2; j > 0; j /= 2) {
+            const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
+            v = ((lane & k) == 0) == ((lane & j) == 0) ? max(v, o) : min(v, o);
+        }
+    return v;
+}
+// The 32 largest of two sorted lists, sorted.
+__device__ __forceinline__ uint32_t merge_lists(uint32_t a, uint32_t b) {
+    const int lane = (int)threadIdx.x % 32;
+    uint32_t v = max(a, __shfl_sync(0xffffffffu, b, 31 - lane));
+#pragma unroll
+    for (int j = 16; j > 0; j /= 2) {
+        const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
+        v = (lane & j) == 0 ? max(v, o) : min(v, o);
+    }
+    return v;
+}
+
+// Log probability, entropy and alternatives.  Phase one: a warp a chunk; besides the sums each lane leaves the place of its
+// largest logit, and each warp keeps the 32 best of those.  The k-th best over the CTA's warps is a bound that the k best
+// logits reach, since each lane's largest is a logit.  Phase two: only the lanes' elements whose largest reaches the bound are
+// read again (about k times 32 or 64, from L2), into a list a warp; the lists' keys are all different, so counting the larger ones
+// gives each key its rank.  The CTAs of a cluster hand the leader their k best.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) cr_token_log_probs_kernel(const VocabArgs a) {
-    __shared__ float sm[kThreads / 32];
-    __shared__ unsigned long long keys[kThreads / 32];
-    const int64_t row = blockIdx.x;
+__global__ void __launch_bounds__(32 * kScoreWarps, 4) cr_token_log_probs_kernel(const VocabArgs a, int cluster, int slots) {
+    using C = Chunk<T, VEC>;
+    extern __shared__ __align__(16) unsigned char dynamic[];
+    __shared__ uint32_t lists[kScoreWarps][32];
+    __shared__ unsigned long long keys[kScoreWarps * 32], ranked[kMaxCluster * 32];
+    __shared__ uint32_t found;
+    Piece *pieces = reinterpret_cast<Piece *>(dynamic);                                    // [slots], the leader's are used
+    uint32_t *tops = reinterpret_cast<uint32_t *>(pieces + slots);                         // [own slots][32]
+    const int rank = (int)(blockIdx.x % (unsigned)cluster);
+    const int64_t row = blockIdx.x / (unsigned)cluster;
+    const int warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x % 32;
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     const float c = a.inverse * kLog2e;
-    const RowStats r = row_stats<T, VEC>(x, a.vocab, c, sm);
-    const bool nothing = r.sum == 0.f;
-    const float log_sum = log2f(r.sum);
-    if (threadIdx.x == 0) {
-        if (a.stats) reinterpret_cast<float2 *>(a.stats)[row] = make_float2(r.m, kLn2 * log_sum);
-        if (a.entropy) a.entropy[row] = nothing ? 0.f : kLn2 * (log_sum - r.turn / r.sum);
-        if (a.logp) {
-            const int64_t id = id_at(a.ids, a.id_bytes, row);
-            a.logp[row] = id < 0 || id >= a.vocab ? 0.f : nothing ? -INFINITY : kLn2 * ((to_float(x[id]) - r.base) * c - log_sum);
+    const int64_t chunks = (a.vocab + C::kElements - 1) / C::kElements;
+    const int own = (slots - rank + cluster - 1) / cluster;
+    if (a.top > 0) {
+        for (int i = threadIdx.x; i < kMaxCluster * 32; i += blockDim.x) ranked[i] = 0;
+        if (threadIdx.x == 0) found = 0;
+    }
+    arrive(cluster);                     // a CTA's memory may be written from outside only once it runs
+    int64_t id = -1;
+    float picked = 0.f;
+    if (a.logp && rank == 0 && warp == 0) {
+        id = id_at(a.ids, a.id_bytes, row);
+        if (id < 0 || id >= a.vocab) id = -1;
+        else picked = to_float(x[id]);
+    }
+    bool started = false;
+    uint32_t best = 0;
+    for (int k = warp; k < own; k += warps) {
+        const int slot = k * cluster + rank;
+        Piece p = {-INFINITY, 0.f, 0.f, 0.f};
+        uint32_t lane_top = 0;
+        for (int64_t chunk = slot; chunk < chunks; chunk += kSlots) {
+            C d;
+            d.load(x, a.vocab, chunk);
+            const float lm = d.largest();
+            Piece q;
+            q.m = warp_max_nan(lm);
+            const float2 s = d.template sums<true>(finite_base(q.m), c);
+            q.sum = warp_sum(s.x);
+            q.turn = warp_sum(s.y);
+            if (q.m == -INFINITY) q.sum = q.turn = 0.f;
+            if (chunk == slot) {
+                p = q;
+            } else {
+                Piece all = {max_nan(p.m, q.m), 0.f, 0.f, 0.f};
+                add_piece(all, p, c);
+                add_piece(all, q, c);
+                p = all;
+            }
+            if (C::index(chunk, lane, 0, 0) < a.vocab) lane_top = max(lane_top, order_of(lm));
+        }
+        if (a.top > 0) {
+            tops[k * 32 + lane] = lane_top;
+            if (__any_sync(0xffffffffu, lane_top > __shfl_sync(0xffffffffu, best, a.top - 1))) best = merge_lists(best, sort_list(lane_top));
+        }
+        if (!started) wait(cluster);
+        started = true;
+        if (lane == 0) {
+            if (cluster == 1) {
+                pieces[slot] = p;
+            } else {
+                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(address_at(&pieces[slot], 0)), "f"(p.m), "f"(p.sum), "f"(p.turn), "f"(0.f)
+                             : "memory");
+            }
         }
     }
-    unsigned long long last = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-        unsigned long long best = 0;
-        for (int64_t v = threadIdx.x; v < a.vocab; v += kThreads) {
-            const unsigned long long key = rank_key(to_float(x[v]), (uint32_t)v);
-            if ((k == 0 || key < last) && key > best) best = key;
+    if (!started) wait(cluster);
+    if (a.top > 0) lists[warp][lane] = best;
+    meet(cluster);
+    __shared__ float result[2];
+    if (rank == 0 && warp == 0) {
+        const Piece all = join(pieces, slots, c);
+        const float base = finite_base(all.m), log_sum = log2f(all.sum);
+        const bool nothing = all.m == -INFINITY;
+        if (lane == 0) {
+            if (a.stats) reinterpret_cast<float2 *>(a.stats)[row] = make_float2(all.m, kLn2 * log_sum);
+            if (a.entropy) a.entropy[row] = nothing ? 0.f : kLn2 * (log_sum - all.turn / all.sum);
+            if (a.logp) a.logp[row] = id < 0 ? 0.f : nothing ? -INFINITY : kLn2 * ((picked - base) * c - log_sum);
+            result[0] = base;
+            result[1] = log_sum;
         }
+    }
+    if (a.top == 0) return;
+    // the bound
+    for (int half = kScoreWarps / 2; half > 0; half /= 2) {
+        if (half >= warps) continue;
+        if (warp < half && warp + half < warps) lists[warp][lane] = merge_lists(lists[warp][lane], lists[warp + half][lane]);
+        __syncthreads();
+    }
+    const uint32_t bound = max(1u, lists[0][a.top - 1]);
+    unsigned long long list = 0, last = 0;        // this warp's best, and the a.top-th of them
+    for (int k = warp; k < own; k += warps) {
+        const int slot = k * cluster + rank;
+        const uint32_t t = tops[k * 32 + lane];
+        for (uint32_t groups = __ballot_sync(0xffffffffu, t >= bound); groups; groups &= groups - 1) {
+            const int g = __ffs(groups) - 1;
+            // the best that this lane's elements can be
+            if (rank_key(__shfl_sync(0xffffffffu, t, g), (uint32_t)C::index(slot, g, 0, 0)) <= last) continue;
+            for (int64_t chunk = slot; chunk < chunks; chunk += kSlots) {
 #pragma unroll
-        for (int o = 16; o > 0; o /= 2) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-        __syncthreads();
-        if (threadIdx.x % 32 == 0) keys[threadIdx.x / 32] = best;
-        __syncthreads();
-        for (int w = 0; w < kThreads / 32; ++w) best = max(best, keys[w]);
-        last = best;
-        if (threadIdx.x == 0) {
-            const uint32_t id = 0xffffffffu - (uint32_t)best;
-            if (a.id_bytes == 4) static_cast<int32_t *>(a.top_ids)[row * a.top + k] = (int32_t)id;
-            else static_cast<long long *>(a.top_ids)[row * a.top + k] = (long long)id;
-            a.top_logp[row * a.top + k] = nothing ? -INFINITY : kLn2 * ((key_value(best) - r.base) * c - log_sum);
+                for (int q = 0; q < C::kLane; q += 32) {
+                    const int64_t v = C::index(chunk, g, (q + lane) / VEC, (q + lane) % VEC);
+                    unsigned long long key = 0;
+                    if (v < a.vocab) key = rank_key(order_of(to_float(x[v])), (uint32_t)v);
+                    const bool may = (uint32_t)(key >> 32) >= bound && key > last;
+                    for (uint32_t some = __ballot_sync(0xffffffffu, may); some; some &= some - 1) {
+                        const unsigned long long next = __shfl_sync(0xffffffffu, key, __ffs(some) - 1);
+                        if (next <= last) continue;
+                        const int place = __popc(__ballot_sync(0xffffffffu, list > next));
+                        const unsigned long long up = __shfl_up_sync(0xffffffffu, list, 1);
+                        list = lane < place ? list : lane == place ? next : up;
+                        last = __shfl_sync(0xffffffffu, list, a.top - 1);
+                    }
+                }
+            }
         }
+    }
+    const bool mine = lane < a.top && list != 0;
+    const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
+    uint32_t at = 0;
+    if (lane == 0 && count) at = atomicAdd(&found, count);
+    at = __shfl_sync(0xffffffffu, at, 0);
+    if (mine) keys[at + lane] = list;
+    __syncthreads();
+    auto put = [&](unsigned long long key, int place) {
+        const uint32_t v = 0xffffffffu - (uint32_t)key;
+        if (a.id_bytes == 4) static_cast<int32_t *>(a.top_ids)[row * a.top + place] = (int32_t)v;
+        else static_cast<long long *>(a.top_ids)[row * a.top + place] = (long long)v;
+        const float f = key_value(key);
+        a.top_logp[row * a.top + place] = isinf(result[1]) && result[1] < 0.f ? -INFINITY : kLn2 * ((f - result[0]) * c - result[1]);
+    };
+    const int n = (int)found;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const unsigned long long key = keys[i];
+        int place = 0;
+        for (int j = 0; j < n; ++j) place += keys[j] > key;
+        if (place >= a.top) continue;
+        if (cluster == 1) put(key, place);
+        else asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(address_at(&ranked[rank * 32 + place], 0)), "l"(key) : "memory");
+    }
+    if (cluster == 1) return;
+    meet(cluster);
+    if (rank != 0) return;
+    for (int i = threadIdx.x; i < cluster * 32; i += blockDim.x) {
+        const unsigned long long key = ranked[i];
+        if (key == 0) continue;
+        int place = 0;
+        for (int j = 0; j < cluster * 32; ++j) place += ranked[j] > key;
+        if (place < a.top) put(key, place);
     }
 }
+
+// ---- their gradient ---------------------------------------------------------------------------------------------------------
+
+constexpr int kGradThreads = 256;
+template <int VEC> __host__ __device__ constexpr int grad_unroll() { return VEC == 1 ? 16 : 4; }
 
 // A tile of a row a block.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) cr_token_log_probs_grad_kernel(const VocabArgs a, unsigned tiles) {
-    constexpr int kUnroll = 4;
-    const int64_t row = blockIdx.x / tiles, first = (int64_t)(blockIdx.x % tiles) * kThreads * kUnroll;
+__global__ void __launch_bounds__(kGradThreads) cr_token_log_probs_grad_kernel(const VocabArgs a, unsigned tiles) {
+    constexpr int kUnroll = grad_unroll<VEC>();
+    const int64_t row = blockIdx.x / tiles, first = (int64_t)(blockIdx.x % tiles) * kGradThreads * kUnroll;
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     T *d = static_cast<T *>(a.dlogits) + row * a.ld_d;
     const int64_t nvec = a.vocab / VEC;
@@ -149,7 +422,7 @@ __global__ void __launch_bounds__(kThreads) cr_token_log_probs_grad_kernel(const
     const float level = gb != 0.f ? fmaf(gb, a.entropy[row], ga) : ga, turn = gb * kLn2;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-        const int64_t v = first + u * kThreads + (int)threadIdx.x;
+        const int64_t v = first + u * kGradThreads + (int)threadIdx.x;
         if (v >= nvec) break;
         float f[VEC] = {};
         if (!none) {
@@ -166,64 +439,143 @@ __global__ void __launch_bounds__(kThreads) cr_token_log_probs_grad_kernel(const
 
 // ---- distillation --------------------------------------------------------------------------------------------------------
 
-constexpr int kMostTop = 1024;
+constexpr int kSeenWords = 256;
 
+// One warp takes the teacher: its shares, and the loss once the row's sums are there.  The others take a chunk each, keep it in
+// registers over the exchange of the sums (the last one, where a warp has several) and write the gradient; then they mend the
+// elements of their own chunk that the teacher names.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) cr_distill_kernel(const VocabArgs a) {
-    __shared__ float sm[kThreads / 32];
-    __shared__ float share[kMostTop], logit[kMostTop];
-    __shared__ int32_t named[kMostTop];
-    const int64_t row = blockIdx.x;
+__global__ void __launch_bounds__(32 * (kDistillWarps + 1), 4) cr_distill_kernel(const VocabArgs a, int cluster, int slots) {
+    using C = Chunk<T, VEC>;
+    extern __shared__ __align__(16) unsigned char dynamic[];
+    Piece *pieces = reinterpret_cast<Piece *>(dynamic);               // [slots]
+    float *share = reinterpret_cast<float *>(pieces + slots);         // [top]
+    float *logit = share + a.top;
+    float *merged = logit + a.top;
+    int32_t *named = reinterpret_cast<int32_t *>(merged + a.top);
+    __shared__ int wanted;
+    __shared__ uint32_t seen[kSeenWords], twice[kSeenWords];
+    const int rank = (int)(blockIdx.x % (unsigned)cluster);
+    const int64_t row = blockIdx.x / (unsigned)cluster;
+    const int warps = (int)blockDim.x / 32 - 1, warp = (int)threadIdx.x / 32 - 1, lane = (int)threadIdx.x % 32;   // warp -1: the teacher's
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     T *d = a.dlogits ? static_cast<T *>(a.dlogits) + row * a.ld_d : nullptr;
     const float c = a.inverse * kLog2e;
     const float w = a.weight ? a.weight[row] : 1.f;
-    // the teacher
-    float best = -INFINITY;
-    for (int j = threadIdx.x; j < a.top; j += kThreads) {
-        const int64_t id = id_at(a.ids, a.id_bytes, row * a.top + j);
-        const bool there = id >= 0 && id < a.vocab;
-        named[j] = there ? (int32_t)id : -1;
-        logit[j] = there ? to_float(x[id]) : 0.f;
-        share[j] = there ? a.teacher[row * a.top + j] * c : -INFINITY;
-        best = max_nan(best, share[j]);
-    }
-    best = block_reduce(best, sm, max_nan);
-    const bool left_out = best == -INFINITY;
-    float mass = 0.f;
-    for (int j = threadIdx.x; j < a.top; j += kThreads) mass += exp2_approx(share[j] - best);
-    mass = block_reduce(mass, sm, add);
-    RowStats r = {0.f, 0.f, 1.f, 0.f};
-    if (!left_out && (a.loss || (d && w != 0.f))) r = row_stats<T, VEC>(x, a.vocab, c, sm);
-    const float log_sum = log2f(r.sum), log_mass = log2f(mass);
-    float loss = 0.f;
-    for (int j = threadIdx.x; j < a.top; j += kThreads) {
-        const float u = share[j] - best, p = left_out ? 0.f : exp2_approx(u) / mass;
-        share[j] = p;
-        if (p != 0.f) loss += p * ((u - log_mass) - (r.sum == 0.f ? -INFINITY : (logit[j] - r.base) * c - log_sum));
-    }
-    loss = block_reduce(loss, sm, add);
-    if (threadIdx.x == 0 && a.loss) a.loss[row] = left_out ? 0.f : a.temperature * a.temperature * kLn2 * loss;
-    if (!d) return;
-    const int64_t nvec = a.vocab / VEC;
-    const bool none = left_out || w == 0.f;
-    const float scale = w * a.temperature, factor = r.sum == 0.f ? 0.f : scale / r.sum;
-    for (int64_t v = threadIdx.x; v < nvec; v += kThreads) {
-        float f[VEC] = {};
-        if (!none) {
-            unpack<T, VEC>(load_packed<T, VEC>(x + v * VEC), f);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) f[i] = exp2_approx((f[i] - r.base) * c) * factor;
+    const int64_t chunks = (a.vocab + C::kElements - 1) / C::kElements;
+    const int own = (slots - rank + cluster - 1) / cluster;
+    C data;
+    float mass = 0.f, best = -INFINITY;
+    arrive(cluster);
+    if (warp < 0) {
+        for (int i = lane; i < kSeenWords; i += 32) seen[i] = twice[i] = 0;
+        __syncwarp();
+        for (int j = lane; j < a.top; j += 32) {
+            const int64_t id = id_at(a.ids, a.id_bytes, row * a.top + j);
+            const bool there = id >= 0 && id < a.vocab;
+            named[j] = there ? (int32_t)id : -1;
+            logit[j] = there ? to_float(x[id]) : 0.f;
+            share[j] = there ? a.teacher[row * a.top + j] * c : -INFINITY;
+            best = max_nan(best, share[j]);
+            if (there && d) {
+                const uint32_t bit = 1u << (id % 32), word = (uint32_t)(id / 32) % kSeenWords;
+                if (atomicOr(&seen[word], bit) & bit) atomicOr(&twice[word], bit);
+            }
         }
-        store_packed<T, VEC>(d + v * VEC, pack<T, VEC>(f));
+        best = warp_max_nan(best);
+        for (int j = lane; j < a.top; j += 32) mass += exp2_approx(share[j] - best);
+        mass = warp_sum(mass);
+        if (lane == 0) wanted = best != -INFINITY;
+        wait(cluster);
+    } else {
+        bool started = false;
+        for (int k = warp; k < own; k += warps) {
+            const int slot = k * cluster + rank;
+            Piece p = {-INFINITY, 0.f, 0.f, 0.f};
+            for (int64_t chunk = slot; chunk < chunks; chunk += kSlots) {
+                data.load(x, a.vocab, chunk);
+                Piece q = {warp_max_nan(data.largest()), 0.f, 0.f, 0.f};
+                q.sum = warp_sum(data.template sums<false>(finite_base(q.m), c).x);
+                if (q.m == -INFINITY) q.sum = 0.f;
+                if (chunk == slot) {
+                    p = q;
+                } else {
+                    Piece all = {max_nan(p.m, q.m), 0.f, 0.f, 0.f};
+                    add_piece(all, p, c);
+                    add_piece(all, q, c);
+                    p = all;
+                }
+            }
+            if (!started) wait(cluster);
+            started = true;
+            if (cluster == 1) {
+                if (lane == 0) pieces[slot] = p;
+            } else if (lane < cluster) {
+                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(address_at(&pieces[slot], lane)), "f"(p.m), "f"(p.sum), "f"(0.f), "f"(0.f)
+                             : "memory");
+            }
+        }
+        if (!started) wait(cluster);
     }
-    if (none) return;
-    __syncthreads();
-    for (int j = threadIdx.x; j < a.top; j += kThreads) {
-        if (named[j] < 0) continue;
-        float p = 0.f;     // a token may be named more than once
-        for (int i = 0; i < a.top; ++i) p += named[i] == named[j] ? share[i] : 0.f;
-        d[named[j]] = from_float<T>(fmaf(exp2_approx((logit[j] - r.base) * c), factor, -scale * p));
+    meet(cluster);
+    const Piece all = join(pieces, slots, c);
+    const float base = finite_base(all.m), log_sum = log2f(all.sum);
+    const bool left_out = !wanted, empty = all.m == -INFINITY;
+    // the teacher's shares are needed by all warps
+    if (warp < 0) {
+        const float log_mass = log2f(mass);
+        float loss = 0.f;
+        for (int j = lane; j < a.top; j += 32) {
+            const float u = share[j] - best, p = left_out ? 0.f : exp2_approx(u) / mass;
+            share[j] = p;
+            if (p != 0.f) loss += p * ((u - log_mass) - (empty ? -INFINITY : (logit[j] - base) * c - log_sum));
+        }
+        loss = warp_sum(loss);
+        // A token that is named more than once: each of its places gets the sum, in one order.  `seen` has the tokens' bits, `twice`
+        // those that came again: few others share a bit with them.
+        for (int j0 = 0; d && j0 < a.top; j0 += 32) {
+            const int j = j0 + lane;
+            const bool again = j < a.top && named[j] >= 0 && (twice[(named[j] / 32) % kSeenWords] >> (named[j] % 32) & 1u);
+            for (uint32_t some = __ballot_sync(0xffffffffu, again); some; some &= some - 1) {
+                const int k = j0 + __ffs(some) - 1;
+                float p = 0.f;
+                for (int i = lane; i < a.top; i += 32) p += named[i] == named[k] ? share[i] : 0.f;
+                p = warp_sum(p);
+                if (lane == 0) merged[k] = p;
+            }
+            if (j < a.top && !again) merged[j] = share[j];
+        }
+        if (lane == 0 && rank == 0 && a.loss) a.loss[row] = left_out ? 0.f : a.temperature * a.temperature * kLn2 * loss;
+    }
+    if (!d) return;
+    const bool none = left_out || w == 0.f;
+    if (!none) __syncthreads();
+    if (warp < 0 || warp >= own) return;
+    const float scale = w * a.temperature, factor = empty ? 0.f : scale / all.sum;
+    // the warp's slots from the last one back: that one's last chunk is still in registers
+    const int last = warp + (own - 1 - warp) / warps * warps;
+    bool held = true;
+    for (int k = last; k >= 0; k -= warps) {
+        const int slot = k * cluster + rank;
+        for (int64_t chunk = slot + (chunks - 1 - slot) / kSlots * kSlots; chunk >= 0; chunk -= kSlots) {
+            if (!held && !none) data.load(x, a.vocab, chunk);
+            held = false;
+#pragma unroll
+            for (int u = 0; u < C::kUnroll; ++u) {
+                const int64_t v = C::index(chunk, lane, u, 0);
+                Packed<T, VEC> out = {};
+                if (!none) out = data.scaled(u, base, c, factor);
+                if (v < a.vocab) store_packed<T, VEC>(d + v, out);
+            }
+            if (none) continue;
+            __syncwarp();
+            const int64_t first = chunk * C::kElements;
+            for (int j = lane; j < a.top; j += 32) {
+                const int64_t v = named[j];
+                if (v < first || v >= first + C::kElements) continue;
+                d[v] = from_float<T>(fmaf(exp2_approx((logit[j] - base) * c), factor, -scale * merged[j]));
+            }
+        }
     }
 }
 
@@ -236,37 +588,76 @@ cudaError_t by_form(const VocabArgs &a, F &&f) {
     });
 }
 
+// How a row is shared.  The result does not depend on it.
+struct Share {
+    int cluster, warps, slots;
+};
+Share share_row(int64_t rows, int64_t vocab, int64_t chunk_elements, int most_warps, int sm_count) {
+    Share s;
+    s.slots = (int)std::min<int64_t>(kSlots, (vocab + chunk_elements - 1) / chunk_elements);
+    // as many CTAs as leave every SM at most one, while there are slots for them
+    s.cluster = 1;
+    while (s.cluster < kMaxCluster && s.cluster * 2 <= s.slots && rows * s.cluster * 2 <= sm_count) s.cluster *= 2;
+    s.warps = std::min(most_warps, (s.slots + s.cluster - 1) / s.cluster);
+    return s;
+}
+
+template <typename K>
+cudaError_t launch(K kernel, const VocabArgs &a, const Share &s, int threads, size_t smem, cudaStream_t stream, int64_t *launches) {
+    if (a.rows > 0x7fffffffll / s.cluster) return cudaErrorInvalidValue;
+    if (smem > 32 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.rows * s.cluster));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)s.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = s.cluster > 1 ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, s.cluster, s.slots);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
 }  // namespace
 
-cudaError_t launch_token_log_probs(const VocabArgs &a, const DeviceInfo &, cudaStream_t stream, int64_t *launches) {
+cudaError_t launch_token_log_probs(const VocabArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches) {
     if (a.rows == 0) return cudaSuccess;
     return by_form(a, [&](auto t, auto v) {
-        cr_token_log_probs_kernel<decltype(t), decltype(v)::value><<<(unsigned)a.rows, kThreads, 0, stream>>>(a);
-        const cudaError_t e = cudaGetLastError();
-        if (e == cudaSuccess) ++*launches;
-        return e;
+        using T = decltype(t);
+        constexpr int VEC = decltype(v)::value;
+        const Share s = share_row(a.rows, a.vocab, Chunk<T, VEC>::kElements, kScoreWarps, dev.sm_count);
+        const size_t smem = (size_t)s.slots * sizeof(Piece) + (a.top > 0 ? (size_t)((s.slots + s.cluster - 1) / s.cluster) * 128 : 0);
+        return launch(cr_token_log_probs_kernel<T, VEC>, a, s, 32 * s.warps, smem, stream, launches);
     });
 }
 
 cudaError_t launch_token_log_probs_backward(const VocabArgs &a, cudaStream_t stream, int64_t *launches) {
     if (a.rows == 0) return cudaSuccess;
     return by_form(a, [&](auto t, auto v) {
-        const int64_t nvec = a.vocab / decltype(v)::value, tiles = (nvec + kThreads * 4 - 1) / (kThreads * 4);
+        constexpr int VEC = decltype(v)::value, kTile = kGradThreads * grad_unroll<VEC>();
+        const int64_t nvec = a.vocab / VEC, tiles = (nvec + kTile - 1) / kTile;
         if (a.rows > 0x7fffffffll / tiles) return cudaErrorInvalidValue;
-        cr_token_log_probs_grad_kernel<decltype(t), decltype(v)::value><<<(unsigned)(a.rows * tiles), kThreads, 0, stream>>>(a, (unsigned)tiles);
+        cr_token_log_probs_grad_kernel<decltype(t), VEC><<<(unsigned)(a.rows * tiles), kGradThreads, 0, stream>>>(a, (unsigned)tiles);
         const cudaError_t e = cudaGetLastError();
         if (e == cudaSuccess) ++*launches;
         return e;
     });
 }
 
-cudaError_t launch_distill(const VocabArgs &a, const DeviceInfo &, cudaStream_t stream, int64_t *launches) {
+cudaError_t launch_distill(const VocabArgs &a, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches) {
     if (a.rows == 0) return cudaSuccess;
     return by_form(a, [&](auto t, auto v) {
-        cr_distill_kernel<decltype(t), decltype(v)::value><<<(unsigned)a.rows, kThreads, 0, stream>>>(a);
-        const cudaError_t e = cudaGetLastError();
-        if (e == cudaSuccess) ++*launches;
-        return e;
+        using T = decltype(t);
+        constexpr int VEC = decltype(v)::value;
+        const Share s = share_row(a.rows, a.vocab, Chunk<T, VEC>::kElements, kDistillWarps, dev.sm_count);
+        return launch(cr_distill_kernel<T, VEC>, a, s, 32 * (s.warps + 1), (size_t)s.slots * sizeof(Piece) + (size_t)a.top * 16, stream, launches);
     });
 }
 
