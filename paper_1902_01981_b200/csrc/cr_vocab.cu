@@ -216,7 +216,7 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
     return __uint_as_float((order >> 31) ? order & 0x7fffffffu : ~order);
 }
 
-// Lists of 32 values in descending order, one a lane.
+// 32 values in descending order, one a lane.
 __device__ __forceinline__ uint32_t sort_list(uint32_t v) {
     const int lane = (int)threadIdx.x % 32;
 #pragma unroll
@@ -240,18 +240,21 @@ __device__ __forceinline__ uint32_t merge_lists(uint32_t a, uint32_t b) {
     return v;
 }
 
+// A warp keeps this many logits that reach the bound; where ties bring more, it goes over them again with a sorted list.
+constexpr int kKept = 64;
+
 // Log probability, entropy and alternatives.  Phase one: a warp a chunk; besides the sums each lane leaves the place of its
-// largest logit, and each warp keeps the 32 best of those.  The k-th best over the CTA's warps is a bound that the k best
-// logits reach, since each lane's largest is a logit.  Phase two: only the lanes' elements whose largest reaches the bound are
-// read again (about k times 32 or 64, from L2), into a list a warp; the lists' keys are all different, so counting the larger ones
-// gives each key its rank.  The CTAs of a cluster hand the leader their k best.
+// largest logit, and each warp sorts its lanes' largest.  The k-th of these, merged over the warps, is a bound that at least k
+// logits reach, and hardly more than k do.  Phase two: only the lanes whose largest reaches the bound have their elements
+// read again (32 or 64 each, from L2), four lanes' at a time; what reaches the bound is kept, and as all keys differ, counting
+// the larger ones gives each its rank.  The CTAs of a cluster hand the leader their k best.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(32 * kScoreWarps, 4) cr_token_log_probs_kernel(const VocabArgs a, int cluster, int slots) {
+__global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel(const VocabArgs a, int cluster, int slots) {
     using C = Chunk<T, VEC>;
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ uint32_t lists[kScoreWarps][32];
-    __shared__ unsigned long long keys[kScoreWarps * 32], ranked[kMaxCluster * 32];
-    __shared__ uint32_t found;
+    __shared__ int found;
+    __shared__ unsigned long long keys[kScoreWarps][kKept], together[kScoreWarps * kKept], ranked[kMaxCluster * 32];
     Piece *pieces = reinterpret_cast<Piece *>(dynamic);                                    // [slots], the leader's are used
     uint32_t *tops = reinterpret_cast<uint32_t *>(pieces + slots);                         // [own slots][32]
     const int rank = (int)(blockIdx.x % (unsigned)cluster);
@@ -283,11 +286,10 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 4) cr_token_log_probs_kernel
             C d;
             d.load(x, a.vocab, chunk);
             const float lm = d.largest();
-            Piece q;
-            q.m = warp_max_nan(lm);
-            const float2 s = d.template sums<true>(finite_base(q.m), c);
+            Piece q = {warp_max_nan(lm), 0.f, 0.f, 0.f};
+            const float2 s = a.entropy ? d.template sums<true>(finite_base(q.m), c) : d.template sums<false>(finite_base(q.m), c);
             q.sum = warp_sum(s.x);
-            q.turn = warp_sum(s.y);
+            if (a.entropy) q.turn = warp_sum(s.y);
             if (q.m == -INFINITY) q.sum = q.turn = 0.f;
             if (chunk == slot) {
                 p = q;
@@ -301,7 +303,7 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 4) cr_token_log_probs_kernel
         }
         if (a.top > 0) {
             tops[k * 32 + lane] = lane_top;
-            if (__any_sync(0xffffffffu, lane_top > __shfl_sync(0xffffffffu, best, a.top - 1))) best = merge_lists(best, sort_list(lane_top));
+            best = max(best, lane_top);
         }
         if (!started) wait(cluster);
         started = true;
@@ -315,7 +317,7 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 4) cr_token_log_probs_kernel
         }
     }
     if (!started) wait(cluster);
-    if (a.top > 0) lists[warp][lane] = best;
+    if (a.top > 0) lists[warp][lane] = best = sort_list(best);
     meet(cluster);
     __shared__ float result[2];
     if (rank == 0 && warp == 0) {
@@ -331,46 +333,79 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 4) cr_token_log_probs_kernel
         }
     }
     if (a.top == 0) return;
-    // the bound
     for (int half = kScoreWarps / 2; half > 0; half /= 2) {
         if (half >= warps) continue;
-        if (warp < half && warp + half < warps) lists[warp][lane] = merge_lists(lists[warp][lane], lists[warp + half][lane]);
+        if (warp < half && warp + half < warps) lists[warp][lane] = best = merge_lists(best, lists[warp + half][lane]);
         __syncthreads();
     }
     const uint32_t bound = max(1u, lists[0][a.top - 1]);
-    unsigned long long list = 0, last = 0;        // this warp's best, and the a.top-th of them
+    const float bound_value = key_value((unsigned long long)bound << 32);
+    int count = 0;
+    const uint32_t below = (1u << lane) - 1u;
+    constexpr int kGroups = 32 / C::kUnroll;          // lanes' elements that the warp looks at together, a vector a lane
     for (int k = warp; k < own; k += warps) {
         const int slot = k * cluster + rank;
-        const uint32_t t = tops[k * 32 + lane];
-        for (uint32_t groups = __ballot_sync(0xffffffffu, t >= bound); groups; groups &= groups - 1) {
-            const int g = __ffs(groups) - 1;
-            // the best that this lane's elements can be
-            if (rank_key(__shfl_sync(0xffffffffu, t, g), (uint32_t)C::index(slot, g, 0, 0)) <= last) continue;
-            for (int64_t chunk = slot; chunk < chunks; chunk += kSlots) {
+        uint32_t groups = __ballot_sync(0xffffffffu, tops[k * 32 + lane] >= bound);
+        while (groups) {
+            int g = -1;
 #pragma unroll
-                for (int q = 0; q < C::kLane; q += 32) {
-                    const int64_t v = C::index(chunk, g, (q + lane) / VEC, (q + lane) % VEC);
-                    unsigned long long key = 0;
-                    if (v < a.vocab) key = rank_key(order_of(to_float(x[v])), (uint32_t)v);
-                    const bool may = (uint32_t)(key >> 32) >= bound && key > last;
-                    for (uint32_t some = __ballot_sync(0xffffffffu, may); some; some &= some - 1) {
-                        const unsigned long long next = __shfl_sync(0xffffffffu, key, __ffs(some) - 1);
-                        if (next <= last) continue;
-                        const int place = __popc(__ballot_sync(0xffffffffu, list > next));
-                        const unsigned long long up = __shfl_up_sync(0xffffffffu, list, 1);
-                        list = lane < place ? list : lane == place ? next : up;
-                        last = __shfl_sync(0xffffffffu, list, a.top - 1);
-                    }
+            for (int b = 0; b < kGroups; ++b) {
+                if (lane / C::kUnroll == b) g = __ffs(groups) - 1;
+                groups &= groups - 1;
+            }
+            for (int64_t chunk = slot; chunk < chunks; chunk += kSlots) {
+                const int64_t v = C::index(chunk, g, lane % C::kUnroll, 0);
+                const bool in = g >= 0 && v < a.vocab;
+                float f[VEC];
+                if (in) unpack<T, VEC>(load_packed<T, VEC>(x + v), f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const bool reaches = in && !(f[i] < bound_value);      // a NaN does
+                    const uint32_t some = __ballot_sync(0xffffffffu, reaches);
+                    if (some == 0) continue;
+                    const int at = count + __popc(some & below);
+                    if (reaches && at < kKept) keys[warp][at] = rank_key(order_of(f[i]), (uint32_t)(v + i));
+                    count += __popc(some);
                 }
             }
         }
     }
-    const bool mine = lane < a.top && list != 0;
-    const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
-    uint32_t at = 0;
-    if (lane == 0 && count) at = atomicAdd(&found, count);
+    if (count > kKept) {
+        // the warp's best in a sorted list, and the a.top-th of them
+        unsigned long long list = 0, last = 0;
+        for (int k = warp; k < own; k += warps) {
+            const int slot = k * cluster + rank;
+            const uint32_t t = tops[k * 32 + lane];
+            for (uint32_t groups = __ballot_sync(0xffffffffu, t >= bound); groups; groups &= groups - 1) {
+                const int g = __ffs(groups) - 1;
+                // the best that this lane's elements can be
+                if (rank_key(__shfl_sync(0xffffffffu, t, g), (uint32_t)C::index(slot, g, 0, 0)) <= last) continue;
+                for (int64_t chunk = slot; chunk < chunks; chunk += kSlots) {
+#pragma unroll 1
+                    for (int q = 0; q < C::kLane; q += 32) {
+                        const int64_t v = C::index(chunk, g, (q + lane) / VEC, (q + lane) % VEC);
+                        const unsigned long long key = v < a.vocab ? rank_key(order_of(to_float(x[v])), (uint32_t)v) : 0;
+                        for (uint32_t some = __ballot_sync(0xffffffffu, key > last); some; some &= some - 1) {
+                            const unsigned long long next = __shfl_sync(0xffffffffu, key, __ffs(some) - 1);
+                            if (next <= last) continue;
+                            const int place = __popc(__ballot_sync(0xffffffffu, list > next));
+                            const unsigned long long up = __shfl_up_sync(0xffffffffu, list, 1);
+                            list = lane < place ? list : lane == place ? next : up;
+                            last = __shfl_sync(0xffffffffu, list, a.top - 1);
+                        }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+        keys[warp][lane] = list;
+        count = a.top;
+    }
+    __syncwarp();
+    int at = 0;
+    if (lane == 0 && count > 0) at = atomicAdd(&found, count);
     at = __shfl_sync(0xffffffffu, at, 0);
-    if (mine) keys[at + lane] = list;
+    for (int i = lane; i < count; i += 32) together[at + i] = keys[warp][i];
     __syncthreads();
     auto put = [&](unsigned long long key, int place) {
         const uint32_t v = 0xffffffffu - (uint32_t)key;
@@ -379,11 +414,12 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 4) cr_token_log_probs_kernel
         const float f = key_value(key);
         a.top_logp[row * a.top + place] = isinf(result[1]) && result[1] < 0.f ? -INFINITY : kLn2 * ((f - result[0]) * c - result[1]);
     };
-    const int n = (int)found;
+    const int n = found;
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const unsigned long long key = keys[i];
+        const unsigned long long key = together[i];
         int place = 0;
-        for (int j = 0; j < n; ++j) place += keys[j] > key;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) place += together[j] > key;
         if (place >= a.top) continue;
         if (cluster == 1) put(key, place);
         else asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(address_at(&ranked[rank * 32 + place], 0)), "l"(key) : "memory");
