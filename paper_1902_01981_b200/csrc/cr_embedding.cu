@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kLookupThreads) cr_embedding_kernel(const I *i
 
 // ---- sorting a partition's tokens -----------------------------------------------------------------------------------------
 
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigitBits = 8, kBins = 1 << kDigitBits, kMaxCluster = 8;
+constexpr int kDigitBits = 8, kBins = 1 << kDigitBits, kMaxCluster = 8;
 
 __device__ __forceinline__ void sort_meet(int cluster) {
     if (cluster == 1) {
@@ -80,11 +80,12 @@ __device__ __forceinline__ uint32_t peer_word(const uint32_t *w, int rank) {
 // the lowest up, each pass stable.  A cluster of CTAs takes a partition; each warp owns a run of consecutive entries, counts
 // its digits (lanes with one digit find each other by match), and after the counts of all warps have been summed up it
 // puts its entries in place in order.  The buffers are in global memory (L2).  Bound by latency: a few dependent steps a pass.
-template <typename I>
-__global__ void __launch_bounds__(kSortThreads) cr_token_sort_kernel(const I *ids, int tokens, int64_t vocab, int64_t padding, int passes, uint2 *pairs,
-                                                                     int32_t *counts, int cluster) {
-    __shared__ uint32_t hist[kSortWarps][kBins];
-    __shared__ uint32_t total[kBins], scan[kBins / 32 + 1];
+template <typename I, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const I *ids, int tokens, int64_t vocab, int64_t padding, int passes, uint2 *pairs,
+                                                                   int32_t *counts, int cluster) {
+    static_assert(WARPS * 32 >= kBins, "a thread a bin");
+    __shared__ uint32_t hist[WARPS][kBins];
+    __shared__ uint32_t total[kBins], scan[kBins / 32];
     const int64_t part = blockIdx.x / (unsigned)cluster;
     const int rank = (int)(blockIdx.x % (unsigned)cluster), tid = (int)threadIdx.x, warp = tid / 32, lane = tid % 32;
     const uint32_t below = (1u << lane) - 1u;
@@ -92,13 +93,13 @@ __global__ void __launch_bounds__(kSortThreads) cr_token_sort_kernel(const I *id
     uint2 *buffer[2] = {pairs + part * 2 * tokens, pairs + (part * 2 + 1) * tokens};
     int count = tokens;
     for (int pass = 0; pass < passes; ++pass) {
-        const uint2 *from = buffer[pass & 1];
         // the last pass writes into buffer 0
-        uint2 *to = buffer[(pass & 1) ^ 1];
-        if (passes & 1) { from = buffer[(pass & 1) ^ 1]; to = buffer[pass & 1]; }
-        const int64_t warps = (int64_t)cluster * kSortWarps;
+        const int into = (passes - 1 - pass) & 1;
+        const uint2 *from = buffer[into ^ 1];
+        uint2 *to = buffer[into];
+        const int64_t warps = (int64_t)cluster * WARPS;
         const int64_t each = (count + warps * 32 - 1) / (warps * 32) * 32;
-        const int64_t begin = min((int64_t)count, (rank * kSortWarps + warp) * each), end = min((int64_t)count, begin + each);
+        const int64_t begin = min((int64_t)count, (rank * WARPS + warp) * each), end = min((int64_t)count, begin + each);
         auto entry = [&](int64_t i, uint2 &e) -> uint32_t {      // the digit; kBins: no entry
             if (i >= end) return kBins;
             if (pass == 0) {
@@ -120,11 +121,14 @@ __global__ void __launch_bounds__(kSortThreads) cr_token_sort_kernel(const I *id
             __syncwarp();
         }
         __syncthreads();
+        uint32_t column[WARPS], sum = 0;         // a bin's counts, all in flight at once
         if (tid < kBins) {
-            uint32_t sum = 0;
-            for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t t = hist[w][tid];
-                hist[w][tid] = sum;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) column[w] = hist[w][tid];
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const uint32_t t = column[w];
+                column[w] = sum;
                 sum += t;
             }
             total[tid] = sum;
@@ -132,10 +136,17 @@ __global__ void __launch_bounds__(kSortThreads) cr_token_sort_kernel(const I *id
         sort_meet(cluster);
         uint32_t mine = 0, before = 0, inclusive = 0;
         if (tid < kBins) {
-            for (int r = 0; r < cluster; ++r) {
-                const uint32_t v = cluster == 1 ? total[tid] : peer_word(&total[tid], r);
-                if (r < rank) before += v;
-                mine += v;
+            if (cluster == 1) {
+                mine = sum;
+            } else {
+                uint32_t v[kMaxCluster];
+#pragma unroll
+                for (int r = 0; r < kMaxCluster; ++r) v[r] = r < cluster ? peer_word(&total[tid], r) : 0;
+#pragma unroll
+                for (int r = 0; r < kMaxCluster; ++r) {
+                    if (r < rank) before += v[r];
+                    mine += v[r];
+                }
             }
             inclusive = mine;
 #pragma unroll
@@ -147,13 +158,15 @@ __global__ void __launch_bounds__(kSortThreads) cr_token_sort_kernel(const I *id
         }
         __syncthreads();
         uint32_t all = 0;
+#pragma unroll
         for (int w = 0; w < kBins / 32; ++w) {
             if (w < warp) before += scan[w];
             all += scan[w];
         }
         if (tid < kBins) {
             before += inclusive - mine;
-            for (int w = 0; w < kSortWarps; ++w) hist[w][tid] += before;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) hist[w][tid] = before + column[w];
         }
         __syncthreads();
         for (int64_t i = begin; i < end; i += 32) {
@@ -200,12 +213,12 @@ __device__ __forceinline__ void store_floats(float *p, const float (&v)[VEC], fl
 // write a sum wherever the number changes: into the table's row where the number's first token is in this tile, into the
 // tile's row of pieces where it is not.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const GradArgs a, int across, int slabs) {
+__device__ __forceinline__ void sum_tile(const GradArgs &a, unsigned block, int across, int slabs) {
     constexpr int kUnroll = 8;
     const int per_block = kSumThreads / across;
     const int groups = (a.tiles + per_block - 1) / per_block;
-    const unsigned item = blockIdx.x / (unsigned)slabs;
-    const int slab = (int)(blockIdx.x % (unsigned)slabs);
+    const unsigned item = block / (unsigned)slabs;
+    const int slab = (int)(block % (unsigned)slabs);
     const int64_t part = item / (unsigned)groups;
     const int tile = (int)(item % (unsigned)groups) * per_block + (int)threadIdx.x / across;
     const int col = (slab * across + (int)threadIdx.x % across) * VEC;
@@ -244,63 +257,101 @@ __global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const Gr
     }
 }
 
-// Numbers whose tokens reach into further tiles: the block of the first such tile adds the tiles' pieces to the row.  Eight
-// warps take every eighth piece each and are summed in order.
-__global__ void __launch_bounds__(256) cr_embedding_join_kernel(const GradArgs a, int slabs) {
-    __shared__ float sm[8][32];
-    const unsigned item = blockIdx.x / (unsigned)slabs;
-    const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, col = (int)(blockIdx.x % (unsigned)slabs) * 32 + lane;
-    const int64_t part = item / (unsigned)(a.tiles - 1);
-    const int64_t tile = item % (unsigned)(a.tiles - 1) + 1, n = a.counts[part];
-    const uint2 *pairs = a.pairs + part * 2 * a.tokens;
-    if (tile * a.tile >= n) return;
-    const uint32_t number = pairs[tile * a.tile].x;
-    if (pairs[tile * a.tile - 1].x != number) return;                                              // nothing reaches into this tile
-    if (tile > 1 && pairs[(tile - 1) * a.tile - 1].x == number) return;                            // or it comes from further back
-    float sum = 0.f;
-    for (int64_t t = tile + warp; t * a.tile < n && pairs[t * a.tile].x == number; t += 8)
-        if (col < a.width) sum += a.pieces[(part * a.tiles + t) * a.width + col];
-    sm[warp][lane] = sum;
-    __syncthreads();
-    if (warp != 0 || col >= a.width) return;
-#pragma unroll
-    for (int w = 1; w < 8; ++w) sum += sm[w][lane];
-    float *out = a.dtable + part * a.ld_partition + (int64_t)number * a.ld_row + col;
-    *out += a.scale * sum;
-}
-
-// Rows that no token names.  A block looks its 64 numbers up in the sorted tokens.
-constexpr int kZeroRows = 64;
+// Rows that no token names.  A block looks its 32 numbers up in the sorted tokens.
+constexpr int kZeroRows = 32;
 template <int VEC>
-__global__ void __launch_bounds__(256) cr_embedding_zero_kernel(const GradArgs a, unsigned ranges) {
-    __shared__ uint32_t named[kZeroRows / 32];
-    const int64_t part = blockIdx.x / ranges, v0 = (int64_t)(blockIdx.x % ranges) * kZeroRows;
+__device__ __forceinline__ void zero_rows(const GradArgs &a, unsigned block, unsigned ranges) {
+    __shared__ uint32_t named;
+    const int64_t part = block / ranges, v0 = (int64_t)(block % ranges) * kZeroRows;
     const int rows = (int)min((int64_t)kZeroRows, a.vocab - v0);
-    if (threadIdx.x < kZeroRows / 32) named[threadIdx.x] = 0;
-    __syncthreads();
+    if (threadIdx.x == 0) named = 0;
     if (a.counts) {
         const uint2 *pairs = a.pairs + part * 2 * a.tokens;
-        int64_t low = 0, high = a.counts[part];
-        const int64_t n = high;
+        const int64_t n = a.counts[part];
+        int64_t low = 0, high = n;
         while (low < high) {
             const int64_t mid = (low + high) / 2;
             if ((int64_t)pairs[mid].x < v0) low = mid + 1;
             else high = mid;
         }
-        for (int64_t i = low + (int)threadIdx.x; i < n; i += 256) {
+        __syncthreads();
+        for (int64_t i = low + (int)threadIdx.x; i < n; i += kSumThreads) {
             const int64_t v = (int64_t)pairs[i].x - v0;
             if (v >= rows) break;
-            atomicOr(&named[v / 32], 1u << (v % 32));
+            atomicOr(&named, 1u << v);
         }
-        __syncthreads();
     }
+    __syncthreads();
     const int nvec = a.width / VEC;
     const float zero[VEC] = {};
+    const uint32_t bits = named;
     for (int r = 0; r < rows; ++r) {
-        if (named[r / 32] >> (r % 32) & 1u) continue;
+        if (bits >> r & 1u) continue;
         float *out = a.dtable + part * a.ld_partition + (v0 + r) * a.ld_row;
-        for (int v = (int)threadIdx.x; v < nvec; v += 256) store_floats<VEC>(out + v * VEC, zero, 1.f);
+        for (int v = (int)threadIdx.x; v < nvec; v += kSumThreads) store_floats<VEC>(out + v * VEC, zero, 1.f);
     }
+}
+
+// Both in one grid: the first `sum_blocks` blocks take tiles, the others ranges of rows.  Bound by memory.
+template <typename T, int VEC, int ZERO>
+__global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const GradArgs a, unsigned sum_blocks, int across, int slabs, unsigned ranges) {
+    if (blockIdx.x < sum_blocks) sum_tile<T, VEC>(a, blockIdx.x, across, slabs);
+    else zero_rows<ZERO>(a, blockIdx.x - sum_blocks, ranges);
+}
+
+// Numbers whose tokens reach into further tiles: the block of the first such tile adds the tiles' pieces to the row.  `across`
+// threads take a vector of columns each; the block's threads / across of them that share a column take every such piece each
+// and are summed in order.
+constexpr int kJoinThreads = 256;
+template <int VEC>
+__global__ void __launch_bounds__(kJoinThreads) cr_embedding_join_kernel(const GradArgs a, int across, int slabs) {
+    constexpr int kUnroll = 4;
+    __shared__ float sm[kJoinThreads * VEC];
+    const unsigned item = blockIdx.x / (unsigned)slabs;
+    const int deep = kJoinThreads / across, col0 = (int)threadIdx.x % across, row = (int)threadIdx.x / across;
+    const int col = ((int)(blockIdx.x % (unsigned)slabs) * across + col0) * VEC;
+    const int64_t part = item / (unsigned)(a.tiles - 1);
+    const int64_t tile = item % (unsigned)(a.tiles - 1) + 1, n = a.counts[part];
+    const uint2 *pairs = a.pairs + part * 2 * a.tokens;
+    if (tile * a.tile >= n) return;
+    const uint32_t number = pairs[tile * a.tile].x, earlier = pairs[tile * a.tile - 1].x;
+    const uint32_t before = tile > 1 ? pairs[(tile - 1) * a.tile - 1].x : 0xffffffffu;
+    if (earlier != number || before == number) return;       // nothing reaches into this tile, or it comes from further back
+    const bool in = col < a.width;
+    const float *pieces = a.pieces + part * a.tiles * a.width + col;
+    float sum[VEC] = {};
+    for (int64_t t0 = tile + row;; t0 += deep * kUnroll) {
+        float f[kUnroll][VEC] = {};
+        bool more = true;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t t = t0 + u * deep;
+            const bool reaches = t * a.tile < n && pairs[t * a.tile].x == number;
+            more = reaches;
+            if (!reaches || !in) continue;
+            if constexpr (VEC == 4) {
+                const float4 p = *reinterpret_cast<const float4 *>(pieces + t * a.width);
+                f[u][0] = p.x; f[u][1] = p.y; f[u][2] = p.z; f[u][3] = p.w;
+            } else {
+                f[u][0] = pieces[t * a.width];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i] += f[u][i];
+        if (!more) break;
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sm[(int)threadIdx.x * VEC + i] = sum[i];
+    __syncthreads();
+    if (row != 0 || !in) return;
+    for (int r = 1; r < deep; ++r)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum[i] += sm[(r * across + col0) * VEC + i];
+    float *out = a.dtable + part * a.ld_partition + (int64_t)number * a.ld_row + col;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) out[i] += a.scale * sum[i];
 }
 
 int tile_tokens(int64_t tokens) {
@@ -364,11 +415,13 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         int bits = 1;
         while (bits < 31 && (1ll << bits) < a.vocab) ++bits;
         const int passes = (bits + kDigitBits - 1) / kDigitBits;
+        // a CTA's warps take 32 tokens at a time: eight warps a partition up to 1024 tokens, from there on 32 warps a CTA
+        const bool small = a.tokens <= 1024;
         int cluster = 1;
-        while (cluster < kMaxCluster && a.tokens > (int64_t)cluster * kSortThreads) cluster *= 2;
+        while (!small && cluster < kMaxCluster && a.tokens > (int64_t)cluster * 2048) cluster *= 2;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(a.partitions * cluster));
-        cfg.blockDim = dim3(kSortThreads);
+        cfg.blockDim = dim3(small ? 256 : 1024);
         cfg.stream = stream;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -376,44 +429,47 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = cluster > 1 ? 1 : 0;
-        if (a.id_bytes == 4)
-            e = cudaLaunchKernelEx(&cfg, cr_token_sort_kernel<int32_t>, static_cast<const int32_t *>(a.ids), (int)a.tokens, a.vocab, a.padding, passes, pairs, counts, cluster);
-        else
-            e = cudaLaunchKernelEx(&cfg, cr_token_sort_kernel<long long>, static_cast<const long long *>(a.ids), (int)a.tokens, a.vocab, a.padding, passes, pairs, counts, cluster);
+        auto sort = [&](auto i, auto kernel) {
+            return cudaLaunchKernelEx(&cfg, kernel, static_cast<const decltype(i) *>(a.ids), (int)a.tokens, a.vocab, a.padding, passes, pairs, counts, cluster);
+        };
+        if (a.id_bytes == 4) e = small ? sort(int32_t{}, cr_token_sort_kernel<int32_t, 8>) : sort(int32_t{}, cr_token_sort_kernel<int32_t, 32>);
+        else e = small ? sort((long long){}, cr_token_sort_kernel<long long, 8>) : sort((long long){}, cr_token_sort_kernel<long long, 32>);
         if (e != cudaSuccess) return e;
         ++*launches;
-        e = by_type(a.elem, [&](auto t) {
-            using T = decltype(t);
-            constexpr int VEC = 16 / (int)sizeof(T);
-            const bool wide = table16 && vector_rows(a.elem, a.width, {a.dy}, {a.ld_dy});
-            const int nvec = g.width / (wide ? VEC : 1);
-            int across = 1;
-            while (across < kSumThreads && across < nvec) across *= 2;
-            const int slabs = (nvec + across - 1) / across;
-            const int64_t groups = (g.tiles + kSumThreads / across - 1) / (kSumThreads / across);
-            if (a.partitions * groups > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-            const unsigned blocks = (unsigned)(a.partitions * groups * slabs);
-            if (wide) cr_embedding_sums_kernel<T, VEC><<<blocks, kSumThreads, 0, stream>>>(g, across, slabs);
-            else cr_embedding_sums_kernel<T, 1><<<blocks, kSumThreads, 0, stream>>>(g, across, slabs);
-            return cudaGetLastError();
-        });
-        if (e != cudaSuccess) return e;
-        ++*launches;
-        if (g.tiles > 1) {
-            const int slabs = (g.width + 31) / 32;
-            if (a.partitions * (g.tiles - 1) > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-            cr_embedding_join_kernel<<<(unsigned)(a.partitions * (g.tiles - 1) * slabs), 256, 0, stream>>>(g, slabs);
-            e = cudaGetLastError();
-            if (e != cudaSuccess) return e;
-            ++*launches;
-        }
     }
     const int64_t ranges = (a.vocab + kZeroRows - 1) / kZeroRows;
-    if (a.partitions > 0x7fffffffll / ranges) return cudaErrorInvalidValue;
-    if (table16 && g.width % 4 == 0) cr_embedding_zero_kernel<4><<<(unsigned)(a.partitions * ranges), 256, 0, stream>>>(g, (unsigned)ranges);
-    else cr_embedding_zero_kernel<1><<<(unsigned)(a.partitions * ranges), 256, 0, stream>>>(g, (unsigned)ranges);
-    e = cudaGetLastError();
-    if (e == cudaSuccess) ++*launches;
+    e = by_type(a.elem, [&](auto t) {
+        using T = decltype(t);
+        constexpr int VEC = 16 / (int)sizeof(T);
+        const bool wide = table16 && vector_rows(a.elem, a.width, {a.dy}, {a.ld_dy});
+        const int nvec = g.width / (wide ? VEC : 1);
+        int across = 1;
+        while (across < kSumThreads && across < nvec) across *= 2;
+        const int slabs = (nvec + across - 1) / across;
+        const int64_t groups = (g.tiles + kSumThreads / across - 1) / (kSumThreads / across);
+        if (a.partitions * groups > 0x3fffffffll / slabs || a.partitions > 0x3fffffffll / ranges) return cudaErrorInvalidValue;
+        const unsigned sums = (unsigned)(a.partitions * groups * slabs), blocks = sums + (unsigned)(a.partitions * ranges);
+        const bool zero4 = table16 && g.width % 4 == 0;
+        if (wide) cr_embedding_sums_kernel<T, VEC, 4><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs, (unsigned)ranges);
+        else if (zero4) cr_embedding_sums_kernel<T, 1, 4><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs, (unsigned)ranges);
+        else cr_embedding_sums_kernel<T, 1, 1><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs, (unsigned)ranges);
+        return cudaGetLastError();
+    });
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    if (g.tiles > 1) {
+        const bool four = table16 && g.width % 4 == 0;
+        const int nvec = four ? g.width / 4 : g.width;
+        int across = 1;
+        while (across < 64 && across < nvec) across *= 2;
+        const int slabs = (nvec + across - 1) / across;
+        if (a.partitions * (g.tiles - 1) > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
+        const unsigned blocks = (unsigned)(a.partitions * (g.tiles - 1) * slabs);
+        if (four) cr_embedding_join_kernel<4><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs);
+        else cr_embedding_join_kernel<1><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs);
+        e = cudaGetLastError();
+        if (e == cudaSuccess) ++*launches;
+    }
     return e;
 }
 

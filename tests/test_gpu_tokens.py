@@ -173,12 +173,14 @@ def test_table_gradient(plan, shape, dtype):
     kind = ["i32", "i64"][tokens % 2]
     want, size = O.embedding_backward(ids, f64(dy), vocab, scale, padding)
     d = grads(plan, dev_ids(ids, kind), dy, vocab, scale, padding, ld_pad=[0, 4, 3][width % 3])
-    # a chain of at most `tile` additions, of the pieces of every eighth tile, of eight such sums; rounding of the factor and
-    # the product: each addition's error is 2^-24 of a partial sum, which the sum of the terms' sizes bounds
+    # a chain of at most `tile` additions, then of the pieces: 4 to 256 threads share them, so at most a quarter of the tiles and
+    # 256 sums more, or all tiles one by one; rounding of the factor and the product.  Each addition's error is 2^-24 of a
+    # partial sum, which the sum of the terms' sizes bounds
     tile = 32
     while tokens // tile > 4096:
         tile *= 2
-    chain = min(tokens, tile) + (tokens / tile + 7) // 8 + 10
+    tiles = (tokens + tile - 1) // tile
+    chain = min(tokens, tile) + min(tiles, tiles / 4 + 256) + 4
     check(d, want, "f32", chain * STEP * size)
     again = grads(plan, dev_ids(ids, kind), dy, vocab, scale, padding, ld_pad=[0, 4, 3][width % 3])
     assert torch.equal(d, again)
