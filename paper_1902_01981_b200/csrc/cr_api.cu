@@ -1451,7 +1451,7 @@ cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_b
     cr::EmbeddingArgs a;
     a.ids = ids; a.id_bytes = id_bytes; a.dy = dy; a.ld_dy = ld_dy; a.dtable = dtable; a.ld_row = ld_row; a.ld_partition = ld_partition;
     a.tokens = tokens; a.partitions = partitions; a.vocab = vocab; a.width = width; a.elem = elem; a.scale = (float)scale; a.padding = padding;
-    cudaError_t e = cr::launch_embedding_backward(a, workspace, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
+    cudaError_t e = cr::launch_embedding_backward(a, workspace, plan->dev, reinterpret_cast<cudaStream_t>(stream), &plan->launches);
     if (e != cudaSuccess) { note_cuda(e, "cr_embedding_backward"); return CR_ERR_CUDA; }
     return CR_OK;
 }

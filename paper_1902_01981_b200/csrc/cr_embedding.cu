@@ -7,8 +7,8 @@
 //
 // The gradient's sums have one order.  A partition's tokens are sorted by number, equal numbers in the order of their
 // positions (a radix sort, exact), the sorted sequence is cut into tiles, and a token number's sum is the sum of its
-// tiles' pieces in ascending order.  The tiles depend on the partition's length alone, so a partition gets the same bits
-// alone and in a batch.  Sums are fp32; the scale is applied once, to the sum.
+// tiles' pieces in one order.  The tiles depend on the partition's own tokens, so a partition gets the same bits alone and
+// in a batch.  Sums are fp32; the scale is applied once, to the sum.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -76,25 +76,106 @@ __device__ __forceinline__ uint32_t peer_word(const uint32_t *w, int rank) {
     return v;
 }
 
-// (number, position) of the tokens of a partition that name a row, sorted by number, then position: digits of 8 bits from
+struct GradArgs {
+    const void *dy;
+    float *dtable, *pieces;      // pieces [partitions][tiles][width]: what a tile adds to a sum that began before it
+    uint2 *pairs;                // [partitions][2][tokens]
+    int32_t *bounds;             // [partitions][tiles + 1]: where the tiles begin
+    int32_t *far;                // [partitions][1 + tiles]: count and tiles where a sum first goes on from the tile before
+    int64_t tokens, vocab, padding, ld_dy, ld_row, ld_partition;
+    int width, tile, tiles, passes;
+    float scale;
+};
+
+template <int VEC>
+__device__ __forceinline__ void store_floats(float *p, const float (&v)[VEC], float scale) {
+    if constexpr (VEC == 1) {
+        *p = v[0] * scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 4; ++i)
+            reinterpret_cast<float4 *>(p)[i] = make_float4(v[4 * i] * scale, v[4 * i + 1] * scale, v[4 * i + 2] * scale, v[4 * i + 3] * scale);
+    }
+}
+
+// Zeroes the rows of one range of numbers that no token of the partition names; the tokens are marked in shared memory.
+template <typename I>
+__device__ __forceinline__ void zero_rows(const GradArgs &a, const I *ids, int64_t part, int64_t first, int64_t rows, bool vectors, uint32_t *named, int words) {
+    for (int64_t v0 = first; v0 < first + rows; v0 += (int64_t)words * 32) {
+        const int n = (int)min((int64_t)words * 32, first + rows - v0);
+        for (int i = threadIdx.x; i < words; i += blockDim.x) named[i] = 0;
+        __syncthreads();
+#pragma unroll 4
+        for (int64_t i = threadIdx.x; i < a.tokens; i += blockDim.x) {
+            const int64_t id = (int64_t)ids[i], v = id - v0;
+            if (v >= 0 && v < n && id != a.padding) atomicOr(&named[v / 32], 1u << (v % 32));
+        }
+        __syncthreads();
+        // a warp a row
+        for (int r = (int)threadIdx.x / 32; r < n; r += (int)blockDim.x / 32) {
+            if (named[r / 32] >> (r % 32) & 1u) continue;
+            float *out = a.dtable + part * a.ld_partition + (v0 + r) * a.ld_row;
+            if (vectors)
+                for (int c = (int)threadIdx.x % 32 * 4; c < a.width; c += 128) *reinterpret_cast<float4 *>(out + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+            else
+                for (int c = (int)threadIdx.x % 32; c < a.width; c += 32) out[c] = 0.f;
+        }
+        __syncthreads();
+    }
+}
+
+// Sums of up to this many tokens are not cut.
+constexpr int kWhole = 64;
+
+// Where a tile begins: at position i0, or, where a number of at most kWhole tokens lies across it, at that number's first one.
+// `cut`: a longer one lies across it.  For a warp.
+__device__ __forceinline__ int tile_begin(const uint2 *pairs, int i0, int n, bool &cut) {
+    const int lane = (int)threadIdx.x % 32;
+    const uint32_t number = pairs[i0].x;
+    int back = 0, on = 0;
+#pragma unroll
+    for (int k = 0; k < kWhole / 32; ++k) {
+        const int b = i0 - 1 - k * 32 - lane, f = i0 + k * 32 + lane;
+        const uint32_t same_back = __ballot_sync(0xffffffffu, b >= 0 && pairs[max(b, 0)].x == number);
+        const uint32_t same_on = __ballot_sync(0xffffffffu, f < n && pairs[min(f, n - 1)].x == number);
+        if (back == k * 32) back += same_back == 0xffffffffu ? 32 : __ffs(~same_back) - 1;
+        if (on == k * 32) on += same_on == 0xffffffffu ? 32 : __ffs(~same_on) - 1;
+    }
+    cut = back > 0 && back + on > kWhole;
+    return cut ? i0 : i0 - back;
+}
+
+// Sorts (number, position) of the tokens of a partition that name a row, by number, then position: digits of 8 bits from
 // the lowest up, each pass stable.  A cluster of CTAs takes a partition; each warp owns a run of consecutive entries, counts
 // its digits (lanes with one digit find each other by match), and after the counts of all warps have been summed up it
-// puts its entries in place in order.  The buffers are in global memory (L2).  Bound by latency: a few dependent steps a pass.
+// puts its entries in place in order.  The buffers are in global memory (L2).  Then the sequence is cut into tiles.  Bound by
+// latency, a few dependent steps a pass; meanwhile further CTAs of the grid, `zeroers` for a partition, write the rows that need no
+// sums, which is bound by memory.
 template <typename I, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const I *ids, int tokens, int64_t vocab, int64_t padding, int passes, uint2 *pairs,
-                                                                   int32_t *counts, int cluster) {
+__global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const GradArgs a, const I *ids, int64_t partitions, int cluster, int zeroers,
+                                                                   bool vectors) {
     static_assert(WARPS * 32 >= kBins, "a thread a bin");
     __shared__ uint32_t hist[WARPS][kBins];
     __shared__ uint32_t total[kBins], scan[kBins / 32];
+    const int64_t sorters = a.tokens > 0 ? partitions * cluster : 0;
+    if (blockIdx.x >= sorters) {      // whole clusters: nobody waits for these CTAs
+        const int64_t z = blockIdx.x - sorters, part = z / zeroers;
+        if (part >= partitions) return;
+        const int64_t each = (a.vocab + zeroers - 1) / zeroers, first = z % zeroers * each;
+        if (first < a.vocab) zero_rows(a, ids + part * a.tokens, part, first, min(each, a.vocab - first), vectors, &hist[0][0], WARPS * kBins);
+        return;
+    }
     const int64_t part = blockIdx.x / (unsigned)cluster;
     const int rank = (int)(blockIdx.x % (unsigned)cluster), tid = (int)threadIdx.x, warp = tid / 32, lane = tid % 32;
     const uint32_t below = (1u << lane) - 1u;
-    ids += part * tokens;
-    uint2 *buffer[2] = {pairs + part * 2 * tokens, pairs + (part * 2 + 1) * tokens};
-    int count = tokens;
-    for (int pass = 0; pass < passes; ++pass) {
+    ids += part * a.tokens;
+    uint2 *buffer[2] = {a.pairs + part * 2 * a.tokens, a.pairs + (part * 2 + 1) * a.tokens};
+    int32_t *far = a.far + part * (a.tiles + 1);
+    if (rank == 0 && tid == 0) far[0] = 0;
+    int count = (int)a.tokens;
+    for (int pass = 0; pass < a.passes; ++pass) {
         // the last pass writes into buffer 0
-        const int into = (passes - 1 - pass) & 1;
+        const int into = (a.passes - 1 - pass) & 1;
         const uint2 *from = buffer[into ^ 1];
         uint2 *to = buffer[into];
         const int64_t warps = (int64_t)cluster * WARPS;
@@ -104,7 +185,7 @@ __global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const I *ids,
             if (i >= end) return kBins;
             if (pass == 0) {
                 const int64_t id = (int64_t)ids[i];
-                if (id < 0 || id >= vocab || id == padding) return kBins;
+                if (id < 0 || id >= a.vocab || id == a.padding) return kBins;
                 e = make_uint2((uint32_t)id, (uint32_t)i);
             } else {
                 e = from[i];
@@ -181,64 +262,63 @@ __global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const I *ids,
         count = (int)all;
         sort_meet(cluster);     // the entries are in place, and nobody reads a peer's counts any more
     }
-    if (rank == 0 && tid == 0) counts[part] = count;
+    int32_t *bounds = a.bounds + part * (a.tiles + 1);
+    const uint2 *sorted = buffer[0];
+    for (int64_t t = rank * WARPS + warp; t <= a.tiles; t += (int64_t)cluster * WARPS) {
+        const int64_t i0 = t * a.tile;
+        int begin = (int)min(i0, (int64_t)count);
+        if (t > 0 && i0 < count) {
+            bool cut;
+            begin = tile_begin(sorted, (int)i0, count, cut);
+            if (cut && lane == 0) {
+                // the first tile into which the number reaches: only from a number's first tile on does a sum go on
+                const int64_t earlier = i0 - a.tile;
+                if (earlier == 0 || sorted[earlier - 1].x != sorted[i0].x) far[1 + atomicAdd(&far[0], 1)] = (int32_t)t;
+            }
+        }
+        if (lane == 0) bounds[t] = begin;
+    }
 }
 
 // ---- sums ---------------------------------------------------------------------------------------------------------------
 
-struct GradArgs {
-    const void *dy;
-    float *dtable, *pieces;      // pieces [partitions][tiles][width]: what a tile adds to a sum that began before it
-    const uint2 *pairs;
-    const int32_t *counts;       // null: no tokens
-    int64_t tokens, vocab, ld_dy, ld_row, ld_partition;
-    int width, tile, tiles;
-    float scale;
-};
-
 constexpr int kSumThreads = 128;
-
-template <int VEC>
-__device__ __forceinline__ void store_floats(float *p, const float (&v)[VEC], float scale) {
-    if constexpr (VEC == 1) {
-        *p = v[0] * scale;
-    } else {
-#pragma unroll
-        for (int i = 0; i < VEC / 4; ++i)
-            reinterpret_cast<float4 *>(p)[i] = make_float4(v[4 * i] * scale, v[4 * i + 1] * scale, v[4 * i + 2] * scale, v[4 * i + 3] * scale);
-    }
-}
 
 // A tile of the sorted tokens for a slab of columns: `across` threads, a vector of columns each, walk the tile's tokens and
 // write a sum wherever the number changes: into the table's row where the number's first token is in this tile, into the
-// tile's row of pieces where it is not.
+// tile's row of pieces where it is not.  The pairs of the next tokens are fetched with the rows of these.
 template <typename T, int VEC>
-__device__ __forceinline__ void sum_tile(const GradArgs &a, unsigned block, int across, int slabs) {
+__global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const GradArgs a, int across, int slabs) {
     constexpr int kUnroll = 8;
     const int per_block = kSumThreads / across;
     const int groups = (a.tiles + per_block - 1) / per_block;
-    const unsigned item = block / (unsigned)slabs;
-    const int slab = (int)(block % (unsigned)slabs);
+    const unsigned item = blockIdx.x / (unsigned)slabs;
+    const int slab = (int)(blockIdx.x % (unsigned)slabs);
     const int64_t part = item / (unsigned)groups;
     const int tile = (int)(item % (unsigned)groups) * per_block + (int)threadIdx.x / across;
     const int col = (slab * across + (int)threadIdx.x % across) * VEC;
-    const int64_t first = (int64_t)tile * a.tile, n = a.counts[part];
-    if (first >= n || col >= a.width) return;
-    const int count = (int)min((int64_t)a.tile, n - first);
+    if (tile >= a.tiles || col >= a.width) return;
+    const int32_t *bounds = a.bounds + part * (a.tiles + 1) + tile;
+    const int64_t first = bounds[0];
+    const int count = bounds[1] - bounds[0];
+    if (count <= 0) return;
     const uint2 *pairs = a.pairs + part * 2 * a.tokens + first;
     const T *dy = static_cast<const T *>(a.dy) + part * a.tokens * a.ld_dy + col;
     float *table = a.dtable + part * a.ld_partition + col;
     float *piece = a.pieces + (part * a.tiles + tile) * a.width + col;
+    uint2 e[kUnroll + 1];
     bool began_before = first > 0 && pairs[-1].x == pairs[0].x;
     float acc[VEC] = {};
-    for (int t0 = 0; t0 < count; t0 += kUnroll) {
-        uint2 e[kUnroll + 1];
-        Packed<T, VEC> r[kUnroll];
 #pragma unroll
-        for (int u = 0; u <= kUnroll; ++u) e[u] = t0 + u < count ? pairs[t0 + u] : make_uint2(0xffffffffu, 0);
+    for (int u = 0; u <= kUnroll; ++u) e[u] = u < count ? pairs[u] : make_uint2(0xffffffffu, 0);
+    for (int t0 = 0; t0 < count; t0 += kUnroll) {
+        Packed<T, VEC> r[kUnroll];
+        uint2 next[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
             if (t0 + u < count) r[u] = load_packed<T, VEC>(dy + (int64_t)e[u].y * a.ld_dy);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) next[u] = t0 + kUnroll + 1 + u < count ? pairs[t0 + kUnroll + 1 + u] : make_uint2(0xffffffffu, 0);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             if (t0 + u >= count) break;
@@ -254,69 +334,24 @@ __device__ __forceinline__ void sum_tile(const GradArgs &a, unsigned block, int 
                 for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
             }
         }
+        e[0] = e[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) e[u + 1] = next[u];
     }
 }
 
-// Rows that no token names.  A block looks its 32 numbers up in the sorted tokens.
-constexpr int kZeroRows = 32;
-template <int VEC>
-__device__ __forceinline__ void zero_rows(const GradArgs &a, unsigned block, unsigned ranges) {
-    __shared__ uint32_t named;
-    const int64_t part = block / ranges, v0 = (int64_t)(block % ranges) * kZeroRows;
-    const int rows = (int)min((int64_t)kZeroRows, a.vocab - v0);
-    if (threadIdx.x == 0) named = 0;
-    if (a.counts) {
-        const uint2 *pairs = a.pairs + part * 2 * a.tokens;
-        const int64_t n = a.counts[part];
-        int64_t low = 0, high = n;
-        while (low < high) {
-            const int64_t mid = (low + high) / 2;
-            if ((int64_t)pairs[mid].x < v0) low = mid + 1;
-            else high = mid;
-        }
-        __syncthreads();
-        for (int64_t i = low + (int)threadIdx.x; i < n; i += kSumThreads) {
-            const int64_t v = (int64_t)pairs[i].x - v0;
-            if (v >= rows) break;
-            atomicOr(&named, 1u << v);
-        }
-    }
-    __syncthreads();
-    const int nvec = a.width / VEC;
-    const float zero[VEC] = {};
-    const uint32_t bits = named;
-    for (int r = 0; r < rows; ++r) {
-        if (bits >> r & 1u) continue;
-        float *out = a.dtable + part * a.ld_partition + (v0 + r) * a.ld_row;
-        for (int v = (int)threadIdx.x; v < nvec; v += kSumThreads) store_floats<VEC>(out + v * VEC, zero, 1.f);
-    }
-}
-
-// Both in one grid: the first `sum_blocks` blocks take tiles, the others ranges of rows.  Bound by memory.
-template <typename T, int VEC, int ZERO>
-__global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const GradArgs a, unsigned sum_blocks, int across, int slabs, unsigned ranges) {
-    if (blockIdx.x < sum_blocks) sum_tile<T, VEC>(a, blockIdx.x, across, slabs);
-    else zero_rows<ZERO>(a, blockIdx.x - sum_blocks, ranges);
-}
-
-// Numbers whose tokens reach into further tiles: the block of the first such tile adds the tiles' pieces to the row.  `across`
-// threads take a vector of columns each; the block's threads / across of them that share a column take every such piece each
-// and are summed in order.
+// Numbers whose tokens reach into further tiles: the tiles' pieces are added to the row.  `across` threads take a vector of
+// columns each; the block's threads / across of them that share a column take every such piece each and are summed in order.
 constexpr int kJoinThreads = 256;
 template <int VEC>
-__global__ void __launch_bounds__(kJoinThreads) cr_embedding_join_kernel(const GradArgs a, int across, int slabs) {
+__device__ __forceinline__ void join_pieces(const GradArgs &a, int64_t part, int64_t tile, int slab, int across, float *sm) {
     constexpr int kUnroll = 4;
-    __shared__ float sm[kJoinThreads * VEC];
-    const unsigned item = blockIdx.x / (unsigned)slabs;
     const int deep = kJoinThreads / across, col0 = (int)threadIdx.x % across, row = (int)threadIdx.x / across;
-    const int col = ((int)(blockIdx.x % (unsigned)slabs) * across + col0) * VEC;
-    const int64_t part = item / (unsigned)(a.tiles - 1);
-    const int64_t tile = item % (unsigned)(a.tiles - 1) + 1, n = a.counts[part];
+    const int col = (slab * across + col0) * VEC;
+    const int32_t *bounds = a.bounds + part * (a.tiles + 1);
     const uint2 *pairs = a.pairs + part * 2 * a.tokens;
-    if (tile * a.tile >= n) return;
-    const uint32_t number = pairs[tile * a.tile].x, earlier = pairs[tile * a.tile - 1].x;
-    const uint32_t before = tile > 1 ? pairs[(tile - 1) * a.tile - 1].x : 0xffffffffu;
-    if (earlier != number || before == number) return;       // nothing reaches into this tile, or it comes from further back
+    const int64_t n = bounds[a.tiles];
+    const uint32_t number = pairs[tile * a.tile].x;
     const bool in = col < a.width;
     const float *pieces = a.pieces + part * a.tiles * a.width + col;
     float sum[VEC] = {};
@@ -342,6 +377,7 @@ __global__ void __launch_bounds__(kJoinThreads) cr_embedding_join_kernel(const G
             for (int i = 0; i < VEC; ++i) sum[i] += f[u][i];
         if (!more) break;
     }
+    __syncthreads();             // the memory is free again
 #pragma unroll
     for (int i = 0; i < VEC; ++i) sm[(int)threadIdx.x * VEC + i] = sum[i];
     __syncthreads();
@@ -352,6 +388,15 @@ __global__ void __launch_bounds__(kJoinThreads) cr_embedding_join_kernel(const G
     float *out = a.dtable + part * a.ld_partition + (int64_t)number * a.ld_row + col;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) out[i] += a.scale * sum[i];
+}
+template <int VEC>
+__global__ void __launch_bounds__(kJoinThreads) cr_embedding_join_kernel(const GradArgs a, int across, int slabs, unsigned walkers) {
+    __shared__ float sm[kJoinThreads * VEC];
+    const unsigned item = blockIdx.x / (unsigned)slabs;
+    const int64_t part = item / walkers;
+    const int32_t *far = a.far + part * (a.tiles + 1);
+    const int count = far[0];
+    for (int k = (int)(item % walkers); k < count; k += (int)walkers) join_pieces<VEC>(a, part, far[1 + k], (int)(blockIdx.x % (unsigned)slabs), across, sm);
 }
 
 int tile_tokens(int64_t tokens) {
@@ -364,10 +409,11 @@ size_t align16(size_t b) { return (b + 15) / 16 * 16; }
 
 }  // namespace
 
+// pairs, bounds, far, pieces
 size_t embedding_backward_workspace_bytes(int64_t tokens, int64_t partitions, int64_t width) {
     if (tokens == 0) return 0;
     const int64_t tile = tile_tokens(tokens), tiles = (tokens + tile - 1) / tile;
-    return align16((size_t)(partitions * tokens * 16)) + align16((size_t)partitions * 4) + (size_t)(tiles > 1 ? partitions * tiles * width * 4 : 0);
+    return (size_t)(partitions * tokens * 16) + 2 * align16((size_t)(partitions * (tiles + 1)) * 4) + (size_t)(tiles > 1 ? partitions * tiles * width * 4 : 0);
 }
 
 cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream, int64_t *launches) {
@@ -396,7 +442,7 @@ cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream, int64_
     });
 }
 
-cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, cudaStream_t stream, int64_t *launches) {
+cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches) {
     if (a.partitions == 0 || a.vocab == 0 || a.width == 0) return cudaSuccess;
     GradArgs g = {};
     g.dy = a.dy; g.dtable = a.dtable; g.tokens = a.tokens; g.vocab = a.vocab;
@@ -404,23 +450,38 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
     g.width = (int)a.width; g.scale = a.scale;
     cudaError_t e;
     const bool table16 = aligned16(a.dtable) && a.ld_row % 4 == 0 && (a.partitions == 1 || a.ld_partition % 4 == 0);
+    g.padding = a.padding;
+    g.tile = tile_tokens(a.tokens);
+    g.tiles = (int)((a.tokens + g.tile - 1) / g.tile);
     if (a.tokens > 0) {
-        g.tile = tile_tokens(a.tokens);
-        g.tiles = (int)((a.tokens + g.tile - 1) / g.tile);
-        uint2 *pairs = static_cast<uint2 *>(workspace);
-        int32_t *counts = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + align16((size_t)(a.partitions * a.tokens * 16)));
-        g.pairs = pairs;
-        g.counts = counts;
-        g.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(counts) + align16((size_t)a.partitions * 4));
-        int bits = 1;
-        while (bits < 31 && (1ll << bits) < a.vocab) ++bits;
-        const int passes = (bits + kDigitBits - 1) / kDigitBits;
+        char *p = static_cast<char *>(workspace);
+        const size_t table = align16((size_t)(a.partitions * (g.tiles + 1)) * 4);
+        g.pairs = reinterpret_cast<uint2 *>(p);
+        g.bounds = reinterpret_cast<int32_t *>(p += a.partitions * a.tokens * 16);
+        g.far = reinterpret_cast<int32_t *>(p += table);
+        g.pieces = reinterpret_cast<float *>(p += table);
+    }
+    int bits = 1;
+    while (bits < 31 && (1ll << bits) < a.vocab) ++bits;
+    g.passes = (bits + kDigitBits - 1) / kDigitBits;
+    const bool zero4 = table16 && g.width % 4 == 0;
+    {
         // a CTA's warps take 32 tokens at a time: eight warps a partition up to 1024 tokens, from there on 32 warps a CTA
         const bool small = a.tokens <= 1024;
         int cluster = 1;
         while (!small && cluster < kMaxCluster && a.tokens > (int64_t)cluster * 2048) cluster *= 2;
+        // A CTA that zeroes reads the partition's numbers: with those that sort two an SM (74 a partition instead of 66 left eight a
+        // partition to a second round: 93 -> 76 us of 4 x 16384 tokens over 32000 x 1024), fewer where they would read more than
+        // they write, and each at least 64 KB of rows.
+        const int64_t bytes = a.vocab * a.width * 4;
+        const int64_t least = std::max<int64_t>(64 * 1024, a.tokens * a.id_bytes);
+        const int64_t sorters = a.tokens > 0 ? a.partitions * cluster : 0;
+        const int64_t room = sorters < dev.sm_count ? 2 * dev.sm_count - sorters : 2 * dev.sm_count;
+        const int64_t zeroers = std::max<int64_t>(1, std::min<int64_t>({bytes / least, room / a.partitions, a.vocab}));
+        const int64_t ctas = sorters + (a.partitions * zeroers + cluster - 1) / cluster * cluster;
+        if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(a.partitions * cluster));
+        cfg.gridDim = dim3((unsigned)ctas);
         cfg.blockDim = dim3(small ? 256 : 1024);
         cfg.stream = stream;
         cudaLaunchAttribute attr[1];
@@ -430,14 +491,14 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         cfg.attrs = attr;
         cfg.numAttrs = cluster > 1 ? 1 : 0;
         auto sort = [&](auto i, auto kernel) {
-            return cudaLaunchKernelEx(&cfg, kernel, static_cast<const decltype(i) *>(a.ids), (int)a.tokens, a.vocab, a.padding, passes, pairs, counts, cluster);
+            return cudaLaunchKernelEx(&cfg, kernel, g, static_cast<const decltype(i) *>(a.ids), a.partitions, cluster, (int)zeroers, zero4);
         };
         if (a.id_bytes == 4) e = small ? sort(int32_t{}, cr_token_sort_kernel<int32_t, 8>) : sort(int32_t{}, cr_token_sort_kernel<int32_t, 32>);
         else e = small ? sort((long long){}, cr_token_sort_kernel<long long, 8>) : sort((long long){}, cr_token_sort_kernel<long long, 32>);
         if (e != cudaSuccess) return e;
         ++*launches;
     }
-    const int64_t ranges = (a.vocab + kZeroRows - 1) / kZeroRows;
+    if (a.tokens == 0) return cudaSuccess;
     e = by_type(a.elem, [&](auto t) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T);
@@ -447,26 +508,24 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         while (across < kSumThreads && across < nvec) across *= 2;
         const int slabs = (nvec + across - 1) / across;
         const int64_t groups = (g.tiles + kSumThreads / across - 1) / (kSumThreads / across);
-        if (a.partitions * groups > 0x3fffffffll / slabs || a.partitions > 0x3fffffffll / ranges) return cudaErrorInvalidValue;
-        const unsigned sums = (unsigned)(a.partitions * groups * slabs), blocks = sums + (unsigned)(a.partitions * ranges);
-        const bool zero4 = table16 && g.width % 4 == 0;
-        if (wide) cr_embedding_sums_kernel<T, VEC, 4><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs, (unsigned)ranges);
-        else if (zero4) cr_embedding_sums_kernel<T, 1, 4><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs, (unsigned)ranges);
-        else cr_embedding_sums_kernel<T, 1, 1><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs, (unsigned)ranges);
+        if (a.partitions * groups > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
+        const unsigned blocks = (unsigned)(a.partitions * groups * slabs);
+        if (wide) cr_embedding_sums_kernel<T, VEC><<<blocks, kSumThreads, 0, stream>>>(g, across, slabs);
+        else cr_embedding_sums_kernel<T, 1><<<blocks, kSumThreads, 0, stream>>>(g, across, slabs);
         return cudaGetLastError();
     });
     if (e != cudaSuccess) return e;
     ++*launches;
-    if (g.tiles > 1) {
-        const bool four = table16 && g.width % 4 == 0;
-        const int nvec = four ? g.width / 4 : g.width;
+    if (a.tokens > kWhole) {      // otherwise no sum is cut
+        const int nvec = zero4 ? g.width / 4 : g.width;
         int across = 1;
         while (across < 64 && across < nvec) across *= 2;
         const int slabs = (nvec + across - 1) / across;
-        if (a.partitions * (g.tiles - 1) > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-        const unsigned blocks = (unsigned)(a.partitions * (g.tiles - 1) * slabs);
-        if (four) cr_embedding_join_kernel<4><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs);
-        else cr_embedding_join_kernel<1><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs);
+        const int64_t walkers = std::min<int64_t>(a.tokens / kWhole, std::max<int64_t>(1, 4 * dev.sm_count / a.partitions));
+        if (a.partitions * walkers > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
+        const unsigned blocks = (unsigned)(a.partitions * walkers * slabs);
+        if (zero4) cr_embedding_join_kernel<4><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs, (unsigned)walkers);
+        else cr_embedding_join_kernel<1><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs, (unsigned)walkers);
         e = cudaGetLastError();
         if (e == cudaSuccess) ++*launches;
     }

@@ -117,9 +117,10 @@ __global__ void __launch_bounds__(1024) cr_rms_norm_kernel(const RmsNormArgs a) 
 #pragma unroll
         for (int u = 0; u < kHeld; ++u)
             if (tid + u * nt < nvec) {
-                float z[VEC];
-                norm(tid + u * nt, held[u], z);
-                widen(z);
+                const int64_t v = tid + u * nt;
+                if (h) store_packed<T, VEC>(h + v * VEC, pack<T, VEC>(held[u]));
+                norm(v, held[u], held[u]);
+                widen(held[u]);
             }
         for (int64_t v = tid + (int64_t)kHeld * nt; v < nvec; v += nt) {
             float f[VEC], z[VEC];
@@ -132,32 +133,35 @@ __global__ void __launch_bounds__(1024) cr_rms_norm_kernel(const RmsNormArgs a) 
         dead = top >= 0x7f800000u;
         if (tid == 0) a.scale[row] = rs.scale;
     }
+    auto put_code = [&](int64_t v, const float (&z)[VEC]) {
+        int8_t *q = a.q + row * a.ld_q + v * VEC;
+        if constexpr (VEC == 1) {
+            *q = dead ? (int8_t)0 : (int8_t)code(z[0], rs.mult);
+        } else {
+            uint32_t w[VEC / 4];
+#pragma unroll
+            for (int i = 0; i < VEC / 4; ++i) {
+                const uint32_t lo = __byte_perm(code(z[4 * i], rs.mult), code(z[4 * i + 1], rs.mult), 0x0040);
+                const uint32_t hi = __byte_perm(code(z[4 * i + 2], rs.mult), code(z[4 * i + 3], rs.mult), 0x0040);
+                w[i] = dead ? 0u : __byte_perm(lo, hi, 0x5410);
+            }
+            if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t *>(q) = w[0];
+        }
+    };
     auto put = [&](int64_t v, const float (&f)[VEC]) {
+        if (h) store_packed<T, VEC>(h + v * VEC, pack<T, VEC>(f));
         float z[VEC];
         norm(v, f, z);
-        if (h) store_packed<T, VEC>(h + v * VEC, pack<T, VEC>(f));
-        if constexpr (CODES) {
-            int8_t *q = a.q + row * a.ld_q + v * VEC;
-            if constexpr (VEC == 1) {
-                *q = dead ? (int8_t)0 : (int8_t)code(z[0], rs.mult);
-            } else {
-                uint32_t w[VEC / 4];
-#pragma unroll
-                for (int i = 0; i < VEC / 4; ++i) {
-                    const uint32_t lo = __byte_perm(code(z[4 * i], rs.mult), code(z[4 * i + 1], rs.mult), 0x0040);
-                    const uint32_t hi = __byte_perm(code(z[4 * i + 2], rs.mult), code(z[4 * i + 3], rs.mult), 0x0040);
-                    w[i] = dead ? 0u : __byte_perm(lo, hi, 0x5410);
-                }
-                if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
-                else *reinterpret_cast<uint32_t *>(q) = w[0];
-            }
-        } else {
-            store_packed<T, VEC>(static_cast<T *>(a.y) + row * a.ld_y + v * VEC, pack<T, VEC>(z));
-        }
+        if constexpr (CODES) put_code(v, z);
+        else store_packed<T, VEC>(static_cast<T *>(a.y) + row * a.ld_y + v * VEC, pack<T, VEC>(z));
     };
 #pragma unroll
     for (int u = 0; u < kHeld; ++u)
-        if (tid + u * nt < nvec) put(tid + u * nt, held[u]);
+        if (tid + u * nt < nvec) {
+            if constexpr (CODES) put_code(tid + u * nt, held[u]);     // the sums are stored already
+            else put(tid + u * nt, held[u]);
+        }
     for (int64_t v = tid + (int64_t)kHeld * nt; v < nvec; v += nt) {
         float f[VEC];
         sum_at(v, f);
@@ -167,6 +171,144 @@ __global__ void __launch_bounds__(1024) cr_rms_norm_kernel(const RmsNormArgs a) 
 
 // ---- gradient ------------------------------------------------------------------------------------------------------------
 
+// Rows of a partition that one block adds up: the partition's rows in at most 256 chunks of 4 to 64 rows.
+int64_t chunk_rows(int64_t rows) { return std::min<int64_t>(64, std::max<int64_t>(4, (rows + 255) / 256)); }
+
+// One block a chunk of rows: a thread keeps its columns' gamma and sums of dy xhat in registers over the rows.  Rows of up to
+// grad_held vectors a thread, 512 threads.  Each thread copies its own vectors of the rows to come into shared memory
+// (cp.async, four rows ahead, two of fp32; no barrier, since nobody else reads them); elements that do not lie in vectors are
+// fetched a row ahead into registers.
+constexpr int kGradThreads = 512;
+template <int VEC> __host__ __device__ constexpr int grad_stages() { return VEC == 1 ? 1 : VEC == 4 ? 2 : 4; }
+template <int VEC> __host__ __device__ constexpr int grad_held() { return VEC == 8 ? 2 : 4; }
+template <int VEC> __host__ __device__ constexpr int64_t grad_held_cols() { return (int64_t)kGradThreads * grad_held<VEC>() * VEC; }
+
+template <typename T, int VEC>
+struct RowsAhead {
+    static constexpr int kHeld = grad_held<VEC>();
+    uint4 *mine;                                // this thread's first slot; slots are a block apart
+    Packed<T, VEC> next[VEC == 1 ? 3 * kHeld : 1];
+
+    // Asks for tensor t's vectors of a row.
+    __device__ __forceinline__ void fetch(int stage, int t, const T *row, int nvec) {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            const int v = (int)(threadIdx.x + u * blockDim.x);
+            if (v >= nvec) continue;
+            if constexpr (VEC == 1) {
+                next[t * kHeld + u] = load_packed<T, 1>(row + v);
+            } else {
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine + ((stage * 3 + t) * kHeld + u) * blockDim.x);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + (int64_t)v * VEC) : "memory");
+            }
+        }
+    }
+    __device__ __forceinline__ void asked() const {
+        if constexpr (VEC > 1) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // Waits for all but the latest grad_stages - 1 rows asked for.
+    __device__ __forceinline__ void arrived() const {
+        if constexpr (VEC > 1) asm volatile("cp.async.wait_group %0;" ::"n"(grad_stages<VEC>() - 1) : "memory");
+    }
+    __device__ __forceinline__ void take(int stage, int t, int u, float (&f)[VEC]) const {
+        if constexpr (VEC == 1) {
+            unpack<T, 1>(next[t * kHeld + u], f);
+        } else {
+            const uint4 q = mine[((stage * 3 + t) * kHeld + u) * blockDim.x];
+            Packed<T, VEC> p;
+            p.w[0] = q.x; p.w[1] = q.y; p.w[2] = q.z; p.w[3] = q.w;
+            unpack<T, VEC>(p, f);
+        }
+    }
+};
+
+template <typename T, int VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_grad_rows_kernel(const RmsNormArgs a, float *partial, int64_t ld_partial, int64_t rows_each,
+                                                                             int chunk, int chunks) {
+    constexpr int kHeld = grad_held<VEC>(), kAhead = grad_stages<VEC>();
+    extern __shared__ uint4 staged[];
+    __shared__ float sums[2][32];
+    const int64_t part = blockIdx.x / (unsigned)chunks, first = (int64_t)(blockIdx.x % (unsigned)chunks) * chunk;
+    const int count = (int)min((int64_t)chunk, rows_each - first);
+    const int64_t row0 = part * rows_each + first;
+    const int nvec = (int)(a.cols / VEC), nt = (int)blockDim.x, tid = (int)threadIdx.x;
+    const T *dh = static_cast<const T *>(a.dh);
+    T *dx = static_cast<T *>(a.y);
+    const float over = 1.f / (float)a.cols;
+    RowsAhead<T, VEC> ahead;
+    ahead.mine = staged + tid;
+    auto fetch = [&](int k) {
+        const int64_t row = row0 + k;
+        const int stage = k % kAhead;
+        if (k < count) {
+            ahead.fetch(stage, 0, static_cast<const T *>(a.dy) + row * a.ld_dy, nvec);
+            ahead.fetch(stage, 1, static_cast<const T *>(a.h) + row * a.ld_h, nvec);
+            if (dh) ahead.fetch(stage, 2, dh + row * a.ld_dh, nvec);
+        }
+        ahead.asked();
+    };
+    for (int k = 0; k < kAhead; ++k) fetch(k);
+    float w[kHeld][VEC], acc[kHeld][VEC] = {};
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[u][i] = 1.f;
+        if (a.gamma && tid + u * nt < nvec) load_floats<VEC>(a.gamma + (tid + u * nt) * VEC, w[u]);
+    }
+    float rstd_ahead = a.rstd[row0];
+    for (int k = 0; k < count; ++k) {
+        const float rstd = rstd_ahead;
+        if (k + 1 < count) rstd_ahead = a.rstd[row0 + k + 1];
+        float fg[kHeld][VEC], fx[kHeld][VEC], d[kHeld][VEC] = {}, dot = 0.f;
+        ahead.arrived();
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            if (tid + u * nt >= nvec) continue;
+            ahead.take(k % kAhead, 0, u, fg[u]);
+            ahead.take(k % kAhead, 1, u, fx[u]);
+            if (dh && VEC == 1) ahead.take(k % kAhead, 2, u, d[u]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                fx[u][i] *= rstd;
+                acc[u][i] = fmaf(fg[u][i], fx[u][i], acc[u][i]);
+                fg[u][i] *= w[u][i];
+                dot = fmaf(fg[u][i], fx[u][i], dot);
+            }
+        }
+        // a row's dx may be its own dy, h or dh, which have arrived by now; the rows asked for are not written yet
+        if (VEC == 1) fetch(k + 1);
+        if (dx) {
+            dot = block_sum(dot, sums[k & 1]) * over;
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) {
+                const int v = tid + u * nt;
+                if (v >= nvec) continue;
+                if (dh && VEC > 1) ahead.take(k % kAhead, 2, u, d[u]);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) d[u][i] = fmaf(rstd, fmaf(-fx[u][i], dot, fg[u][i]), d[u][i]);
+                store_packed<T, VEC>(dx + (row0 + k) * a.ld_y + (int64_t)v * VEC, pack<T, VEC>(d[u]));
+            }
+        }
+        if (VEC > 1) fetch(k + kAhead);       // into the slots just read
+    }
+    if (!partial) return;
+    float *out = partial + blockIdx.x * ld_partial;
+    const bool aligned = VEC > 1 && ld_partial % 4 == 0 && (reinterpret_cast<uintptr_t>(partial) & 15u) == 0;
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+        const int v = tid + u * nt;
+        if (v >= nvec) continue;
+        if (aligned) {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) *reinterpret_cast<float4 *>(out + (int64_t)v * VEC + i) = make_float4(acc[u][i], acc[u][i + 1 < VEC ? i + 1 : 0], acc[u][i + 2 < VEC ? i + 2 : 0], acc[u][i + 3 < VEC ? i + 3 : 0]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) out[(int64_t)v * VEC + i] = acc[u][i];
+        }
+    }
+}
+
+// Longer rows in two kernels.
 // A row's (sum g xhat) / C.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(1024) cr_rms_norm_dots_kernel(const RmsNormArgs a, float *dots) {
@@ -187,9 +329,6 @@ __global__ void __launch_bounds__(1024) cr_rms_norm_dots_kernel(const RmsNormArg
     dot = block_sum(dot, sums);
     if (threadIdx.x == 0) dots[row] = dot / (float)a.cols;
 }
-
-// Rows of a partition that one block adds up: the partition's rows in at most 256 chunks of 4 to 64 rows.
-int64_t chunk_rows(int64_t rows) { return std::min<int64_t>(64, std::max<int64_t>(4, (rows + 255) / 256)); }
 
 // dx of a chunk of rows for a slab of columns, and the chunk's sums of dy xhat.
 template <typename T, int VEC>
@@ -303,6 +442,23 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
         const bool wide = vector_rows(a.elem, a.cols, {a.dy, a.dh, a.h, a.y, a.gamma}, {a.ld_dy, a.dh ? a.ld_dh : 0, a.ld_h, a.y ? a.ld_y : 0});
         auto go = [&](auto v) {
             constexpr int V = decltype(v)::value;
+            float *sums = !a.dgamma ? nullptr : chunks > 1 ? partial : a.dgamma;
+            const int64_t ld_sums = chunks > 1 ? a.cols : a.ld_gamma;
+            if (a.cols <= grad_held_cols<V>()) {
+                if (a.partitions * chunks > 0x7fffffffll) return cudaErrorInvalidValue;
+                const int64_t nvec = a.cols / V, held = grad_held<V>();
+                const int threads = (int)std::max<int64_t>(32, (nvec + held * 32 - 1) / (held * 32) * 32);
+                const size_t smem = V == 1 ? 0 : (size_t)grad_stages<V>() * 3 * held * threads * 16;
+                auto kernel = threads <= 256 ? cr_rms_norm_grad_rows_kernel<T, V, 256> : cr_rms_norm_grad_rows_kernel<T, V, kGradThreads>;
+                if (smem > 48 * 1024) {
+                    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+                    if (e != cudaSuccess) return e;
+                }
+                kernel<<<(unsigned)(a.partitions * chunks), threads, smem, stream>>>(a, sums, ld_sums, each, chunk, chunks);
+                const cudaError_t e = cudaGetLastError();
+                if (e == cudaSuccess) ++*launches;
+                return e;
+            }
             if (a.y) {
                 cr_rms_norm_dots_kernel<T, V><<<(unsigned)a.rows, row_threads<T, V>(a.cols), 0, stream>>>(a, dots);
                 const cudaError_t e = cudaGetLastError();
@@ -313,9 +469,8 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
             const int threads = (int)std::min<int64_t>(128, (nvec + 31) / 32 * 32);
             const int64_t slabs = (nvec + threads - 1) / threads;
             if (a.partitions * chunks > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-            float *sums = !a.dgamma ? nullptr : chunks > 1 ? partial : a.dgamma;
             cr_rms_norm_grad_kernel<T, V><<<(unsigned)(a.partitions * chunks * slabs), threads, 0, stream>>>(
-                a, dots, sums, chunks > 1 ? a.cols : a.ld_gamma, each, chunk, chunks, (int)slabs);
+                a, dots, sums, ld_sums, each, chunk, chunks, (int)slabs);
             const cudaError_t e = cudaGetLastError();
             if (e == cudaSuccess) ++*launches;
             return e;

@@ -141,6 +141,9 @@ TABLES = [
     (2, 4097, 256, 264, 0, 0),
     (1, 20000, 300, 20, 0, 2),
     (5, 64, 1000, 1032, 0, 0),
+    (2, 64, 1, 8, 0, 0),           # the longest sum that is not cut
+    (2, 65, 1, 8, 0, 0),           # the shortest that is
+    (1, 2100, 40, 516, 0, 0),      # sums of about 64 tokens
     (24, 39, 5004, 12, 0, 0),
     (1, 140000, 40, 8, 0, 0),      # longer tiles
 ]
@@ -180,7 +183,7 @@ def test_table_gradient(plan, shape, dtype):
     while tokens // tile > 4096:
         tile *= 2
     tiles = (tokens + tile - 1) // tile
-    chain = min(tokens, tile) + min(tiles, tiles / 4 + 256) + 4
+    chain = min(tokens, tile + 63) + min(tiles, tiles / 4 + 256) + 4      # a tile may begin up to 63 tokens early
     check(d, want, "f32", chain * STEP * size)
     again = grads(plan, dev_ids(ids, kind), dy, vocab, scale, padding, ld_pad=[0, 4, 3][width % 3])
     assert torch.equal(d, again)
