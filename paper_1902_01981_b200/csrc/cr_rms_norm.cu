@@ -54,118 +54,158 @@ __device__ __forceinline__ void load_floats(const float *p, float (&v)[VEC]) {
     }
 }
 
-// Vectors of a row that a thread keeps in registers.
+// A row is cut into pieces that a warp takes at once: kHeld vectors (or elements, where rows do not lie in vectors) a lane, a
+// warp's width apart, so that the addresses differ by constants.
 template <int VEC> __host__ __device__ constexpr int held_vectors() { return VEC == 1 ? 16 : 4; }
+template <typename T, int VEC>
+struct RowPiece {
+    static constexpr int kHeld = held_vectors<VEC>();
+    float f[kHeld][VEC];
 
-// One block a row.  The first vectors of each thread stay in registers as fp32 sums between the statistics and the output;
-// longer rows are read again (from L2).  Everything is read before the block's first barrier or by the thread that
-// writes it, so outputs may be the inputs' own buffers.
-template <typename T, int VEC, bool CODES>
-__global__ void __launch_bounds__(1024) cr_rms_norm_kernel(const RmsNormArgs a) {
-    constexpr int kHeld = held_vectors<VEC>();
+    // Vectors of this lane of piece `piece` that lie in a row of nvec.
+    static __device__ __forceinline__ int have(int64_t piece, int64_t nvec) {
+        const int64_t left = nvec - piece * kHeld * 32 - (int)threadIdx.x % 32;
+        return left >= (kHeld - 1) * 32 + 1 ? kHeld : left <= 0 ? 0 : (int)(left + 31) / 32;
+    }
+    static __device__ __forceinline__ int64_t offset(int64_t piece) { return (piece * kHeld * 32 + (int)threadIdx.x % 32) * VEC; }
+
+    // x + r of the piece; zeros where there is no more row.  x and r point at the lane's first vector.
+    __device__ __forceinline__ void load(const T *x, const T *r, int n) {
+        Packed<T, VEC> px[kHeld], pr[kHeld];
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+            if (n == kHeld || u < n) px[u] = load_packed<T, VEC>(x + u * 32 * VEC);
+        if (r) {
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u)
+                if (n == kHeld || u < n) pr[u] = load_packed<T, VEC>(r + u * 32 * VEC);
+        }
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            const bool in = n == kHeld || u < n;
+            float g[VEC];
+            unpack<T, VEC>(px[u], f[u]);
+            if (r) unpack<T, VEC>(pr[u], g);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[u][i] = in ? (r ? f[u][i] + g[i] : f[u][i]) : 0.f;
+        }
+    }
+    __device__ __forceinline__ float squares() const {
+        float s = 0.f;
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s = fmaf(f[u][i], f[u][i], s);
+        return s;
+    }
+    __device__ __forceinline__ void store(T *p, int n) const {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+            if (n == kHeld || u < n) store_packed<T, VEC>(p + u * 32 * VEC, pack<T, VEC>(f[u]));
+    }
+    // The sums times rstd and gamma.
+    __device__ __forceinline__ void norm(const float *gamma, float rstd, int n) {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            float g[VEC];
+            if (gamma && (n == kHeld || u < n)) load_floats<VEC>(gamma + u * 32 * VEC, g);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[u][i] = f[u][i] * rstd * (gamma ? g[i] : 1.f);
+        }
+    }
+    __device__ __forceinline__ uint32_t largest(int n) const {
+        uint32_t top = 0;
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (n == kHeld || u < n) top = max(top, __float_as_uint(f[u][i]) & 0x7fffffffu);
+        return top;
+    }
+    __device__ __forceinline__ void store_codes(int8_t *q, float mult, bool dead, int n) const {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            if (n != kHeld && u >= n) continue;
+            if constexpr (VEC == 1) {
+                q[u * 32] = dead ? (int8_t)0 : (int8_t)code(f[u][0], mult);
+            } else {
+                uint32_t w[VEC / 4];
+#pragma unroll
+                for (int i = 0; i < VEC / 4; ++i) {
+                    const uint32_t lo = __byte_perm(code(f[u][4 * i], mult), code(f[u][4 * i + 1], mult), 0x0040);
+                    const uint32_t hi = __byte_perm(code(f[u][4 * i + 2], mult), code(f[u][4 * i + 3], mult), 0x0040);
+                    w[i] = dead ? 0u : __byte_perm(lo, hi, 0x5410);
+                }
+                if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q + u * 32 * 8) = make_uint2(w[0], w[1]);
+                else *reinterpret_cast<uint32_t *>(q + u * 32 * 4) = w[0];
+            }
+        }
+    }
+};
+
+// One block a row.  A warp's piece stays in registers between the statistics and the output; rows of more pieces than a block
+// has warps (LONG) are read again for each (from L2).  Everything is read before the block's first barrier or by the thread
+// that writes it, so outputs may be the inputs' own buffers.
+constexpr int kRowWarps = 16;
+template <typename T, int VEC, bool CODES, bool LONG>
+__global__ void __launch_bounds__(32 * kRowWarps) cr_rms_norm_kernel(const RmsNormArgs a) {
+    using P = RowPiece<T, VEC>;
     __shared__ float sums[32];
     __shared__ uint32_t tops[32];
     const int64_t row = blockIdx.x;
     const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
     const T *r = a.residual ? static_cast<const T *>(a.residual) + row * a.ld_residual : nullptr;
     T *h = a.h ? static_cast<T *>(a.h) + row * a.ld_h : nullptr;
-    const int64_t nvec = a.cols / VEC;
-    const int nt = (int)blockDim.x, tid = (int)threadIdx.x;
-    auto sum_at = [&](int64_t v, float (&f)[VEC]) {
-        unpack<T, VEC>(load_packed<T, VEC>(x + v * VEC), f);
-        if (r) {
-            float g[VEC];
-            unpack<T, VEC>(load_packed<T, VEC>(r + v * VEC), g);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) f[i] += g[i];
-        }
+    const int64_t nvec = a.cols / VEC, pieces = (nvec + P::kHeld * 32 - 1) / (P::kHeld * 32);
+    const int warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32;
+    P p;
+    auto load = [&](int64_t piece) { p.load(x + P::offset(piece), r ? r + P::offset(piece) : nullptr, P::have(piece, nvec)); };
+    // f(piece) for the warp's pieces
+    auto each = [&](auto &&f) {
+        if constexpr (LONG)
+            for (int64_t piece = warp; piece < pieces; piece += warps) f(piece);
+        else
+            f((int64_t)warp);
     };
-    float held[kHeld][VEC];
-#pragma unroll
-    for (int u = 0; u < kHeld; ++u)
-        if (tid + u * nt < nvec) sum_at(tid + u * nt, held[u]);
     float squares = 0.f;
-#pragma unroll
-    for (int u = 0; u < kHeld; ++u)
-        if (tid + u * nt < nvec) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) squares = fmaf(held[u][i], held[u][i], squares);
-        }
-    for (int64_t v = tid + (int64_t)kHeld * nt; v < nvec; v += nt) {
-        float f[VEC];
-        sum_at(v, f);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) squares = fmaf(f[i], f[i], squares);
-    }
+    each([&](int64_t piece) {
+        load(piece);
+        squares += p.squares();
+    });
     const float rstd = 1.f / sqrtf(block_sum(squares, sums) / (float)a.cols + a.eps);
-    if (a.rstd && tid == 0) a.rstd[row] = rstd;
-    // y of vector v in place of its sum
-    auto norm = [&](int64_t v, const float (&f)[VEC], float (&z)[VEC]) {
-        float g[VEC];
-        if (a.gamma) load_floats<VEC>(a.gamma + v * VEC, g);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) z[i] = f[i] * rstd * (a.gamma ? g[i] : 1.f);
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+    // y of the piece in the place of the sums, which are stored
+    auto norm = [&](int64_t piece, bool store) {
+        const int n = P::have(piece, nvec);
+        if (store && h) p.store(h + P::offset(piece), n);
+        p.norm(a.gamma ? a.gamma + P::offset(piece) : nullptr, rstd, n);
     };
-    RowScale rs = {0.f, 0.f};
-    bool dead = false;
     if constexpr (CODES) {
         uint32_t top = 0;
-        auto widen = [&](const float (&z)[VEC]) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) top = max(top, __float_as_uint(z[i]) & 0x7fffffffu);
-        };
-#pragma unroll
-        for (int u = 0; u < kHeld; ++u)
-            if (tid + u * nt < nvec) {
-                const int64_t v = tid + u * nt;
-                if (h) store_packed<T, VEC>(h + v * VEC, pack<T, VEC>(held[u]));
-                norm(v, held[u], held[u]);
-                widen(held[u]);
-            }
-        for (int64_t v = tid + (int64_t)kHeld * nt; v < nvec; v += nt) {
-            float f[VEC], z[VEC];
-            sum_at(v, f);
-            norm(v, f, z);
-            widen(z);
-        }
+        each([&](int64_t piece) {
+            if constexpr (LONG) load(piece);
+            norm(piece, !LONG);
+            top = max(top, p.largest(P::have(piece, nvec)));
+        });
         top = block_max(top, tops);
-        rs = row_scale(top);
-        dead = top >= 0x7f800000u;
-        if (tid == 0) a.scale[row] = rs.scale;
-    }
-    auto put_code = [&](int64_t v, const float (&z)[VEC]) {
-        int8_t *q = a.q + row * a.ld_q + v * VEC;
-        if constexpr (VEC == 1) {
-            *q = dead ? (int8_t)0 : (int8_t)code(z[0], rs.mult);
-        } else {
-            uint32_t w[VEC / 4];
-#pragma unroll
-            for (int i = 0; i < VEC / 4; ++i) {
-                const uint32_t lo = __byte_perm(code(z[4 * i], rs.mult), code(z[4 * i + 1], rs.mult), 0x0040);
-                const uint32_t hi = __byte_perm(code(z[4 * i + 2], rs.mult), code(z[4 * i + 3], rs.mult), 0x0040);
-                w[i] = dead ? 0u : __byte_perm(lo, hi, 0x5410);
+        const RowScale rs = row_scale(top);
+        const bool dead = top >= 0x7f800000u;      // an infinity or a NaN: codes 0
+        if (threadIdx.x == 0) a.scale[row] = rs.scale;
+        int8_t *q = a.q + row * a.ld_q;
+        each([&](int64_t piece) {
+            if constexpr (LONG) {
+                load(piece);
+                norm(piece, true);
             }
-            if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
-            else *reinterpret_cast<uint32_t *>(q) = w[0];
-        }
-    };
-    auto put = [&](int64_t v, const float (&f)[VEC]) {
-        if (h) store_packed<T, VEC>(h + v * VEC, pack<T, VEC>(f));
-        float z[VEC];
-        norm(v, f, z);
-        if constexpr (CODES) put_code(v, z);
-        else store_packed<T, VEC>(static_cast<T *>(a.y) + row * a.ld_y + v * VEC, pack<T, VEC>(z));
-    };
-#pragma unroll
-    for (int u = 0; u < kHeld; ++u)
-        if (tid + u * nt < nvec) {
-            if constexpr (CODES) put_code(tid + u * nt, held[u]);     // the sums are stored already
-            else put(tid + u * nt, held[u]);
-        }
-    for (int64_t v = tid + (int64_t)kHeld * nt; v < nvec; v += nt) {
-        float f[VEC];
-        sum_at(v, f);
-        put(v, f);
+            p.store_codes(q + P::offset(piece), rs.mult, dead, P::have(piece, nvec));
+        });
+    } else {
+        T *y = static_cast<T *>(a.y) + row * a.ld_y;
+        each([&](int64_t piece) {
+            if constexpr (LONG) load(piece);
+            norm(piece, true);
+            p.store(y + P::offset(piece), P::have(piece, nvec));
+        });
     }
 }
 
@@ -180,7 +220,7 @@ int64_t chunk_rows(int64_t rows) { return std::min<int64_t>(64, std::max<int64_t
 // fetched a row ahead into registers.
 constexpr int kGradThreads = 512;
 template <int VEC> __host__ __device__ constexpr int grad_stages() { return VEC == 1 ? 1 : VEC == 4 ? 2 : 4; }
-template <int VEC> __host__ __device__ constexpr int grad_held() { return VEC == 8 ? 2 : 4; }
+template <int VEC> __host__ __device__ constexpr int grad_held() { return VEC == 8 ? 2 : VEC == 4 ? 4 : 8; }
 template <int VEC> __host__ __device__ constexpr int64_t grad_held_cols() { return (int64_t)kGradThreads * grad_held<VEC>() * VEC; }
 
 template <typename T, int VEC>
@@ -189,17 +229,16 @@ struct RowsAhead {
     uint4 *mine;                                // this thread's first slot; slots are a block apart
     Packed<T, VEC> next[VEC == 1 ? 3 * kHeld : 1];
 
-    // Asks for tensor t's vectors of a row.
-    __device__ __forceinline__ void fetch(int stage, int t, const T *row, int nvec) {
+    // Asks for tensor t's vectors of a row: `have` of them, a warp's width apart.
+    __device__ __forceinline__ void fetch(int stage, int t, const T *row, int have) {
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
-            const int v = (int)(threadIdx.x + u * blockDim.x);
-            if (v >= nvec) continue;
+            if (u >= have) continue;
             if constexpr (VEC == 1) {
-                next[t * kHeld + u] = load_packed<T, 1>(row + v);
+                next[t * kHeld + u] = load_packed<T, 1>(row + u * 32);
             } else {
                 const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine + ((stage * 3 + t) * kHeld + u) * blockDim.x);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + (int64_t)v * VEC) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + u * 32 * VEC) : "memory");
             }
         }
     }
@@ -231,19 +270,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_g
     const int64_t part = blockIdx.x / (unsigned)chunks, first = (int64_t)(blockIdx.x % (unsigned)chunks) * chunk;
     const int count = (int)min((int64_t)chunk, rows_each - first);
     const int64_t row0 = part * rows_each + first;
-    const int nvec = (int)(a.cols / VEC), nt = (int)blockDim.x, tid = (int)threadIdx.x;
+    const int lane = (int)threadIdx.x % 32, v0 = (int)(threadIdx.x / 32) * kHeld * 32 + lane;      // this thread's first vector
+    const int left = (int)(a.cols / VEC) - v0, have = left <= 0 ? 0 : min(kHeld, (left + 31) / 32), col = v0 * VEC;
     const T *dh = static_cast<const T *>(a.dh);
     T *dx = static_cast<T *>(a.y);
     const float over = 1.f / (float)a.cols;
     RowsAhead<T, VEC> ahead;
-    ahead.mine = staged + tid;
+    ahead.mine = staged + threadIdx.x;
     auto fetch = [&](int k) {
         const int64_t row = row0 + k;
         const int stage = k % kAhead;
         if (k < count) {
-            ahead.fetch(stage, 0, static_cast<const T *>(a.dy) + row * a.ld_dy, nvec);
-            ahead.fetch(stage, 1, static_cast<const T *>(a.h) + row * a.ld_h, nvec);
-            if (dh) ahead.fetch(stage, 2, dh + row * a.ld_dh, nvec);
+            ahead.fetch(stage, 0, static_cast<const T *>(a.dy) + row * a.ld_dy + col, have);
+            ahead.fetch(stage, 1, static_cast<const T *>(a.h) + row * a.ld_h + col, have);
+            if (dh) ahead.fetch(stage, 2, dh + row * a.ld_dh + col, have);
         }
         ahead.asked();
     };
@@ -253,7 +293,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_g
     for (int u = 0; u < kHeld; ++u) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) w[u][i] = 1.f;
-        if (a.gamma && tid + u * nt < nvec) load_floats<VEC>(a.gamma + (tid + u * nt) * VEC, w[u]);
+        if (a.gamma && u < have) load_floats<VEC>(a.gamma + col + u * 32 * VEC, w[u]);
     }
     float rstd_ahead = a.rstd[row0];
     for (int k = 0; k < count; ++k) {
@@ -263,7 +303,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_g
         ahead.arrived();
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
-            if (tid + u * nt >= nvec) continue;
+            if (u >= have) continue;
             ahead.take(k % kAhead, 0, u, fg[u]);
             ahead.take(k % kAhead, 1, u, fx[u]);
             if (dh && VEC == 1) ahead.take(k % kAhead, 2, u, d[u]);
@@ -281,29 +321,27 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_g
             dot = block_sum(dot, sums[k & 1]) * over;
 #pragma unroll
             for (int u = 0; u < kHeld; ++u) {
-                const int v = tid + u * nt;
-                if (v >= nvec) continue;
+                if (u >= have) continue;
                 if (dh && VEC > 1) ahead.take(k % kAhead, 2, u, d[u]);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) d[u][i] = fmaf(rstd, fmaf(-fx[u][i], dot, fg[u][i]), d[u][i]);
-                store_packed<T, VEC>(dx + (row0 + k) * a.ld_y + (int64_t)v * VEC, pack<T, VEC>(d[u]));
+                store_packed<T, VEC>(dx + (row0 + k) * a.ld_y + col + u * 32 * VEC, pack<T, VEC>(d[u]));
             }
         }
         if (VEC > 1) fetch(k + kAhead);       // into the slots just read
     }
     if (!partial) return;
-    float *out = partial + blockIdx.x * ld_partial;
+    float *out = partial + blockIdx.x * ld_partial + col;
     const bool aligned = VEC > 1 && ld_partial % 4 == 0 && (reinterpret_cast<uintptr_t>(partial) & 15u) == 0;
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) {
-        const int v = tid + u * nt;
-        if (v >= nvec) continue;
+        if (u >= have) continue;
         if (aligned) {
 #pragma unroll
-            for (int i = 0; i < VEC; i += 4) *reinterpret_cast<float4 *>(out + (int64_t)v * VEC + i) = make_float4(acc[u][i], acc[u][i + 1 < VEC ? i + 1 : 0], acc[u][i + 2 < VEC ? i + 2 : 0], acc[u][i + 3 < VEC ? i + 3 : 0]);
+            for (int i = 0; i < VEC; i += 4) *reinterpret_cast<float4 *>(out + u * 32 * VEC + i) = make_float4(acc[u][i], acc[u][i + 1 < VEC ? i + 1 : 0], acc[u][i + 2 < VEC ? i + 2 : 0], acc[u][i + 3 < VEC ? i + 3 : 0]);
         } else {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) out[(int64_t)v * VEC + i] = acc[u][i];
+            for (int i = 0; i < VEC; ++i) out[u * 32 * VEC + i] = acc[u][i];
         }
     }
 }
@@ -407,7 +445,10 @@ cudaError_t launch_rms_norm(const RmsNormArgs &a, cudaStream_t stream, int64_t *
         if (a.q) wide = wide && reinterpret_cast<uintptr_t>(a.q) % VEC == 0 && a.ld_q % VEC == 0;
         auto go = [&](auto v, auto codes) {
             constexpr int V = decltype(v)::value;
-            cr_rms_norm_kernel<T, V, decltype(codes)::value != 0><<<(unsigned)a.rows, row_threads<T, V>(a.cols), 0, stream>>>(a);
+            constexpr bool kCodes = decltype(codes)::value != 0;
+            const int64_t pieces = (a.cols / V + held_vectors<V>() * 32 - 1) / (held_vectors<V>() * 32);
+            if (pieces <= kRowWarps) cr_rms_norm_kernel<T, V, kCodes, false><<<(unsigned)a.rows, 32 * (unsigned)pieces, 0, stream>>>(a);
+            else cr_rms_norm_kernel<T, V, kCodes, true><<<(unsigned)a.rows, 32 * (unsigned)kRowWarps, 0, stream>>>(a);
         };
         if (wide) a.q ? go(Int<VEC>{}, Int<1>{}) : go(Int<VEC>{}, Int<0>{});
         else a.q ? go(Int<1>{}, Int<1>{}) : go(Int<1>{}, Int<0>{});

@@ -125,53 +125,60 @@ struct Chunk {
             return max_nan(__low2float(m), __high2float(m));
         }
     }
-    // The lane's sum of 2^u, and of 2^u u where it is wanted.
-    template <bool TURN>
-    __device__ __forceinline__ float2 sums(float base, float c) const {
+    // f(a pair of the lane's logits) for all of them.
+    template <typename F>
+    __device__ __forceinline__ void for_pairs(F &&f) const {
         if constexpr (VEC == 1) {
-            float s[2] = {}, t[2] = {};
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                float w = (to_float(r[u].e) - base) * c;
-                if constexpr (TURN) w = max_nan(w, kLeast);
-                const float e = exp2_approx(w);
-                s[u & 1] += e;
-                if constexpr (TURN) t[u & 1] = fmaf(e, w, t[u & 1]);
-            }
-            return make_float2(s[0] + s[1], t[0] + t[1]);
+            for (int u = 0; u < kUnroll; u += 2) f(f2(to_float(r[u].e), to_float(r[u + 1].e)));
         } else {
-            const F2 shift = f2(-base), factor = f2(c);
-            F2 s = f2(0.f), t = f2(0.f);
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
                 F2 v[VEC / 2];
                 unpack2<T, VEC>(r[u], v);
 #pragma unroll
-                for (int i = 0; i < VEC / 2; ++i) {
-                    F2 w = mul2(add2(v[i], shift), factor);
-                    if constexpr (TURN) w = f2(max_nan(low(w), kLeast), max_nan(high(w), kLeast));
-                    const F2 e = f2(exp2_approx(low(w)), exp2_approx(high(w)));
-                    s = add2(s, e);
-                    if constexpr (TURN) t = fma2(e, w, t);
-                }
+                for (int i = 0; i < VEC / 2; ++i) f(v[i]);
             }
-            return make_float2(low(s) + high(s), low(t) + high(t));
         }
     }
-    // 2^u factor of vector k.
-    __device__ __forceinline__ Packed<T, VEC> scaled(int k, float base, float c, float factor) const {
+    // The lane's sum of 2^u, and of 2^u u where it is wanted.
+    template <bool TURN>
+    __device__ __forceinline__ float2 sums(float base, float c) const {
+        const F2 shift = f2(-base), factor = f2(c);
+        F2 s = f2(0.f), t = f2(0.f);
+        for_pairs([&](F2 v) {
+            F2 w = mul2(add2(v, shift), factor);
+            if constexpr (TURN) w = f2(max_nan(low(w), kLeast), max_nan(high(w), kLeast));
+            const F2 e = f2(exp2_approx(low(w)), exp2_approx(high(w)));
+            s = add2(s, e);
+            if constexpr (TURN) t = fma2(e, w, t);
+        });
+        return make_float2(low(s) + high(s), low(t) + high(t));
+    }
+    // Puts f(pair) in the places of the lane's pairs, in a row of the chunk's layout.
+    template <typename F>
+    __device__ __forceinline__ void store(T *d, int64_t vocab, int64_t chunk, F &&f) const {
+        const int lane = (int)threadIdx.x % 32;
+        T *p = d + index(chunk, lane, 0, 0);
+        const bool full = (chunk + 1) * kElements <= vocab;
+        // vectors (or elements) of the lane that lie in the row
+        const int have = full ? kUnroll : (int)max((int64_t)0, min((int64_t)kUnroll, (vocab / VEC - chunk * kUnroll * 32 - lane + 31) / 32));
         if constexpr (VEC == 1) {
-            const float f[1] = {exp2_approx((to_float(r[k].e) - base) * c) * factor};
-            return pack<T, 1>(f);
-        } else {
-            F2 v[VEC / 2];
-            unpack2<T, VEC>(r[k], v);
 #pragma unroll
-            for (int i = 0; i < VEC / 2; ++i) {
-                const F2 w = mul2(add2(v[i], f2(-base)), f2(c));
-                v[i] = mul2(f2(exp2_approx(low(w)), exp2_approx(high(w))), f2(factor));
+            for (int u = 0; u < kUnroll; u += 2) {
+                const F2 v = f(f2(to_float(r[u].e), to_float(r[u + 1].e)));
+                if (full || u < have) p[u * 32] = from_float<T>(low(v));
+                if (full || u + 1 < have) p[(u + 1) * 32] = from_float<T>(high(v));
             }
-            return pack2<T, VEC>(v);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                F2 v[VEC / 2];
+                unpack2<T, VEC>(r[u], v);
+#pragma unroll
+                for (int i = 0; i < VEC / 2; ++i) v[i] = f(v[i]);
+                if (full || u < have) store_packed<T, VEC>(p + u * 32 * VEC, pack2<T, VEC>(v));
+            }
         }
     }
 };
@@ -438,39 +445,43 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel
 
 // ---- their gradient ---------------------------------------------------------------------------------------------------------
 
-constexpr int kGradThreads = 256;
-template <int VEC> __host__ __device__ constexpr int grad_unroll() { return VEC == 1 ? 16 : 4; }
+constexpr int kGradWarps = 8;
 
-// A tile of a row a block.
+// A warp a chunk of a row; all loads come before the first store, which may go to the same memory.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kGradThreads) cr_token_log_probs_grad_kernel(const VocabArgs a, unsigned tiles) {
-    constexpr int kUnroll = grad_unroll<VEC>();
-    const int64_t row = blockIdx.x / tiles, first = (int64_t)(blockIdx.x % tiles) * kGradThreads * kUnroll;
+__global__ void __launch_bounds__(32 * kGradWarps) cr_token_log_probs_grad_kernel(const VocabArgs a, unsigned chunks, int64_t items) {
+    using C = Chunk<T, VEC>;
+    const int64_t item = (int64_t)blockIdx.x * kGradWarps + threadIdx.x / 32;
+    if (item >= items) return;
+    const int64_t row = item < 0x7fffffffll ? (unsigned)item / chunks : item / chunks, chunk = item - row * chunks;
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     T *d = static_cast<T *>(a.dlogits) + row * a.ld_d;
-    const int64_t nvec = a.vocab / VEC;
-    const float c = a.inverse * kLog2e;
-    const float m = a.stats[2 * row], base = isinf(m) ? 0.f : m, log_sum = a.stats[2 * row + 1] * kLog2e;
+    C data;
+    data.load(x, a.vocab, chunk);
     int64_t id = a.dlogp ? id_at(a.ids, a.id_bytes, row) : -1;
-    if (id < 0 || id >= a.vocab) id = -1;
+    if (id >= a.vocab) id = -1;
+    const bool here = id >= 0 && id / C::kElements == chunk;
+    const float picked = here ? to_float(x[id]) : 0.f;
+    const float2 stats = reinterpret_cast<const float2 *>(a.stats)[row];
     const float ga = id >= 0 ? a.dlogp[row] * a.inverse : 0.f, gb = a.dentropy ? a.dentropy[row] * a.inverse : 0.f;
-    const bool none = (ga == 0.f && gb == 0.f) || m == -INFINITY;
+    const bool none = (ga == 0.f && gb == 0.f) || stats.x == -INFINITY;
+    // log2 p = (x - base) c - log_sum;  dx = -p (ga + gb (log p + H)), and ga more at the token
+    const float c = a.inverse * kLog2e, base = finite_base(stats.x), log_sum = stats.y * kLog2e;
     const float level = gb != 0.f ? fmaf(gb, a.entropy[row], ga) : ga, turn = gb * kLn2;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int64_t v = first + u * kGradThreads + (int)threadIdx.x;
-        if (v >= nvec) break;
-        float f[VEC] = {};
-        if (!none) {
-            unpack<T, VEC>(load_packed<T, VEC>(x + v * VEC), f);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float w = max_nan((f[i] - base) * c - log_sum, kLeast);     // log2 p
-                f[i] = (v * VEC + i == id ? ga : 0.f) - exp2_approx(w) * fmaf(turn, w, level);
-            }
-        }
-        store_packed<T, VEC>(d + v * VEC, pack<T, VEC>(f));
+    if (none) {
+        data.store(d, a.vocab, chunk, [](F2) { return f2(0.f); });
+        return;
     }
+    const F2 shift = f2(-base), factor = f2(c), minus_log = f2(-log_sum), minus_turn = f2(-turn), minus_level = f2(-level);
+    data.store(d, a.vocab, chunk, [&](F2 v) {
+        F2 w = fma2(add2(v, shift), factor, minus_log);
+        w = f2(max_nan(low(w), kLeast), max_nan(high(w), kLeast));
+        return mul2(f2(exp2_approx(low(w)), exp2_approx(high(w))), fma2(minus_turn, w, minus_level));
+    });
+    if (!here) return;
+    __syncwarp();
+    const float w = max_nan(fmaf(picked - base, c, -log_sum), kLeast);
+    if (threadIdx.x % 32 == 0) d[id] = from_float<T>(ga + exp2_approx(w) * fmaf(-turn, w, -level));
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------------------
@@ -481,7 +492,7 @@ constexpr int kSeenWords = 256;
 // registers over the exchange of the sums (the last one, where a warp has several) and write the gradient; then they mend the
 // elements of their own chunk that the teacher names.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(32 * (kDistillWarps + 1), 4) cr_distill_kernel(const VocabArgs a, int cluster, int slots) {
+__global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr_distill_kernel(const VocabArgs a, int cluster, int slots) {
     using C = Chunk<T, VEC>;
     extern __shared__ __align__(16) unsigned char dynamic[];
     Piece *pieces = reinterpret_cast<Piece *>(dynamic);               // [slots]
@@ -596,14 +607,14 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), 4) cr_distill_kernel
         for (int64_t chunk = slot + (chunks - 1 - slot) / kSlots * kSlots; chunk >= 0; chunk -= kSlots) {
             if (!held && !none) data.load(x, a.vocab, chunk);
             held = false;
-#pragma unroll
-            for (int u = 0; u < C::kUnroll; ++u) {
-                const int64_t v = C::index(chunk, lane, u, 0);
-                Packed<T, VEC> out = {};
-                if (!none) out = data.scaled(u, base, c, factor);
-                if (v < a.vocab) store_packed<T, VEC>(d + v, out);
+            if (none) {
+                data.store(d, a.vocab, chunk, [](F2) { return f2(0.f); });
+                continue;
             }
-            if (none) continue;
+            data.store(d, a.vocab, chunk, [&](F2 v) {
+                const F2 w = mul2(add2(v, f2(-base)), f2(c));
+                return mul2(f2(exp2_approx(low(w)), exp2_approx(high(w))), f2(factor));
+            });
             __syncwarp();
             const int64_t first = chunk * C::kElements;
             for (int j = lane; j < a.top; j += 32) {
@@ -677,10 +688,11 @@ cudaError_t launch_token_log_probs(const VocabArgs &a, const DeviceInfo &dev, cu
 cudaError_t launch_token_log_probs_backward(const VocabArgs &a, cudaStream_t stream, int64_t *launches) {
     if (a.rows == 0) return cudaSuccess;
     return by_form(a, [&](auto t, auto v) {
-        constexpr int VEC = decltype(v)::value, kTile = kGradThreads * grad_unroll<VEC>();
-        const int64_t nvec = a.vocab / VEC, tiles = (nvec + kTile - 1) / kTile;
-        if (a.rows > 0x7fffffffll / tiles) return cudaErrorInvalidValue;
-        cr_token_log_probs_grad_kernel<decltype(t), VEC><<<(unsigned)(a.rows * tiles), kGradThreads, 0, stream>>>(a, (unsigned)tiles);
+        using T = decltype(t);
+        constexpr int VEC = decltype(v)::value;
+        const int64_t chunks = (a.vocab + Chunk<T, VEC>::kElements - 1) / Chunk<T, VEC>::kElements, items = a.rows * chunks;
+        if ((items + kGradWarps - 1) / kGradWarps > 0x7fffffffll) return cudaErrorInvalidValue;
+        cr_token_log_probs_grad_kernel<T, VEC><<<(unsigned)((items + kGradWarps - 1) / kGradWarps), 32 * kGradWarps, 0, stream>>>(a, (unsigned)chunks, items);
         const cudaError_t e = cudaGetLastError();
         if (e == cudaSuccess) ++*launches;
         return e;
