@@ -1432,7 +1432,7 @@ cr_status_t cr_embedding(cr_plan_t *plan, const void *ids, int32_t id_bytes, con
 
 size_t cr_embedding_backward_workspace_bytes(const cr_plan_t *plan, int64_t tokens, int64_t partitions, int64_t vocab, int64_t width) {
     if (!plan || !good_embedding(tokens, partitions, vocab, width) || partitions == 0 || vocab == 0 || width == 0) return 0;
-    return cr::embedding_backward_workspace_bytes(tokens, partitions, width);
+    return cr::embedding_backward_workspace_bytes(tokens, partitions, vocab, width);
 }
 
 cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_bytes, const void *dy, int64_t ld_dy,
@@ -1445,7 +1445,7 @@ cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_b
     if (partitions == 0 || vocab == 0 || width == 0) return CR_OK;
     if (!dtable || !on_float(dtable) || !good_rows(vocab, width, ld_row) || !good_rows(partitions, vocab * ld_row, ld_partition)) return CR_ERR_INVALID_ARG;
     if (tokens > 0 && (!ids || !dy || !good_rows(tokens * partitions, width, ld_dy) || !on_element(dy, elem))) return CR_ERR_INVALID_ARG;
-    const size_t need = cr::embedding_backward_workspace_bytes(tokens, partitions, width);
+    const size_t need = cr::embedding_backward_workspace_bytes(tokens, partitions, vocab, width);
     if (need && (!workspace || workspace_bytes < need)) return CR_ERR_OOM;
     if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CR_ERR_INVALID_ARG;
     cr::EmbeddingArgs a;

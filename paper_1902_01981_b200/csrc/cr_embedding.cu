@@ -58,13 +58,9 @@ __global__ void __launch_bounds__(kLookupThreads) cr_embedding_kernel(const I *i
 
 // ---- sorting a partition's tokens -----------------------------------------------------------------------------------------
 
-constexpr int kDigitBits = 8, kBins = 1 << kDigitBits, kMaxCluster = 8;
+constexpr int kDigitBits = 8, kBins = 1 << kDigitBits, kMaxCluster = 8, kSortOneCta = 2048;
 
-__device__ __forceinline__ void sort_meet(int cluster) {
-    if (cluster == 1) {
-        __syncthreads();
-        return;
-    }
+__device__ __forceinline__ void sort_meet() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -82,8 +78,9 @@ struct GradArgs {
     uint2 *pairs;                // [partitions][2][tokens]
     int32_t *bounds;             // [partitions][tiles + 1]: where the tiles begin
     int32_t *far;                // [partitions][1 + tiles]: count and tiles where a sum first goes on from the tile before
+    uint32_t *named;             // [partitions][words]: a bit a number, set if a token names it; null: no tokens
     int64_t tokens, vocab, padding, ld_dy, ld_row, ld_partition;
-    int width, tile, tiles, passes;
+    int width, tile, tiles, passes, words;
     float scale;
 };
 
@@ -95,32 +92,6 @@ __device__ __forceinline__ void store_floats(float *p, const float (&v)[VEC], fl
 #pragma unroll
         for (int i = 0; i < VEC / 4; ++i)
             reinterpret_cast<float4 *>(p)[i] = make_float4(v[4 * i] * scale, v[4 * i + 1] * scale, v[4 * i + 2] * scale, v[4 * i + 3] * scale);
-    }
-}
-
-// Zeroes the rows of one range of numbers that no token of the partition names; the tokens are marked in shared memory.
-template <typename I>
-__device__ __forceinline__ void zero_rows(const GradArgs &a, const I *ids, int64_t part, int64_t first, int64_t rows, bool vectors, uint32_t *named, int words) {
-    for (int64_t v0 = first; v0 < first + rows; v0 += (int64_t)words * 32) {
-        const int n = (int)min((int64_t)words * 32, first + rows - v0);
-        for (int i = threadIdx.x; i < words; i += blockDim.x) named[i] = 0;
-        __syncthreads();
-#pragma unroll 4
-        for (int64_t i = threadIdx.x; i < a.tokens; i += blockDim.x) {
-            const int64_t id = (int64_t)ids[i], v = id - v0;
-            if (v >= 0 && v < n && id != a.padding) atomicOr(&named[v / 32], 1u << (v % 32));
-        }
-        __syncthreads();
-        // a warp a row
-        for (int r = (int)threadIdx.x / 32; r < n; r += (int)blockDim.x / 32) {
-            if (named[r / 32] >> (r % 32) & 1u) continue;
-            float *out = a.dtable + part * a.ld_partition + (v0 + r) * a.ld_row;
-            if (vectors)
-                for (int c = (int)threadIdx.x % 32 * 4; c < a.width; c += 128) *reinterpret_cast<float4 *>(out + c) = make_float4(0.f, 0.f, 0.f, 0.f);
-            else
-                for (int c = (int)threadIdx.x % 32; c < a.width; c += 32) out[c] = 0.f;
-        }
-        __syncthreads();
     }
 }
 
@@ -145,48 +116,178 @@ __device__ __forceinline__ int tile_begin(const uint2 *pairs, int i0, int n, boo
     return cut ? i0 : i0 - back;
 }
 
+// The lanes that hold this lane's digit: a vote a bit (the match instruction takes the distinct values one after the other,
+// about a hundred cycles of an SM for a warp's random digits: 57 us for 16384 tokens).  Without meaning for a lane that has none.
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool has) {
+    uint32_t peers = __ballot_sync(0xffffffffu, has);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+        const bool one = d >> b & 1u;
+        const uint32_t m = __ballot_sync(0xffffffffu, one);
+        peers &= one ? m : ~m;
+    }
+    return peers;
+}
+
+// This thread's bin: what the warps before each warp have counted, in place of each warp's count; returns the sum.
+__device__ __forceinline__ uint32_t sum_warps(uint32_t (*hist)[kBins], int warps) {
+    uint32_t sum = 0;
+#pragma unroll
+    for (int w0 = 0; w0 < 32; w0 += 8) {
+        uint32_t c[8];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) c[w] = w0 + w < warps ? hist[w0 + w][threadIdx.x] : 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            if (w0 + w < warps) hist[w0 + w][threadIdx.x] = sum;
+            sum += c[w];
+        }
+    }
+    return sum;
+}
+
+// Marks the numbers that occur, and cuts the sorted sequence into tiles: the threads of a partition, `first` among `all`, and its
+// warps.  a.named is zero and far[0] is zero by now.
+__device__ __forceinline__ void cut_tiles(const GradArgs &a, int64_t part, const uint2 *sorted, int count, int first, int all) {
+    uint32_t *named = a.named + part * a.words;
+    for (int i = first; i < count; i += all) {
+        const uint32_t v = sorted[i].x;
+        if (i == 0 || sorted[i - 1].x != v) atomicOr(&named[v / 32], 1u << (v % 32));
+    }
+    int32_t *bounds = a.bounds + part * (a.tiles + 1), *far = a.far + part * (a.tiles + 1);
+    for (int64_t t = first / 32; t <= a.tiles; t += all / 32) {
+        const int64_t i0 = t * a.tile;
+        int begin = (int)min(i0, (int64_t)count);
+        if (t > 0 && i0 < count) {
+            bool cut;
+            begin = tile_begin(sorted, (int)i0, count, cut);
+            if (cut && first % 32 == 0) {
+                // the first tile into which the number reaches: only from a number's first tile on does a sum go on
+                const int64_t earlier = i0 - a.tile;
+                if (earlier == 0 || sorted[earlier - 1].x != sorted[i0].x) far[1 + atomicAdd(&far[0], 1)] = (int32_t)t;
+            }
+        }
+        if (first % 32 == 0) bounds[t] = begin;
+    }
+}
+
 // Sorts (number, position) of the tokens of a partition that name a row, by number, then position: digits of 8 bits from
-// the lowest up, each pass stable.  A cluster of CTAs takes a partition; each warp owns a run of consecutive entries, counts
-// its digits (lanes with one digit find each other by match), and after the counts of all warps have been summed up it
-// puts its entries in place in order.  The buffers are in global memory (L2).  Then the sequence is cut into tiles.  Bound by
-// latency, a few dependent steps a pass; meanwhile further CTAs of the grid, `zeroers` for a partition, write the rows that need no
-// sums, which is bound by memory.
-template <typename I, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const GradArgs a, const I *ids, int64_t partitions, int cluster, int zeroers,
-                                                                   bool vectors) {
+// the lowest up, each pass stable.  Up to 1024 EACH tokens, one CTA, everything on the chip: a thread holds EACH entries, lanes with
+// one digit find each other, which gives an entry its rank among its warp's; the counts of the warps and digits
+// are summed up, and the entries go to their places in shared memory.  Then the sequence is cut into tiles.  Bound by latency,
+// a few dependent steps an entry and pass.
+template <typename I, int EACH>
+__global__ void __launch_bounds__(1024, 1) cr_token_sort_kernel(const GradArgs a, const I *ids) {
+    extern __shared__ uint2 entries[];           // [32 EACH warps]
+    __shared__ uint32_t hist[32][kBins], base[kBins], scan[kBins / 32];
+    const int64_t part = blockIdx.x;
+    const int tid = (int)threadIdx.x, nt = (int)blockDim.x, warp = tid / 32, lane = tid % 32, warps = nt / 32;
+    const uint32_t below = (1u << lane) - 1u;
+    const int mine = warp * 32 * EACH + lane;    // this thread's entries are 32 apart
+    ids += part * a.tokens;
+    if (tid == 0) a.far[part * (a.tiles + 1)] = 0;
+    for (int w = tid; w < a.words; w += nt) a.named[part * a.words + w] = 0;
+    uint32_t key[EACH], place[EACH];             // a place: position in the low half, rank in the high half
+    bool in[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int i = mine + k * 32;
+        const int64_t id = i < a.tokens ? (int64_t)ids[i] : -1;
+        in[k] = id >= 0 && id < a.vocab && id != a.padding;
+        key[k] = (uint32_t)id;
+        place[k] = (uint32_t)i;
+    }
+    int count = 0;
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * kDigitBits;
+        for (int b = lane; b < kBins; b += 32) hist[warp][b] = 0;
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const uint32_t d = in[k] ? (key[k] >> shift) & (kBins - 1) : kBins;
+            const uint32_t peers = same_digit(d, in[k]);
+            const uint32_t before = in[k] ? hist[warp][d] : 0;
+            place[k] = (place[k] & 0xffffu) | (before + __popc(peers & below)) << 16;
+            __syncwarp();
+            if (in[k] && (peers & below) == 0) hist[warp][d] = before + __popc(peers);
+            __syncwarp();
+        }
+        __syncthreads();
+        uint32_t sum = 0, inclusive = 0;
+        if (tid < kBins) {
+            sum = sum_warps(hist, warps);
+            inclusive = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t v = __shfl_up_sync(0xffffffffu, inclusive, o);
+                if (lane >= o) inclusive += v;
+            }
+            if (lane == 31) scan[warp] = inclusive;
+        }
+        __syncthreads();
+        uint32_t before = 0;
+        count = 0;
+#pragma unroll
+        for (int w = 0; w < kBins / 32; ++w) {
+            if (w < warp) before += scan[w];
+            count += (int)scan[w];
+        }
+        if (tid < kBins) base[tid] = before + inclusive - sum;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            if (!in[k]) continue;
+            const uint32_t d = (key[k] >> shift) & (kBins - 1);
+            entries[base[d] + hist[warp][d] + (place[k] >> 16)] = make_uint2(key[k], place[k] & 0xffffu);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int i = mine + k * 32;
+            in[k] = i < count;
+            if (!in[k]) continue;
+            key[k] = entries[i].x;
+            place[k] = entries[i].y;
+        }
+    }
+    uint2 *pairs = a.pairs + part * 2 * a.tokens;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+        if (in[k]) pairs[mine + k * 32] = make_uint2(key[k], place[k] & 0xffffu);
+    cut_tiles(a, part, entries, count, tid, nt);
+}
+
+// More tokens: a cluster of CTAs takes a partition; each warp owns a run of consecutive entries and goes over it twice a
+// pass, first counting, then putting them in place, kBatch times 32 of them in flight.  The buffers are in global memory (L2).
+template <typename I>
+__global__ void __launch_bounds__(1024, 1) cr_token_sort_cluster_kernel(const GradArgs a, const I *ids) {
+    constexpr int WARPS = 32, cluster = kMaxCluster;
     static_assert(WARPS * 32 >= kBins, "a thread a bin");
     __shared__ uint32_t hist[WARPS][kBins];
-    __shared__ uint32_t total[kBins], scan[kBins / 32];
-    const int64_t sorters = a.tokens > 0 ? partitions * cluster : 0;
-    if (blockIdx.x >= sorters) {      // whole clusters: nobody waits for these CTAs
-        const int64_t z = blockIdx.x - sorters, part = z / zeroers;
-        if (part >= partitions) return;
-        const int64_t each = (a.vocab + zeroers - 1) / zeroers, first = z % zeroers * each;
-        if (first < a.vocab) zero_rows(a, ids + part * a.tokens, part, first, min(each, a.vocab - first), vectors, &hist[0][0], WARPS * kBins);
-        return;
-    }
+    __shared__ uint32_t total[kBins], base[kBins], scan[kBins / 32];
     const int64_t part = blockIdx.x / (unsigned)cluster;
     const int rank = (int)(blockIdx.x % (unsigned)cluster), tid = (int)threadIdx.x, warp = tid / 32, lane = tid % 32;
     const uint32_t below = (1u << lane) - 1u;
     ids += part * a.tokens;
     uint2 *buffer[2] = {a.pairs + part * 2 * a.tokens, a.pairs + (part * 2 + 1) * a.tokens};
-    int32_t *far = a.far + part * (a.tiles + 1);
-    if (rank == 0 && tid == 0) far[0] = 0;
+    if (rank == 0 && tid == 0) a.far[part * (a.tiles + 1)] = 0;
+    uint32_t *named = a.named + part * a.words;
+    for (int w = rank * WARPS * 32 + tid; w < a.words; w += cluster * WARPS * 32) named[w] = 0;
     int count = (int)a.tokens;
     for (int pass = 0; pass < a.passes; ++pass) {
         // the last pass writes into buffer 0
         const int into = (a.passes - 1 - pass) & 1;
         const uint2 *from = buffer[into ^ 1];
         uint2 *to = buffer[into];
-        const int64_t warps = (int64_t)cluster * WARPS;
-        const int64_t each = (count + warps * 32 - 1) / (warps * 32) * 32;
-        const int64_t begin = min((int64_t)count, (rank * WARPS + warp) * each), end = min((int64_t)count, begin + each);
-        auto entry = [&](int64_t i, uint2 &e) -> uint32_t {      // the digit; kBins: no entry
+        constexpr unsigned kShares = 32 * cluster * WARPS;
+        const unsigned each = ((unsigned)count + kShares - 1) / kShares * 32;      // positions and sums of a few fit 32 bits unsigned
+        const unsigned begin = min((unsigned)count, (unsigned)(rank * WARPS + warp) * each), end = min((unsigned)count, begin + each);
+        auto entry = [&](unsigned i, uint2 &e) -> uint32_t {      // the digit; kBins: no entry
             if (i >= end) return kBins;
             if (pass == 0) {
                 const int64_t id = (int64_t)ids[i];
                 if (id < 0 || id >= a.vocab || id == a.padding) return kBins;
-                e = make_uint2((uint32_t)id, (uint32_t)i);
+                e = make_uint2((uint32_t)id, i);
             } else {
                 e = from[i];
             }
@@ -194,40 +295,32 @@ __global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const GradArg
         };
         for (int b = lane; b < kBins; b += 32) hist[warp][b] = 0;
         __syncwarp();
-        for (int64_t i = begin; i < end; i += 32) {
+        constexpr int kBatch = 4;
+        for (unsigned i = begin; i < end; i += 32 * kBatch) {
             uint2 e;
-            const uint32_t d = entry(i + lane, e);
-            const uint32_t peers = __match_any_sync(0xffffffffu, d);
-            if (d < kBins && (peers & below) == 0) hist[warp][d] += __popc(peers);
-            __syncwarp();
+            uint32_t d[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) d[k] = entry(i + k * 32 + lane, e);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (i + k * 32 >= end) break;
+                const uint32_t peers = same_digit(d[k], d[k] < kBins);
+                if (d[k] < kBins && (peers & below) == 0) hist[warp][d[k]] += __popc(peers);
+                __syncwarp();
+            }
         }
         __syncthreads();
-        uint32_t column[WARPS], sum = 0;         // a bin's counts, all in flight at once
-        if (tid < kBins) {
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) column[w] = hist[w][tid];
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                const uint32_t t = column[w];
-                column[w] = sum;
-                sum += t;
-            }
-            total[tid] = sum;
-        }
-        sort_meet(cluster);
+        if (tid < kBins) total[tid] = sum_warps(hist, WARPS);
+        sort_meet();
         uint32_t mine = 0, before = 0, inclusive = 0;
         if (tid < kBins) {
-            if (cluster == 1) {
-                mine = sum;
-            } else {
-                uint32_t v[kMaxCluster];
+            uint32_t v[cluster];
 #pragma unroll
-                for (int r = 0; r < kMaxCluster; ++r) v[r] = r < cluster ? peer_word(&total[tid], r) : 0;
+            for (int r = 0; r < cluster; ++r) v[r] = peer_word(&total[tid], r);
 #pragma unroll
-                for (int r = 0; r < kMaxCluster; ++r) {
-                    if (r < rank) before += v[r];
-                    mine += v[r];
-                }
+            for (int r = 0; r < cluster; ++r) {
+                if (r < rank) before += v[r];
+                mine += v[r];
             }
             inclusive = mine;
 #pragma unroll
@@ -244,60 +337,51 @@ __global__ void __launch_bounds__(32 * WARPS) cr_token_sort_kernel(const GradArg
             if (w < warp) before += scan[w];
             all += scan[w];
         }
-        if (tid < kBins) {
-            before += inclusive - mine;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) hist[w][tid] = before + column[w];
-        }
+        if (tid < kBins) base[tid] = before + inclusive - mine;
         __syncthreads();
-        for (int64_t i = begin; i < end; i += 32) {
-            uint2 e;
-            const uint32_t d = entry(i + lane, e);
-            const uint32_t peers = __match_any_sync(0xffffffffu, d);
-            if (d < kBins) to[hist[warp][d] + __popc(peers & below)] = e;
-            __syncwarp();
-            if (d < kBins && (peers & below) == 0) hist[warp][d] += __popc(peers);
-            __syncwarp();
-        }
-        count = (int)all;
-        sort_meet(cluster);     // the entries are in place, and nobody reads a peer's counts any more
-    }
-    int32_t *bounds = a.bounds + part * (a.tiles + 1);
-    const uint2 *sorted = buffer[0];
-    for (int64_t t = rank * WARPS + warp; t <= a.tiles; t += (int64_t)cluster * WARPS) {
-        const int64_t i0 = t * a.tile;
-        int begin = (int)min(i0, (int64_t)count);
-        if (t > 0 && i0 < count) {
-            bool cut;
-            begin = tile_begin(sorted, (int)i0, count, cut);
-            if (cut && lane == 0) {
-                // the first tile into which the number reaches: only from a number's first tile on does a sum go on
-                const int64_t earlier = i0 - a.tile;
-                if (earlier == 0 || sorted[earlier - 1].x != sorted[i0].x) far[1 + atomicAdd(&far[0], 1)] = (int32_t)t;
+        for (unsigned i = begin; i < end; i += 32 * kBatch) {
+            uint2 e[kBatch];
+            uint32_t d[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) d[k] = entry(i + k * 32 + lane, e[k]);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (i + k * 32 >= end) break;
+                const uint32_t peers = same_digit(d[k], d[k] < kBins);
+                if (d[k] < kBins) to[base[d[k]] + hist[warp][d[k]] + __popc(peers & below)] = e[k];
+                __syncwarp();
+                if (d[k] < kBins && (peers & below) == 0) hist[warp][d[k]] += __popc(peers);
+                __syncwarp();
             }
         }
-        if (lane == 0) bounds[t] = begin;
+        count = (int)all;
+        sort_meet();     // the entries are in place, and nobody reads a peer's counts any more
     }
+    cut_tiles(a, part, buffer[0], count, rank * WARPS * 32 + tid, cluster * WARPS * 32);
 }
 
 // ---- sums ---------------------------------------------------------------------------------------------------------------
 
 constexpr int kSumThreads = 128;
 
-// A tile of the sorted tokens for a slab of columns: `across` threads, a vector of columns each, walk the tile's tokens and
+// A tile of the sorted tokens for a slab of columns: `across` threads, kHeld vectors of columns each, walk the tile's tokens and
 // write a sum wherever the number changes: into the table's row where the number's first token is in this tile, into the
 // tile's row of pieces where it is not.  The pairs of the next tokens are fetched with the rows of these.
+template <int VEC> __host__ __device__ constexpr int sum_held() { return VEC == 1 ? 4 : 1; }
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const GradArgs a, int across, int slabs) {
-    constexpr int kUnroll = 8;
+__device__ __forceinline__ void sum_tile(const GradArgs &a, unsigned block, int across, int slabs) {
+    constexpr int kUnroll = 8, kHeld = sum_held<VEC>();
     const int per_block = kSumThreads / across;
     const int groups = (a.tiles + per_block - 1) / per_block;
-    const unsigned item = blockIdx.x / (unsigned)slabs;
-    const int slab = (int)(blockIdx.x % (unsigned)slabs);
+    const unsigned item = block / (unsigned)slabs;
+    const int slab = (int)(block % (unsigned)slabs);
     const int64_t part = item / (unsigned)groups;
     const int tile = (int)(item % (unsigned)groups) * per_block + (int)threadIdx.x / across;
-    const int col = (slab * across + (int)threadIdx.x % across) * VEC;
+    const int col = (slab * kHeld * across + (int)threadIdx.x % across) * VEC, step = across * VEC;
     if (tile >= a.tiles || col >= a.width) return;
+    bool in[kHeld];
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q) in[q] = col + q * step < a.width;
     const int32_t *bounds = a.bounds + part * (a.tiles + 1) + tile;
     const int64_t first = bounds[0];
     const int count = bounds[1] - bounds[0];
@@ -308,36 +392,70 @@ __global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const Gr
     float *piece = a.pieces + (part * a.tiles + tile) * a.width + col;
     uint2 e[kUnroll + 1];
     bool began_before = first > 0 && pairs[-1].x == pairs[0].x;
-    float acc[VEC] = {};
+    float acc[kHeld][VEC] = {};
 #pragma unroll
     for (int u = 0; u <= kUnroll; ++u) e[u] = u < count ? pairs[u] : make_uint2(0xffffffffu, 0);
     for (int t0 = 0; t0 < count; t0 += kUnroll) {
-        Packed<T, VEC> r[kUnroll];
+        Packed<T, VEC> r[kUnroll][kHeld];
         uint2 next[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-            if (t0 + u < count) r[u] = load_packed<T, VEC>(dy + (int64_t)e[u].y * a.ld_dy);
+        for (int u = 0; u < kUnroll; ++u) {
+            const T *row = dy + (int64_t)e[u].y * a.ld_dy;
+#pragma unroll
+            for (int q = 0; q < kHeld; ++q)
+                if (t0 + u < count && in[q]) r[u][q] = load_packed<T, VEC>(row + q * step);
+        }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) next[u] = t0 + kUnroll + 1 + u < count ? pairs[t0 + kUnroll + 1 + u] : make_uint2(0xffffffffu, 0);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             if (t0 + u >= count) break;
-            float f[VEC];
-            unpack<T, VEC>(r[u], f);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[i] += f[i];
+            for (int q = 0; q < kHeld; ++q) {
+                float f[VEC];
+                unpack<T, VEC>(r[u][q], f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[q][i] += f[i];
+            }
             if (e[u + 1].x != e[u].x) {
-                if (began_before) store_floats<VEC>(piece, acc, 1.f);
-                else store_floats<VEC>(table + (int64_t)e[u].x * a.ld_row, acc, a.scale);
+                float *out = began_before ? piece : table + (int64_t)e[u].x * a.ld_row;
+                const float scale = began_before ? 1.f : a.scale;
                 began_before = false;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+                for (int q = 0; q < kHeld; ++q) {
+                    if (in[q]) store_floats<VEC>(out + q * step, acc[q], scale);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[q][i] = 0.f;
+                }
             }
         }
         e[0] = e[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) e[u + 1] = next[u];
     }
+}
+
+// Zeroes those of 32 rows that no token names, a warp a row: vectors from the row's first 16-byte boundary on.
+__device__ __forceinline__ void zero_rows(const GradArgs &a, unsigned block) {
+    const int64_t part = block / (unsigned)a.words, word = block % (unsigned)a.words;
+    const uint32_t named = a.named ? a.named[part * a.words + word] : 0;
+    const int rows = (int)min((int64_t)32, a.vocab - word * 32), lane = (int)threadIdx.x % 32;
+    for (int r = (int)threadIdx.x / 32; r < rows; r += kSumThreads / 32) {
+        if (named >> r & 1u) continue;
+        float *out = a.dtable + part * a.ld_partition + (word * 32 + r) * a.ld_row;
+        const int head = min(a.width, (int)((16 - (reinterpret_cast<uintptr_t>(out) & 15u)) / 4) % 4), body = (a.width - head) / 4 * 4;
+        if (lane < head) out[lane] = 0.f;
+#pragma unroll 4
+        for (int c = lane * 4; c < body; c += 128) *reinterpret_cast<float4 *>(out + head + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (lane < a.width - head - body) out[head + body + lane] = 0.f;
+    }
+}
+
+// Sums and zeroes in one grid: the first `sum_blocks` blocks take tiles.  Bound by memory.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const GradArgs a, unsigned sum_blocks, int across, int slabs) {
+    if (blockIdx.x < sum_blocks) sum_tile<T, VEC>(a, blockIdx.x, across, slabs);
+    else zero_rows(a, blockIdx.x - sum_blocks);
 }
 
 // Numbers whose tokens reach into further tiles: the tiles' pieces are added to the row.  `across` threads take a vector of
@@ -409,11 +527,12 @@ size_t align16(size_t b) { return (b + 15) / 16 * 16; }
 
 }  // namespace
 
-// pairs, bounds, far, pieces
-size_t embedding_backward_workspace_bytes(int64_t tokens, int64_t partitions, int64_t width) {
+// pairs, bounds, far, named, pieces
+size_t embedding_backward_workspace_bytes(int64_t tokens, int64_t partitions, int64_t vocab, int64_t width) {
     if (tokens == 0) return 0;
     const int64_t tile = tile_tokens(tokens), tiles = (tokens + tile - 1) / tile;
-    return (size_t)(partitions * tokens * 16) + 2 * align16((size_t)(partitions * (tiles + 1)) * 4) + (size_t)(tiles > 1 ? partitions * tiles * width * 4 : 0);
+    return (size_t)(partitions * tokens * 16) + 2 * align16((size_t)(partitions * (tiles + 1)) * 4) + align16((size_t)(partitions * ((vocab + 31) / 32)) * 4) +
+           (size_t)(tokens > kWhole ? partitions * tiles * width * 4 : 0);
 }
 
 cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream, int64_t *launches) {
@@ -453,78 +572,80 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
     g.padding = a.padding;
     g.tile = tile_tokens(a.tokens);
     g.tiles = (int)((a.tokens + g.tile - 1) / g.tile);
+    g.words = (int)((a.vocab + 31) / 32);
     if (a.tokens > 0) {
         char *p = static_cast<char *>(workspace);
         const size_t table = align16((size_t)(a.partitions * (g.tiles + 1)) * 4);
         g.pairs = reinterpret_cast<uint2 *>(p);
         g.bounds = reinterpret_cast<int32_t *>(p += a.partitions * a.tokens * 16);
         g.far = reinterpret_cast<int32_t *>(p += table);
-        g.pieces = reinterpret_cast<float *>(p += table);
-    }
-    int bits = 1;
-    while (bits < 31 && (1ll << bits) < a.vocab) ++bits;
-    g.passes = (bits + kDigitBits - 1) / kDigitBits;
-    const bool zero4 = table16 && g.width % 4 == 0;
-    {
-        // a CTA's warps take 32 tokens at a time: eight warps a partition up to 1024 tokens, from there on 32 warps a CTA
-        const bool small = a.tokens <= 1024;
-        int cluster = 1;
-        while (!small && cluster < kMaxCluster && a.tokens > (int64_t)cluster * 2048) cluster *= 2;
-        // A CTA that zeroes reads the partition's numbers: with those that sort two an SM (74 a partition instead of 66 left eight a
-        // partition to a second round: 93 -> 76 us of 4 x 16384 tokens over 32000 x 1024), fewer where they would read more than
-        // they write, and each at least 64 KB of rows.
-        const int64_t bytes = a.vocab * a.width * 4;
-        const int64_t least = std::max<int64_t>(64 * 1024, a.tokens * a.id_bytes);
-        const int64_t sorters = a.tokens > 0 ? a.partitions * cluster : 0;
-        const int64_t room = sorters < dev.sm_count ? 2 * dev.sm_count - sorters : 2 * dev.sm_count;
-        const int64_t zeroers = std::max<int64_t>(1, std::min<int64_t>({bytes / least, room / a.partitions, a.vocab}));
-        const int64_t ctas = sorters + (a.partitions * zeroers + cluster - 1) / cluster * cluster;
-        if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)ctas);
-        cfg.blockDim = dim3(small ? 256 : 1024);
-        cfg.stream = stream;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)cluster;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = cluster > 1 ? 1 : 0;
-        auto sort = [&](auto i, auto kernel) {
-            return cudaLaunchKernelEx(&cfg, kernel, g, static_cast<const decltype(i) *>(a.ids), a.partitions, cluster, (int)zeroers, zero4);
-        };
-        if (a.id_bytes == 4) e = small ? sort(int32_t{}, cr_token_sort_kernel<int32_t, 8>) : sort(int32_t{}, cr_token_sort_kernel<int32_t, 32>);
-        else e = small ? sort((long long){}, cr_token_sort_kernel<long long, 8>) : sort((long long){}, cr_token_sort_kernel<long long, 32>);
+        g.named = reinterpret_cast<uint32_t *>(p += table);
+        g.pieces = reinterpret_cast<float *>(p += align16((size_t)(a.partitions * g.words) * 4));
+        int bits = 1;
+        while (bits < 31 && (1ll << bits) < a.vocab) ++bits;
+        g.passes = (bits + kDigitBits - 1) / kDigitBits;
+        auto by_ids = [&](auto &&f) { return a.id_bytes == 4 ? f(int32_t{}) : f((long long){}); };
+        if (a.tokens <= kSortOneCta) {
+            e = by_ids([&](auto i) {
+                using I = decltype(i);
+                auto go = [&](auto each, auto kernel) -> cudaError_t {
+                    constexpr int EACH = decltype(each)::value;
+                    const int warps = std::max(kBins / 32, (int)((a.tokens + 32 * EACH - 1) / (32 * EACH)));
+                    const size_t smem = (size_t)warps * 32 * EACH * sizeof(uint2);
+                    if (smem > 8 * 1024) {       // beside the counters' 34 KB
+                        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+                        if (e != cudaSuccess) return e;
+                    }
+                    kernel<<<(unsigned)a.partitions, 32 * warps, smem, stream>>>(g, static_cast<const I *>(a.ids));
+                    return cudaGetLastError();
+                };
+                if (a.tokens <= 1024) return go(Int<1>{}, cr_token_sort_kernel<I, 1>);
+                return go(Int<2>{}, cr_token_sort_kernel<I, 2>);
+            });
+        } else {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(a.partitions * kMaxCluster));
+            cfg.blockDim = dim3(1024);
+            cfg.stream = stream;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = kMaxCluster;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            e = by_ids([&](auto i) { return cudaLaunchKernelEx(&cfg, cr_token_sort_cluster_kernel<decltype(i)>, g, static_cast<const decltype(i) *>(a.ids)); });
+        }
         if (e != cudaSuccess) return e;
         ++*launches;
     }
-    if (a.tokens == 0) return cudaSuccess;
     e = by_type(a.elem, [&](auto t) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T);
         const bool wide = table16 && vector_rows(a.elem, a.width, {a.dy}, {a.ld_dy});
         const int nvec = g.width / (wide ? VEC : 1);
+        const int held = wide ? 1 : sum_held<1>();
         int across = 1;
-        while (across < kSumThreads && across < nvec) across *= 2;
-        const int slabs = (nvec + across - 1) / across;
+        while (across < kSumThreads && across * held < nvec) across *= 2;
+        const int slabs = (nvec + across * held - 1) / (across * held);
         const int64_t groups = (g.tiles + kSumThreads / across - 1) / (kSumThreads / across);
-        if (a.partitions * groups > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-        const unsigned blocks = (unsigned)(a.partitions * groups * slabs);
-        if (wide) cr_embedding_sums_kernel<T, VEC><<<blocks, kSumThreads, 0, stream>>>(g, across, slabs);
-        else cr_embedding_sums_kernel<T, 1><<<blocks, kSumThreads, 0, stream>>>(g, across, slabs);
+        if (a.partitions * groups > 0x3fffffffll / slabs || a.partitions > 0x3fffffffll / g.words) return cudaErrorInvalidValue;
+        const unsigned sums = (unsigned)(a.partitions * groups * slabs), blocks = sums + (unsigned)(a.partitions * g.words);
+        if (wide) cr_embedding_sums_kernel<T, VEC><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs);
+        else cr_embedding_sums_kernel<T, 1><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs);
         return cudaGetLastError();
     });
     if (e != cudaSuccess) return e;
     ++*launches;
     if (a.tokens > kWhole) {      // otherwise no sum is cut
-        const int nvec = zero4 ? g.width / 4 : g.width;
+        const bool four = table16 && g.width % 4 == 0;
+        const int nvec = four ? g.width / 4 : g.width;
         int across = 1;
         while (across < 64 && across < nvec) across *= 2;
         const int slabs = (nvec + across - 1) / across;
         const int64_t walkers = std::min<int64_t>(a.tokens / kWhole, std::max<int64_t>(1, 4 * dev.sm_count / a.partitions));
         if (a.partitions * walkers > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
         const unsigned blocks = (unsigned)(a.partitions * walkers * slabs);
-        if (zero4) cr_embedding_join_kernel<4><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs, (unsigned)walkers);
+        if (four) cr_embedding_join_kernel<4><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs, (unsigned)walkers);
         else cr_embedding_join_kernel<1><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs, (unsigned)walkers);
         e = cudaGetLastError();
         if (e == cudaSuccess) ++*launches;

@@ -105,7 +105,7 @@ struct EmbeddingArgs {
     float scale = 1.f;
 };
 cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream, int64_t *launches);
-size_t embedding_backward_workspace_bytes(int64_t tokens, int64_t partitions, int64_t width);
+size_t embedding_backward_workspace_bytes(int64_t tokens, int64_t partitions, int64_t vocab, int64_t width);
 cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, const DeviceInfo &dev, cudaStream_t stream, int64_t *launches);
 
 struct RmsNormArgs {
