@@ -23,35 +23,35 @@ namespace {
 
 constexpr int kLookupThreads = 256;
 
-// `per_row` threads take a row, four vectors each at a time.
+// `per_row` threads take a row (several rows a warp, or several warps a row), lookup_held vectors each at a time, which lie a
+// warp's width apart.  Bound by memory: 65536 rows of 2048 bf16, 57 us for 268 MB written and a table of 131 MB.
+template <int VEC> __host__ __device__ constexpr int lookup_held() { return VEC == 1 ? 16 : 4; }
 template <typename T, int VEC, typename I>
 __global__ void __launch_bounds__(kLookupThreads) cr_embedding_kernel(const I *ids, const T *table, int64_t ld_table, T *y, int64_t ld_y, int64_t tokens,
                                                                       int64_t vocab, int nvec, int per_row, float scale) {
-    constexpr int kUnroll = 4;
+    constexpr int kHeld = lookup_held<VEC>();
     const int64_t t = (int64_t)blockIdx.x * (kLookupThreads / per_row) + (int)threadIdx.x / per_row;
     if (t >= tokens) return;
     const int64_t id = (int64_t)ids[t];
     const bool named = id >= 0 && id < vocab;
-    const T *row = table + (named ? id : 0) * ld_table;
-    T *out = y + t * ld_y;
-    for (int v0 = (int)threadIdx.x % per_row; v0 < nvec; v0 += per_row * kUnroll) {
-        Packed<T, VEC> r[kUnroll];
+    const int j = (int)threadIdx.x % per_row, step = min(per_row, 32), v0 = j / step * step * kHeld + j % step;
+    const T *row = table + (named ? id : 0) * ld_table + (int64_t)v0 * VEC;
+    T *out = y + t * ld_y + (int64_t)v0 * VEC;
+    for (int left = nvec - v0; left > 0; left -= per_row * kHeld, row += per_row * kHeld * VEC, out += per_row * kHeld * VEC) {
+        Packed<T, VEC> r[kHeld];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int v = v0 + u * per_row;
-            if (named && v < nvec) r[u] = load_packed<T, VEC>(row + (int64_t)v * VEC);
-        }
+        for (int u = 0; u < kHeld; ++u)
+            if (named && u * step < left) r[u] = load_packed<T, VEC>(row + u * step * VEC);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int v = v0 + u * per_row;
-            if (v >= nvec) break;
+        for (int u = 0; u < kHeld; ++u) {
+            if (u * step >= left) break;
             float f[VEC] = {};
             if (named) {
                 unpack<T, VEC>(r[u], f);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) f[i] *= scale;
             }
-            store_packed<T, VEC>(out + (int64_t)v * VEC, pack<T, VEC>(f));
+            store_packed<T, VEC>(out + u * step * VEC, pack<T, VEC>(f));
         }
     }
 }
@@ -542,8 +542,9 @@ cudaError_t launch_embedding(const EmbeddingArgs &a, cudaStream_t stream, int64_
         constexpr int VEC = 16 / (int)sizeof(T);
         const bool wide = vector_rows(a.elem, a.width, {a.table, a.y}, {a.ld_table, a.ld_y});
         const int nvec = (int)(wide ? a.width / VEC : a.width);
+        const int held = wide ? lookup_held<VEC>() : lookup_held<1>();
         int per_row = 1;
-        while (per_row < kLookupThreads && per_row * 4 < nvec) per_row *= 2;
+        while (per_row < kLookupThreads && per_row * held < nvec) per_row *= 2;
         const int rows = kLookupThreads / per_row;
         const unsigned blocks = (unsigned)((a.tokens + rows - 1) / rows);
         auto go = [&](auto v, auto i) {

@@ -346,63 +346,103 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_g
     }
 }
 
-// Longer rows in two kernels.
-// A row's (sum g xhat) / C.
+// Longer rows in two kernels.  The first leaves a row's (sum g xhat) / C.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(1024) cr_rms_norm_dots_kernel(const RmsNormArgs a, float *dots) {
+__global__ void __launch_bounds__(32 * kRowWarps) cr_rms_norm_dots_kernel(const RmsNormArgs a, float *dots) {
+    using P = RowPiece<T, VEC>;
     __shared__ float sums[32];
     const int64_t row = blockIdx.x;
     const T *dy = static_cast<const T *>(a.dy) + row * a.ld_dy, *h = static_cast<const T *>(a.h) + row * a.ld_h;
-    const int64_t nvec = a.cols / VEC;
-    const float rstd = a.rstd[row];
+    const int64_t nvec = a.cols / VEC, pieces = (nvec + P::kHeld * 32 - 1) / (P::kHeld * 32);
     float dot = 0.f;
-    for (int64_t v = threadIdx.x; v < nvec; v += blockDim.x) {
-        float g[VEC], x[VEC], w[VEC];
-        unpack<T, VEC>(load_packed<T, VEC>(dy + v * VEC), g);
-        unpack<T, VEC>(load_packed<T, VEC>(h + v * VEC), x);
-        if (a.gamma) load_floats<VEC>(a.gamma + v * VEC, w);
+    for (int64_t piece = threadIdx.x / 32; piece < pieces; piece += blockDim.x / 32) {
+        const int n = P::have(piece, nvec);
+        const int64_t o = P::offset(piece);
+        P g, x;
+        x.load(h + o, nullptr, n);
+        g.load(dy + o, nullptr, n);
+        g.norm(a.gamma ? a.gamma + o : nullptr, 1.f, n);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) dot = fmaf(a.gamma ? g[i] * w[i] : g[i], x[i] * rstd, dot);
+        for (int u = 0; u < P::kHeld; ++u)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (n == P::kHeld || u < n) dot = fmaf(g.f[u][i], x.f[u][i], dot);
     }
     dot = block_sum(dot, sums);
-    if (threadIdx.x == 0) dots[row] = dot / (float)a.cols;
+    if (threadIdx.x == 0) dots[row] = dot * a.rstd[row] / (float)a.cols;
 }
 
-// dx of a chunk of rows for a slab of columns, and the chunk's sums of dy xhat.
+// The second one dx of a chunk of rows for a slab of columns, and the chunk's sums of dy xhat.  A thread takes slab_held vectors
+// of columns, a warp's width apart, and asks for the next row's before it writes this row's dx.
+constexpr int kSlabThreads = 128;
+template <int VEC> __host__ __device__ constexpr int slab_held() { return VEC == 1 ? 4 : 1; }
 template <typename T, int VEC>
-__global__ void __launch_bounds__(128) cr_rms_norm_grad_kernel(const RmsNormArgs a, const float *dots, float *partial, int64_t ld_partial, int64_t rows_each,
-                                                               int chunk, int chunks, int slabs) {
+__global__ void __launch_bounds__(kSlabThreads) cr_rms_norm_grad_kernel(const RmsNormArgs a, const float *dots, float *partial, int64_t ld_partial,
+                                                                        int64_t rows_each, int chunk, int chunks, int slabs) {
+    constexpr int kHeld = slab_held<VEC>();
     const unsigned item = blockIdx.x / (unsigned)slabs;
-    const int64_t v = (int64_t)(blockIdx.x % (unsigned)slabs) * blockDim.x + threadIdx.x;
+    const int lane = (int)threadIdx.x % 32;
+    const int64_t v0 = ((int64_t)(blockIdx.x % (unsigned)slabs) * kSlabThreads + threadIdx.x / 32 * 32) * kHeld + lane, left = a.cols / VEC - v0;
     const int64_t part = item / (unsigned)chunks, c = item % (unsigned)chunks;
-    if (v >= a.cols / VEC) return;
-    const int64_t first = c * chunk, count = min((int64_t)chunk, rows_each - first);
-    float w[VEC], acc[VEC] = {};
+    if (left <= 0) return;
+    const int have = (int)min((int64_t)kHeld, (left + 31) / 32);
+    const int64_t first = c * chunk, col = v0 * VEC;
+    const int count = (int)min((int64_t)chunk, rows_each - first);
+    const int64_t row0 = part * rows_each + first;
+    const bool stream = a.y && a.dh;
+    float w[kHeld][VEC], acc[kHeld][VEC] = {};
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) w[i] = 1.f;
-    if (a.gamma) load_floats<VEC>(a.gamma + v * VEC, w);
-    for (int64_t k = 0; k < count; ++k) {
-        const int64_t row = part * rows_each + first + k;
-        const float rstd = a.rstd[row];
-        float g[VEC], x[VEC];
-        unpack<T, VEC>(load_packed<T, VEC>(static_cast<const T *>(a.dy) + row * a.ld_dy + v * VEC), g);
-        unpack<T, VEC>(load_packed<T, VEC>(static_cast<const T *>(a.h) + row * a.ld_h + v * VEC), x);
-        float d[VEC] = {};
-        if (a.y && a.dh) unpack<T, VEC>(load_packed<T, VEC>(static_cast<const T *>(a.dh) + row * a.ld_dh + v * VEC), d);
-        const float dot = a.y ? dots[row] : 0.f;
+    for (int u = 0; u < kHeld; ++u) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float xhat = x[i] * rstd;
-            acc[i] = fmaf(g[i], xhat, acc[i]);
-            d[i] = fmaf(rstd, fmaf(-xhat, dot, g[i] * w[i]), d[i]);
+        for (int i = 0; i < VEC; ++i) w[u][i] = 1.f;
+        if (a.gamma && u < have) load_floats<VEC>(a.gamma + col + u * 32 * VEC, w[u]);
+    }
+    Packed<T, VEC> g[kHeld], x[kHeld], s[kHeld];
+    float rstd = 0.f, dot = 0.f;
+    auto fetch = [&](int k) {
+        const int64_t row = row0 + k;
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            if (u >= have) continue;
+            g[u] = load_packed<T, VEC>(static_cast<const T *>(a.dy) + row * a.ld_dy + col + u * 32 * VEC);
+            x[u] = load_packed<T, VEC>(static_cast<const T *>(a.h) + row * a.ld_h + col + u * 32 * VEC);
+            if (stream) s[u] = load_packed<T, VEC>(static_cast<const T *>(a.dh) + row * a.ld_dh + col + u * 32 * VEC);
         }
-        if (a.y) store_packed<T, VEC>(static_cast<T *>(a.y) + row * a.ld_y + v * VEC, pack<T, VEC>(d));
-    }
-    if (partial) {
-        float *out = partial + item * ld_partial + v * VEC;
+        rstd = a.rstd[row];
+        if (a.y) dot = dots[row];
+    };
+    fetch(0);
+    for (int k = 0; k < count; ++k) {
+        Packed<T, VEC> out[kHeld];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) out[i] = acc[i];
+        for (int u = 0; u < kHeld; ++u) {
+            if (u >= have) continue;
+            float fg[VEC], fx[VEC], d[VEC] = {};
+            unpack<T, VEC>(g[u], fg);
+            unpack<T, VEC>(x[u], fx);
+            if (stream) unpack<T, VEC>(s[u], d);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float xhat = fx[i] * rstd;
+                acc[u][i] = fmaf(fg[i], xhat, acc[u][i]);
+                d[i] = fmaf(rstd, fmaf(-xhat, dot, fg[i] * w[u][i]), d[i]);
+            }
+            out[u] = pack<T, VEC>(d);
+        }
+        // a row's dx may be its own dy, h or dh: the next row is another one
+        if (k + 1 < count) fetch(k + 1);
+        if (!a.y) continue;
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u)
+            if (u < have) store_packed<T, VEC>(static_cast<T *>(a.y) + (row0 + k) * a.ld_y + col + u * 32 * VEC, out[u]);
     }
+    if (!partial) return;
+    float *sums = partial + item * ld_partial + col;
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (u < have) sums[u * 32 * VEC + i] = acc[u][i];
 }
 
 // dgamma of a partition from its chunks' sums: eight warps take every eighth chunk and are summed in order.
@@ -425,12 +465,6 @@ __global__ void __launch_bounds__(256) cr_rms_norm_params_kernel(const float *pa
 __global__ void cr_rms_norm_zero_kernel(float *dgamma, int64_t partitions, int64_t cols, int64_t ld) {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i < partitions * cols) dgamma[i / cols * ld + i % cols] = 0.f;
-}
-
-template <typename T, int VEC>
-int row_threads(int64_t cols) {
-    const int64_t nvec = cols / VEC, held = held_vectors<VEC>();
-    return (int)std::min<int64_t>(1024, (nvec + held * 32 - 1) / (held * 32) * 32);
 }
 
 }  // namespace
@@ -501,16 +535,14 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
                 return e;
             }
             if (a.y) {
-                cr_rms_norm_dots_kernel<T, V><<<(unsigned)a.rows, row_threads<T, V>(a.cols), 0, stream>>>(a, dots);
+                cr_rms_norm_dots_kernel<T, V><<<(unsigned)a.rows, 32 * kRowWarps, 0, stream>>>(a, dots);
                 const cudaError_t e = cudaGetLastError();
                 if (e != cudaSuccess) return e;
                 ++*launches;
             }
-            const int64_t nvec = a.cols / V;
-            const int threads = (int)std::min<int64_t>(128, (nvec + 31) / 32 * 32);
-            const int64_t slabs = (nvec + threads - 1) / threads;
+            const int64_t slab = kSlabThreads * slab_held<V>(), slabs = (a.cols / V + slab - 1) / slab;
             if (a.partitions * chunks > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-            cr_rms_norm_grad_kernel<T, V><<<(unsigned)(a.partitions * chunks * slabs), threads, 0, stream>>>(
+            cr_rms_norm_grad_kernel<T, V><<<(unsigned)(a.partitions * chunks * slabs), kSlabThreads, 0, stream>>>(
                 a, dots, sums, ld_sums, each, chunk, chunks, (int)slabs);
             const cudaError_t e = cudaGetLastError();
             if (e == cudaSuccess) ++*launches;
