@@ -215,13 +215,13 @@ __global__ void __launch_bounds__(32 * kRowWarps) cr_rms_norm_kernel(const RmsNo
 int64_t chunk_rows(int64_t rows) { return std::min<int64_t>(64, std::max<int64_t>(4, (rows + 255) / 256)); }
 
 // One block a chunk of rows: a thread keeps its columns' gamma and sums of dy xhat in registers over the rows.  Rows of up to
-// grad_held vectors a thread, 512 threads.  Each thread copies its own vectors of the rows to come into shared memory
+// grad_held vectors a thread.  Each thread copies its own vectors of the rows to come into shared memory
 // (cp.async, four rows ahead, two of fp32; no barrier, since nobody else reads them); elements that do not lie in vectors are
 // fetched a row ahead into registers.
-constexpr int kGradThreads = 512;
+template <int VEC> __host__ __device__ constexpr int grad_threads() { return VEC == 1 ? 1024 : 512; }
 template <int VEC> __host__ __device__ constexpr int grad_stages() { return VEC == 1 ? 1 : VEC == 4 ? 2 : 4; }
-template <int VEC> __host__ __device__ constexpr int grad_held() { return VEC == 8 ? 2 : VEC == 4 ? 4 : 8; }
-template <int VEC> __host__ __device__ constexpr int64_t grad_held_cols() { return (int64_t)kGradThreads * grad_held<VEC>() * VEC; }
+template <int VEC> __host__ __device__ constexpr int grad_held() { return VEC == 8 ? 2 : 4; }
+template <int VEC> __host__ __device__ constexpr int64_t grad_held_cols() { return (int64_t)grad_threads<VEC>() * grad_held<VEC>() * VEC; }
 
 template <typename T, int VEC>
 struct RowsAhead {
@@ -347,8 +347,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_g
 }
 
 // Longer rows in two kernels.  The first leaves a row's (sum g xhat) / C.
+constexpr int kDotWarps = 8;
 template <typename T, int VEC>
-__global__ void __launch_bounds__(32 * kRowWarps) cr_rms_norm_dots_kernel(const RmsNormArgs a, float *dots) {
+__global__ void __launch_bounds__(32 * kDotWarps, 3) cr_rms_norm_dots_kernel(const RmsNormArgs a, float *dots) {
     using P = RowPiece<T, VEC>;
     __shared__ float sums[32];
     const int64_t row = blockIdx.x;
@@ -524,7 +525,7 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
                 const int64_t nvec = a.cols / V, held = grad_held<V>();
                 const int threads = (int)std::max<int64_t>(32, (nvec + held * 32 - 1) / (held * 32) * 32);
                 const size_t smem = V == 1 ? 0 : (size_t)grad_stages<V>() * 3 * held * threads * 16;
-                auto kernel = threads <= 256 ? cr_rms_norm_grad_rows_kernel<T, V, 256> : cr_rms_norm_grad_rows_kernel<T, V, kGradThreads>;
+                auto kernel = threads <= 256 ? cr_rms_norm_grad_rows_kernel<T, V, 256> : cr_rms_norm_grad_rows_kernel<T, V, grad_threads<V>()>;
                 if (smem > 48 * 1024) {
                     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
                     if (e != cudaSuccess) return e;
@@ -535,7 +536,7 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
                 return e;
             }
             if (a.y) {
-                cr_rms_norm_dots_kernel<T, V><<<(unsigned)a.rows, 32 * kRowWarps, 0, stream>>>(a, dots);
+                cr_rms_norm_dots_kernel<T, V><<<(unsigned)a.rows, 32 * kDotWarps, 0, stream>>>(a, dots);
                 const cudaError_t e = cudaGetLastError();
                 if (e != cudaSuccess) return e;
                 ++*launches;
