@@ -693,34 +693,32 @@ def _ids_ptr(t, shape):
         import torch
         _id_bytes.update({torch.int32: 4, torch.int64: 8})
     n = _id_bytes.get(t.dtype)
-    if n is None:
-        raise ValueError(f"expected int32 or int64 token numbers, got {t.dtype}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected contiguous token numbers on the device")
-    if t.shape != shape:
-        raise ValueError(f"expected token numbers of shape {tuple(shape)}, got {tuple(t.shape)}")
+    if n is None or not t.is_cuda or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"expected contiguous int32 or int64 token numbers of shape {tuple(shape)} on the device, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr(), n
 
 
-def _one_type(*tensors) -> int:
-    """cr_elem_t of tensors that must share it (None: left out)."""
-    kept = [t for t in tensors if t is not None]
-    if any(t.dtype != kept[0].dtype for t in kept):
+def _rows_like(t, x, shape):
+    """_row_ptr of a tensor (None -> NULL) that must have x's element type."""
+    if t is None:
+        return 0, 0
+    if t.dtype != x.dtype:
         raise ValueError("the tensors must have one element type")
-    return _elem(kept[0])
+    return _row_ptr(t, shape)
 
 
 def cr_embedding(plan: int, ids, table, y, scale: float = 1.0, stream=None) -> None:
     """y [..., width] = scale * table [vocab, width] at ids [...]; a number outside the table gives a zero row."""
     if table.dim() != 2 or y.dim() < 1:
         raise ValueError("expected table [vocab, width] and y [..., width]")
-    vocab, width = table.shape
-    e = _one_type(table, y)
+    shape = table.shape
+    vocab, width = shape
     ip, ib = _ids_ptr(ids, y.shape[:-1])
-    tp, ldt = _row_ptr(table, table.shape)
-    yp, ldy = _row_ptr(y, (*ids.shape, width))
-    _check(lib().cr_embedding(plan, ip, ib, tp, ldt, yp, ldy, ids.numel(), vocab, width, e, scale, _stream_ptr(stream)),
-           "cr_embedding")
+    tp, ldt = _row_ptr(table, shape)
+    yp, ldy = _rows_like(y, table, (*ids.shape, width))
+    _check(lib().cr_embedding(plan, ip, ib, tp, ldt, yp, ldy, ids.numel(), vocab, width, _elem(table), scale,
+                              _stream_ptr(stream)), "cr_embedding")
 
 
 def _table_gradient(ids, dtable):
@@ -765,20 +763,21 @@ def cr_embedding_backward(plan: int, ids, dy, dtable, scale: float = 1.0, paddin
 
 
 def _rows_and_cols(x):
-    if x.dim() < 1 or x.shape[-1] < 1:
+    shape = x.shape
+    if len(shape) < 1 or shape[-1] < 1:
         raise ValueError("expected rows of at least one element")
-    return x.numel() // x.shape[-1], x.shape[-1]
+    return x.numel() // shape[-1], shape[-1]
 
 
 def cr_rms_norm(plan: int, x, gamma, y, residual=None, h=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
     """h = x + residual, y = h / sqrt(mean h^2 + eps) * gamma over the last dimension of x; h (the residual stream) and
     rstd (one number a row, contiguous) are what the backward pass takes."""
     rows, cols = _rows_and_cols(x)
-    e, shape = _one_type(x, residual, h, y), x.shape
+    e, shape = _elem(x), x.shape
     xp, ldx = _row_ptr(x, shape)
-    rp, ldr = (0, 0) if residual is None else _row_ptr(residual, shape)
-    hp, ldh = (0, 0) if h is None else _row_ptr(h, shape)
-    yp, ldy = _row_ptr(y, shape)
+    rp, ldr = _rows_like(residual, x, shape)
+    hp, ldh = _rows_like(h, x, shape)
+    yp, ldy = _rows_like(y, x, shape)
     _check(lib().cr_rms_norm(plan, xp, ldx, rp, ldr, _vector_ptr(gamma, cols), hp, ldh, yp, ldy, _vector_ptr(rstd, rows), rows,
                              cols, e, eps, _stream_ptr(stream)), "cr_rms_norm")
 
@@ -787,10 +786,10 @@ def cr_rms_norm_codes(plan: int, x, gamma, q, scale, residual=None, h=None, rstd
     """cr_rms_norm with y as int8 codes q (shape of x) and a scale for each row, as cr_int8_product takes them; a row stride
     of q that is a multiple of 16 lets it take its tensor-core form."""
     rows, cols = _rows_and_cols(x)
-    e, shape = _one_type(x, residual, h), x.shape
+    e, shape = _elem(x), x.shape
     xp, ldx = _row_ptr(x, shape)
-    rp, ldr = (0, 0) if residual is None else _row_ptr(residual, shape)
-    hp, ldh = (0, 0) if h is None else _row_ptr(h, shape)
+    rp, ldr = _rows_like(residual, x, shape)
+    hp, ldh = _rows_like(h, x, shape)
     qp, ldq = _codes_ptr(q, shape)
     _check(lib().cr_rms_norm_codes(plan, xp, ldx, rp, ldr, _vector_ptr(gamma, cols), hp, ldh, qp, ldq, _vector_ptr(scale, rows),
                                    _vector_ptr(rstd, rows), rows, cols, e, eps, _stream_ptr(stream)), "cr_rms_norm_codes")
@@ -806,11 +805,11 @@ def cr_rms_norm_backward(plan: int, dy, h, gamma, rstd, dx=None, dgamma=None, dh
     """dx = gradient of x and residual from dy and, by the residual stream, dh (None: none); dgamma [partitions, cols] (rows
     may lie inside wider rows) for equal runs of rows."""
     rows, cols = _rows_and_cols(h)
-    e, shape = _one_type(h, dy, dh, dx), h.shape
-    gp, ldg = _row_ptr(dy, shape)
+    e, shape = _elem(h), h.shape
+    gp, ldg = _rows_like(dy, h, shape)
     hp, ldh = _row_ptr(h, shape)
-    sp, lds = (0, 0) if dh is None else _row_ptr(dh, shape)
-    dp, ldd = (0, 0) if dx is None else _row_ptr(dx, shape)
+    sp, lds = _rows_like(dh, h, shape)
+    dp, ldd = _rows_like(dx, h, shape)
     parts, pp, ldp = 1, 0, cols
     if dgamma is not None:
         if dgamma.dim() != 2 or dgamma.shape[1] != cols or _elem(dgamma) != CR_ELEM_F32:
@@ -823,9 +822,11 @@ def cr_rms_norm_backward(plan: int, dy, h, gamma, rstd, dx=None, dgamma=None, dh
 
 
 def _logits(x):
-    if x.dim() != 2 or x.shape[1] < 1:
+    """(rows, vocab, address, row stride, cr_elem_t)"""
+    shape = x.shape
+    if len(shape) != 2 or shape[1] < 1:
         raise ValueError("expected logits [rows, vocab]")
-    return (*x.shape, *_row_ptr(x, x.shape), _elem(x))
+    return (*shape, *_row_ptr(x, shape), _elem(x))
 
 
 def cr_token_log_probs(plan: int, logits, ids, logp=None, stats=None, entropy=None, top_logp=None, top_ids=None,
@@ -857,8 +858,7 @@ def cr_token_log_probs_backward(plan: int, logits, ids, stats, entropy, dlogp, d
     ip, ib = (0, 8) if ids is None else _ids_ptr(ids, (rows,))
     if (dlogp is not None and ids is None) or (dentropy is not None and entropy is None) or stats is None:
         raise ValueError("dlogp needs ids, dentropy needs entropy, both need stats")
-    _one_type(logits, dlogits)
-    dp, ldd = _row_ptr(dlogits, logits.shape)
+    dp, ldd = _rows_like(dlogits, logits, logits.shape)
     _check(lib().cr_token_log_probs_backward(plan, xp, ld, ip, ib, _vector_ptr(stats, 2 * rows), _vector_ptr(entropy, rows),
                                              _vector_ptr(dlogp, rows), _vector_ptr(dentropy, rows), dp, ldd, rows, vocab, e,
                                              temperature, _stream_ptr(stream)), "cr_token_log_probs_backward")
@@ -875,7 +875,6 @@ def cr_distill(plan: int, logits, teacher_ids, teacher, loss=None, dlogits=None,
     ip, ib = _ids_ptr(teacher_ids, (rows, top))
     dp, ldd = 0, vocab
     if dlogits is not None:
-        _one_type(logits, dlogits)
-        dp, ldd = _row_ptr(dlogits, logits.shape)
+        dp, ldd = _rows_like(dlogits, logits, logits.shape)
     _check(lib().cr_distill(plan, xp, ld, ip, ib, _vector_ptr(teacher, rows * top), top, _vector_ptr(weight, rows),
                             _vector_ptr(loss, rows), dp, ldd, rows, vocab, e, temperature, _stream_ptr(stream)), "cr_distill")
