@@ -679,7 +679,9 @@ cudaError_t launch_token_log_probs(const VocabArgs &a, const DeviceInfo &dev, cu
     return by_form(a, [&](auto t, auto v) {
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value;
-        const Share s = share_row(a.rows, a.vocab, Chunk<T, VEC>::kElements, kScoreWarps, dev.sm_count);
+        // Many rows: half the warps a row, so that while one row joins its pieces and ranks its alternatives others are read (4096 x
+        // 32000, 20 alternatives: 71 us, with eight warps 77); few rows: as many as fit (128000 x 1 in a cluster: 10 us, with four 13).
+        const Share s = share_row(a.rows, a.vocab, Chunk<T, VEC>::kElements, a.rows >= 4 * dev.sm_count ? kScoreWarps / 2 : kScoreWarps, dev.sm_count);
         const size_t smem = (size_t)s.slots * sizeof(Piece) + (a.top > 0 ? (size_t)((s.slots + s.cluster - 1) / s.cluster) * 128 : 0);
         return launch(cr_token_log_probs_kernel<T, VEC>, a, s, 32 * s.warps, smem, stream, launches);
     });
