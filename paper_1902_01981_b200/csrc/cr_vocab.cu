@@ -186,22 +186,24 @@ struct Chunk {
 struct Piece {
     float m, sum, turn, unused;
 };
-// b's numbers, taken relative to m, added to `a` (which is relative to m as well).
+// b's numbers added to a's, relative to a's largest logit.
+template <bool TURN>
 __device__ __forceinline__ void add_piece(Piece &a, const Piece &b, float c) {
     if (b.m == -INFINITY) return;
     const float d = max_nan((finite_base(b.m) - finite_base(a.m)) * c, kLeast), f = exp2_approx(d);
     a.sum = fmaf(b.sum, f, a.sum);
-    a.turn = fmaf(fmaf(b.sum, d, b.turn), f, a.turn);
+    if constexpr (TURN) a.turn = fmaf(fmaf(b.sum, d, b.turn), f, a.turn);
 }
 // Joins the slots; every lane gets the result.
+template <bool TURN>
 __device__ __forceinline__ Piece join(const Piece *slots, int count, float c) {
     const int lane = (int)threadIdx.x % 32;
     float m = -INFINITY;
     for (int j = lane; j < count; j += 32) m = max_nan(m, slots[j].m);
     Piece a = {warp_max_nan(m), 0.f, 0.f, 0.f};
-    for (int j = lane; j < count; j += 32) add_piece(a, slots[j], c);
+    for (int j = lane; j < count; j += 32) add_piece<TURN>(a, slots[j], c);
     a.sum = warp_sum(a.sum);
-    a.turn = warp_sum(a.turn);
+    if constexpr (TURN) a.turn = warp_sum(a.turn);
     return a;
 }
 
@@ -302,8 +304,8 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel
                 p = q;
             } else {
                 Piece all = {max_nan(p.m, q.m), 0.f, 0.f, 0.f};
-                add_piece(all, p, c);
-                add_piece(all, q, c);
+                add_piece<true>(all, p, c);
+                add_piece<true>(all, q, c);
                 p = all;
             }
             if (C::index(chunk, lane, 0, 0) < a.vocab) lane_top = max(lane_top, order_of(lm));
@@ -328,7 +330,7 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel
     meet(cluster);
     __shared__ float result[2];
     if (rank == 0 && warp == 0) {
-        const Piece all = join(pieces, slots, c);
+        const Piece all = join<true>(pieces, slots, c);
         const float base = finite_base(all.m), log_sum = log2f(all.sum);
         const bool nothing = all.m == -INFINITY;
         if (lane == 0) {
@@ -486,22 +488,27 @@ __global__ void __launch_bounds__(32 * kGradWarps) cr_token_log_probs_grad_kerne
 
 // ---- distillation --------------------------------------------------------------------------------------------------------
 
-constexpr int kSeenWords = 256;
+// Words of the teacher warp's marks: 64 bits a token, so that few of them share one with another.
+__host__ __device__ constexpr uint32_t seen_words(int top) {
+    uint32_t w = 64;
+    while (w < 2u * (uint32_t)top) w *= 2;
+    return w;
+}
 
 // One warp takes the teacher: its shares, and the loss once the row's sums are there.  The others take a chunk each, keep it in
-// registers over the exchange of the sums (the last one, where a warp has several) and write the gradient; then they mend the
-// elements of their own chunk that the teacher names.
+// registers over the exchange of the sums (the last one, where a warp has several) and write the gradient; then they put in the
+// elements of their own chunk that the teacher names, which its warp has worked out.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr_distill_kernel(const VocabArgs a, int cluster, int slots) {
+__global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr_distill_kernel(const VocabArgs a, int cluster, int slots, uint32_t words) {
     using C = Chunk<T, VEC>;
     extern __shared__ __align__(16) unsigned char dynamic[];
     Piece *pieces = reinterpret_cast<Piece *>(dynamic);               // [slots]
     float *share = reinterpret_cast<float *>(pieces + slots);         // [top]
     float *logit = share + a.top;
-    float *merged = logit + a.top;
-    int32_t *named = reinterpret_cast<int32_t *>(merged + a.top);
+    float *mended = logit + a.top;
+    int32_t *named = reinterpret_cast<int32_t *>(mended + a.top);
     __shared__ int wanted;
-    __shared__ uint32_t seen[kSeenWords], twice[kSeenWords];
+    uint32_t *seen = reinterpret_cast<uint32_t *>(named + a.top), *twice = seen + words;     // [words] each
     const int rank = (int)(blockIdx.x % (unsigned)cluster);
     const int64_t row = blockIdx.x / (unsigned)cluster;
     const int warps = (int)blockDim.x / 32 - 1, warp = (int)threadIdx.x / 32 - 1, lane = (int)threadIdx.x % 32;   // warp -1: the teacher's
@@ -515,8 +522,8 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
     float mass = 0.f, best = -INFINITY;
     arrive(cluster);
     if (warp < 0) {
-        for (int i = lane; i < kSeenWords; i += 32) seen[i] = twice[i] = 0;
-        __syncwarp();
+        for (int i = lane; i < words; i += 32) seen[i] = twice[i] = 0;
+#pragma unroll 4
         for (int j = lane; j < a.top; j += 32) {
             const int64_t id = id_at(a.ids, a.id_bytes, row * a.top + j);
             const bool there = id >= 0 && id < a.vocab;
@@ -524,11 +531,14 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
             logit[j] = there ? to_float(x[id]) : 0.f;
             share[j] = there ? a.teacher[row * a.top + j] * c : -INFINITY;
             best = max_nan(best, share[j]);
-            if (there && d) {
-                const uint32_t bit = 1u << (id % 32), word = (uint32_t)(id / 32) % kSeenWords;
-                if (atomicOr(&seen[word], bit) & bit) atomicOr(&twice[word], bit);
-            }
         }
+        __syncwarp();
+        for (int j = lane; d && j < a.top; j += 32) {
+            if (named[j] < 0) continue;
+            const uint32_t bit = 1u << (named[j] % 32), word = (uint32_t)(named[j] / 32) % words;
+            if (atomicOr(&seen[word], bit) & bit) atomicOr(&twice[word], bit);
+        }
+        __syncwarp();
         best = warp_max_nan(best);
         for (int j = lane; j < a.top; j += 32) mass += exp2_approx(share[j] - best);
         mass = warp_sum(mass);
@@ -548,8 +558,8 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
                     p = q;
                 } else {
                     Piece all = {max_nan(p.m, q.m), 0.f, 0.f, 0.f};
-                    add_piece(all, p, c);
-                    add_piece(all, q, c);
+                    add_piece<false>(all, p, c);
+                    add_piece<false>(all, q, c);
                     p = all;
                 }
             }
@@ -565,9 +575,10 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
         if (!started) wait(cluster);
     }
     meet(cluster);
-    const Piece all = join(pieces, slots, c);
+    const Piece all = join<false>(pieces, slots, c);
     const float base = finite_base(all.m), log_sum = log2f(all.sum);
     const bool left_out = !wanted, empty = all.m == -INFINITY;
+    const float scale = w * a.temperature, factor = empty ? 0.f : scale / all.sum;
     // the teacher's shares are needed by all warps
     if (warp < 0) {
         const float log_mass = log2f(mass);
@@ -582,15 +593,19 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
         // those that came again: few others share a bit with them.
         for (int j0 = 0; d && j0 < a.top; j0 += 32) {
             const int j = j0 + lane;
-            const bool again = j < a.top && named[j] >= 0 && (twice[(named[j] / 32) % kSeenWords] >> (named[j] % 32) & 1u);
+            const bool again = j < a.top && named[j] >= 0 && (twice[(uint32_t)(named[j] / 32) % words] >> (named[j] % 32) & 1u);
             for (uint32_t some = __ballot_sync(0xffffffffu, again); some; some &= some - 1) {
                 const int k = j0 + __ffs(some) - 1;
                 float p = 0.f;
                 for (int i = lane; i < a.top; i += 32) p += named[i] == named[k] ? share[i] : 0.f;
                 p = warp_sum(p);
-                if (lane == 0) merged[k] = p;
+                if (lane == 0) mended[k] = p;
             }
-            if (j < a.top && !again) merged[j] = share[j];
+            __syncwarp();
+            if (j < a.top) {      // the gradient there
+                const float p = again ? mended[j] : share[j];
+                mended[j] = fmaf(exp2_approx((logit[j] - base) * c), factor, -scale * p);
+            }
         }
         if (lane == 0 && rank == 0 && a.loss) a.loss[row] = left_out ? 0.f : a.temperature * a.temperature * kLn2 * loss;
     }
@@ -598,7 +613,6 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
     const bool none = left_out || w == 0.f;
     if (!none) __syncthreads();
     if (warp < 0 || warp >= own) return;
-    const float scale = w * a.temperature, factor = empty ? 0.f : scale / all.sum;
     // the warp's slots from the last one back: that one's last chunk is still in registers
     const int last = warp + (own - 1 - warp) / warps * warps;
     bool held = true;
@@ -616,12 +630,9 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
                 return mul2(f2(exp2_approx(low(w)), exp2_approx(high(w))), f2(factor));
             });
             __syncwarp();
-            const int64_t first = chunk * C::kElements;
-            for (int j = lane; j < a.top; j += 32) {
-                const int64_t v = named[j];
-                if (v < first || v >= first + C::kElements) continue;
-                d[v] = from_float<T>(fmaf(exp2_approx((logit[j] - base) * c), factor, -scale * merged[j]));
-            }
+            const uint32_t first = (uint32_t)chunk * C::kElements;
+            for (int j = lane; j < a.top; j += 32)       // a place that names nothing is 2^32 - 1, beyond every chunk's last element
+                if ((uint32_t)named[j] - first < (uint32_t)C::kElements) d[named[j]] = from_float<T>(mended[j]);
         }
     }
 }
@@ -649,8 +660,8 @@ Share share_row(int64_t rows, int64_t vocab, int64_t chunk_elements, int most_wa
     return s;
 }
 
-template <typename K>
-cudaError_t launch(K kernel, const VocabArgs &a, const Share &s, int threads, size_t smem, cudaStream_t stream, int64_t *launches) {
+template <typename K, typename... More>
+cudaError_t launch(K kernel, const VocabArgs &a, const Share &s, int threads, size_t smem, cudaStream_t stream, int64_t *launches, More... more) {
     if (a.rows > 0x7fffffffll / s.cluster) return cudaErrorInvalidValue;
     if (smem > 32 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -667,7 +678,7 @@ cudaError_t launch(K kernel, const VocabArgs &a, const Share &s, int threads, si
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = s.cluster > 1 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, s.cluster, s.slots);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, s.cluster, s.slots, more...);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -707,7 +718,8 @@ cudaError_t launch_distill(const VocabArgs &a, const DeviceInfo &dev, cudaStream
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value;
         const Share s = share_row(a.rows, a.vocab, Chunk<T, VEC>::kElements, kDistillWarps, dev.sm_count);
-        return launch(cr_distill_kernel<T, VEC>, a, s, 32 * (s.warps + 1), (size_t)s.slots * sizeof(Piece) + (size_t)a.top * 16, stream, launches);
+        const uint32_t words = seen_words(a.top);
+        return launch(cr_distill_kernel<T, VEC>, a, s, 32 * (s.warps + 1), (size_t)s.slots * sizeof(Piece) + (size_t)a.top * 16 + words * 8, stream, launches, words);
     });
 }
 
