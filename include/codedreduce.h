@@ -455,8 +455,9 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
  * that couples no samples, the loss over a vocabulary and the scores of given tokens.  The conventions are those of the
  * layers above: rows of consecutive elements at a row stride `ld` (>= their length), cr_elem_t elements, fp32 arithmetic
  * rounded once, gradients of parameters per partition in fp32, no atomics in a sum, and an order of every sum that follows
- * from the row's length (for a parameter's gradient the partition's sizes too), the element type and whether ALL tensors of
- * the call have 16-byte aligned bases and row strides and whole 16-byte vectors in a row.
+ * from the row's length (for a parameter's gradient the partition's sizes too, for a table's its tokens), the element type
+ * and whether ALL tensors of the call (gamma and dtable too) have 16-byte aligned bases and row strides and whole 16-byte
+ * vectors in a row.
  *   - Token numbers are 32- or 64-bit integers, `id_bytes` 4 or 8, aligned to their size and next to each other.  A number
  *     outside [0, vocab) names no token (padding): that is not an error.
  *   - Like the other device calls these only enqueue kernels and can be captured in a CUDA graph. */
@@ -472,7 +473,8 @@ cr_status_t cr_embedding(cr_plan_t *plan, const void *ids, int32_t id_bytes, con
  * row stride ld_row and partition stride ld_partition (>= vocab * ld_row), written whole: rows that no token names become
  * zero.  Tokens of number `padding` take no part (-1: all do; for a table whose padding row is looked up and not trained).
  * A row's tokens are added in the order of their positions, in pieces whose ends depend on the partition's own tokens.
- * workspace: device scratch of cr_embedding_backward_workspace_bytes (CR_ERR_OOM if smaller), 16-byte aligned. */
+ * workspace: device scratch of cr_embedding_backward_workspace_bytes (CR_ERR_OOM if smaller), 16-byte aligned.
+ * tokens <= 2^30 a partition, partitions <= 2^24. */
 size_t cr_embedding_backward_workspace_bytes(const cr_plan_t *plan, int64_t tokens, int64_t partitions, int64_t vocab, int64_t width);
 cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_bytes, const void *dy, int64_t ld_dy,
                                   float *dtable, int64_t ld_row, int64_t ld_partition, int64_t tokens, int64_t partitions,
@@ -483,7 +485,7 @@ cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_b
  *   h = x + residual (residual NULL: h = x),  rstd = 1 / sqrt(mean of h^2 + eps),  y = h rstd gamma
  * The norm is taken of the fp32 sum; h (NULL: not wanted) is that sum rounded once, the residual stream that goes on and
  * what the backward pass takes.  gamma fp32 [cols] or NULL (ones); rstd fp32 [rows] or NULL.  y or h may be x or residual
- * itself (same stride).  rows of zeros need eps > 0; a row whose sum of squares leaves the range of a float has no result.
+ * itself (same stride), not each other.  Rows of zeros need eps > 0; a row whose sum of squares leaves the range of a float has no result.
  * 0 <= rows <= 2^31 - 1, 1 <= cols <= 2^31 - 1, eps >= 0. */
 cr_status_t cr_rms_norm(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r, const float *gamma,
                         void *h, int64_t ld_h, void *y, int64_t ld_y, float *rstd, int64_t rows, int64_t cols, int32_t elem,

@@ -189,7 +189,8 @@ def _current_stream() -> int:
     """Raw handle of torch.cuda.current_stream(), without the object around it (3.4 -> 0.2 us a call)."""
     global _current_stream
     import torch
-    device, raw = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+    torch.cuda.current_device()          # brings CUDA up
+    device, raw = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _current_stream = lambda: raw(device())  # noqa: E731
     return _current_stream()
 
@@ -236,7 +237,8 @@ def cr_plan_create(n: int, L: int, s: int, P: int, d: int, code: int = CR_CODE_C
 
 def cr_plan_destroy(plan: int) -> None:
     _groups_of_plan.pop(plan, None)      # the handle may be reused by a later plan
-    _group_norm_workspace.cache_clear()
+    for known in (_group_norm_workspace, _embedding_workspace, _rms_norm_workspace):
+        known.cache_clear()
     _check(lib().cr_plan_destroy(plan), "cr_plan_destroy")
 
 
@@ -712,11 +714,13 @@ def cr_embedding(plan: int, ids, table, y, scale: float = 1.0, stream=None) -> N
     """y [..., width] = scale * table [vocab, width] at ids [...]; a number outside the table gives a zero row."""
     if table.dim() != 2 or y.dim() < 1:
         raise ValueError("expected table [vocab, width] and y [..., width]")
-    shape = table.shape
+    shape, out = table.shape, y.shape
     vocab, width = shape
-    ip, ib = _ids_ptr(ids, y.shape[:-1])
+    ip, ib = _ids_ptr(ids, out[:-1])
+    if out[-1] != width:
+        raise ValueError(f"expected rows of {width} elements, got {out[-1]}")
     tp, ldt = _row_ptr(table, shape)
-    yp, ldy = _rows_like(y, table, (*ids.shape, width))
+    yp, ldy = _rows_like(y, table, out)
     _check(lib().cr_embedding(plan, ip, ib, tp, ldt, yp, ldy, ids.numel(), vocab, width, _elem(table), scale,
                               _stream_ptr(stream)), "cr_embedding")
 
@@ -724,18 +728,24 @@ def cr_embedding(plan: int, ids, table, y, scale: float = 1.0, stream=None) -> N
 def _table_gradient(ids, dtable):
     """(partitions, tokens of each, vocab, width) of ids [tokens] with dtable [vocab, width], or ids [partitions, ...] with
     dtable [partitions, vocab, width]."""
-    if dtable.dim() == 2:
-        return 1, ids.numel(), *dtable.shape
-    if dtable.dim() != 3 or ids.dim() < 1 or ids.shape[0] != dtable.shape[0]:
+    shape = dtable.shape
+    if len(shape) == 2:
+        return 1, ids.numel(), *shape
+    if len(shape) != 3 or ids.dim() < 1 or ids.shape[0] != shape[0]:
         raise ValueError("expected ids [partitions, ...] and dtable [partitions, vocab, width]")
-    parts = ids.shape[0]
-    return parts, ids.numel() // parts if parts else 0, *dtable.shape[1:]
+    parts = shape[0]
+    return parts, ids.numel() // parts if parts else 0, shape[1], shape[2]
+
+
+@functools.lru_cache(maxsize=256)
+def _embedding_workspace(plan: int, parts: int, tokens: int, vocab: int, width: int) -> int:
+    """The workspace is a function of these, so a loop asks once."""
+    return lib().cr_embedding_backward_workspace_bytes(plan, tokens, parts, vocab, width)
 
 
 def cr_embedding_backward_workspace_bytes(plan: int, ids, dtable) -> int:
     """Scratch of cr_embedding_backward for these tensors."""
-    parts, tokens, vocab, width = _table_gradient(ids, dtable)
-    return lib().cr_embedding_backward_workspace_bytes(plan, tokens, parts, vocab, width)
+    return _embedding_workspace(plan, *_table_gradient(ids, dtable))
 
 
 def cr_embedding_backward(plan: int, ids, dy, dtable, scale: float = 1.0, padding: int = -1, workspace=None,
@@ -795,10 +805,14 @@ def cr_rms_norm_codes(plan: int, x, gamma, q, scale, residual=None, h=None, rstd
                                    _vector_ptr(rstd, rows), rows, cols, e, eps, _stream_ptr(stream)), "cr_rms_norm_codes")
 
 
+@functools.lru_cache(maxsize=256)
+def _rms_norm_workspace(plan: int, rows: int, cols: int, partitions: int) -> int:
+    return lib().cr_rms_norm_backward_workspace_bytes(plan, rows, cols, partitions)
+
+
 def cr_rms_norm_backward_workspace_bytes(plan: int, h, partitions: int = 1) -> int:
     """Scratch of cr_rms_norm_backward for rows like h's."""
-    rows, cols = _rows_and_cols(h)
-    return lib().cr_rms_norm_backward_workspace_bytes(plan, rows, cols, partitions)
+    return _rms_norm_workspace(plan, *_rows_and_cols(h), partitions)
 
 
 def cr_rms_norm_backward(plan: int, dy, h, gamma, rstd, dx=None, dgamma=None, dh=None, workspace=None, stream=None) -> None:

@@ -1370,7 +1370,7 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
 
 namespace {
 
-constexpr int64_t kMost31 = 0x7fffffffll;
+constexpr int64_t kMost31 = 0x7fffffffll, kMostSorted = 1ll << 30;     // positions that are counted a block ahead in 31 bits
 bool good_ids(const void *ids, int32_t id_bytes) {
     return (id_bytes == 4 || id_bytes == 8) && (reinterpret_cast<uintptr_t>(ids) & (uintptr_t)(id_bytes - 1)) == 0;
 }
@@ -1380,8 +1380,8 @@ bool good_factor(double f) { return f >= -3.4e38 && f <= 3.4e38; }
 bool good_temperature(double t) { return t >= 1e-18 && t <= 1e18; }
 bool good_extents(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kMost31 && cols >= 1 && cols <= kMost31; }
 
-bool good_embedding(int64_t tokens, int64_t partitions, int64_t vocab, int64_t width) {
-    return tokens >= 0 && tokens <= kMost31 && vocab >= 0 && vocab <= kMost31 && width >= 0 && width <= (1 << 24) && partitions >= 0 &&
+bool good_embedding(int64_t tokens, int64_t most, int64_t partitions, int64_t vocab, int64_t width) {
+    return tokens >= 0 && tokens <= most && vocab >= 0 && vocab <= kMost31 && width >= 0 && width <= (1 << 24) && partitions >= 0 &&
            partitions <= (1 << 24) && (tokens == 0 || partitions <= (1ll << 40) / tokens);
 }
 
@@ -1417,7 +1417,7 @@ cr_status_t cr_embedding(cr_plan_t *plan, const void *ids, int32_t id_bytes, con
                          int64_t ld_y, int64_t tokens, int64_t vocab, int64_t width, int32_t elem, double scale, void *stream) {
     cr_status_t st = check_device_plan(plan);
     if (st != CR_OK) return st;
-    if (!good_embedding(tokens, 1, vocab, width) || !known_elem(elem) || !good_ids(ids, id_bytes) || !good_factor(scale)) return CR_ERR_INVALID_ARG;
+    if (!good_embedding(tokens, kMost31, 1, vocab, width) || !known_elem(elem) || !good_ids(ids, id_bytes) || !good_factor(scale)) return CR_ERR_INVALID_ARG;
     if (tokens == 0 || width == 0) return CR_OK;
     if (!ids || (!table && vocab > 0) || !y || !good_rows(vocab, width, ld_table) || !good_rows(tokens, width, ld_y) || !on_element(table, elem) ||
         !on_element(y, elem))
@@ -1431,7 +1431,7 @@ cr_status_t cr_embedding(cr_plan_t *plan, const void *ids, int32_t id_bytes, con
 }
 
 size_t cr_embedding_backward_workspace_bytes(const cr_plan_t *plan, int64_t tokens, int64_t partitions, int64_t vocab, int64_t width) {
-    if (!plan || !good_embedding(tokens, partitions, vocab, width) || partitions == 0 || vocab == 0 || width == 0) return 0;
+    if (!plan || !good_embedding(tokens, kMostSorted, partitions, vocab, width) || partitions == 0 || vocab == 0 || width == 0) return 0;
     return cr::embedding_backward_workspace_bytes(tokens, partitions, vocab, width);
 }
 
@@ -1441,7 +1441,7 @@ cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_b
                                   size_t workspace_bytes, void *stream) {
     cr_status_t st = check_device_plan(plan);
     if (st != CR_OK) return st;
-    if (!good_embedding(tokens, partitions, vocab, width) || !known_elem(elem) || !good_ids(ids, id_bytes) || !good_factor(scale)) return CR_ERR_INVALID_ARG;
+    if (!good_embedding(tokens, kMostSorted, partitions, vocab, width) || !known_elem(elem) || !good_ids(ids, id_bytes) || !good_factor(scale)) return CR_ERR_INVALID_ARG;
     if (partitions == 0 || vocab == 0 || width == 0) return CR_OK;
     if (!dtable || !on_float(dtable) || !good_rows(vocab, width, ld_row) || !good_rows(partitions, vocab * ld_row, ld_partition)) return CR_ERR_INVALID_ARG;
     if (tokens > 0 && (!ids || !dy || !good_rows(tokens * partitions, width, ld_dy) || !on_element(dy, elem))) return CR_ERR_INVALID_ARG;
@@ -1459,7 +1459,7 @@ cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_b
 cr_status_t cr_rms_norm(cr_plan_t *plan, const void *x, int64_t ld_x, const void *residual, int64_t ld_r, const float *gamma,
                         void *h, int64_t ld_h, void *y, int64_t ld_y, float *rstd, int64_t rows, int64_t cols, int32_t elem,
                         double eps, void *stream) {
-    if (rows > 0 && (!y || !good_rows(rows, cols, ld_y))) return CR_ERR_INVALID_ARG;
+    if (rows > 0 && (!y || y == h || !good_rows(rows, cols, ld_y))) return CR_ERR_INVALID_ARG;
     cr::RmsNormArgs a;
     a.x = x; a.ld_x = ld_x; a.residual = residual; a.ld_residual = ld_r; a.gamma = gamma; a.h = h; a.ld_h = ld_h; a.y = y; a.ld_y = ld_y;
     a.rstd = rstd; a.rows = rows; a.cols = cols;

@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(32 * kGradWarps) cr_token_log_probs_grad_kerne
         data.store(d, a.vocab, chunk, [](F2) { return f2(0.f); });
         return;
     }
+    __syncwarp();        // every lane has read what the stores may overwrite
     const F2 shift = f2(-base), factor = f2(c), minus_log = f2(-log_sum), minus_turn = f2(-turn), minus_level = f2(-level);
     data.store(d, a.vocab, chunk, [&](F2 v) {
         F2 w = fma2(add2(v, shift), factor, minus_log);

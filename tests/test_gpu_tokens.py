@@ -674,6 +674,7 @@ def test_refusals(plan):
     wrong(lambda: B.cr_embedding_backward(plan, ids, x, dt.view(2, 4, 64), workspace=scratch(need)))
     refused(bad, lambda: B.cr_rms_norm(plan, x, None, x, eps=-1.0))
     refused(bad, lambda: B.cr_rms_norm(plan, x, None, x, eps=float("nan")))
+    refused(bad, lambda: B.cr_rms_norm(plan, x, None, x, h=x))          # two outputs in one place
     wrong(lambda: B.cr_rms_norm(plan, x, v, x))
     wrong(lambda: B.cr_rms_norm(plan, x, None, x.half()))
     wrong(lambda: B.cr_rms_norm(plan, x, None, x, residual=x[:3]))
