@@ -279,6 +279,28 @@ __device__ __forceinline__ RowScale row_scale(uint32_t largest_bits) {
 // rounds to even.  |x * mult| <= 127 (1 + 2^-23), so no code leaves the range.
 __device__ __forceinline__ uint32_t code(float x, float mult) { return __float_as_uint(__fadd_rn(__fmul_rn(x, mult), 12582912.f)); }
 
+// ---- kernels in a row --------------------------------------------------------------------------------
+//
+// The kernels of one call that follow each other are launched ahead of time (programmatic stream serialisation): a kernel
+// whose blocks have all begun lets the next one's be placed, which wait there until it has ended and its writes are
+// visible.  Every block of such a kernel waits, before anything else: otherwise it could end before its predecessor.
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+inline cudaError_t launch_next(void (*kernel)(P...), unsigned blocks, unsigned threads, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // ---- what the launch wrappers share ---------------------------------------------------------------
 
 template <typename F>

@@ -180,6 +180,7 @@ template <typename I, int EACH>
 __global__ void __launch_bounds__(1024, 1) cr_token_sort_kernel(const GradArgs a, const I *ids) {
     extern __shared__ uint2 entries[];           // [32 EACH warps]
     __shared__ uint32_t hist[32][kBins], base[kBins], scan[kBins / 32];
+    let_next_begin();
     const int64_t part = blockIdx.x;
     const int tid = (int)threadIdx.x, nt = (int)blockDim.x, warp = tid / 32, lane = tid % 32, warps = nt / 32;
     const uint32_t below = (1u << lane) - 1u;
@@ -265,6 +266,7 @@ __global__ void __launch_bounds__(1024, 1) cr_token_sort_cluster_kernel(const Gr
     static_assert(WARPS * 32 >= kBins, "a thread a bin");
     __shared__ uint32_t hist[WARPS][kBins];
     __shared__ uint32_t total[kBins], base[kBins], scan[kBins / 32];
+    let_next_begin();
     const int64_t part = blockIdx.x / (unsigned)cluster;
     const int rank = (int)(blockIdx.x % (unsigned)cluster), tid = (int)threadIdx.x, warp = tid / 32, lane = tid % 32;
     const uint32_t below = (1u << lane) - 1u;
@@ -454,6 +456,8 @@ __device__ __forceinline__ void zero_rows(const GradArgs &a, unsigned block) {
 // Sums and zeroes in one grid: the first `sum_blocks` blocks take tiles.  Bound by memory.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kSumThreads) cr_embedding_sums_kernel(const GradArgs a, unsigned sum_blocks, int across, int slabs) {
+    let_next_begin();
+    if (a.named) wait_for_previous();        // null: nothing was launched before
     if (blockIdx.x < sum_blocks) sum_tile<T, VEC>(a, blockIdx.x, across, slabs);
     else zero_rows(a, blockIdx.x - sum_blocks);
 }
@@ -510,6 +514,7 @@ __device__ __forceinline__ void join_pieces(const GradArgs &a, int64_t part, int
 template <int VEC>
 __global__ void __launch_bounds__(kJoinThreads) cr_embedding_join_kernel(const GradArgs a, int across, int slabs, unsigned walkers) {
     __shared__ float sm[kJoinThreads * VEC];
+    wait_for_previous();
     const unsigned item = blockIdx.x / (unsigned)slabs;
     const int64_t part = item / walkers;
     const int32_t *far = a.far + part * (a.tiles + 1);
@@ -631,8 +636,9 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         const int64_t groups = (g.tiles + kSumThreads / across - 1) / (kSumThreads / across);
         if (a.partitions * groups > 0x3fffffffll / slabs || a.partitions > 0x3fffffffll / g.words) return cudaErrorInvalidValue;
         const unsigned sums = (unsigned)(a.partitions * groups * slabs), blocks = sums + (unsigned)(a.partitions * g.words);
-        if (wide) cr_embedding_sums_kernel<T, VEC><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs);
-        else cr_embedding_sums_kernel<T, 1><<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs);
+        auto kernel = wide ? cr_embedding_sums_kernel<T, VEC> : cr_embedding_sums_kernel<T, 1>;
+        if (a.tokens > 0) return launch_next(kernel, blocks, kSumThreads, stream, g, sums, across, slabs);
+        kernel<<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs);
         return cudaGetLastError();
     });
     if (e != cudaSuccess) return e;
@@ -646,9 +652,7 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         const int64_t walkers = std::min<int64_t>(a.tokens / kWhole, std::max<int64_t>(1, 4 * dev.sm_count / a.partitions));
         if (a.partitions * walkers > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
         const unsigned blocks = (unsigned)(a.partitions * walkers * slabs);
-        if (four) cr_embedding_join_kernel<4><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs, (unsigned)walkers);
-        else cr_embedding_join_kernel<1><<<blocks, kJoinThreads, 0, stream>>>(g, across, slabs, (unsigned)walkers);
-        e = cudaGetLastError();
+        e = launch_next(four ? cr_embedding_join_kernel<4> : cr_embedding_join_kernel<1>, blocks, kJoinThreads, stream, g, across, slabs, (unsigned)walkers);
         if (e == cudaSuccess) ++*launches;
     }
     return e;

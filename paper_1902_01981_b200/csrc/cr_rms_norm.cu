@@ -267,6 +267,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) cr_rms_norm_g
     constexpr int kHeld = grad_held<VEC>(), kAhead = grad_stages<VEC>();
     extern __shared__ uint4 staged[];
     __shared__ float sums[2][32];
+    let_next_begin();
     const int64_t part = blockIdx.x / (unsigned)chunks, first = (int64_t)(blockIdx.x % (unsigned)chunks) * chunk;
     const int count = (int)min((int64_t)chunk, rows_each - first);
     const int64_t row0 = part * rows_each + first;
@@ -352,6 +353,7 @@ template <typename T, int VEC>
 __global__ void __launch_bounds__(32 * kDotWarps, 3) cr_rms_norm_dots_kernel(const RmsNormArgs a, float *dots) {
     using P = RowPiece<T, VEC>;
     __shared__ float sums[32];
+    let_next_begin();
     const int64_t row = blockIdx.x;
     const T *dy = static_cast<const T *>(a.dy) + row * a.ld_dy, *h = static_cast<const T *>(a.h) + row * a.ld_h;
     const int64_t nvec = a.cols / VEC, pieces = (nvec + P::kHeld * 32 - 1) / (P::kHeld * 32);
@@ -381,6 +383,8 @@ template <typename T, int VEC>
 __global__ void __launch_bounds__(kSlabThreads) cr_rms_norm_grad_kernel(const RmsNormArgs a, const float *dots, float *partial, int64_t ld_partial,
                                                                         int64_t rows_each, int chunk, int chunks, int slabs) {
     constexpr int kHeld = slab_held<VEC>();
+    let_next_begin();
+    if (dots) wait_for_previous();       // null: no dx is wanted, and nothing was launched before
     const unsigned item = blockIdx.x / (unsigned)slabs;
     const int lane = (int)threadIdx.x % 32;
     const int64_t v0 = ((int64_t)(blockIdx.x % (unsigned)slabs) * kSlabThreads + threadIdx.x / 32 * 32) * kHeld + lane, left = a.cols / VEC - v0;
@@ -449,6 +453,7 @@ __global__ void __launch_bounds__(kSlabThreads) cr_rms_norm_grad_kernel(const Rm
 // dgamma of a partition from its chunks' sums: eight warps take every eighth chunk and are summed in order.
 __global__ void __launch_bounds__(256) cr_rms_norm_params_kernel(const float *partial, int chunks, int64_t cols, float *dgamma, int64_t ld, unsigned slabs) {
     __shared__ float sm[8][32];
+    wait_for_previous();
     const int64_t part = blockIdx.x / slabs;
     const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32;
     const int64_t col = (int64_t)(blockIdx.x % slabs) * 32 + lane;
@@ -543,9 +548,14 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
             }
             const int64_t slab = kSlabThreads * slab_held<V>(), slabs = (a.cols / V + slab - 1) / slab;
             if (a.partitions * chunks > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-            cr_rms_norm_grad_kernel<T, V><<<(unsigned)(a.partitions * chunks * slabs), kSlabThreads, 0, stream>>>(
-                a, dots, sums, ld_sums, each, chunk, chunks, (int)slabs);
-            const cudaError_t e = cudaGetLastError();
+            const unsigned blocks = (unsigned)(a.partitions * chunks * slabs);
+            cudaError_t e;
+            if (a.y) {
+                e = launch_next(cr_rms_norm_grad_kernel<T, V>, blocks, kSlabThreads, stream, a, dots, sums, ld_sums, each, chunk, chunks, (int)slabs);
+            } else {
+                cr_rms_norm_grad_kernel<T, V><<<blocks, kSlabThreads, 0, stream>>>(a, nullptr, sums, ld_sums, each, chunk, chunks, (int)slabs);
+                e = cudaGetLastError();
+            }
             if (e == cudaSuccess) ++*launches;
             return e;
         };
@@ -554,8 +564,7 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
     if (e != cudaSuccess || !a.dgamma || chunks == 1) return e;
     const int64_t slabs = (a.cols + 31) / 32;
     if (a.partitions > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-    cr_rms_norm_params_kernel<<<(unsigned)(a.partitions * slabs), 256, 0, stream>>>(partial, chunks, a.cols, a.dgamma, a.ld_gamma, (unsigned)slabs);
-    e = cudaGetLastError();
+    e = launch_next(cr_rms_norm_params_kernel, (unsigned)(a.partitions * slabs), 256, stream, partial, chunks, a.cols, a.dgamma, a.ld_gamma, (unsigned)slabs);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
