@@ -116,8 +116,8 @@ __device__ __forceinline__ int tile_begin(const uint2 *pairs, int i0, int n, boo
     return cut ? i0 : i0 - back;
 }
 
-// The lanes that hold this lane's digit: a vote a bit (the match instruction takes the distinct values one after the other,
-// about a hundred cycles of an SM for a warp's random digits: 57 us for 16384 tokens).  Without meaning for a lane that has none.
+// The lanes that hold this lane's digit, by a vote a bit (the match instruction in its place: 51 instead of 46 us for 65536
+// tokens).  Without meaning for a lane that has none.
 __device__ __forceinline__ uint32_t same_digit(uint32_t d, bool has) {
     uint32_t peers = __ballot_sync(0xffffffffu, has);
 #pragma unroll

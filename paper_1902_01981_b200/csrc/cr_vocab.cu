@@ -18,7 +18,6 @@
 namespace cr {
 namespace {
 
-
 constexpr float kLn2 = 0.6931471805599453f;
 // Exponents below this are zero in fp32; the clamp keeps 0 * -infinity out of the entropy.
 constexpr float kLeast = -160.f;
@@ -580,7 +579,7 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
     const float base = finite_base(all.m), log_sum = log2f(all.sum);
     const bool left_out = !wanted, empty = all.m == -INFINITY;
     const float scale = w * a.temperature, factor = empty ? 0.f : scale / all.sum;
-    // the teacher's shares are needed by all warps
+    // the shares, the loss, and for all warps the gradient at the elements that the teacher names
     if (warp < 0) {
         const float log_mass = log2f(mass);
         float loss = 0.f;

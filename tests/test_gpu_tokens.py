@@ -429,6 +429,27 @@ def test_log_probs_rows_do_not_see_each_other(plan, dtype):
             assert all(torch.equal(a, b[rows]) for a, b in zip(part, out))
 
 
+@pytest.mark.parametrize("vocab", [9001, 9008, 70000])
+def test_a_few_rows_have_the_bits_of_many(plan, vocab):
+    """However many warps and CTAs share a row: scores, alternatives, loss and gradients."""
+    x, rng = logits_of((700, vocab, 0, 0), "bf16", 8)
+    x = x.contiguous()
+    ids, tid, t = dev_ids(rng.integers(0, vocab, 700), "i64"), dev_ids(rng.integers(0, vocab, (700, 20)), "i64"), dev32(rng.standard_normal((700, 20)))
+
+    def run(rows):
+        n = rows.stop - rows.start
+        out = [torch.empty(n, device="cuda"), torch.empty((n, 2), device="cuda"), torch.empty(n, device="cuda"),
+               torch.empty((n, 20), device="cuda"), torch.empty((n, 20), dtype=torch.int64, device="cuda"), torch.empty(n, device="cuda"),
+               torch.empty_like(x[rows])]
+        B.cr_token_log_probs(plan, x[rows], ids[rows], *out[:5])
+        B.cr_distill(plan, x[rows], tid[rows], t[rows], *out[5:])
+        return out
+
+    whole = run(slice(0, 700))
+    for rows in (slice(0, 1), slice(16, 55), slice(300, 600)):
+        assert all(torch.equal(a.nan_to_num(), b[rows].nan_to_num()) for a, b in zip(run(rows), whole))
+
+
 def test_log_probs_of_odd_rows(plan):
     inf, nan = float("inf"), float("nan")
     for dtype in TYPES:
