@@ -429,12 +429,13 @@ def test_log_probs_rows_do_not_see_each_other(plan, dtype):
             assert all(torch.equal(a, b[rows]) for a, b in zip(part, out))
 
 
-@pytest.mark.parametrize("vocab", [9001, 9008, 70000])
-def test_a_few_rows_have_the_bits_of_many(plan, vocab):
-    """However many warps and CTAs share a row: scores, alternatives, loss and gradients."""
-    x, rng = logits_of((700, vocab, 0, 0), "bf16", 8)
+@pytest.mark.parametrize("vocab,dtype,count", [(9001, "bf16", 700), (9008, "bf16", 700), (70000, "bf16", 700), (20000, "bf16", 1000), (32000, "f16", 900),
+                                               (40008, "bf16", 450), (131080, "bf16", 120), (9004, "f32", 900), (20000, "f32", 450)])
+def test_a_few_rows_have_the_bits_of_many(plan, vocab, dtype, count):
+    """However many warps and CTAs share a row, or walk over rows: scores, alternatives, loss and gradients."""
+    x, rng = logits_of((count, vocab, 0, 0), dtype, 8)
     x = x.contiguous()
-    ids, tid, t = dev_ids(rng.integers(0, vocab, 700), "i64"), dev_ids(rng.integers(0, vocab, (700, 20)), "i64"), dev32(rng.standard_normal((700, 20)))
+    ids, tid, t = dev_ids(rng.integers(0, vocab, count), "i64"), dev_ids(rng.integers(0, vocab, (count, 20)), "i64"), dev32(rng.standard_normal((count, 20)))
 
     def run(rows):
         n = rows.stop - rows.start
@@ -445,8 +446,8 @@ def test_a_few_rows_have_the_bits_of_many(plan, vocab):
         B.cr_distill(plan, x[rows], tid[rows], t[rows], *out[5:])
         return out
 
-    whole = run(slice(0, 700))
-    for rows in (slice(0, 1), slice(16, 55), slice(300, 600)):
+    whole = run(slice(0, count))
+    for rows in (slice(0, 1), slice(16, 55), slice(count // 3, count // 3 + 48), slice(count - 1, count)):
         assert all(torch.equal(a.nan_to_num(), b[rows].nan_to_num()) for a, b in zip(run(rows), whole))
 
 
@@ -495,7 +496,8 @@ def test_log_probs_of_odd_rows(plan):
 # ------------------------------------------------------------------------------------------------ distillation
 
 DISTILS = [(1, 1, 0, 0, 1), (3, 8, 0, 0, 3), (39, 5004, 4, 0, 16), (39, 5004, 4, 1, 16), (4, 257, 0, 0, 64), (2, 32000, 0, 0, 64), (3, 50257, 0, 0, 20),
-           (1, 128000, 0, 0, 8), (2, 262145, 0, 0, 5), (300, 200, 0, 0, 200), (700, 1024, 8, 0, 1024), (1, 300000, 0, 0, 300), (5, 2048, 0, 0, 33)]
+           (1, 128000, 0, 0, 8), (2, 262145, 0, 0, 5), (300, 200, 0, 0, 200), (700, 1024, 8, 0, 1024), (1, 300000, 0, 0, 300), (5, 2048, 0, 0, 33),
+           (900, 17000, 0, 0, 128), (460, 33000, 8, 0, 40), (120, 131080, 0, 0, 12)]      # CTAs, pairs and eights of them that walk over rows
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
