@@ -661,7 +661,8 @@ Share share_row(int64_t rows, int64_t vocab, int64_t chunk_elements, int most_wa
     // as many CTAs as leave every SM at most one, while there are slots for them
     s.cluster = 1;
     while (s.cluster < kMaxCluster && s.cluster * 2 <= s.slots && rows * s.cluster * 2 <= sm_count) s.cluster *= 2;
-    s.warps = std::min(most_warps, (s.slots + s.cluster - 1) / s.cluster);
+    const int own = (s.slots + s.cluster - 1) / s.cluster, turns = (own + most_warps - 1) / most_warps;
+    s.warps = (own + turns - 1) / turns;       // the fewest that need no more turns
     return s;
 }
 
