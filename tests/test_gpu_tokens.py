@@ -189,6 +189,21 @@ def test_table_gradient(plan, shape, dtype):
     assert torch.equal(d, again)
 
 
+@pytest.mark.parametrize("tokens", [5, 64, 1500, 5000])
+def test_table_gradient_of_padding(plan, tokens):
+    """Partitions without a named token beside one that has a single one; an infinite gradient stays in its row."""
+    ids = torch.full((3, tokens), -1, dtype=torch.int64, device="cuda")
+    ids[1, tokens // 2] = 6
+    ids[2, :] = 3                                     # the padding's own number
+    dy = torch.randn(3, tokens, 40, device="cuda")
+    dy[1, tokens // 2, 7] = float("inf")
+    dy[0, 0, 0] = float("nan")                        # of a token that names nothing
+    d = grads(plan, ids, dy, 50, scale=2.0, padding=3)
+    want = torch.zeros((3, 50, 40), device="cuda")
+    want[1, 6] = 2 * dy[1, tokens // 2]
+    assert torch.equal(d, want)
+
+
 def test_table_gradient_of_a_partition_has_the_bits_of_the_batch(plan):
     rng = np.random.default_rng(5)
     ids = dev_ids(np.minimum((500 ** rng.random((6, 3000))).astype(np.int64) - 1, 499), "i64")
