@@ -352,7 +352,8 @@ def test_norm_backward_parts(plan):
 
 # rows, vocab, pad, shift
 VOCABS = [(1, 1, 0, 0), (2, 3, 0, 0), (3, 8, 0, 0), (5, 33, 0, 0), (4, 257, 0, 0), (39, 5004, 4, 0), (39, 5004, 4, 1), (7, 1000, 0, 0), (2, 32000, 0, 0),
-          (3, 50257, 0, 0), (300, 200, 0, 0), (1, 128000, 0, 0), (2, 262145, 0, 0), (1, 300000, 0, 0), (700, 1024, 8, 0), (3, 2048, 0, 0), (3, 2056, 0, 0)]
+          (3, 50257, 0, 0), (300, 200, 0, 0), (1, 128000, 0, 0), (2, 262145, 0, 0), (1, 300000, 0, 0), (700, 1024, 8, 0), (3, 2048, 0, 0), (3, 2056, 0, 0),
+          (2, 1100001, 0, 0), (1, 2200000, 0, 0)]        # more chunks than slots
 
 
 def logits_of(shape, dtype, seed, masked=0.2):
@@ -447,7 +448,7 @@ def test_log_probs_rows_do_not_see_each_other(plan, dtype):
 @pytest.mark.parametrize("vocab,dtype,count", [(9001, "bf16", 700), (9008, "bf16", 700), (70000, "bf16", 700), (20000, "bf16", 1000), (32000, "f16", 900),
                                                (40008, "bf16", 450), (131080, "bf16", 120), (9004, "f32", 900), (20000, "f32", 450)])
 def test_a_few_rows_have_the_bits_of_many(plan, vocab, dtype, count):
-    """However many warps and CTAs share a row, or walk over rows: scores, alternatives, loss and gradients."""
+    """However many warps and CTAs share a row: scores, alternatives, loss and gradients."""
     x, rng = logits_of((count, vocab, 0, 0), dtype, 8)
     x = x.contiguous()
     ids, tid, t = dev_ids(rng.integers(0, vocab, count), "i64"), dev_ids(rng.integers(0, vocab, (count, 20)), "i64"), dev32(rng.standard_normal((count, 20)))
@@ -512,7 +513,7 @@ def test_log_probs_of_odd_rows(plan):
 
 DISTILS = [(1, 1, 0, 0, 1), (3, 8, 0, 0, 3), (39, 5004, 4, 0, 16), (39, 5004, 4, 1, 16), (4, 257, 0, 0, 64), (2, 32000, 0, 0, 64), (3, 50257, 0, 0, 20),
            (1, 128000, 0, 0, 8), (2, 262145, 0, 0, 5), (300, 200, 0, 0, 200), (700, 1024, 8, 0, 1024), (1, 300000, 0, 0, 300), (5, 2048, 0, 0, 33),
-           (900, 17000, 0, 0, 128), (460, 33000, 8, 0, 40), (120, 131080, 0, 0, 12)]      # CTAs, pairs and eights of them that walk over rows
+           (900, 17000, 0, 0, 128), (460, 33000, 8, 0, 40), (120, 131080, 0, 0, 12), (2, 1100001, 0, 0, 9), (1, 2200000, 0, 0, 40)]      # many rows; more chunks than slots
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
