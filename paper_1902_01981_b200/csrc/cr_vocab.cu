@@ -449,21 +449,31 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel
 
 constexpr int kGradWarps = 8;
 
-// A warp a chunk of a row; all loads come before the first store, which may go to the same memory.  Bound by memory: 2048 x 32000
-// bf16 42 us (6.2 TB/s), 1024 x 50257 fp32 in odd rows 63 us (6.5 TB/s).
-template <typename T, int VEC>
-__global__ void __launch_bounds__(32 * kGradWarps) cr_token_log_probs_grad_kernel(const VocabArgs a, unsigned chunks, int64_t items) {
+// A warp a chunk of a row; all loads come before the first store, which may go to the same memory.  Nothing is summed, so rows off
+// the 16-byte boundaries (PEEL) may be taken from their first boundary on, which x and dx have in one place: the elements
+// in front of it and behind the last vector are the first chunk's.  Bound by memory: 2048 x 32000 bf16 42 us (6.2 TB/s), 2048 x
+// 32001 48 us (67 by elements), 1024 x 50257 fp32 63 us (6.5 TB/s).
+template <typename T, int VEC, bool PEEL>
+__global__ void __launch_bounds__(32 * kGradWarps, 4) cr_token_log_probs_grad_kernel(const VocabArgs a, unsigned chunks, int64_t items) {
     using C = Chunk<T, VEC>;
     const int64_t item = (int64_t)blockIdx.x * kGradWarps + threadIdx.x / 32;
     if (item >= items) return;
     const int64_t row = item < 0x7fffffffll ? (unsigned)item / chunks : item / chunks, chunk = item - row * chunks;
+    const int lane = (int)threadIdx.x % 32;
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     T *d = static_cast<T *>(a.dlogits) + row * a.ld_d;
+    int head = 0;
+    if constexpr (PEEL) head = (int)min(a.vocab, (int64_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15u)) % 16 / sizeof(T)));
+    const int64_t body = PEEL ? (a.vocab - head) / VEC * VEC : a.vocab;
     C data;
-    data.load(x, a.vocab, chunk);
+    data.load(x + head, body, chunk);
+    // lanes 0 .. 7 the head's, 8 .. 15 the tail's (fewer than eight each)
+    const int64_t edge = lane < 8 ? (lane < head ? lane : a.vocab) : head + body + lane - 8;
+    const bool at_edge = PEEL && chunk == 0 && lane < 16 && edge < a.vocab;
+    const float edge_logit = at_edge ? to_float(x[edge]) : 0.f;
     int64_t id = a.dlogp ? id_at(a.ids, a.id_bytes, row) : -1;
     if (id >= a.vocab) id = -1;
-    const bool here = id >= 0 && id / C::kElements == chunk;
+    const bool here = id >= head && id < head + body && (id - head) / C::kElements == chunk;
     const float picked = here ? to_float(x[id]) : 0.f;
     const float2 stats = reinterpret_cast<const float2 *>(a.stats)[row];
     const float ga = id >= 0 ? a.dlogp[row] * a.inverse : 0.f, gb = a.dentropy ? a.dentropy[row] * a.inverse : 0.f;
@@ -471,21 +481,25 @@ __global__ void __launch_bounds__(32 * kGradWarps) cr_token_log_probs_grad_kerne
     // log2 p = (x - base) c - log_sum;  dx = -p (ga + gb (log p + H)), and ga more at the token
     const float c = a.inverse * kLog2e, base = finite_base(stats.x), log_sum = stats.y * kLog2e;
     const float level = gb != 0.f ? fmaf(gb, a.entropy[row], ga) : ga, turn = gb * kLn2;
+    auto one = [&](float v, bool token) {
+        const float w = max_nan(fmaf(v - base, c, -log_sum), kLeast);
+        return (token ? ga : 0.f) + exp2_approx(w) * fmaf(-turn, w, -level);
+    };
+    __syncwarp();        // every lane has read what the stores may overwrite
+    if (at_edge) d[edge] = from_float<T>(none ? 0.f : one(edge_logit, edge == id));
     if (none) {
-        data.store(d, a.vocab, chunk, [](F2) { return f2(0.f); });
+        data.store(d + head, body, chunk, [](F2) { return f2(0.f); });
         return;
     }
-    __syncwarp();        // every lane has read what the stores may overwrite
     const F2 shift = f2(-base), factor = f2(c), minus_log = f2(-log_sum), minus_turn = f2(-turn), minus_level = f2(-level);
-    data.store(d, a.vocab, chunk, [&](F2 v) {
+    data.store(d + head, body, chunk, [&](F2 v) {
         F2 w = fma2(add2(v, shift), factor, minus_log);
         w = f2(max_nan(low(w), kLeast), max_nan(high(w), kLeast));
         return mul2(f2(exp2_approx(low(w)), exp2_approx(high(w))), fma2(minus_turn, w, minus_level));
     });
     if (!here) return;
     __syncwarp();
-    const float w = max_nan(fmaf(picked - base, c, -log_sum), kLeast);
-    if (threadIdx.x % 32 == 0) d[id] = from_float<T>(ga + exp2_approx(w) * fmaf(-turn, w, -level));
+    if (lane == 0) d[id] = from_float<T>(one(picked, true));
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------------------
@@ -706,15 +720,25 @@ cudaError_t launch_token_log_probs(const VocabArgs &a, const DeviceInfo &dev, cu
 
 cudaError_t launch_token_log_probs_backward(const VocabArgs &a, cudaStream_t stream, int64_t *launches) {
     if (a.rows == 0) return cudaSuccess;
-    return by_form(a, [&](auto t, auto v) {
+    auto go = [&](auto t, auto v, auto peel) {
         using T = decltype(t);
         constexpr int VEC = decltype(v)::value;
         const int64_t chunks = (a.vocab + Chunk<T, VEC>::kElements - 1) / Chunk<T, VEC>::kElements, items = a.rows * chunks;
         if ((items + kGradWarps - 1) / kGradWarps > 0x7fffffffll) return cudaErrorInvalidValue;
-        cr_token_log_probs_grad_kernel<T, VEC><<<(unsigned)((items + kGradWarps - 1) / kGradWarps), 32 * kGradWarps, 0, stream>>>(a, (unsigned)chunks, items);
+        cr_token_log_probs_grad_kernel<T, VEC, decltype(peel)::value != 0><<<(unsigned)((items + kGradWarps - 1) / kGradWarps), 32 * kGradWarps, 0, stream>>>(
+            a, (unsigned)chunks, items);
         const cudaError_t e = cudaGetLastError();
         if (e == cudaSuccess) ++*launches;
         return e;
+    };
+    return by_form(a, [&](auto t, auto v) {
+        using T = decltype(t);
+        constexpr int VEC = decltype(v)::value;
+        if constexpr (VEC == 1 && sizeof(T) == 2) {      // for fp32 the elements alone are as fast (65 against 67 us)
+            const uintptr_t apart = reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.dlogits);
+            if (apart % 16 == 0 && (a.ld - a.ld_d) * 2 % 16 == 0) return go(t, Int<8>{}, Int<1>{});
+        }
+        return go(t, v, Int<0>{});
     });
 }
 

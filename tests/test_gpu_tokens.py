@@ -423,6 +423,9 @@ def test_log_probs_forward_and_backward(plan, shape, dtype):
         # p is off by what log p is off (and ex2); each term by a few roundings; 1 - p where p is near one
         check(d, want, dtype, (size[:, None] * (p * (4 * arith[:, None] + 12 * STEP) + 2 * STEP * (np.arange(vocab) == ids[:, None])) / temperature))
         assert outside_untouched(d)
+        other = place(np.zeros((rows, vocab)), dtype, pad + 1, shift + 3)       # rows that lie elsewhere relative to 16 bytes
+        B.cr_token_log_probs_backward(plan, x, dids, stats, entropy, da, db, other, temperature=temperature)
+        assert torch.equal(other, d) and outside_untouched(other)
         if da is a and db is b:
             y = x.clone() if x.is_contiguous() else x
             if y is not x:
