@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
             const bool there = id >= 0 && id < a.vocab;
             named[j] = there ? (int32_t)id : -1;
             logit[j] = there ? to_float(x[id]) : 0.f;
-            share[j] = there ? a.teacher[row * a.top + j] * c : -INFINITY;
+            share[j] = there ? a.teacher[row * a.top + j] : -INFINITY;      // as it is: its difference to the largest comes first
             best = max_nan(best, share[j]);
         }
         __syncwarp();
@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
         }
         __syncwarp();
         best = warp_max_nan(best);
-        for (int j = lane; j < a.top; j += 32) mass += exp2_approx(share[j] - best);
+        for (int j = lane; j < a.top; j += 32) mass += exp2_approx((share[j] - best) * c);
         mass = warp_sum(mass);
         if (lane == 0) wanted = best != -INFINITY;
         wait(cluster);
@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
         const float log_mass = log2f(mass);
         float loss = 0.f;
         for (int j = lane; j < a.top; j += 32) {
-            const float u = share[j] - best, p = left_out ? 0.f : exp2_approx(u) / mass;
+            const float u = (share[j] - best) * c, p = left_out ? 0.f : exp2_approx(u) / mass;
             share[j] = p;
             if (p != 0.f) loss += p * ((u - log_mass) - (empty ? -INFINITY : (logit[j] - base) * c - log_sum));
         }

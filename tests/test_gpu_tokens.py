@@ -586,6 +586,39 @@ def test_distillation_of_odd_rows(plan):
     assert f64(loss)[5] == inf and np.allclose(f64(d)[5, :8], -1 / 8) and not d[5, 8:].any()
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("temperature", [0.7, 1.0, 2.0])
+def test_distillation_from_teachers_far_from_zero(plan, temperature, dtype):
+    """A constant per row drops out of the teacher's logits: offsets, rows of the type's lowest and of nearly its largest value."""
+    rng = np.random.default_rng(21)
+    lowest, top, vocab = np.finfo(np.float32).min, 16, 1000
+    t = (3 * rng.standard_normal((9, top))).astype(np.float32)
+    for r, offset in enumerate((0, 30, 1e3, 1e4, 1e5, -1e5)):
+        t[r] += np.float32(offset)
+    t[6] = lowest
+    t[7, 4:], t[7, :4] = lowest, 3e38
+    t[8, 1:], t[8, 0] = lowest, 0.5                   # masked by the lowest value: all that counts is the first
+    rows = len(t)
+    x, _ = logits_of((rows, vocab, 0, 0), dtype, 5, 0.0)
+    x64, weight = f64(x), (1 + 0.1 * rng.standard_normal(rows)).astype(np.float32)
+    ids = np.stack([rng.permutation(vocab)[:top] for _ in range(rows)])
+    want, want_d = O.distill(x64, ids, t, weight, temperature)
+    loss, d = torch.full((rows,), float("nan"), device="cuda"), place(np.zeros((rows, vocab)), dtype)
+    B.cr_distill(plan, x, dev_ids(ids, "i64"), dev32(t), loss, d, dev32(weight), temperature)
+    # differences to the largest are exact up to half a step of their own, so that the bounds of test_distillation hold with the
+    # span of those that have a share, wherever the row lies
+    near = t.astype(np.float64) - t.max(1, keepdims=True)
+    span = np.abs(np.where(near < -200, 0, near)).max(1) / temperature
+    steps = (6 * span + top + 40) * STEP
+    arith = log_arith(x64, temperature) + steps
+    lp, _, _ = O.log_p(x64, temperature)
+    sizes = np.abs(lp).max(1) + span + np.log(top)
+    check(loss, want, "f32", temperature ** 2 * (2 * arith + (top / 256 + 20) * STEP * sizes + 4 * steps * sizes))
+    p = np.exp(lp)
+    share = np.abs(want_d / (weight * temperature)[:, None] - p)
+    check(d, want_d, dtype, np.abs(weight)[:, None] * temperature * (p * (4 * arith[:, None] + 12 * STEP) + share * (4 * steps[:, None] + (top + 8) * STEP)))
+
+
 def test_distillation_by_differences(plan):
     """The gradient is that of the loss."""
     rng = np.random.default_rng(0)
