@@ -39,6 +39,9 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 __device__ __forceinline__ float finite_base(float m) { return isinf(m) ? 0.f : m; }
+// log p of a logit from the logarithm to base two of its row's sum.  Without the detour over base two for the logit itself: that of
+// one at the type's lowest value, times log2(e), would leave the range.
+__device__ __forceinline__ float natural_log_p(float x, float base, float inverse, float log2_sum) { return (x - base) * inverse - kLn2 * log2_sum; }
 
 // ---- a cluster of CTAs on a row --------------------------------------------------------------------------------------------
 
@@ -336,7 +339,7 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel
         if (lane == 0) {
             if (a.stats) reinterpret_cast<float2 *>(a.stats)[row] = make_float2(all.m, kLn2 * log_sum);
             if (a.entropy) a.entropy[row] = nothing ? 0.f : kLn2 * (log_sum - all.turn / all.sum);
-            if (a.logp) a.logp[row] = id < 0 ? 0.f : nothing ? -INFINITY : kLn2 * ((picked - base) * c - log_sum);
+            if (a.logp) a.logp[row] = id < 0 ? 0.f : nothing ? -INFINITY : natural_log_p(picked, base, a.inverse, log_sum);
             result[0] = base;
             result[1] = log_sum;
         }
@@ -421,7 +424,7 @@ __global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel
         if (a.id_bytes == 4) static_cast<int32_t *>(a.top_ids)[row * a.top + place] = (int32_t)v;
         else static_cast<long long *>(a.top_ids)[row * a.top + place] = (long long)v;
         const float f = key_value(key);
-        a.top_logp[row * a.top + place] = isinf(result[1]) && result[1] < 0.f ? -INFINITY : kLn2 * ((f - result[0]) * c - result[1]);
+        a.top_logp[row * a.top + place] = isinf(result[1]) && result[1] < 0.f ? -INFINITY : natural_log_p(f, result[0], a.inverse, result[1]);
     };
     const int n = found;
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
@@ -599,12 +602,13 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
     const float scale = w * a.temperature, factor = empty ? 0.f : scale / all.sum;
     // the shares, the loss, and for all warps the gradient at the elements that the teacher names
     if (warp < 0) {
-        const float log_mass = log2f(mass);
+        // T sum_j t_j (log t_j - log p_j): logits are not divided by T here, so that large differences under T < 1 stay in range
+        const float between = a.temperature * kLn2 * (log_sum - log2f(mass));
         float loss = 0.f;
         for (int j = lane; j < a.top; j += 32) {
-            const float u = (share[j] - best) * c, p = left_out ? 0.f : exp2_approx(u) / mass;
+            const float u = share[j] - best, p = left_out ? 0.f : exp2_approx(u * c) / mass;
             share[j] = p;
-            if (p != 0.f) loss += p * ((u - log_mass) - (empty ? -INFINITY : (logit[j] - base) * c - log_sum));
+            if (p != 0.f) loss += p * (empty ? INFINITY : u - (logit[j] - base) + between);
         }
         loss = warp_sum(loss);
         __syncwarp();
@@ -626,7 +630,7 @@ __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr
                 mended[j] = fmaf(exp2_approx((logit[j] - base) * c), factor, -scale * p);
             }
         }
-        if (lane == 0 && rank == 0 && a.loss) a.loss[row] = left_out ? 0.f : a.temperature * a.temperature * kLn2 * loss;
+        if (lane == 0 && rank == 0 && a.loss) a.loss[row] = left_out ? 0.f : a.temperature * loss;
     }
     if (!d) return;
     const bool none = left_out || w == 0.f;

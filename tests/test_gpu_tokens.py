@@ -512,6 +512,49 @@ def test_log_probs_of_odd_rows(plan):
             assert not d.any()                         # nothing from above: zero whatever the logits hold
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_numbers_of_tokens_at_the_lowest_value(plan, dtype):
+    """Tokens masked by the type's lowest value, not by -infinity, have a log probability that fp32 can hold."""
+    for vocab in (40, 1000, 50257):
+        rng = np.random.default_rng(vocab)
+        lowest = torch.finfo(TYPES[dtype]).min
+        values = rng.standard_normal((6, vocab))
+        values[:, 5:] = lowest                        # fewer tokens than alternatives are left
+        x = place(values, dtype)
+        x[2] = lowest
+        x64, ids = f64(x), np.array([0, 7, 7, vocab - 1, 4, 5])
+        for temperature in (1.0, 2.0):
+            logp, ent = torch.empty(6, device="cuda"), torch.empty(6, device="cuda")
+            tl, ti = torch.empty((6, 8), device="cuda"), torch.empty((6, 8), dtype=torch.int64, device="cuda")
+            B.cr_token_log_probs(plan, x, dev_ids(ids, "i64"), logp, None, ent, tl, ti, temperature=temperature)
+            want, _, _, want_e, order, want_top = O.token_log_probs(x64, ids, temperature, 8)
+            assert np.isfinite(want).all() and np.isfinite(want_top).all() and np.array_equal(ti.cpu().numpy(), order)
+            # the difference, its product with the rounded reciprocal and the last subtraction on terms of their own size, the
+            # logarithm of a sum as in log_arith
+            near = 4 * STEP * np.log(vocab) + (min(vocab, 1100) + 40) * STEP
+            check(logp, want, "f32", 6 * STEP * np.abs(want) + near)
+            check(tl, want_top, "f32", 6 * STEP * np.abs(want_top) + near)
+            check(ent, want_e, "f32", (6 * 8 + min(vocab, 1100) + 40) * STEP * (1 + 8 + np.log(vocab)))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_distillation_of_tokens_at_the_lowest_value(plan, dtype):
+    """The teacher wants a token that the student masks by the type's lowest value: a large loss that fp32 can hold."""
+    lowest = torch.finfo(TYPES[dtype]).min
+    x = torch.randn(4, 1000, device="cuda").to(TYPES[dtype])
+    x[1, 2], x[2, :] = lowest, lowest
+    x[3, 8:] = lowest
+    ids, t = np.tile(np.arange(8), (4, 1)), np.zeros((4, 8), dtype=np.float32)
+    for temperature in (0.5, 1.0, 2.0):
+        loss, d = torch.empty(4, device="cuda"), torch.empty_like(x)
+        want, want_d = O.distill(f64(x), ids, t, None, temperature)
+        # eight shares of 1/8; the factor T^2 (1/8) |log p| of the lowest value is below the largest fp32 number
+        assert np.isfinite(want.astype(np.float32)).all()
+        B.cr_distill(plan, x, dev_ids(ids, "i64"), dev32(t), loss, d, temperature=temperature)
+        check(loss, want, "f32", temperature ** 2 * 1100 * STEP + 16 * STEP * np.abs(want))
+        check(d, want_d, dtype, temperature * 1200 * STEP * np.abs(want_d).max())
+
+
 # ------------------------------------------------------------------------------------------------ distillation
 
 DISTILS = [(1, 1, 0, 0, 1), (3, 8, 0, 0, 3), (39, 5004, 4, 0, 16), (39, 5004, 4, 1, 16), (4, 257, 0, 0, 64), (2, 32000, 0, 0, 64), (3, 50257, 0, 0, 20),
