@@ -1357,7 +1357,7 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
     if (!good_rows(tokens, inner, ld_x) || !good_rows(outer, inner, ld_w) || !good_rows(tokens, outer, ld_y)) return CR_ERR_INVALID_ARG;
     cr::Int8ProductArgs a;
     a.x = x; a.ld_x = ld_x; a.x_scale = x_scale; a.w = w; a.ld_w = ld_w; a.w_scale = w_scale; a.bias = bias;
-    a.y = y; a.ld_y = ld_y; a.tokens = tokens; a.outer = outer; a.inner = inner; a.elem = elem; a.device = plan->device;
+    a.y = y; a.ld_y = ld_y; a.tokens = tokens; a.outer = outer; a.inner = inner; a.elem = elem;
     cudaError_t e = cr::launch_int8_product(a, plan->d_status, plan->dev, plan->tune, plan->encode,
                                             reinterpret_cast<cudaStream_t>(stream), &plan->launches);
     if (e != cudaSuccess) { note_cuda(e, "cr_int8_product"); return CR_ERR_CUDA; }

@@ -601,7 +601,8 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
                     const int warps = std::max(kBins / 32, (int)((a.tokens + 32 * EACH - 1) / (32 * EACH)));
                     const size_t smem = (size_t)warps * 32 * EACH * sizeof(uint2);
                     if (smem > 8 * 1024) {       // beside the counters' 34 KB
-                        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+                        static std::atomic<uint64_t> told{0};      // one for each EACH and type of ids
+                        const cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(kernel), told);
                         if (e != cudaSuccess) return e;
                     }
                     kernel<<<(unsigned)a.partitions, 32 * warps, smem, stream>>>(g, static_cast<const I *>(a.ids));

@@ -533,14 +533,6 @@ CUresult encode_codes(EncodeTiledFn encode, CUtensorMap *map, const void *base, 
 
 constexpr int kStaticSmem = 8 * 128 * 4;   // at most: the scales of eight read-out warps
 
-cudaError_t allow_most_smem(const void *kernel, std::atomic<uint64_t> &told, int device, const DeviceInfo &dev) {
-    // told once per device: the largest dynamic shared memory of a block, whatever this call needs
-    if (device <= 63 && (told.load(std::memory_order_relaxed) >> device & 1)) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem_optin - kStaticSmem);
-    if (e == cudaSuccess && device <= 63) told.fetch_or(1ull << device, std::memory_order_relaxed);
-    return e;
-}
-
 TcArgs tc_args(const Int8ProductArgs &p, int tile_tokens, int tile_channels, int *status, const Tuning &tune) {
     TcArgs a;
     a.x_scale = p.x_scale; a.w_scale = p.w_scale; a.bias = p.bias; a.y = p.y; a.ld_y = p.ld_y;
@@ -564,7 +556,7 @@ cudaError_t launch_pair(const Int8ProductArgs &p, int *status, const DeviceInfo 
         encode_codes(encode, &map_x, p.x, p.inner, p.tokens, p.ld_x, 128) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
     static std::atomic<uint64_t> told{0};
-    cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_int8_product_pair_kernel<T>), told, p.device, dev);
+    cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_int8_product_pair_kernel<T>), told);
     if (e != cudaSuccess) return e;
     const size_t smem = (size_t)kPairStages * (kRows + 128) * kChunk + (2 * kPairStages + 5) * 8 + 16 + 1024;
     const unsigned pairs = (unsigned)std::min<int64_t>(tiles, dev.sm_count / 2);
@@ -596,7 +588,7 @@ cudaError_t launch_tc(const Int8ProductArgs &p, int *status, const DeviceInfo &d
         encode_codes(encode, &map_x, p.x, p.inner, p.tokens, p.ld_x, TN) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
     static std::atomic<uint64_t> told{0};
-    cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_int8_product_kernel<T, TN>), told, p.device, dev);
+    cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_int8_product_kernel<T, TN>), told);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : std::min<int64_t>(tiles, dev.sm_count)));

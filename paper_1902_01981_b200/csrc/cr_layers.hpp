@@ -85,7 +85,6 @@ struct Int8ProductArgs {
     int64_t tokens = 0, outer = 0, inner = 0;
     int64_t ld_x = 0, ld_w = 0, ld_y = 0;
     int elem = 0;
-    int device = 0;
 };
 cudaError_t launch_int8_product(const Int8ProductArgs &a, int *status, const DeviceInfo &dev, const Tuning &tune,
                                 EncodeTiledFn encode, cudaStream_t stream, int64_t *launches);

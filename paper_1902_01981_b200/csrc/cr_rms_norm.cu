@@ -534,7 +534,8 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
                 const size_t smem = V == 1 ? 0 : (size_t)grad_stages<V>() * 3 * held * threads * 16;
                 auto kernel = threads <= 256 ? cr_rms_norm_grad_rows_kernel<T, V, 256> : cr_rms_norm_grad_rows_kernel<T, V, grad_threads<V>()>;
                 if (smem > 48 * 1024) {
-                    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+                    static std::atomic<uint64_t> told[2] = {};     // one for each of the two kernels
+                    const cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(kernel), told[threads <= 256]);
                     if (e != cudaSuccess) return e;
                 }
                 kernel<<<(unsigned)(a.partitions * chunks), threads, smem, stream>>>(a, sums, ld_sums, each, chunk, chunks);

@@ -685,10 +685,10 @@ Share share_row(int64_t rows, int64_t vocab, int64_t chunk_elements, int most_wa
 }
 
 template <typename K, typename... More>
-cudaError_t launch(K kernel, const VocabArgs &a, const Share &s, int threads, size_t smem, cudaStream_t stream, int64_t *launches, More... more) {
+cudaError_t launch(K kernel, std::atomic<uint64_t> &told, const VocabArgs &a, const Share &s, int threads, size_t smem, cudaStream_t stream, int64_t *launches, More... more) {
     if (a.rows > 0x7fffffffll / s.cluster) return cudaErrorInvalidValue;
     if (smem > 32 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(kernel), told);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
@@ -718,7 +718,8 @@ cudaError_t launch_token_log_probs(const VocabArgs &a, const DeviceInfo &dev, cu
         // 32000, 20 alternatives: 71 us, with eight warps 77); few rows: as many as fit (128000 x 1 in a cluster: 10 us, with four 13).
         const Share s = share_row(a.rows, a.vocab, Chunk<T, VEC>::kElements, a.rows >= 4 * dev.sm_count ? kScoreWarps / 2 : kScoreWarps, dev.sm_count);
         const size_t smem = (size_t)s.slots * sizeof(Piece) + (a.top > 0 ? (size_t)((s.slots + s.cluster - 1) / s.cluster) * 128 : 0);
-        return launch(cr_token_log_probs_kernel<T, VEC>, a, s, 32 * s.warps, smem, stream, launches);
+        static std::atomic<uint64_t> told{0};
+        return launch(cr_token_log_probs_kernel<T, VEC>, told, a, s, 32 * s.warps, smem, stream, launches);
     });
 }
 
@@ -753,7 +754,8 @@ cudaError_t launch_distill(const VocabArgs &a, const DeviceInfo &dev, cudaStream
         constexpr int VEC = decltype(v)::value;
         const Share s = share_row(a.rows, a.vocab, Chunk<T, VEC>::kElements, kDistillWarps, dev.sm_count);
         const uint32_t words = seen_words(a.top);
-        return launch(cr_distill_kernel<T, VEC>, a, s, 32 * (s.warps + 1), (size_t)s.slots * sizeof(Piece) + (size_t)a.top * 16 + words * 8, stream, launches, words);
+        static std::atomic<uint64_t> told{0};
+        return launch(cr_distill_kernel<T, VEC>, told, a, s, 32 * (s.warps + 1), (size_t)s.slots * sizeof(Piece) + (size_t)a.top * 16 + words * 8, stream, launches, words);
     });
 }
 

@@ -753,6 +753,70 @@ def test_capture_and_other_streams(plan):
     assert all(torch.equal(a, b) for a, b in zip(want, outs))
 
 
+def test_threads_with_plans_of_their_own():
+    """Calls of one kind from several host threads, a plan each, whose kernels need different amounts of shared memory, all above
+    what a kernel has without asking: no call may take from another what it has asked for."""
+    import sys
+    import threading
+    lib, f32 = B.lib(), B.CR_ELEM_F32
+    count, keep = 8, []
+    plans = [B.cr_plan_create(4, 2, 1, 24, 1024, device=0) for _ in range(count)]
+
+    def new(shape, value, dtype=torch.float32):
+        keep.append(torch.full(shape, value, dtype=dtype, device="cuda"))
+        return keep[-1].data_ptr()
+
+    # the C calls with their arguments ready, so that the threads spend their time inside them
+    def sorts(p, tokens, stream):
+        need = lib.cr_embedding_backward_workspace_bytes(p, tokens, 1, 3, 4)
+        args = (new((tokens,), 0, torch.int64), 8, new((tokens, 4), 1.0), 4, new((3, 4), 7.0), 4, 12, tokens, 1, 3, 4, f32, 1.0, -1,
+                new((need,), 0, torch.uint8), need, stream)
+        return lambda: lib.cr_embedding_backward(p, *args)
+
+    def norms(p, cols, stream):
+        x, dx = new((2, cols), 1.0), new((2, cols), 7.0)
+        args = (x, cols, x, cols, None, new((2,), 1.0), None, 0, dx, cols, None, cols, 1, 2, cols, f32, new((64,), 0, torch.uint8), 64, stream)
+        return lambda: lib.cr_rms_norm_backward(p, *args)
+
+    def distils(p, vocab, stream):
+        args = (new((1, vocab), 0.0), vocab, new((1, 1024), 0, torch.int64), 8, new((1, 1024), 0.0), 1024, None, new((1,), 7.0), None, 0, 1, vocab,
+                f32, 1.0, stream)
+        return lambda: lib.cr_distill(p, *args)
+
+    def scores(p, vocab, stream):
+        args = (new((75, vocab), 0.0), vocab, None, 8, 75, vocab, f32, 1.0, None, None, None, 1, new((75, 1), 7.0), new((75, 1), 0, torch.int64), stream)
+        return lambda: lib.cr_token_log_probs(p, *args)
+
+    interval = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        for make, sizes, times in ((sorts, (1100, 2048), 6000), (norms, (4864, 8192), 6000), (norms, (2560, 4096), 6000), (distils, (4096, 262144), 6000),
+                                   (scores, (245760, 327680), 250)):
+            streams = [torch.cuda.Stream() for _ in range(count)]
+            calls = [make(plans[i], sizes[i % 2], streams[i].cuda_stream) for i in range(count)]
+            torch.cuda.synchronize()
+            failed, begin = [0] * count, threading.Barrier(count)
+
+            def work(i):
+                begin.wait()
+                for _ in range(times):
+                    failed[i] += calls[i]() != B.CR_OK
+
+            threads = [threading.Thread(target=work, args=(i,)) for i in range(count)]
+            for t in threads:
+                t.start()
+            for t in threads:
+                t.join()
+            torch.cuda.synchronize()
+            assert not any(failed), (make.__name__, sizes, failed)
+            keep.clear()
+    finally:
+        sys.setswitchinterval(interval)
+        torch.cuda.synchronize()
+        for p in plans:
+            B.cr_plan_destroy(p)
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 
 def test_refusals(plan):
