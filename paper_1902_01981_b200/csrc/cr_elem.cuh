@@ -6,7 +6,6 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
-#include <atomic>
 #include <cstdint>
 #include <initializer_list>
 
@@ -315,21 +314,6 @@ inline cudaError_t by_type(int elem, F &&f) {
 template <int V> struct Int { static constexpr int value = V; };
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-// Lets a kernel have the largest dynamic shared memory of a block beside its static one, whatever this call needs: the limit belongs to
-// the kernel on the device, so a call that set its own size would take from another thread's what that has just asked for.
-// `told`, one for each kernel: the devices that know.
-inline cudaError_t allow_most_smem(const void *kernel, std::atomic<uint64_t> &told) {
-    int device = 0, most = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    if (device <= 63 && (told.load(std::memory_order_relaxed) >> device & 1)) return cudaSuccess;
-    cudaFuncAttributes own;
-    e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, device);
-    if (e == cudaSuccess) e = cudaFuncGetAttributes(&own, kernel);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)own.sharedSizeBytes);
-    if (e == cudaSuccess && device <= 63) told.fetch_or(1ull << device, std::memory_order_relaxed);
-    return e;
-}
 // The vector form needs whole 16-byte vectors in every row.
 inline bool vector_rows(int elem, int64_t channels, std::initializer_list<const void *> ptrs, std::initializer_list<int64_t> lds) {
     const int vec = 16 / elem_bytes(elem);

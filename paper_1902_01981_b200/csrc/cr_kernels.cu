@@ -1610,7 +1610,8 @@ static int rows_per_box(int m, int cap) {
 template <typename T, int LMAX, int NCW>
 static cudaError_t run_fused(const CUtensorMap &map, const FusedArgs &fa, int grid, size_t smem, cudaStream_t stream) {
     auto kern = cr_fused_tma_kernel<T, LMAX, NCW>;
-    cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<uint64_t> told{0};
+    cudaError_t err = allow_most_smem(reinterpret_cast<const void *>(kern), told);
     if (err != cudaSuccess) return err;
     kern<<<grid, (NCW + 1) * 32, smem, stream>>>(map, fa);
     return cudaGetLastError();
@@ -1641,8 +1642,9 @@ static cudaError_t run_fused_ncw(int ncw, int lmax, const CUtensorMap &map, cons
 template <typename T, int LMAX, int NCW>
 static int fused_resident(size_t smem) {
     auto kern = cr_fused_tma_kernel<T, LMAX, NCW>;
+    static std::atomic<uint64_t> told{0};
     int blocks = 0;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+    if (allow_most_smem(reinterpret_cast<const void *>(kern), told) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kern, (NCW + 1) * 32, smem) != cudaSuccess) {
         (void)cudaGetLastError();
         return 0;
@@ -1769,7 +1771,8 @@ cudaError_t launch_fused_tma(const AggArgs &a, const DeviceInfo &dev, const Tuni
 template <typename T, int LMAX, int NLW, int NRW, bool SHARE>
 static cudaError_t run_batch(const CUtensorMap &map, const BatchArgs &ba, int grid, size_t smem, cudaStream_t stream) {
     auto kern = cr_fused_batch_tma_kernel<T, LMAX, NLW, NRW, SHARE>;
-    cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<uint64_t> told{0};
+    cudaError_t err = allow_most_smem(reinterpret_cast<const void *>(kern), told);
     if (err != cudaSuccess) return err;
     kern<<<grid, (NLW + NRW) * 32, smem, stream>>>(map, ba);
     return cudaGetLastError();
@@ -2111,7 +2114,8 @@ static cudaError_t run_partial_fused(const PgArgs &pa, int csplit, bool fit_one_
     const bool general = pa.slots_per_item != 1 || pa.coeff != nullptr;
     auto kern = general ? (pa.loss == 1 ? cr_partial_fused_kernel<KPT, true, true> : cr_partial_fused_kernel<KPT, true, false>)
                         : (pa.loss == 1 ? cr_partial_fused_kernel<KPT, false, true> : cr_partial_fused_kernel<KPT, false, false>);
-    cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<uint64_t> told[4] = {};       // one for each of the four kernels
+    cudaError_t err = allow_most_smem(reinterpret_cast<const void *>(kern), told[2 * general + (pa.loss == 1)]);
     if (err != cudaSuccess) return err;
     if (csplit > 8) {
         err = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);

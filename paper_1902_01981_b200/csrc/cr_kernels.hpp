@@ -4,6 +4,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 namespace cr {
@@ -38,6 +39,22 @@ struct DeviceInfo {
     int smem_optin = 0;  // bytes of dynamic shared memory a CTA may opt in to
     int smem_per_sm = 0;
 };
+
+// Lets a kernel have the largest dynamic shared memory of a block beside its static one, whatever this call needs: the limit belongs to
+// the kernel on the device, so a call that set its own size would take from another thread's what that has just asked for.
+// `told`, one for each kernel: the devices that know.
+inline cudaError_t allow_most_smem(const void *kernel, std::atomic<uint64_t> &told) {
+    int device = 0, most = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device <= 63 && (told.load(std::memory_order_relaxed) >> device & 1)) return cudaSuccess;
+    cudaFuncAttributes own;
+    e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, device);
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&own, kernel);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)own.sharedSizeBytes);
+    if (e == cudaSuccess && device <= 63) told.fetch_or(1ull << device, std::memory_order_relaxed);
+    return e;
+}
 
 struct AggArgs {
     const void *G;        // [N*m][d]

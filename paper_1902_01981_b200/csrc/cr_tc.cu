@@ -698,7 +698,8 @@ cudaError_t launch_partial_gradients_multi(const float *X, const float *y, const
         ra.items = items; ra.ipt = ipt; ra.sub_rows = sub_rows;
         ra.K = K; ra.loss = loss; ra.stages = 4; ra.kchunks = (int)((d + kBoxCols - 1) / kBoxCols); ra.status = status; ra.wait_ns = tune.wait_limit_ns;
         const size_t smem = (size_t)ra.stages * (kTileM * kBoxCols * 4 + 2 * kModels * kBoxCols * 4) + (2 * ra.stages + 1) * 8 + 16 + 1024;
-        cudaError_t e = cudaFuncSetAttribute(cr_tc_residual_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        static std::atomic<uint64_t> told{0};
+        cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(cr_tc_residual_kernel), told);
         if (e != cudaSuccess) return e;
         const dim3 grid = ipt > 1 ? dim3(1, (unsigned)((items + ipt - 1) / ipt)) : dim3((unsigned)(rows_pad / kTileM), (unsigned)items);
         cr_tc_residual_kernel<<<grid, 192, smem, stream>>>(mapX, mapWh, mapWl, ra);
@@ -714,7 +715,8 @@ cudaError_t launch_partial_gradients_multi(const float *X, const float *y, const
             ga.stages = tune.tc_stages ? tune.tc_stages : 2;
             const size_t smem = (size_t)ga.stages * (kTileM / kBoxCols) * kRowsB * kBoxCols * 4 + 2 * kRowsB * kBoxCols * 4 +
                                 (2 * ga.stages + 5) * 8 + 16 + 1024;
-            e = cudaFuncSetAttribute(cr_tc_gradient_short_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            static std::atomic<uint64_t> told{0};
+            e = allow_most_smem(reinterpret_cast<const void *>(cr_tc_gradient_short_kernel), told);
             if (e != cudaSuccess) return e;
             // CTAs per item: enough to give every SM about two CTAs, each with several column tiles
             int dev = 0, sms = 148;
@@ -729,7 +731,8 @@ cudaError_t launch_partial_gradients_multi(const float *X, const float *y, const
             return cudaSuccess;
         }
         const size_t smem = (size_t)ga.stages * ((kTileM / kBoxCols + 2) * kRowsB * kBoxCols * 4) + (2 * ga.stages + 1) * 8 + 16 + 1024;
-        e = cudaFuncSetAttribute(cr_tc_gradient_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        static std::atomic<uint64_t> told{0};
+        e = allow_most_smem(reinterpret_cast<const void *>(cr_tc_gradient_kernel), told);
         if (e != cudaSuccess) return e;
         cr_tc_gradient_kernel<<<dim3((unsigned)((d + kTileM - 1) / kTileM), (unsigned)items), 192, smem, stream>>>(mapXg, mapRh, mapRl, ga);
         e = cudaGetLastError();
