@@ -212,7 +212,8 @@ __global__ void __launch_bounds__(32 * kRowWarps) cr_rms_norm_kernel(const RmsNo
 
 // ---- gradient ------------------------------------------------------------------------------------------------------------
 
-// Rows of a partition that one block adds up: the partition's rows in at most 256 chunks of 4 to 64 rows.
+// Rows of a partition that one block adds up: 4 to 64, so that up to 16384 rows make 256 chunks at most; longer partitions have
+// a chunk for every 64 rows (a longer chain in the sums of the chunks: an eighth of them, one after the other).
 int64_t chunk_rows(int64_t rows) { return std::min<int64_t>(64, std::max<int64_t>(4, (rows + 255) / 256)); }
 
 // One block a chunk of rows: a thread keeps its columns' gamma and sums of dy xhat in registers over the rows.  Rows of up to

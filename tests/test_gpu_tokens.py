@@ -348,6 +348,30 @@ def test_norm_backward_parts(plan):
     B.cr_rms_norm(plan, none, gamma, none)
 
 
+# rows, cols, partitions: more chunks of 64 rows than 256, in one kernel and in two
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape", [(40000, 8, 1), (34000, 7, 2), (16500, 8200, 1)])
+def test_norm_gradient_of_long_partitions(plan, shape, dtype):
+    rows, cols, parts = shape
+    rng = np.random.default_rng(rows)
+    if cols > 100:
+        gen = torch.Generator(device="cuda").manual_seed(rows)
+        h, dy = (torch.randn(rows, cols, generator=gen, device="cuda").to(TYPES[dtype]) for _ in range(2))
+    else:
+        h, dy = place(rng.standard_normal((rows, cols)), dtype), place(rng.standard_normal((rows, cols)), dtype)
+    rstd = dev32(1 + 0.1 * rng.random(rows))
+    dg, dx = torch.full((parts, cols), float("nan"), device="cuda"), torch.empty_like(h)
+    need = B.cr_rms_norm_backward_workspace_bytes(plan, h, parts)
+    ws = scratch(need)
+    B.cr_rms_norm_backward(plan, dy, h, None, rstd, dx, dg, workspace=ws[:need])
+    assert whole(ws, need)
+    terms = dy.double() * h.double() * rstd.double()[:, None]
+    want, size = f64(terms.view(parts, -1, cols).sum(1)), f64(terms.abs().view(parts, -1, cols).sum(1))
+    # a chain of 64 rows, then every eighth chunk one after the other, then eight sums; three roundings a term
+    chunks = -(-(rows // parts) // 64)
+    check(dg, want, "f32", (64 + -(-chunks // 8) + 8 + 4) * STEP * size)
+
+
 # ------------------------------------------------------------------------------------------------ log probabilities
 
 # rows, vocab, pad, shift
