@@ -79,6 +79,26 @@ def test_a_worker_gets_the_bits_of_its_partition():
         net.close()
 
 
+def test_a_worker_gets_the_bits_of_its_norm_gradient():
+    """The gradient of gamma, and that of the state, of one partition alone."""
+    from examples.coded_tokens import CodedTokens
+    net = CodedTokens(rows=50, vocab=300, width=24, seed=5)
+    try:
+        net.step(inputs.straggler_masks(4, 2, 1, 1, seed=2, exactly_s=True)[0], rate=0.0)
+        dx, dgamma = net.dy.clone(), net.dgamma.clone()
+        torch.mm(net.dlogits, net.head, out=net.dy.view(-1, net.width))         # the step has written dx over it
+        dy = net.dy.clone()
+        assert not torch.equal(dy, dx)
+        for p in (7, 0, 23):
+            one, rows = slice(p, p + 1), slice(p * net.rows, (p + 1) * net.rows)
+            net.dgamma[one] = float("nan")
+            ws = torch.empty(B.cr_rms_norm_backward_workspace_bytes(net.norm_plan, net.h[one]), dtype=torch.uint8, device="cuda")
+            B.cr_rms_norm_backward(net.norm_plan, dy[one], net.h[one], net.gamma, net.rstd[rows], net.dy[one], net.dgamma[one], workspace=ws)
+            assert torch.equal(net.dgamma, dgamma) and torch.equal(net.dy[one], dx[one])
+    finally:
+        net.close()
+
+
 def test_answers_in_eight_bits():
     from examples.coded_tokens import CodedTokens
     net = CodedTokens(rows=40, vocab=333, width=64, seed=6)
