@@ -777,6 +777,59 @@ def test_capture_and_other_streams(plan):
     assert all(torch.equal(a, b) for a, b in zip(want, outs))
 
 
+def test_a_stream_of_its_own(plan):
+    """Every call in another stream's order: its inputs come late there, its outputs and workspaces are its own."""
+    rng = np.random.default_rng(4)
+    parts, tokens, vocab, width = 3, 900, 700, 64
+    rows = parts * tokens
+    ids = dev_ids(rng.integers(0, vocab, (parts, tokens)), "i64")
+    table, gamma = dev32(rng.standard_normal((vocab, width))), dev32(1 + 0.1 * rng.standard_normal(width))
+    tid, t = dev_ids(rng.integers(0, vocab, (rows, 4)), "i64"), dev32(rng.standard_normal((rows, 4)))
+    da, db = dev32(rng.standard_normal(rows)), dev32(rng.standard_normal(rows))
+    logits, dh = dev32(2 * rng.standard_normal((rows, vocab))), dev32(rng.standard_normal((parts, tokens, width)))
+    nan = lambda *shape: torch.full(shape, float("nan"), device="cuda")  # noqa: E731
+
+    def outputs():
+        o = dict(y=nan(parts, tokens, width), h=nan(parts, tokens, width), n=nan(parts, tokens, width), rstd=nan(rows), scale=nan(rows),
+                 q=torch.full((parts, tokens, width), 7, dtype=torch.int8, device="cuda"), lp=nan(rows), st=nan(rows, 2), en=nan(rows), tl=nan(rows, 6),
+                 ti=torch.full((rows, 6), -7, device="cuda"), ds=nan(rows, vocab), loss=nan(rows), dl=nan(rows, vocab), dx=nan(parts, tokens, width),
+                 dg=nan(parts, width), dt=nan(parts, vocab, width))
+        w1 = scratch(B.cr_embedding_backward_workspace_bytes(plan, ids, o["dt"]))
+        w2 = scratch(B.cr_rms_norm_backward_workspace_bytes(plan, o["y"], parts))
+        return o, w1, w2
+
+    def step(o, w1, w2):
+        B.cr_embedding(plan, ids, table, o["y"], scale=2.0)
+        B.cr_rms_norm(plan, o["y"], gamma, o["n"], residual=dh, h=o["h"], rstd=o["rstd"])
+        B.cr_rms_norm_codes(plan, o["y"], gamma, o["q"], o["scale"])
+        B.cr_token_log_probs(plan, logits, ids.view(-1), o["lp"], o["st"], o["en"], o["tl"], o["ti"])
+        B.cr_token_log_probs_backward(plan, logits, ids.view(-1), o["st"], o["en"], da, db, o["ds"])
+        B.cr_distill(plan, logits, tid, t, o["loss"], o["dl"])
+        B.cr_rms_norm_backward(plan, dh, o["h"], gamma, o["rstd"], o["dx"], o["dg"], workspace=w2)
+        B.cr_embedding_backward(plan, ids, o["dx"], o["dt"], scale=2.0, workspace=w1)
+
+    # once without a second stream, on the old inputs
+    before = outputs()
+    step(*before)
+    there = outputs()
+    late = [x.clone() for x in (table, logits, dh, t)]
+    late = [x.mul_(0.5).add_(0.25) for x in late]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)                 # about ten milliseconds, in which a call in the wrong stream reads the old inputs
+        for x, new in zip((table, logits, dh, t), late):
+            x.copy_(new)
+        step(*there)
+    torch.cuda.synchronize()
+    here = outputs()
+    step(*here)
+    for name, want in here[0].items():
+        assert torch.equal(there[0][name], want), name
+        if name != "ti":                              # the order of the logits is that of half of them and a quarter
+            assert not torch.equal(before[0][name], want), name
+
+
 def test_threads_with_plans_of_their_own():
     """Calls of one kind from several host threads, a plan each, whose kernels need different amounts of shared memory, all above
     what a kernel has without asking: no call may take from another what it has asked for."""
