@@ -1012,3 +1012,106 @@ def test_offsets_beyond_32_bits(plan):
     B.cr_embedding_backward(plan, ids[:3], x, dt, workspace=ws)
     B.cr_embedding_backward(plan, ids[:3], dx, dt2, workspace=ws)
     assert torch.equal(dt, dt2)
+
+
+# ------------------------------------------------------------------------------------------------ the largest sizes
+
+MOST = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("tokens", [70, 3000])
+def test_gradient_of_the_longest_table(plan, tokens):
+    """Numbers of 31 bits: four digits, in one CTA's sort and in the cluster's."""
+    rng = np.random.default_rng(tokens)
+    ids = rng.integers(0, MOST, tokens)
+    ids[::7], ids[1::7], ids[2::11], ids[3::13] = MOST - 1, 0, MOST, -1
+    ids[4::17] = 1 << 24
+    dy = torch.randn(tokens, 1, device="cuda")
+    table = torch.full((MOST, 1), float("nan"), device="cuda")
+    need = B.cr_embedding_backward_workspace_bytes(plan, dev_ids(ids, "i64"), table)
+    B.cr_embedding_backward(plan, dev_ids(ids, "i64"), dy, table, workspace=scratch(need)[:need])
+    named = (ids >= 0) & (ids < MOST)
+    where, back = np.unique(ids[named], return_inverse=True)
+    want, size = np.zeros(len(where)), np.zeros(len(where))
+    np.add.at(want, back, f64(dy)[named, 0])
+    np.add.at(size, back, np.abs(f64(dy)[named, 0]))
+    check(table[torch.from_numpy(where).cuda(), 0], want, "f32", (95 + tokens / 32 + 4) * STEP * size)
+    assert int(torch.count_nonzero(table)) == np.count_nonzero(want)
+    if tokens == 70:
+        y = torch.empty((tokens, 1), device="cuda")
+        B.cr_embedding(plan, dev_ids(ids, "i64"), table, y)
+        check(y[:, 0], np.where(named, f64(table[torch.from_numpy(np.where(named, ids, 0)).cuda(), 0]), 0), "f32", 0)
+
+
+def test_many_partitions(plan):
+    parts = 70000
+    ids = torch.arange(parts, device="cuda").view(parts, 1) % 5 - 1
+    dy = torch.randn(parts, 1, 4, device="cuda")
+    d = torch.full((parts, 3, 4), float("nan"), device="cuda")
+    need = B.cr_embedding_backward_workspace_bytes(plan, ids, d)
+    B.cr_embedding_backward(plan, ids, dy, d, workspace=scratch(need)[:need])
+    want = torch.zeros_like(d)
+    named = ((ids >= 0) & (ids < 3))[:, 0]
+    want[named, ids[named, 0]] = dy[named, 0]
+    assert torch.equal(d, want)
+    x, g, rstd = torch.randn(parts, 16, device="cuda"), torch.randn(parts, 16, device="cuda"), torch.rand(parts, device="cuda")
+    dx, dg = torch.empty_like(x), torch.full((parts, 16), float("nan"), device="cuda")
+    ws = scratch(B.cr_rms_norm_backward_workspace_bytes(plan, x, parts))
+    B.cr_rms_norm_backward(plan, g, x, None, rstd, dx, dg, workspace=ws)
+    want_dx, want_dg, size = O.rms_norm_backward(f64(g), f64(x), None, f64(rstd), None, parts)
+    check(dg, want_dg, "f32", 3 * STEP * size)
+
+
+@pytest.mark.parametrize("vocab", [MOST, MOST - 7])
+def test_the_longest_rows_of_logits(plan, vocab):
+    """One row of 2^31 logits, off and on the 16-byte boundaries: a few that stand out, all others alike."""
+    x = torch.full((1, vocab), -1.0, dtype=torch.bfloat16, device="cuda")
+    where = [5, vocab - 1, vocab - 2000, 1 << 30, vocab // 3]
+    x[0, where] = torch.tensor([20.0, 19.0, 18.0, 17.0, 16.0], dtype=torch.bfloat16, device="cuda")
+    x64 = np.array([20.0, 19.0, 18.0, 17.0, 16.0])
+    total = np.exp(x64 - 20).sum() + (vocab - 5) * np.exp(-21.0)
+    log_sum = np.log(total)
+    # a chain of one addition for each of a lane's 64 elements, 2048 chunks of a slot with two roundings each, the levels of joining
+    arith = (64 + 2 * 2048 + 60 + 6 * 21) * STEP
+    ids = torch.tensor([vocab - 1], device="cuda")
+    logp, stats, ent = torch.empty(1, device="cuda"), torch.empty((1, 2), device="cuda"), torch.empty(1, device="cuda")
+    tl, ti = torch.empty((1, 8), device="cuda"), torch.empty((1, 8), dtype=torch.int64, device="cuda")
+    B.cr_token_log_probs(plan, x, ids, logp, stats, ent, tl, ti)
+    assert ti[0].tolist() == where + [0, 1, 2]
+    check(tl[0], np.concatenate([x64, [-1, -1, -1]]) - 20 - log_sum, "f32", arith)
+    check(logp, [-1 - log_sum], "f32", arith)
+    p = np.exp(x64 - 20) / total
+    rest = (vocab - 5) * np.exp(-21.0) / total
+    check(ent, [-(p * np.log(p)).sum() + rest * (21 + log_sum)], "f32", arith * 23)
+    t = torch.tensor([[1.0, 2.0, 0.5]], device="cuda")
+    tid = torch.tensor([[vocab - 1, 7, 5]], device="cuda")
+    loss, d = torch.empty(1, device="cuda"), torch.empty_like(x)
+    B.cr_distill(plan, x, tid, t, loss, d)
+    share = np.exp([1.0, 2.0, 0.5]) / np.exp([1.0, 2.0, 0.5]).sum()
+    lp = np.array([-1.0, -21.0, 0.0]) - log_sum
+    check(loss, [(share * (np.log(share) - lp)).sum()], "f32", 2 * arith)
+    at = lambda g: f64(g[0, [vocab - 1, 7, 5, vocab - 2000, 6, vocab - 2]])  # noqa: E731
+    q = np.exp(np.array([19.0, -1, 20, 18, -1, -1]) - 20) / total
+    got = at(d)
+    assert np.all(np.abs(got - (q - np.concatenate([share, [0, 0, 0]]))) <= 2.0 ** -8 * 1.01 * np.abs(got) + arith * np.maximum(q, 1e-9) + 8 * STEP)
+    assert abs(float(d[0, 8:1 << 20].double().sum()) / ((1 << 20) - 8) / q[4] - 1) <= 2.0 ** -8 + arith
+    one = torch.ones(1, device="cuda")
+    B.cr_token_log_probs_backward(plan, x, ids, stats, ent, one, None, x)
+    hot = np.array([1.0, 0, 0, 0, 0, 0])
+    got = at(x)
+    assert np.all(np.abs(got - (hot - q)) <= 2.0 ** -8 * 1.01 * np.abs(got) + arith * np.maximum(q, 1e-9) + 8 * STEP)
+
+
+@pytest.mark.parametrize("cols", [MOST, MOST - 7])
+def test_norm_of_the_longest_rows(plan, cols):
+    x = torch.full((1, cols), 0.5, dtype=torch.bfloat16, device="cuda")
+    x[0, [3, cols - 1]] = torch.tensor([1000.0, -2000.0], dtype=torch.bfloat16, device="cuda")
+    mean = ((cols - 2) * 0.25 + 1e6 + 4e6) / cols
+    rstd = torch.empty(1, device="cuda")
+    B.cr_rms_norm(plan, x, None, x, rstd=rstd, eps=0.0)
+    # 16 warps go over 2^22 pieces of 512 (2^20 of 1024) elements: a chain of a quarter of a million additions, then of each piece's own
+    pieces = -(-cols // 512) / 16
+    check(rstd, [mean ** -0.5], "f32", (pieces + 600) / 2 * STEP * mean ** -0.5)
+    got = f64(x[0, [3, cols - 1, 0, cols - 2, cols // 2]])
+    want = np.array([1000.0, -2000.0, 0.5, 0.5, 0.5]) * mean ** -0.5
+    assert np.all(np.abs(got - want) <= (2.0 ** -8 * 1.01 + (pieces + 600) / 2 * STEP) * np.abs(want))
