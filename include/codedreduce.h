@@ -474,7 +474,8 @@ cr_status_t cr_embedding(cr_plan_t *plan, const void *ids, int32_t id_bytes, con
  * zero.  Tokens of number `padding` take no part (-1: all do; for a table whose padding row is looked up and not trained).
  * A row's tokens are added in the order of their positions, in pieces whose ends depend on the partition's own tokens.
  * workspace: device scratch of cr_embedding_backward_workspace_bytes (CR_ERR_OOM if smaller), 16-byte aligned.
- * tokens <= 2^30 a partition, partitions <= 2^24. */
+ * tokens <= 2^30 a partition, partitions <= 2^24, partitions * tokens <= 2^40, partitions * ceil(vocab / 32) <= 3 * 2^29
+ * (whose tables would take 200 GB). */
 size_t cr_embedding_backward_workspace_bytes(const cr_plan_t *plan, int64_t tokens, int64_t partitions, int64_t vocab, int64_t width);
 cr_status_t cr_embedding_backward(cr_plan_t *plan, const void *ids, int32_t id_bytes, const void *dy, int64_t ld_dy,
                                   float *dtable, int64_t ld_row, int64_t ld_partition, int64_t tokens, int64_t partitions,

@@ -1371,6 +1371,7 @@ cr_status_t cr_int8_product(cr_plan_t *plan, const int8_t *x, int64_t ld_x, cons
 namespace {
 
 constexpr int64_t kMost31 = 0x7fffffffll, kMostSorted = 1ll << 30;     // positions that are counted a block ahead in 31 bits
+constexpr int64_t kMostZeroed = 3ll << 29;     // blocks that zero 32 rows of a table each, beside at most 2^29 that add up
 bool good_ids(const void *ids, int32_t id_bytes) {
     return (id_bytes == 4 || id_bytes == 8) && (reinterpret_cast<uintptr_t>(ids) & (uintptr_t)(id_bytes - 1)) == 0;
 }
@@ -1382,7 +1383,7 @@ bool good_extents(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kMos
 
 bool good_embedding(int64_t tokens, int64_t most, int64_t partitions, int64_t vocab, int64_t width) {
     return tokens >= 0 && tokens <= most && vocab >= 0 && vocab <= kMost31 && width >= 0 && width <= (1 << 24) && partitions >= 0 &&
-           partitions <= (1 << 24) && (tokens == 0 || partitions <= (1ll << 40) / tokens);
+           partitions <= (1 << 24) && (tokens == 0 || partitions <= (1ll << 40) / tokens) && partitions * ((vocab + 31) / 32) <= kMostZeroed;
 }
 
 cr::VocabArgs vocab_args(const void *logits, int64_t ld, const void *ids, int32_t id_bytes, int64_t rows, int64_t vocab, int32_t elem, double t) {

@@ -575,12 +575,21 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
     g.dy = a.dy; g.dtable = a.dtable; g.tokens = a.tokens; g.vocab = a.vocab;
     g.ld_dy = a.ld_dy; g.ld_row = a.ld_row; g.ld_partition = a.ld_partition;
     g.width = (int)a.width; g.scale = a.scale;
-    cudaError_t e;
     const bool table16 = aligned16(a.dtable) && a.ld_row % 4 == 0 && (a.partitions == 1 || a.ld_partition % 4 == 0);
     g.padding = a.padding;
     g.tile = tile_tokens(a.tokens);
     g.tiles = (int)((a.tokens + g.tile - 1) / g.tile);
     g.words = (int)((a.vocab + 31) / 32);
+    // the grid of the sums and zeroes
+    const int vec = 16 / elem_bytes(a.elem);
+    const bool wide = table16 && vector_rows(a.elem, a.width, {a.dy}, {a.ld_dy});
+    const int nvec = g.width / (wide ? vec : 1), held = wide ? 1 : sum_held<1>();
+    int across = 1;
+    while (across < kSumThreads && across * held < nvec) across *= 2;
+    const int slabs = (nvec + across * held - 1) / (across * held);
+    const int64_t groups = (g.tiles + kSumThreads / across - 1) / (kSumThreads / across);
+    if (a.partitions * groups > ((1ll << 29) - 1) / slabs) return cudaErrorInvalidValue;     // more than the gradients that fit a device
+    const unsigned sums = (unsigned)(a.partitions * groups * slabs), blocks = sums + (unsigned)(a.partitions * g.words);
     if (a.tokens > 0) {
         char *p = static_cast<char *>(workspace);
         const size_t table = align16((size_t)(a.partitions * (g.tiles + 1)) * 4);
@@ -592,6 +601,7 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         int bits = 1;
         while (bits < 31 && (1ll << bits) < a.vocab) ++bits;
         g.passes = (bits + kDigitBits - 1) / kDigitBits;
+        cudaError_t e;
         auto by_ids = [&](auto &&f) { return a.id_bytes == 4 ? f(int32_t{}) : f((long long){}); };
         if (a.tokens <= kSortOneCta) {
             e = by_ids([&](auto i) {
@@ -627,18 +637,9 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
         if (e != cudaSuccess) return e;
         ++*launches;
     }
-    e = by_type(a.elem, [&](auto t) {
+    cudaError_t e = by_type(a.elem, [&](auto t) {
         using T = decltype(t);
         constexpr int VEC = 16 / (int)sizeof(T);
-        const bool wide = table16 && vector_rows(a.elem, a.width, {a.dy}, {a.ld_dy});
-        const int nvec = g.width / (wide ? VEC : 1);
-        const int held = wide ? 1 : sum_held<1>();
-        int across = 1;
-        while (across < kSumThreads && across * held < nvec) across *= 2;
-        const int slabs = (nvec + across * held - 1) / (across * held);
-        const int64_t groups = (g.tiles + kSumThreads / across - 1) / (kSumThreads / across);
-        if (a.partitions * groups > 0x3fffffffll / slabs || a.partitions > 0x3fffffffll / g.words) return cudaErrorInvalidValue;
-        const unsigned sums = (unsigned)(a.partitions * groups * slabs), blocks = sums + (unsigned)(a.partitions * g.words);
         auto kernel = wide ? cr_embedding_sums_kernel<T, VEC> : cr_embedding_sums_kernel<T, 1>;
         if (a.tokens > 0) return launch_next(kernel, blocks, kSumThreads, stream, g, sums, across, slabs);
         kernel<<<blocks, kSumThreads, 0, stream>>>(g, sums, across, slabs);
@@ -648,14 +649,15 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs &a, void *workspace, c
     ++*launches;
     if (a.tokens > kWhole) {      // otherwise no sum is cut
         const bool four = table16 && g.width % 4 == 0;
-        const int nvec = four ? g.width / 4 : g.width;
-        int across = 1;
-        while (across < 64 && across < nvec) across *= 2;
-        const int slabs = (nvec + across - 1) / across;
+        const int join_nvec = four ? g.width / 4 : g.width;
+        int join_across = 1;
+        while (join_across < 64 && join_across < join_nvec) join_across *= 2;
+        const int join_slabs = (join_nvec + join_across - 1) / join_across;
         const int64_t walkers = std::min<int64_t>(a.tokens / kWhole, std::max<int64_t>(1, 4 * dev.sm_count / a.partitions));
-        if (a.partitions * walkers > 0x7fffffffll / slabs) return cudaErrorInvalidValue;
-        const unsigned blocks = (unsigned)(a.partitions * walkers * slabs);
-        e = launch_next(four ? cr_embedding_join_kernel<4> : cr_embedding_join_kernel<1>, blocks, kJoinThreads, stream, g, across, slabs, (unsigned)walkers);
+        if (a.partitions * walkers > 0x7fffffffll / join_slabs) return cudaErrorInvalidValue;
+        const unsigned joins = (unsigned)(a.partitions * walkers * join_slabs);
+        e = launch_next(four ? cr_embedding_join_kernel<4> : cr_embedding_join_kernel<1>, joins, kJoinThreads, stream, g, join_across, join_slabs,
+                        (unsigned)walkers);
         if (e == cudaSuccess) ++*launches;
     }
     return e;

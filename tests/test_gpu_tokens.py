@@ -975,6 +975,15 @@ def test_refusals(plan):
     B.cr_plan_destroy(host)
 
 
+def test_tables_beyond_the_grid_are_refused(plan):
+    """More rows of tables than blocks that could zero them (more than the device holds): an argument that is refused, not a launch
+    that fails."""
+    n = B.cr_plan_launch_count(plan)
+    for parts, vocab in ((1 << 24, 4096), (800, 2 ** 31 - 1)):
+        assert B.lib().cr_embedding_backward(plan, None, 8, None, 1, 16, 1, vocab, 0, parts, vocab, 1, B.CR_ELEM_F32, 1.0, -1, None, 0, None) == B.CR_ERR_INVALID_ARG
+    assert B.cr_plan_launch_count(plan) == n
+
+
 # ------------------------------------------------------------------------------------------------ long strides
 
 def test_offsets_beyond_32_bits(plan):

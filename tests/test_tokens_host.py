@@ -55,6 +55,15 @@ def test_workspaces(plan):
     assert ask(16384, 4096, 8) == 16384 * 4 + 8 * 256 * 4096 * 4
 
 
+def test_workspaces_of_tables_up_to_the_device(plan):
+    """Asked for as long as such tables could lie on a device, and not beyond."""
+    ask = lambda *a: B.lib().cr_embedding_backward_workspace_bytes(plan, *a)  # noqa: E731
+    for parts, vocab in ((1 << 24, 2080), (1 << 24, 32), (24, 2 ** 31 - 1)):
+        assert parts * vocab * 4 > 1 << 30 and ask(1, parts, vocab, 1) > 0
+    for parts, vocab in ((1 << 24, 4096), (800, 2 ** 31 - 1)):
+        assert parts * vocab * 4 > 200e9 and ask(1, parts, vocab, 1) == 0
+
+
 def test_a_host_only_plan_does_no_device_work(plan):
     assert B.lib().cr_rms_norm(plan, 16, 8, None, 0, None, None, 0, 16, 8, None, 1, 8, B.CR_ELEM_F32, 1e-5, None) == B.CR_ERR_CUDA
     assert B.lib().cr_embedding(plan, 16, 8, 16, 8, 16, 8, 1, 1, 8, B.CR_ELEM_F32, 1.0, None) == B.CR_ERR_CUDA
