@@ -508,17 +508,17 @@ cr_status_t cr_rms_norm_backward(cr_plan_t *plan, const void *dy, int64_t ld_dy,
                                  float *dgamma, int64_t ld_gamma, int64_t partitions, int64_t rows, int64_t cols, int32_t elem,
                                  void *workspace, size_t workspace_bytes, void *stream);
 
-/* Scores over logits [rows][vocab] at temperature T > 0.  With m the row's largest logit and
+/* Scores over logits [rows][vocab] at temperature T, 1e-18 to 1e18 (here and below).  With m the row's largest logit and
  * log_sum = log sum_v e^{(x_v - m) / T}, log p_v = (x_v - m) / T - log_sum:
  *   logp[r] = log p of token ids[r] (0 where it names none),  entropy[r] = -sum_v p_v log p_v,
  *   stats[r] = {m, log_sum} (what the backward pass takes; the log of the partition function is m / T + log_sum),
  *   top_ids, top_logp [rows][top]: the `top` largest logits in descending order, equal ones by ascending index, and their
  *   log p.  top_ids are of id_bytes.
  * All outputs fp32; each of logp, stats, entropy may be NULL, the last two are there if top > 0 (0 <= top <= 32, <= vocab).
- * Logits of -infinity are masked out.  A row that is -infinity throughout has no distribution: log p = -infinity, entropy 0,
+ * Logits of -infinity are masked out (those of the type's lowest value keep a log p).  A row that is -infinity throughout has no distribution: log p = -infinity, entropy 0,
  * its alternatives are the lowest indices.  A NaN makes all of its row's numbers NaN, and is the best alternative; a row with
  * +infinity has log p = -infinity for its finite logits and NaN for the infinite ones and the entropy.
- * 0 <= rows <= 2^31 - 1, 1 <= vocab <= 2^31 - 1. */
+ * stats is 8-byte aligned.  0 <= rows <= 2^31 - 1, 1 <= vocab <= 2^31 - 1. */
 cr_status_t cr_token_log_probs(cr_plan_t *plan, const void *logits, int64_t ld, const void *ids, int32_t id_bytes,
                                int64_t rows, int64_t vocab, int32_t elem, double temperature, float *logp, float *stats,
                                float *entropy, int32_t top, float *top_logp, void *top_ids, void *stream);

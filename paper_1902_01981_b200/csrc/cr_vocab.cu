@@ -6,7 +6,8 @@
 //   t = softmax over the teacher's k logits / T,  loss = T^2 sum_j t_j (log t_j - log p_{id_j}),  dx_v = w T (p_v - sum_{j: id_j = v} t_j)
 //
 // With c = log2(e) / T and the row's largest logit m, e^{z_v - m/T} = 2^{(x_v - m) c}.  The difference comes first: it is exact
-// near m, and a row whose logits are all the type's lowest value stays in range.  What a row keeps for its gradient is m and
+// near m, and a row whose logits are all the type's lowest value stays in range; the teacher's logits are taken relative to their
+// largest in the same way, and a log p is formed without base two, which would take the lowest value out of range.  What a row keeps for its gradient is m and
 // log sum_v e^{(x_v - m)/T}, not their sum, which would round the second one away where m is large.
 #include <cuda_runtime.h>
 
@@ -259,7 +260,8 @@ constexpr int kKept = 64;
 // logits reach, and hardly more than k do.  Phase two: only the lanes whose largest reaches the bound have their elements
 // read again (32 or 64 each, from L2), four lanes' at a time; what reaches the bound is kept, and as all keys differ, counting
 // the larger ones gives each its rank.  The CTAs of a cluster hand the leader their k best.  4096 x 32000 bf16: 52 us without
-// alternatives (5.0 TB/s), 72 with 20 of them, whose steps are short and wait for each other.
+// alternatives (5.0 TB/s), 72 with 20 of them, whose steps are short and wait for each other.  Five blocks of eight warps leave 48
+// registers, of which 72 to 96 bytes are spilled.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(32 * kScoreWarps, 5) cr_token_log_probs_kernel(const VocabArgs a, int cluster, int slots) {
     using C = Chunk<T, VEC>;
@@ -517,8 +519,8 @@ __host__ __device__ constexpr uint32_t seen_words(int top) {
 // One warp takes the teacher: its shares, and the loss once the row's sums are there.  The others take a chunk each, keep it in
 // registers over the exchange of the sums (the last one, where a warp has several) and write the gradient; then they put in the
 // elements of their own chunk that the teacher names, which its warp has worked out.  8192 x 32000 bf16, 64 named: 204 us (5.1 TB/s
-// of the bytes that it cannot do without), between the two powers of two an element (128 us of their unit) and the memory (163):
-// eight warps a row and four rows an SM hide them best (16 warps 263, 4 warps 217).
+// of the bytes that it cannot do without), between the two powers of two an element (113 us of their unit, 16 a clock and SM at
+// 1965 MHz) and the memory (163): eight warps a row and four rows an SM hide them best (16 warps 263, 4 warps 217).
 template <typename T, int VEC>
 __global__ void __launch_bounds__(32 * (kDistillWarps + 1), VEC == 1 ? 3 : 4) cr_distill_kernel(const VocabArgs a, int cluster, int slots, uint32_t words) {
     using C = Chunk<T, VEC>;
@@ -676,7 +678,8 @@ struct Share {
 Share share_row(int64_t rows, int64_t vocab, int64_t chunk_elements, int most_warps, int sm_count) {
     Share s;
     s.slots = (int)std::min<int64_t>(kSlots, (vocab + chunk_elements - 1) / chunk_elements);
-    // as many CTAs as leave every SM at most one, while there are slots for them
+    // as many CTAs as leave every SM at most one, while there are slots for them.  That leaves SMs idle where
+    // rows are few: 39 rows of 128000 bf16 (two CTAs each) 16.4 us, 75 rows (one) 22.5, no less than 148 rows
     s.cluster = 1;
     while (s.cluster < kMaxCluster && s.cluster * 2 <= s.slots && rows * s.cluster * 2 <= sm_count) s.cluster *= 2;
     const int own = (s.slots + s.cluster - 1) / s.cluster, turns = (own + most_warps - 1) / most_warps;
