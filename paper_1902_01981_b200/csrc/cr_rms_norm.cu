@@ -534,7 +534,7 @@ cudaError_t launch_rms_norm_backward(const RmsNormArgs &a, float *workspace, cud
                 const int threads = (int)std::max<int64_t>(32, (nvec + held * 32 - 1) / (held * 32) * 32);
                 const size_t smem = V == 1 ? 0 : (size_t)grad_stages<V>() * 3 * held * threads * 16;
                 auto kernel = threads <= 256 ? cr_rms_norm_grad_rows_kernel<T, V, 256> : cr_rms_norm_grad_rows_kernel<T, V, grad_threads<V>()>;
-                if (smem > 48 * 1024) {
+                if (smem > 32 * 1024) {       // 48 KB without asking, of which the block's sums take some
                     static std::atomic<uint64_t> told[2] = {};     // one for each of the two kernels
                     const cudaError_t e = allow_most_smem(reinterpret_cast<const void *>(kernel), told[threads <= 256]);
                     if (e != cudaSuccess) return e;

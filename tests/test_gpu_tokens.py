@@ -830,6 +830,53 @@ def test_a_stream_of_its_own(plan):
             assert not torch.equal(before[0][name], want), name
 
 
+FIRST_CALLS = """
+import sys
+import torch
+from paper_1902_01981_b200 import binding as B
+plan = B.cr_plan_create(4, 2, 1, 24, 1024, device=0)
+failed = []
+
+def call(what, f):
+    try:
+        f()
+    except B.CodedReduceError as e:
+        failed.append((what, str(e)))
+
+new = lambda *shape, dtype=torch.float32: torch.ones(shape, dtype=dtype, device="cuda")
+for dtype in (torch.float32, torch.bfloat16, torch.float16):
+    for cols in range(32, 8193, 32):
+        x, rstd, dx = new(2, cols, dtype=dtype), new(2), new(2, cols, dtype=dtype)
+        ws = new(64, dtype=torch.uint8)
+        call(("norm gradient", dtype, cols), lambda: B.cr_rms_norm_backward(plan, x, x, None, rstd, dx, workspace=ws))
+    for top in range(64, 1025, 64):
+        for vocab in (2048, 65536, 524288):
+            x, ids, t, loss = new(1, vocab, dtype=dtype), torch.arange(top, device="cuda").view(1, -1), new(1, top), new(1)
+            call(("distillation", dtype, vocab, top), lambda: B.cr_distill(plan, x, ids, t, loss))
+    for chunks in range(128, 257, 16):
+        x, ids, t = new(75, chunks * 1024, dtype=dtype), new(75, 1, dtype=torch.int64), new(75, 1)
+        call(("scores", dtype, chunks), lambda: B.cr_token_log_probs(plan, x, None, top_logp=t, top_ids=ids))
+for kind in (torch.int32, torch.int64):
+    for tokens in range(64, 2049, 64):
+        ids, dy, dt = new(tokens, dtype=kind), new(tokens, 4), new(3, 4)
+        ws = new(B.cr_embedding_backward_workspace_bytes(plan, ids, dt), dtype=torch.uint8)
+        call(("table gradient", kind, tokens), lambda: B.cr_embedding_backward(plan, ids, dy, dt, workspace=ws))
+torch.cuda.synchronize()
+print(failed[:4], len(failed))
+sys.exit(len(failed) > 0)
+"""
+
+
+def test_first_calls_of_a_process():
+    """Sizes in ascending order in a process of its own: no call may live on shared memory that a larger one has asked for."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-2000:]
+
+
 def test_threads_with_plans_of_their_own():
     """Calls of one kind from several host threads, a plan each, whose kernels need different amounts of shared memory, all above
     what a kernel has without asking: no call may take from another what it has asked for."""
